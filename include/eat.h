@@ -341,6 +341,88 @@ eat_status_t eat_ppl_trend(const void* h, int32_t S, int32_t d, const void* w_vo
                            const int32_t* target, double* nll_sum, int32_t* count, double* ppl_prev,
                            int8_t* trend_out, float* nll_out, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---- cross entropy of the LM head ------------------------------------------
+ *
+ * The language-model loss of T positions with its gradients, over the whole
+ * vocabulary, without a row of logits kept (at most 1 GiB of bf16 gradients of
+ * a piece of the vocabulary at a time).  With z_t = h_t . W_V^T (bf16 in, fp32
+ * accumulation), n the positions that count (target_t != ignore) and
+ * c = scale / (mean ? max(n, 1) : 1):
+ *
+ *   nll_t = log(1 + sum_{v != y} exp(z_tv - z_ty)),  y = target_t
+ *   loss  = c sum_t nll_t                    (0 when no position counts)
+ *   G_tv  = softmax(z_t)_v - [v = y]         (bf16; 0 where t does not count)
+ *   dh_t  = c sum_v G_tv W_V[v]     dW_V[v] = c sum_t G_tv h_t
+ *
+ * A position that does not count has nll 0 and dh 0 and reaches nothing else,
+ * whatever its hidden row holds (NaN and infinities too).  A target outside
+ * [0, V) that is not `ignore`, or a NaN in the row, gives a NaN nll, a NaN
+ * loss and NaN in what the row reaches (its dh, all of dW_V). */
+typedef enum { EAT_CE_DH = 1, EAT_CE_DW = 2 } eat_ce_grads_t;
+
+/* Workspace bytes for T positions (0 <= T <= 2^20), width d (a multiple of
+ * 64, at most 65536: EAT_ERR_UNSUPPORTED beyond) and vocabulary V (1..2^24)
+ * with the gradients `grads` (eat_ce_grads_t bits).  EAT_ERR_INVALID_ARG
+ * otherwise. */
+eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grads, size_t* bytes);
+
+/* One call (formulas above).
+ *   h         [T][d] bf16 hidden rows;  w_vocab [V][d] bf16 LM head
+ *   target    [T] int32;  ignore: the target of a position that does not count
+ *   mean      1: the mean over the positions that count, 0: their sum
+ *   scale     finite factor of the loss and its gradients
+ *   loss_out  [1] fp32;  nll_out [T] fp32 or NULL;  count_out [1] int32 (n) or NULL
+ *   dh        [T][d] bf16 or NULL; it may be h itself
+ *   dw        [V][d] bf16 or NULL; must not overlap w_vocab
+ *   ws        workspace of eat_ce_workspace_size bytes, 256-byte aligned
+ * T = 0 gives loss 0, n 0 and dw 0 (h and target may then be NULL).  Every sum
+ * has a fixed order: results are bit-reproducible.  Enqueues on `stream` only;
+ * no synchronisation, no allocation, no memset.  Errors: EAT_ERR_INVALID_ARG,
+ * EAT_ERR_UNSUPPORTED, EAT_ERR_WORKSPACE, EAT_ERR_HIP. */
+eat_status_t eat_ce_loss(const void* h, int32_t T, int32_t d, const void* w_vocab, int32_t V, const int32_t* target,
+                         int32_t ignore, int32_t mean, float scale, float* loss_out, float* nll_out,
+                         int32_t* count_out, void* dh, void* dw, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- balance loss of the router ---------------------------------------------
+ *
+ * The load-balancing term of a router's training objective, with the entropy
+ * regulariser on the token-averaged routing probabilities (Sec. 3.5), the
+ * per-expert counts and the gradients.  From the probabilities p and the
+ * selections m that eat_route writes (any mode; the selections are constants),
+ * over the n tokens that are valid:
+ *
+ *   C_e = sum_t m_te     f_e = C_e / max(sum_j C_j, 1)     P_e = sum_t p_te / max(n, 1)
+ *   loss = coef E sum_e f_e P_e + entropy_coef sum_e P_e log P_e      (0 log 0 = 0)
+ *   q_e  = coef E f_e + entropy_coef (log P_e + 1)                    (= dloss / dP_e)
+ *   dz_te = p_te (q_e - sum_j q_j p_tj) / max(n, 1)    of the scaled scores
+ *           z = inv_temperature x . W_r^T  (p = softmax(z), with expert_scale too)
+ *   dx_t = inv_temperature sum_e dz_te W_r[e]
+ *   dW_r[e] = inv_temperature sum_t dz_te x_t
+ *
+ * A uniform load gives coef + entropy_coef log(1/E).  A token that is not
+ * valid has dz 0 and dx 0 and reaches nothing else, whatever its rows of x and
+ * p hold.  A token that selected no expert counts in n and P alone. */
+eat_status_t eat_balance_workspace_size(eat_handle_t h, int32_t T, size_t* bytes);
+
+/* One call for layer h (its E, d_model, act_dtype and inv_temperature).
+ *   x         [T][d_model] act_dtype (only dw_router reads it; else may be NULL)
+ *   w_router  [E][d_model] fp32 (only dx reads it; else may be NULL)
+ *   prob      [T][E] fp32, mask [T][W] uint64, as eat_route writes them
+ *   valid     [T] bytes, 0: the token does not count; NULL: all do
+ *   coef, entropy_coef   finite
+ *   loss_out  [1] fp32;  count_out [E] int64 (C) and mean_prob_out [E] fp32 (P), or NULL
+ *   dlogits   [T][E] fp32 (dz), dx [T][d_model] act_dtype, dw_router [E][d_model]
+ *             fp32: each may be NULL; dlogits may be prob itself, dx x itself
+ *             where dw_router is NULL
+ *   ws        workspace of eat_balance_workspace_size(h, T) bytes, 256-byte aligned
+ * T = 0 gives loss 0, counts 0, P 0 and dw_router 0.  Every sum has a fixed
+ * order.  Enqueues on `stream` only; no synchronisation, no allocation, no
+ * memset.  Errors: EAT_ERR_INVALID_ARG, EAT_ERR_WORKSPACE, EAT_ERR_HIP. */
+eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const float* w_router, const float* prob,
+                              const uint64_t* mask, const uint8_t* valid, float coef, float entropy_coef,
+                              float* loss_out, int64_t* count_out, float* mean_prob_out, float* dlogits, void* dx,
+                              float* dw_router, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ---- packed expert weights -------------------------------------------------
  *
  * Write the PACKED form (eat_layout_t) of `groups` row-major bf16 matrices

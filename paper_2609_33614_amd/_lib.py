@@ -20,6 +20,7 @@ EAT_NOALLOC_SCRATCH_BYTES = 256 << 20      # include/eat.h
 EAT_MODE_EAT, EAT_MODE_TOPK, EAT_MODE_TOPP = 0, 1, 2
 EAT_F32, EAT_BF16 = 0, 1
 EAT_LAYOUT_ROWS, EAT_LAYOUT_PACKED = 0, 1
+EAT_CE_DH, EAT_CE_DW = 1, 2
 (EAT_STAGE_BEGIN, EAT_STAGE_ROUTED, EAT_STAGE_PERMUTED, EAT_STAGE_UP, EAT_STAGE_DOWN, EAT_STAGE_SHARED,
  EAT_STAGE_COMBINED, EAT_STAGE_END, EAT_NUM_STAGE_EVENTS) = range(9)
 MODES = {"eat": EAT_MODE_EAT, "topk": EAT_MODE_TOPK, "topp": EAT_MODE_TOPP}
@@ -90,12 +91,21 @@ def load() -> C.CDLL:
         lib.eat_pack_weights.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, P, P]
     if hasattr(lib, "eat_moe_forward_noalloc"):
         lib.eat_moe_forward_noalloc.argtypes = lib.eat_moe_forward.argtypes[:15] + [P]
+    if hasattr(lib, "eat_ce_loss"):
+        lib.eat_ce_workspace_size.argtypes = [C.c_int32] * 4 + [C.POINTER(C.c_size_t)]
+        lib.eat_ce_loss.argtypes = [P, C.c_int32, C.c_int32, P, C.c_int32, P, C.c_int32, C.c_int32, C.c_float, P, P, P,
+                                    P, P, P, C.c_size_t, P]
+    if hasattr(lib, "eat_balance_loss"):
+        lib.eat_balance_workspace_size.argtypes = [P, C.c_int32, C.POINTER(C.c_size_t)]
+        lib.eat_balance_loss.argtypes = [P, P, C.c_int32, P, P, P, P, C.c_float, C.c_float, P, P, P, P, P, P, P,
+                                         C.c_size_t, P]
     lib.eat_status_string.argtypes = [C.c_int]
     lib.eat_status_string.restype = C.c_char_p
     for name in ("eat_params_default", "eat_create", "eat_destroy", "eat_workspace_size", "eat_route_workspace_size",
                  "eat_reset_accounts", "eat_route", "eat_moe_forward", "eat_moe_forward_profiled",
                  "eat_stack_workspace_size", "eat_stack_forward", "eat_ppl_workspace_size", "eat_ppl_reset",
-                 "eat_ppl_trend", "eat_pack_weights", "eat_moe_forward_noalloc"):
+                 "eat_ppl_trend", "eat_pack_weights", "eat_moe_forward_noalloc", "eat_ce_workspace_size", "eat_ce_loss",
+                 "eat_balance_workspace_size", "eat_balance_loss"):
         if hasattr(lib, name):
             getattr(lib, name).restype = st
     _lib = lib
@@ -262,3 +272,30 @@ def eat_ppl_trend(h, S: int, d: int, w_vocab, V: int, target, nll_sum, count, pp
 def eat_pack_weights(src, groups: int, M: int, K: int, dst, stream=None) -> None:
     _check(load().eat_pack_weights(_ptr(src), int(groups), int(M), int(K), _ptr(dst), _stream(stream)),
            "eat_pack_weights")
+
+
+def eat_ce_workspace_size(T: int, d: int, V: int, grads: int = 0) -> int:
+    b = C.c_size_t()
+    _check(load().eat_ce_workspace_size(int(T), int(d), int(V), int(grads), C.byref(b)), "eat_ce_workspace_size")
+    return b.value
+
+
+def eat_ce_loss(h, T: int, d: int, w_vocab, V: int, target, ignore: int, mean: int, scale: float, loss_out, nll_out,
+                count_out, dh, dw, ws, ws_bytes: int, stream=None) -> None:
+    _check(load().eat_ce_loss(_ptr(h), int(T), int(d), _ptr(w_vocab), int(V), _ptr(target), int(ignore), int(mean),
+                              float(scale), _ptr(loss_out), _ptr(nll_out), _ptr(count_out), _ptr(dh), _ptr(dw),
+                              _ptr(ws), int(ws_bytes), _stream(stream)), "eat_ce_loss")
+
+
+def eat_balance_workspace_size(handle: int, T: int) -> int:
+    b = C.c_size_t()
+    _check(load().eat_balance_workspace_size(handle, int(T), C.byref(b)), "eat_balance_workspace_size")
+    return b.value
+
+
+def eat_balance_loss(handle: int, x, T: int, w_router, prob, mask, valid, coef: float, entropy_coef: float, loss_out,
+                     count_out, mean_prob_out, dlogits, dx, dw_router, ws, ws_bytes: int, stream=None) -> None:
+    _check(load().eat_balance_loss(handle, _ptr(x), int(T), _ptr(w_router), _ptr(prob), _ptr(mask), _ptr(valid),
+                                   float(coef), float(entropy_coef), _ptr(loss_out), _ptr(count_out),
+                                   _ptr(mean_prob_out), _ptr(dlogits), _ptr(dx), _ptr(dw_router), _ptr(ws),
+                                   int(ws_bytes), _stream(stream)), "eat_balance_loss")

@@ -43,7 +43,7 @@ SAN_CFLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=un
               "-Xarch_host", "-fno-omit-frame-pointer", "-Xarch_host", "-fno-sanitize-recover=all"]
 SAN_LDFLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-shared-libsan"]
 SOURCES = ["api.cpp", "route.hip", "permute.hip", "expert.hip", "wide.hip", "combine.hip", "ppl.hip", "pack.hip",
-           "noalloc.hip"]
+           "noalloc.hip", "ce.hip", "balance.hip"]
 
 
 def _compile(src: str, extra=(), tag: str = "") -> str:

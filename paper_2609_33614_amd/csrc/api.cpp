@@ -15,6 +15,7 @@
 namespace {
 
 constexpr int32_t kMaxTokens = 1 << 24;
+constexpr int32_t kMaxCeTokens = 1 << 20, kMaxVocab = 1 << 24, kMaxCeWidth = 1 << 16;
 
 bool finite(float v) { return isfinite(v) != 0; }
 bool in01(float v) { return finite(v) && v >= 0.f && v <= 1.f; }
@@ -513,6 +514,64 @@ eat_status_t eat_ppl_trend(const void* h, int32_t S, int32_t d, const void* w_vo
     if (e == hipSuccess)
         e = eat::launch_ppl(z, splits, stride, S, V, static_cast<const uint16_t*>(h),
                             static_cast<const uint16_t*>(w_vocab), d, target, nll_sum, count, ppl_prev, trend_out, nll_out, stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grads, size_t* bytes) {
+    if (!bytes || T < 0 || T > kMaxCeTokens || d < 64 || d % 64 || V < 1 || V > kMaxVocab) return EAT_ERR_INVALID_ARG;
+    if (grads < 0 || grads > (EAT_CE_DH | EAT_CE_DW)) return EAT_ERR_INVALID_ARG;
+    if (d > kMaxCeWidth) return EAT_ERR_UNSUPPORTED;
+    *bytes = eat::plan_ce(T, d, V, (grads & EAT_CE_DH) != 0, (grads & EAT_CE_DW) != 0).total;
+    return EAT_OK;
+}
+
+eat_status_t eat_ce_loss(const void* h, int32_t T, int32_t d, const void* w_vocab, int32_t V, const int32_t* target,
+                         int32_t ignore, int32_t mean, float scale, float* loss_out, float* nll_out,
+                         int32_t* count_out, void* dh, void* dw, void* ws, size_t ws_bytes, hipStream_t stream) {
+    size_t need = 0;
+    const eat_status_t st = eat_ce_workspace_size(T, d, V, (dh ? EAT_CE_DH : 0) | (dw ? EAT_CE_DW : 0), &need);
+    if (st != EAT_OK) return st;
+    if ((mean != 0 && mean != 1) || !finite(scale)) return EAT_ERR_INVALID_ARG;
+    if (!w_vocab || !loss_out || (T > 0 && (!h || !target))) return EAT_ERR_INVALID_ARG;
+    if (!aligned(h, 16) || !aligned(w_vocab, 16) || !aligned(target, 4) || !aligned(loss_out, 4) ||
+        !aligned(nll_out, 4) || !aligned(count_out, 4) || !aligned(dh, 16) || !aligned(dw, 16))
+        return EAT_ERR_INVALID_ARG;
+    if (!ws || ws_bytes < need) return EAT_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
+    const eat::CeCall c{static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(w_vocab), target, T, d, V, ignore,
+                        mean, scale, loss_out, nll_out, count_out, static_cast<uint16_t*>(dh),
+                        static_cast<uint16_t*>(dw)};
+    (void)hipGetLastError();
+    const hipError_t e = eat::launch_ce(eat::plan_ce(T, d, V, dh != nullptr, dw != nullptr), c,
+                                        static_cast<char*>(ws), stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+eat_status_t eat_balance_workspace_size(eat_handle_t h, int32_t T, size_t* bytes) {
+    if (!h || !bytes || T < 0 || T > h->max_tokens) return EAT_ERR_INVALID_ARG;
+    *bytes = eat::plan_balance(h->p, T).total;
+    return EAT_OK;
+}
+
+eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const float* w_router, const float* prob,
+                              const uint64_t* mask, const uint8_t* valid, float coef, float entropy_coef,
+                              float* loss_out, int64_t* count_out, float* mean_prob_out, float* dlogits, void* dx,
+                              float* dw_router, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (!h || T < 0 || T > h->max_tokens) return EAT_ERR_INVALID_ARG;
+    if (!finite(coef) || !finite(entropy_coef)) return EAT_ERR_INVALID_ARG;
+    if (!loss_out || (T > 0 && (!prob || !mask))) return EAT_ERR_INVALID_ARG;
+    if ((dx && !w_router) || (dw_router && T > 0 && !x)) return EAT_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(w_router, 16) || !aligned(prob, 4) || !aligned(mask, 8) || !aligned(loss_out, 4) ||
+        !aligned(count_out, 8) || !aligned(mean_prob_out, 4) || !aligned(dlogits, 4) || !aligned(dx, 16) ||
+        !aligned(dw_router, 16))
+        return EAT_ERR_INVALID_ARG;
+    const eat::BalancePlan b = eat::plan_balance(h->p, T);
+    if (!ws || ws_bytes < b.total) return EAT_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
+    const eat::BalanceCall c{x, w_router, prob, mask, valid, T, coef, entropy_coef, loss_out, count_out, mean_prob_out,
+                             dlogits, dx, dw_router};
+    (void)hipGetLastError();
+    const hipError_t e = eat::launch_balance(h->p, b, c, static_cast<char*>(ws), stream);
     return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
 }
 

@@ -240,6 +240,55 @@ hipError_t launch_ppl(const float* z, int splits, int64_t stride, int32_t S, int
                       hipStream_t s);
 hipError_t launch_ppl_reset(int32_t S, double* nll_sum, int32_t* count, double* ppl_prev, hipStream_t s);
 
+// LM-head cross entropy with gradients (ce.hip): the workspace carve-up (byte
+// offsets) and the choices it depends on, then one call.
+struct CePlan {
+    size_t head, coef, rows, tc, zt, nllc, stats, hc, part, g, dhp, total;
+    int rows_pad;            // rows of the row arrays: T rounded up to whole tiles
+    int tile, tiles;         // head rows per column tile of the first pass, and their number
+    int piece;               // head rows whose G is held at a time
+    int splits;              // reduction slices of dh
+    int parts;               // fp32 slices of dh held (0: it is written directly)
+};
+struct CeCall {
+    const uint16_t* h;       // [T][d]
+    const uint16_t* w;       // [V][d]
+    const int32_t* target;   // [T]
+    int32_t T, d, V, ignore, mean;
+    float scale;
+    float* loss;
+    float* nll;              // [T] or null
+    int32_t* count;          // or null
+    uint16_t* dh;            // [T][d] or null
+    uint16_t* dw;            // [V][d] or null
+};
+CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw);
+hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s);
+
+// The router's balance loss with gradients (balance.hip).
+struct BalancePlan {
+    size_t head, q, sum, cnt, dz, dwp, total;
+    int blocks;              // workgroups of the column sums
+    int splits;              // token slices of dw_router
+};
+struct BalanceCall {
+    const void* x;
+    const float* w_router;
+    const float* prob;
+    const uint64_t* mask;
+    const uint8_t* valid;
+    int32_t T;
+    float coef, entropy_coef;
+    float* loss;
+    int64_t* count;
+    float* mean_prob;
+    float* dlogits;
+    void* dx;
+    float* dw;
+};
+BalancePlan plan_balance(const eat_params_t& p, int32_t T);
+hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const BalanceCall& c, char* ws, hipStream_t s);
+
 // Forward entry points (api.cpp): host-side argument checks, and the
 // enqueue of one layer forward into a workspace of plan_workspace(h, T).total
 // bytes at `ws` (arguments checked, T > 0).  `residual` (bf16 [T][d] or

@@ -13,6 +13,15 @@ import torch
 from . import _lib as L
 
 
+def _expect(name: str, t: Optional[torch.Tensor], dtype, shape) -> None:
+    """Refuse a tensor (None passes) whose type or shape the library would misread."""
+    if t is None:
+        return
+    dtypes = dtype if isinstance(dtype, tuple) else (dtype,)
+    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected {' or '.join(str(v) for v in dtypes)} {list(shape)}, got {t.dtype} {list(t.shape)}")
+
+
 class EatLayer:
     def __init__(self, params: L.eat_params_t, max_tokens: int, weights: Dict[str, torch.Tensor],
                  device: str = "cuda"):
@@ -26,6 +35,7 @@ class EatLayer:
         self.p_total = torch.zeros(E, dtype=torch.float32, device=self.device)
         self.c_s = torch.zeros(E, dtype=torch.float32, device=self.device)
         self._ws: Optional[torch.Tensor] = None
+        self._bws: Optional[torch.Tensor] = None
 
     # account state -------------------------------------------------------
     @property
@@ -84,6 +94,34 @@ class EatLayer:
                     ws, ws.numel(), stream)
         return mask, k, gate, prob
 
+    def balance_loss(self, x: Optional[torch.Tensor], prob: torch.Tensor, mask: torch.Tensor,
+                     valid: Optional[torch.Tensor] = None, coef: float = 0.01, entropy_coef: float = 0.0,
+                     dlogits: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                     dw_router: Optional[torch.Tensor] = None, stream=None):
+        """The router's balance loss (eat_balance_loss) of the ``prob`` and
+        ``mask`` that ``route`` returned for ``x``: (loss [1], selections per
+        expert [E] int64, mean probabilities [E]).  The gradients are written
+        to the tensors given.  ``valid`` [T] (bool or uint8): tokens that count."""
+        T, E, d = prob.shape[0], self.params.E, self.params.d_model
+        act = torch.bfloat16 if self.params.act_dtype == L.EAT_BF16 else torch.float32
+        W = L.mask_words(E)
+        _expect("prob", prob, torch.float32, (T, E))
+        _expect("mask", mask, (torch.int64, torch.uint64), (T,) if mask.dim() == 1 and W == 1 else (T, W))
+        _expect("x", x, act, (T, d))
+        _expect("valid", valid, (torch.bool, torch.uint8), (T,))
+        _expect("dlogits", dlogits, torch.float32, (T, E))
+        _expect("dx", dx, act, (T, d))
+        _expect("dw_router", dw_router, torch.float32, (E, d))
+        loss = torch.empty(1, dtype=torch.float32, device=self.device)
+        count = torch.empty(E, dtype=torch.int64, device=self.device)
+        mean = torch.empty(E, dtype=torch.float32, device=self.device)
+        need = L.eat_balance_workspace_size(self.handle, T)
+        if self._bws is None or self._bws.numel() < need:
+            self._bws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        L.eat_balance_loss(self.handle, x, T, self.w["w_router"], prob, mask, valid, coef, entropy_coef, loss, count,
+                           mean, dlogits, dx, dw_router, self._bws, self._bws.numel(), stream)
+        return loss, count, mean
+
     def close(self) -> None:
         if self.handle:
             L.eat_destroy(self.handle)
@@ -119,6 +157,43 @@ class PplSignal:
         L.eat_ppl_trend(h, self.S, self.d, self.w, self.V, target, self.nll_sum, self.count, self.ppl_prev,
                         self.trend, self.nll, self.ws, self.ws.numel(), stream)
         return self.trend
+
+
+class CrossEntropy:
+    """Cross entropy of an LM head ``w_vocab`` [V][d] bf16 (eat_ce_loss):
+    ``loss(h, target)`` returns the loss [1] of the positions whose target is
+    not ``ignore``; NLLs, their count and the gradients of ``h`` and of the
+    head are written to the tensors given."""
+
+    def __init__(self, w_vocab: torch.Tensor, ignore: int = -100):
+        if w_vocab.dim() != 2:
+            raise ValueError("w_vocab: expected [V][d]")
+        _expect("w_vocab", w_vocab, torch.bfloat16, tuple(w_vocab.shape))
+        self.w, self.ignore = w_vocab, int(ignore)
+        self.V, self.d = w_vocab.shape
+        self._ws: Optional[torch.Tensor] = None
+
+    def workspace(self, T: int, grads: int) -> torch.Tensor:
+        need = L.eat_ce_workspace_size(T, self.d, self.V, grads)
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.w.device)
+        return self._ws
+
+    def loss(self, h: torch.Tensor, target: torch.Tensor, mean: bool = True, scale: float = 1.0,
+             nll: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+             dh: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        T = h.shape[0]
+        _expect("h", h, torch.bfloat16, (T, self.d))
+        _expect("target", target, torch.int32, (T,))
+        _expect("nll", nll, torch.float32, (T,))
+        _expect("count", count, torch.int32, (1,))
+        _expect("dh", dh, torch.bfloat16, (T, self.d))
+        _expect("dw", dw, torch.bfloat16, (self.V, self.d))
+        out = torch.empty(1, dtype=torch.float32, device=self.w.device)
+        ws = self.workspace(T, (L.EAT_CE_DH if dh is not None else 0) | (L.EAT_CE_DW if dw is not None else 0))
+        L.eat_ce_loss(h, T, self.d, self.w, self.V, target, self.ignore, int(mean), scale, out, nll, count, dh, dw, ws,
+                      ws.numel(), stream)
+        return out
 
 
 def layerwise_caps(n_layers: int, lower: int, k_lower: int, k_upper: int):

@@ -1,0 +1,85 @@
+"""Refusals of eat_ce_loss and eat_balance_loss: all on the host, before any
+HIP call (fake addresses that nothing reads)."""
+import os
+
+import pytest
+
+from paper_2609_33614_amd import _lib as L
+
+pytestmark = pytest.mark.skipif(not os.path.exists(L.LIB_PATH), reason="libeat.so not built")
+
+F = 1 << 20           # an aligned address
+
+
+def refused(status, fn, *args, **kw):
+    with pytest.raises(L.EatError) as e:
+        fn(*args, **kw)
+    assert e.value.status == status, e.value
+
+
+@pytest.mark.parametrize("T,d,V,grads,status", [
+    (-1, 64, 10, 0, L.EAT_ERR_INVALID_ARG), (2 ** 20 + 1, 64, 10, 0, L.EAT_ERR_INVALID_ARG),
+    (1, 0, 10, 0, L.EAT_ERR_INVALID_ARG), (1, 65, 10, 0, L.EAT_ERR_INVALID_ARG), (1, 32, 10, 0, L.EAT_ERR_INVALID_ARG),
+    (1, 64, 0, 0, L.EAT_ERR_INVALID_ARG), (1, 64, 2 ** 24 + 1, 0, L.EAT_ERR_INVALID_ARG),
+    (1, 64, 10, 4, L.EAT_ERR_INVALID_ARG), (1, 64, 10, -1, L.EAT_ERR_INVALID_ARG),
+    (1, 65600, 10, 0, L.EAT_ERR_UNSUPPORTED)])
+def test_ce_shapes(T, d, V, grads, status):
+    refused(status, L.eat_ce_workspace_size, T, d, V, grads)
+
+
+def test_ce_workspace_is_bounded():
+    """At most 1 GiB of G at a time, a pair of floats per position and 128 to
+    256 head rows, the counted rows' copies and fp32 slices of dh; never T V
+    floats."""
+    loss = L.eat_ce_workspace_size(8192, 4096, 128256, 0)
+    both = L.eat_ce_workspace_size(8192, 4096, 128256, L.EAT_CE_DH | L.EAT_CE_DW)
+    assert loss < 2 ** 28 < both < 2 ** 30 + 2 ** 29
+    T, d, V = 2 ** 20, 64, 2 ** 17
+    assert L.eat_ce_workspace_size(T, d, V, L.EAT_CE_DW) < 2 ** 30 + T * V // 32 + T * (2 * d + 64)
+    assert L.eat_ce_workspace_size(0, 64, 10, 3) > 0
+
+
+def test_ce_validation_happens_on_the_host():
+    T, d, V = 100, 128, 1000
+    n = L.eat_ce_workspace_size(T, d, V, 3)
+
+    def go(h=F, T=T, d=d, w=F, V=V, y=F, ignore=-100, mean=1, scale=1.0, loss=F, nll=F, count=F, dh=F, dw=F, ws=F, wsn=n):
+        L.eat_ce_loss(h, T, d, w, V, y, ignore, mean, scale, loss, nll, count, dh, dw, ws, wsn, stream=0)
+
+    bad = L.EAT_ERR_INVALID_ARG
+    for kw in (dict(h=None), dict(w=None), dict(y=None), dict(loss=None), dict(mean=2), dict(mean=-1),
+               dict(scale=float("nan")), dict(scale=float("inf")), dict(T=-1), dict(d=96), dict(V=0),
+               dict(h=F + 8), dict(w=F + 2), dict(y=F + 2), dict(loss=F + 1), dict(nll=F + 2), dict(count=F + 1),
+               dict(dh=F + 8), dict(dw=F + 4), dict(ws=F + 128), dict(T=0, w=None)):
+        refused(bad, go, **kw)
+    refused(L.EAT_ERR_WORKSPACE, go, ws=None)
+    refused(L.EAT_ERR_WORKSPACE, go, wsn=n - 1)
+    refused(L.EAT_ERR_UNSUPPORTED, go, d=65600)
+
+
+@pytest.fixture
+def handle():
+    h = L.eat_create(L.eat_params_default(mode="topk", E=60, d_model=128, d_ffn=64, top_k=4), 256)
+    yield h
+    L.eat_destroy(h)
+
+
+def test_balance_validation_happens_on_the_host(handle):
+    T = 100
+    n = L.eat_balance_workspace_size(handle, T)
+    bad = L.EAT_ERR_INVALID_ARG
+
+    def go(h=handle, x=F, T=T, w=F, prob=F, mask=F, valid=F, coef=0.01, ent=0.0, loss=F, count=F, mean=F, dz=F, dx=F,
+           dw=F, ws=F, wsn=n):
+        L.eat_balance_loss(h, x, T, w, prob, mask, valid, coef, ent, loss, count, mean, dz, dx, dw, ws, wsn, stream=0)
+
+    for kw in (dict(h=None), dict(T=-1), dict(T=257), dict(prob=None), dict(mask=None), dict(loss=None),
+               dict(coef=float("nan")), dict(ent=float("inf")), dict(x=None), dict(w=None), dict(x=F + 8),
+               dict(w=F + 4), dict(prob=F + 2), dict(mask=F + 4), dict(loss=F + 2), dict(count=F + 4), dict(mean=F + 1),
+               dict(dz=F + 2), dict(dx=F + 8), dict(dw=F + 8), dict(ws=F + 64)):
+        refused(bad, go, **kw)
+    refused(L.EAT_ERR_WORKSPACE, go, ws=None)
+    refused(L.EAT_ERR_WORKSPACE, go, wsn=n - 1)
+    refused(bad, L.eat_balance_workspace_size, handle, 257)
+    refused(bad, L.eat_balance_workspace_size, handle, -1)
+    refused(bad, L.eat_balance_workspace_size, None, 1)
