@@ -344,8 +344,8 @@ eat_status_t eat_ppl_trend(const void* h, int32_t S, int32_t d, const void* w_vo
 /* ---- cross entropy of the LM head ------------------------------------------
  *
  * The language-model loss of T positions with its gradients, over the whole
- * vocabulary, without a row of logits kept (at most 1 GiB of bf16 gradients of
- * a piece of the vocabulary at a time).  With z_t = h_t . W_V^T (bf16 in, fp32
+ * vocabulary, which is taken in pieces: no logits are kept, and the logits'
+ * gradient of one piece at a time, in bf16.  With z_t = h_t . W_V^T (bf16 in, fp32
  * accumulation), n the positions that count (target_t != ignore) and
  * c = scale / (mean ? max(n, 1) : 1):
  *
@@ -362,9 +362,13 @@ typedef enum { EAT_CE_DH = 1, EAT_CE_DW = 2 } eat_ce_grads_t;
 
 /* Workspace bytes for T positions (0 <= T <= 2^20), width d (a multiple of
  * 64, at most 65536: EAT_ERR_UNSUPPORTED beyond) and vocabulary V (1..2^24)
- * with the gradients `grads` (eat_ce_grads_t bits).  EAT_ERR_INVALID_ARG
- * otherwise. */
-eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grads, size_t* bytes);
+ * with the gradients `grads` (eat_ce_grads_t bits).  *bytes: the largest a
+ * call has a use for (pieces of up to 4 GiB); *min_bytes (or NULL): the
+ * smallest it takes (pieces of 4096 entries).  Any size between them is taken
+ * as it is, with pieces that fit: the first piece costs a pass over its
+ * gradient, every other one the product z of its entries again.
+ * EAT_ERR_INVALID_ARG otherwise. */
+eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grads, size_t* bytes, size_t* min_bytes);
 
 /* One call (formulas above).
  *   h         [T][d] bf16 hidden rows;  w_vocab [V][d] bf16 LM head
@@ -374,9 +378,10 @@ eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grad
  *   loss_out  [1] fp32;  nll_out [T] fp32 or NULL;  count_out [1] int32 (n) or NULL
  *   dh        [T][d] bf16 or NULL; it may be h itself
  *   dw        [V][d] bf16 or NULL; must not overlap w_vocab
- *   ws        workspace of eat_ce_workspace_size bytes, 256-byte aligned
+ *   ws        workspace of min_bytes or more (eat_ce_workspace_size), 256-byte aligned
  * T = 0 gives loss 0, n 0 and dw 0 (h and target may then be NULL).  Every sum
- * has a fixed order: results are bit-reproducible.  Enqueues on `stream` only;
+ * has a fixed order: results are bit-reproducible (the gradients for one
+ * workspace size: the pieces' rounding depends on it).  Enqueues on `stream` only;
  * no synchronisation, no allocation, no memset.  Errors: EAT_ERR_INVALID_ARG,
  * EAT_ERR_UNSUPPORTED, EAT_ERR_WORKSPACE, EAT_ERR_HIP. */
 eat_status_t eat_ce_loss(const void* h, int32_t T, int32_t d, const void* w_vocab, int32_t V, const int32_t* target,

@@ -92,7 +92,7 @@ def load() -> C.CDLL:
     if hasattr(lib, "eat_moe_forward_noalloc"):
         lib.eat_moe_forward_noalloc.argtypes = lib.eat_moe_forward.argtypes[:15] + [P]
     if hasattr(lib, "eat_ce_loss"):
-        lib.eat_ce_workspace_size.argtypes = [C.c_int32] * 4 + [C.POINTER(C.c_size_t)]
+        lib.eat_ce_workspace_size.argtypes = [C.c_int32] * 4 + [C.POINTER(C.c_size_t)] * 2
         lib.eat_ce_loss.argtypes = [P, C.c_int32, C.c_int32, P, C.c_int32, P, C.c_int32, C.c_int32, C.c_float, P, P, P,
                                     P, P, P, C.c_size_t, P]
     if hasattr(lib, "eat_balance_loss"):
@@ -274,10 +274,12 @@ def eat_pack_weights(src, groups: int, M: int, K: int, dst, stream=None) -> None
            "eat_pack_weights")
 
 
-def eat_ce_workspace_size(T: int, d: int, V: int, grads: int = 0) -> int:
-    b = C.c_size_t()
-    _check(load().eat_ce_workspace_size(int(T), int(d), int(V), int(grads), C.byref(b)), "eat_ce_workspace_size")
-    return b.value
+def eat_ce_workspace_size(T: int, d: int, V: int, grads: int = 0) -> "tuple[int, int]":
+    """(the largest workspace a call has a use for, the smallest it takes)."""
+    b, least = C.c_size_t(), C.c_size_t()
+    _check(load().eat_ce_workspace_size(int(T), int(d), int(V), int(grads), C.byref(b), C.byref(least)),
+           "eat_ce_workspace_size")
+    return b.value, least.value
 
 
 def eat_ce_loss(h, T: int, d: int, w_vocab, V: int, target, ignore: int, mean: int, scale: float, loss_out, nll_out,

@@ -517,33 +517,35 @@ eat_status_t eat_ppl_trend(const void* h, int32_t S, int32_t d, const void* w_vo
     return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
 }
 
-eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grads, size_t* bytes) {
+eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grads, size_t* bytes, size_t* min_bytes) {
     if (!bytes || T < 0 || T > kMaxCeTokens || d < 64 || d % 64 || V < 1 || V > kMaxVocab) return EAT_ERR_INVALID_ARG;
     if (grads < 0 || grads > (EAT_CE_DH | EAT_CE_DW)) return EAT_ERR_INVALID_ARG;
     if (d > kMaxCeWidth) return EAT_ERR_UNSUPPORTED;
-    *bytes = eat::plan_ce(T, d, V, (grads & EAT_CE_DH) != 0, (grads & EAT_CE_DW) != 0).total;
+    const bool dh = (grads & EAT_CE_DH) != 0, dw = (grads & EAT_CE_DW) != 0;
+    *bytes = eat::plan_ce(T, d, V, dh, dw, SIZE_MAX).total;
+    if (min_bytes) *min_bytes = eat::plan_ce(T, d, V, dh, dw, 0).total;
     return EAT_OK;
 }
 
 eat_status_t eat_ce_loss(const void* h, int32_t T, int32_t d, const void* w_vocab, int32_t V, const int32_t* target,
                          int32_t ignore, int32_t mean, float scale, float* loss_out, float* nll_out,
                          int32_t* count_out, void* dh, void* dw, void* ws, size_t ws_bytes, hipStream_t stream) {
-    size_t need = 0;
-    const eat_status_t st = eat_ce_workspace_size(T, d, V, (dh ? EAT_CE_DH : 0) | (dw ? EAT_CE_DW : 0), &need);
+    size_t most = 0;
+    const eat_status_t st = eat_ce_workspace_size(T, d, V, (dh ? EAT_CE_DH : 0) | (dw ? EAT_CE_DW : 0), &most, nullptr);
     if (st != EAT_OK) return st;
     if ((mean != 0 && mean != 1) || !finite(scale)) return EAT_ERR_INVALID_ARG;
     if (!w_vocab || !loss_out || (T > 0 && (!h || !target))) return EAT_ERR_INVALID_ARG;
     if (!aligned(h, 16) || !aligned(w_vocab, 16) || !aligned(target, 4) || !aligned(loss_out, 4) ||
         !aligned(nll_out, 4) || !aligned(count_out, 4) || !aligned(dh, 16) || !aligned(dw, 16))
         return EAT_ERR_INVALID_ARG;
-    if (!ws || ws_bytes < need) return EAT_ERR_WORKSPACE;
+    const eat::CePlan p = eat::plan_ce(T, d, V, dh != nullptr, dw != nullptr, ws_bytes);
+    if (!ws || ws_bytes < p.total) return EAT_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
     const eat::CeCall c{static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(w_vocab), target, T, d, V, ignore,
                         mean, scale, loss_out, nll_out, count_out, static_cast<uint16_t*>(dh),
                         static_cast<uint16_t*>(dw)};
     (void)hipGetLastError();
-    const hipError_t e = eat::launch_ce(eat::plan_ce(T, d, V, dh != nullptr, dw != nullptr), c,
-                                        static_cast<char*>(ws), stream);
+    const hipError_t e = eat::launch_ce(p, c, static_cast<char*>(ws), stream);
     return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
 }
 

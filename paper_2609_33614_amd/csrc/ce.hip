@@ -71,8 +71,9 @@ struct GemmArgs {
     int splits;                // slices of the reduction (PART)
     int col0;                  // LSE, GRAD: vocabulary index of column 0
     int xcds;
-    void* out;                 // GRAD, ROWS: bf16; PART: fp32 slices
+    void* out;                 // GRAD, ROWS, LSE: bf16; PART: fp32 slices
     int64_t ldo, split_stride;
+    int kept;                  // LSE: columns below it leave exp(z - the tile's maximum) in out
     const int32_t* rows;       // ROWS: destination of each output row (or null: itself)
     const float* coef;         // ROWS: factor c
     int add;                   // PART: add to what the slices hold
@@ -170,6 +171,10 @@ __device__ __forceinline__ bf16x8 fragment(const uint8_t* st, int i0, int s) {
 struct Item {
     int a0, b0, sp;
 };
+
+// The reference of a row's exponentials over a tile with maximum m (infinite
+// where all are -inf, whose sum is 0, or some +inf: then 0).
+__device__ __forceinline__ float tile_ref(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
 
 __device__ __forceinline__ float swap_halves(float v) { return __shfl_xor(v, 32, kWave); }
 
@@ -297,9 +302,15 @@ __global__ __launch_bounds__(C::kThreads) void ce_gemm(GemmArgs g) {
             wave_lds_sync();
         };
         if constexpr (OUT == LSE) {
-            float2* const red = reinterpret_cast<float2*>(ring);       // [WA][NB]
+            // the waves' maxima of a row, then its exponentials over the tile's
+            // maximum and their sum: the tile's first columns may be kept
+            float* const redm = reinterpret_cast<float*>(ring + 4096);       // [WA][NB], beside wave 0's rows
+            float* const reds = redm + C::WA * C::NB;
+            static_assert(4096 + 8 * C::WA * C::NB <= C::STAGES * C::kStage / C::kWaves, "within wave 0's share");
             const int v0 = cur.a0 + arow + 4 * lh;
             const bool tail = cur.a0 + C::NA > g.na;
+            const bool kept = cur.a0 < g.kept;
+            const int at = (wave % C::WA) * C::NB + brow + l32;
 #pragma unroll
             for (int j = 0; j < FB; ++j) {
                 const int row = cur.b0 + brow + 32 * j + l32;
@@ -319,30 +330,40 @@ __global__ __launch_bounds__(C::kThreads) void ce_gemm(GemmArgs g) {
 #pragma unroll
                     for (int q = 0; q < 16; ++q) m = fmaxf(m, acc[i][j][q]);
                 m = fmaxf(m, swap_halves(m));
-                // (an infinite maximum is no reference for the exponents: all
-                // are -inf: the sum is 0; some are +inf: it is set below)
-                const float ref = fabsf(m) == INFINITY ? 0.f : m;
+                if (lh == 0) redm[at + 32 * j] = m;
+            }
+            lds_barrier();
+#pragma unroll
+            for (int j = 0; j < FB; ++j) {
+                float m = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < C::WA; ++w) m = fmaxf(m, redm[w * C::NB + brow + 32 * j + l32]);
+                const float ref = tile_ref(m);
                 float s = 0.f;
 #pragma unroll
                 for (int i = 0; i < FA; ++i)
 #pragma unroll
-                    for (int q = 0; q < 16; ++q)
-                        s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], kLog2e, -ref * kLog2e));
+                    for (int q = 0; q < 16; ++q) {
+                        acc[i][j][q] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], kLog2e, -ref * kLog2e));
+                        s += acc[i][j][q];
+                    }
                 s += swap_halves(s);
-                if (m == INFINITY && s == s) s = 1.f;
-                if (lh == 0) red[(wave % C::WA) * C::NB + brow + 32 * j + l32] = float2{m, s};
+                if (lh == 0) reds[at + 32 * j] = s;
+                const int row0 = cur.b0 + brow + 32 * j;
+                if (kept && row0 < nb)
+                    store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q]; },
+                            [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; },
+                            nb - row0);
             }
             lds_barrier();
             for (int r = threadIdx.x; r < C::NB; r += C::kThreads) {
-                float2 p[C::WA];
                 float m = -INFINITY, s = 0.f;
 #pragma unroll
                 for (int w = 0; w < C::WA; ++w) {
-                    p[w] = red[w * C::NB + r];
-                    m = fmaxf(m, p[w].x);
+                    m = fmaxf(m, redm[w * C::NB + r]);
+                    s += reds[w * C::NB + r];
                 }
-#pragma unroll
-                for (int w = 0; w < C::WA; ++w) s += p[w].x == m ? p[w].y : p[w].y * __expf(p[w].x - m);
+                if (m == INFINITY && s == s) s = 1.f;      // (some are +inf: the row's NLL is)
                 if (cur.b0 + r < nb) g.part[static_cast<size_t>(cur.a0 / C::NA) * g.ldpart + cur.b0 + r] = float2{m, s};
             }
         } else if (active) {
@@ -573,6 +594,56 @@ __global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(const float2* __
     }
 }
 
+// G of the columns whose exponentials the first pass kept, in place: a tile of
+// the first pass x 64 rows per workgroup, 16 bytes per lane.  Twice the piece's
+// bytes against taking its product again (4096 rows of 32000 columns, d 4096:
+// see launch_ce).  Rows behind the list up to a whole reduction chunk: zeros.
+constexpr int kScaleThreads = 256, kScaleRows = 64;
+template <int NA>
+__global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __restrict__ part, int ldpart,
+                                                              const float2* __restrict__ stats,
+                                                              const int32_t* __restrict__ tc,
+                                                              const int32_t* __restrict__ head, uint16_t* g, int64_t ldg) {
+    constexpr int V = NA / 8, R = kScaleThreads / V;       // lanes per row, rows at a time
+    __shared__ float4 row[kScaleRows];                     // factor, G at the target, target's column (bits)
+    const int n = head[0], pad = head[1];
+    const int r0 = blockIdx.y * kScaleRows, c0 = blockIdx.x * NA;
+    if (r0 >= pad) return;
+    const int tid = threadIdx.x;
+    if (tid < kScaleRows) {
+        const int i = r0 + tid;
+        float4 v{0.f, 0.f, __int_as_float(-1), 0.f};
+        if (i < n) {
+            const float2 st = stats[i];
+            const float m = part[static_cast<size_t>(blockIdx.x) * ldpart + i].x;
+            v = float4{m == -INFINITY ? 0.f * st.x : __builtin_amdgcn_exp2f(fmaf(tile_ref(m), kLog2e, -st.x)), st.y,
+                       __int_as_float(tc[i] - c0), 0.f};
+        }
+        row[tid] = v;
+    }
+    uint16_t* const at = g + (r0 + tid / V) * ldg + c0 + 8 * (tid % V);
+    uint4 v[kScaleRows / R];
+#pragma unroll
+    for (int k = 0; k < kScaleRows / R; ++k) v[k] = *reinterpret_cast<const uint4*>(at + k * R * ldg);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kScaleRows / R; ++k) {
+        const int r = tid / V + k * R;
+        const float4 p = row[r];
+        const int rel = __float_as_int(p.z) - 8 * (tid % V);
+        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        uint32_t o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float lo = __uint_as_float(w[e] << 16) * p.x, hi = __uint_as_float(w[e] & 0xffff0000u) * p.x;
+            lo = rel == 2 * e ? p.y : lo;
+            hi = rel == 2 * e + 1 ? p.y : hi;
+            o[e] = r0 + r < n ? pack_bf16x2(lo, hi) : 0u;
+        }
+        *reinterpret_cast<uint4*>(at + k * R * ldg) = uint4{o[0], o[1], o[2], o[3]};
+    }
+}
+
 // dh of the listed rows: its slices added in order, times c.
 constexpr int kJoinThreads = 256;
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int splits, int64_t stride,
@@ -628,40 +699,53 @@ hipError_t launch_gemm(GemmArgs g, hipStream_t s) {
 // Calls of few rows take the tile of 64 rows, which streams the head.
 bool small_call(int T) { return T <= Small::NB; }
 
-constexpr size_t kPieceBytes = size_t{1} << 30;      // most G held at a time
+// G held at a time: a piece of the vocabulary whose G takes kPieceBytes at
+// most (1.4% of the card's memory) and, with a smaller workspace, what fits,
+// from kMinPiece columns on.  The first piece costs a pass over its G, every
+// other one its product again.
+constexpr size_t kPieceBytes = size_t{4} << 30;
+constexpr int kMinPiece = 4096;
 
 }  // namespace
 
-CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw) {
+CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) {
     CePlan p{};
-    auto up = [](size_t v) { return (v + 255) & ~size_t(255); };
-    size_t off = 0;
-    auto take = [&](size_t bytes) { const size_t at = off; off += up(bytes); return at; };
     p.rows_pad = small_call(T) ? Small::NB : (T + Big::NB - 1) / Big::NB * Big::NB;
     const size_t tp = p.rows_pad;
     p.tile = small_call(T) ? Small::NA : Big::NA;
     p.tiles = (V + p.tile - 1) / p.tile;
-    const size_t vpad = (static_cast<size_t>(V) + 255) / 256 * 256;
-    p.piece = static_cast<int>(std::min(vpad, std::max<size_t>(256, kPieceBytes / (2 * tp) / 256 * 256)));
-    const int pieces = static_cast<int>((vpad + p.piece - 1) / p.piece);
-    // dh: slices of the piece until the CUs have an item each, none under 4 chunks
+    const int vpad = (V + 255) / 256 * 256;
+    const int least = std::min(vpad, kMinPiece);
+    auto fit = [&](size_t room) {
+        return static_cast<int>(std::max<size_t>(least, std::min<size_t>(vpad, room / (2 * tp) / 256 * 256)));
+    };
+    // dh: slices of the reduction until the CUs have an item each, none under 4 chunks
     const int nb = small_call(T) ? Small::NB : Big::NB;
     const int64_t items = static_cast<int64_t>((T + nb - 1) / nb) * ((d + p.tile - 1) / p.tile);
     p.splits = 1;
-    while (dh && items * p.splits * 2 <= 256 && p.piece / kBK / (p.splits * 2) >= 4) p.splits *= 2;
-    p.parts = dh && (p.splits > 1 || pieces > 1) ? p.splits : 0;
-    p.head = take(16);
-    p.coef = take(4);
-    p.rows = take(static_cast<size_t>(T) * 4);
-    p.tc = take(tp * 4);
-    p.zt = take(tp * 8);
-    p.nllc = take(tp * 8);
-    p.stats = take(tp * 8);
-    p.hc = take(tp * d * 2);
-    p.part = take(tp * p.tiles * 8);
-    p.g = take(dh || dw ? tp * p.piece * 2 : 0);
-    p.dhp = take(static_cast<size_t>(p.parts) * tp * d * 4);
-    p.total = off;
+    while (dh && items * p.splits * 2 <= 256 && vpad / kBK / (p.splits * 2) >= 4) p.splits *= 2;
+    auto layout = [&](int piece) {
+        size_t off = 0;
+        auto take = [&](size_t n) { const size_t at = off; off += (n + 255) & ~size_t(255); return at; };
+        p.piece = piece;
+        p.parts = dh && (p.splits > 1 || piece < vpad) ? p.splits : 0;
+        p.head = take(16);
+        p.coef = take(4);
+        p.rows = take(static_cast<size_t>(T) * 4);
+        p.tc = take(tp * 4);
+        p.zt = take(tp * 8);
+        p.nllc = take(tp * 8);
+        p.stats = take(tp * 8);
+        p.hc = take(tp * d * 2);
+        p.part = take(tp * p.tiles * 8);
+        p.dhp = take(static_cast<size_t>(p.parts) * tp * d * 4);
+        p.g = off;
+        p.total = off + (dh || dw ? tp * piece * 2 : 0);
+    };
+    layout(fit(kPieceBytes));
+    if (p.total <= bytes || (!dh && !dw)) return p;
+    layout(least < vpad ? least : vpad);
+    if (bytes > p.total) layout(std::min(vpad, fit(bytes - p.g)));
     return p;
 }
 
@@ -690,6 +774,7 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
     z.b = hc; z.ldb = d; z.nb = T; z.nb_dev = head;
     z.K = d; z.splits = 1;
     z.part = part; z.ldpart = p.rows_pad; z.target = tc;
+    z.out = gbuf; z.ldo = p.piece; z.kept = c.dh || c.dw ? p.piece : 0;
     e = small ? launch_gemm<Small, false, false, LSE>(z, s) : launch_gemm<Big, false, false, LSE>(z, s);
     if (e != hipSuccess) return e;
     row_kernel<<<std::max(1, (T + kWave - 1) / kWave), kRowWaves * kWave, 0, s>>>(part, p.tiles, p.rows_pad, head, rows, tc, zt, c.scale,
@@ -699,11 +784,17 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
     for (int v0 = 0; v0 < V && e == hipSuccess; v0 += p.piece) {
         const int nv = std::min(p.piece, V - v0);
         const uint16_t* w = c.w + static_cast<size_t>(v0) * d;
-        GemmArgs q = z;
-        q.a = w; q.na = nv; q.col0 = v0;
-        q.stats = stats;
-        q.out = gbuf; q.ldo = p.piece;
-        e = small ? launch_gemm<Small, false, false, GRAD>(q, s) : launch_gemm<Big, false, false, GRAD>(q, s);
+        if (v0 == 0) {
+            const dim3 grid((nv + p.tile - 1) / p.tile, p.rows_pad / kScaleRows);
+            if (small) scale_kernel<Small::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
+            else scale_kernel<Big::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
+            e = hipGetLastError();
+        } else {
+            GemmArgs q = z;
+            q.a = w; q.na = nv; q.col0 = v0;
+            q.stats = stats;
+            e = small ? launch_gemm<Small, false, false, GRAD>(q, s) : launch_gemm<Big, false, false, GRAD>(q, s);
+        }
         if (e == hipSuccess && c.dh) {
             GemmArgs a{};
             a.a = w; a.lda = d; a.na = d; a.a_rows = nv;

@@ -262,7 +262,9 @@ struct CeCall {
     uint16_t* dh;            // [T][d] or null
     uint16_t* dw;            // [V][d] or null
 };
-CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw);
+// The plan for a workspace of `bytes` (0: the smallest a call takes, SIZE_MAX:
+// the largest it has a use for); its total exceeds `bytes` where they do not do.
+CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes);
 hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s);
 
 // The router's balance loss with gradients (balance.hip).

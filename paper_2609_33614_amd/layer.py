@@ -163,21 +163,26 @@ class CrossEntropy:
     """Cross entropy of an LM head ``w_vocab`` [V][d] bf16 (eat_ce_loss):
     ``loss(h, target)`` returns the loss [1] of the positions whose target is
     not ``ignore``; NLLs, their count and the gradients of ``h`` and of the
-    head are written to the tensors given."""
+    head are written to the tensors given.  ``max_workspace``: bytes of
+    workspace to stay under where a call can (the vocabulary is then taken in
+    smaller pieces).  Calls of one object share its workspace: order them on
+    one stream."""
 
-    def __init__(self, w_vocab: torch.Tensor, ignore: int = -100):
+    def __init__(self, w_vocab: torch.Tensor, ignore: int = -100, max_workspace: Optional[int] = None):
         if w_vocab.dim() != 2:
             raise ValueError("w_vocab: expected [V][d]")
         _expect("w_vocab", w_vocab, torch.bfloat16, tuple(w_vocab.shape))
-        self.w, self.ignore = w_vocab, int(ignore)
+        self.w, self.ignore, self.max_workspace = w_vocab, int(ignore), max_workspace
         self.V, self.d = w_vocab.shape
         self._ws: Optional[torch.Tensor] = None
 
     def workspace(self, T: int, grads: int) -> torch.Tensor:
-        need = L.eat_ce_workspace_size(T, self.d, self.V, grads)
+        need, least = L.eat_ce_workspace_size(T, self.d, self.V, grads)
+        if self.max_workspace is not None:
+            need = min(need, max(least, int(self.max_workspace)))
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.w.device)
-        return self._ws
+        return self._ws[:need]        # (its size decides the pieces, so a call's does not depend on earlier ones)
 
     def loss(self, h: torch.Tensor, target: torch.Tensor, mean: bool = True, scale: float = 1.0,
              nll: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,

@@ -28,20 +28,23 @@ def test_ce_shapes(T, d, V, grads, status):
 
 
 def test_ce_workspace_is_bounded():
-    """At most 1 GiB of G at a time, a pair of floats per position and 128 to
-    256 head rows, the counted rows' copies and fp32 slices of dh; never T V
-    floats."""
-    loss = L.eat_ce_workspace_size(8192, 4096, 128256, 0)
-    both = L.eat_ce_workspace_size(8192, 4096, 128256, L.EAT_CE_DH | L.EAT_CE_DW)
-    assert loss < 2 ** 28 < both < 2 ** 30 + 2 ** 29
+    """At most 4 GiB of G at a time (4096 columns in the smallest), a pair of
+    floats per position and 128 to 256 head rows, the counted rows' copies and
+    fp32 slices of dh; never T V floats."""
+    loss, least = L.eat_ce_workspace_size(8192, 4096, 128256, 0)
+    assert loss == least < 2 ** 28
+    both, least = L.eat_ce_workspace_size(8192, 4096, 128256, L.EAT_CE_DH | L.EAT_CE_DW)
+    assert least < 2 ** 26 + 2 ** 29 and 8192 * 128256 * 2 < both < 8192 * 128256 * 2 + 2 ** 29
     T, d, V = 2 ** 20, 64, 2 ** 17
-    assert L.eat_ce_workspace_size(T, d, V, L.EAT_CE_DW) < 2 ** 30 + T * V // 32 + T * (2 * d + 64)
-    assert L.eat_ce_workspace_size(0, 64, 10, 3) > 0
+    most, least = L.eat_ce_workspace_size(T, d, V, L.EAT_CE_DW)
+    rest = T * V // 32 + T * (2 * d + 64)
+    assert most < max(2 ** 32, 8192 * T) + rest and least <= 8192 * T + rest
+    assert min(L.eat_ce_workspace_size(0, 64, 10, 3)) > 0
 
 
 def test_ce_validation_happens_on_the_host():
     T, d, V = 100, 128, 1000
-    n = L.eat_ce_workspace_size(T, d, V, 3)
+    n = L.eat_ce_workspace_size(T, d, V, 3)[1]
 
     def go(h=F, T=T, d=d, w=F, V=V, y=F, ignore=-100, mean=1, scale=1.0, loss=F, nll=F, count=F, dh=F, dw=F, ws=F, wsn=n):
         L.eat_ce_loss(h, T, d, w, V, y, ignore, mean, scale, loss, nll, count, dh, dw, ws, wsn, stream=0)

@@ -6,8 +6,9 @@ eps_z = d 2^-24 max_v sum |h w|, and its exponent's argument by a few 2^-24
 |z| more.  The NLL is log(1 + R) of the other logits' distance to the target's
 (taken in fp64): off by (1 - p_y) times the rest's error, V-term sums in fp32
 trees adding 2^-24 per level (under 100 levels), and one rounding to fp32.  G
-is off by those of two logits (its own and the denominator), relative, and one
-rounding to bf16 (2^-8); a product of K terms in fp32 by K 2^-24 of the sum of
+is off by those of two logits (its own and the denominator), relative, and two
+roundings to bf16 (2^-8 each: the exponential as it is kept, then times its
+row's factor); a product of K terms in fp32 by K 2^-24 of the sum of
 absolute terms; the output by one rounding to bf16."""
 import numpy as np
 import pytest
@@ -37,10 +38,10 @@ def make(T, d, V, seed=0, ignored=None, lift=8.0):
     return h.cuda(), w.cuda(), y.cuda()
 
 
-def call(h, w, y, mean=True, scale=1.0, dh=True, dw=True, ignore=IGN, guard=512, poison=True):
+def call(h, w, y, mean=True, scale=1.0, dh=True, dw=True, ignore=IGN, guard=512, poison=True, most=None):
     """One call with its outputs inside larger buffers that must keep their
     surroundings, and a workspace full of NaN patterns."""
-    ce = CrossEntropy(w, ignore=ignore)
+    ce = CrossEntropy(w, ignore=ignore, max_workspace=most)
     T = h.shape[0]
 
     def out(shape, dtype):
@@ -91,7 +92,7 @@ def reference(h, w, y, mean, scale, ignore=IGN):
         eps = torch.zeros(0, 1, dtype=torch.float64, device=h.device)
     bn = torch.zeros(T, dtype=torch.float64, device=h.device)
     bn[rows] = (-torch.expm1(-nll) * eps * (1 + eps) + u * nll + 2.0 ** -140)[:, 0]
-    eg = 2.0 ** -8 + 2.02 * eps
+    eg = 2 * 2.0 ** -8 + 2.0 ** -16 + 2.02 * eps
     bh = torch.zeros_like(dh)
     ga = G.abs()
     bh[rows] = abs(c) * ((ga * (eg + V * u)) @ wd.abs())
@@ -188,15 +189,25 @@ def test_confident_and_repeated_targets(T, d, V):
     check(f"ce confident {T}", call(h, w, y), reference(h, w, y, True, 1.0))
 
 
-def test_several_pieces_of_the_vocabulary():
-    """More than 1 GiB of G: two pieces, the second one not whole."""
-    T, d, V = 300, 64, 2 ** 20 + 2 ** 17 + 33
-    g = torch.Generator(device="cuda").manual_seed(1)
-    h = torch.randn(T, d, generator=g, device="cuda").to(torch.bfloat16)
-    w = torch.randn(V, d, generator=g, device="cuda").mul_(0.3).to(torch.bfloat16)
-    y = torch.randint(0, V, (T,), generator=g, device="cuda").to(torch.int32)
-    y[:5] = torch.tensor([0, V - 1, 2 ** 20 - 1, 2 ** 20, IGN], dtype=torch.int32)
-    check("ce pieces", call(h, w, y), reference(h, w, y, True, 1.0))
+@pytest.mark.parametrize("T,V", [(40, 4096 * 2 + 33), (300, 4096 * 4 + 1), (300, 4097), (300, 4096 * 3)])
+def test_several_pieces_of_the_vocabulary(T, V):
+    """The smallest workspace (pieces of 4096 entries), one between, and the
+    largest: the loss is the same bits, the gradients within the same bound."""
+    d = 192
+    h, w, y = make(T, d, V, ignored=0.1)
+    y[:5] = torch.tensor([0, V - 1, 4095, 4096, IGN], dtype=torch.int32)
+    ref = reference(h, w, y, True, 1.0)
+    full = call(h, w, y)
+    most, least = L.eat_ce_workspace_size(T, d, V, 3)
+    assert least < most
+    for size in (0, (least + most) // 2, most):
+        got = call(h, w, y, most=size)
+        check(f"ce pieces {T} {V} {size}", got, ref)
+        assert torch.equal(got["loss"], full["loss"]) and torch.equal(got["nll"], full["nll"])
+        again = call(h, w, y, most=size)
+        assert torch.equal(got["dh"], again["dh"]) and torch.equal(got["dw"], again["dw"])
+        for kw in (dict(dh=False), dict(dw=False)):
+            check(f"ce pieces {T} {V} {size} {kw}", call(h, w, y, most=size, **kw), ref)
 
 
 @pytest.mark.parametrize("T", [48, 320])
