@@ -2,16 +2,23 @@
 //
 // stat_kernel sums the probabilities (fp64) and counts the selections of every
 // expert, a share of the tokens per workgroup; the last workgroup to finish
-// adds the shares in order and forms the loss and q = dloss / dP.  dz_kernel
-// makes the scores' gradient dz = p (q - <q, p>) / n row by row, dx_kernel
-// its product with the router weights, dw_kernel with x (fp32 matrix
-// instructions), over slices of the tokens that dw_join_kernel adds in order.
+// adds the shares in order and forms the loss and q = dloss / dP.  prep_kernel
+// makes the scores' gradient dz = p (q - <q, p>) / n row by row.
+//
+// The products of dz with the router weights (dx) and with x (dW_r), small
+// calls: dx_kernel and dw_kernel on fp32 matrix instructions, straight from
+// memory.  Larger ones: the bf16 instructions, which are 16 times as fast, on
+// fp32 numbers written as sums of bf16 parts (each part the rounding of what the
+// ones before leave, so three hold 24 bits or more, two 16): dz in three parts, x
+// as it is (bf16) or in three, the router weights in two (dx in bf16) or three.
+// dW_r takes every product of parts, dx those above its precision (loss_gemm's
+// FOLD).  Tokens that do not count are left out of the reduction (loss_gemm's
+// GATHER), so nothing of theirs is read.
 #include <math.h>
 
 #include <algorithm>
 
-#include "eat_device.h"
-#include "eat_internal.h"
+#include "loss_gemm.h"
 
 namespace eat {
 namespace {
@@ -26,7 +33,7 @@ struct StatArgs {
     const uint8_t* valid;
     int T, E;
     float coef, entropy_coef;
-    int32_t* head;             // {workgroups done}
+    int32_t* head;             // {., ., workgroups done}
     float* q;                  // [E] dloss / dP_e / max(n, 1)
     double* sum;               // [blocks][E]
     int32_t* cnt;              // [blocks][E + 1]: selections, then valid tokens
@@ -97,8 +104,8 @@ __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
     __threadfence();
     __syncthreads();
     if (threadIdx.x == 0)
-        last = __hip_atomic_fetch_add(a.head, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
-               static_cast<int>(gridDim.x) - 1;
+        last = gridDim.x == 1 || __hip_atomic_fetch_add(a.head + 2, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
+                                     static_cast<int>(gridDim.x) - 1;
     __syncthreads();
     if (!last) return;
     __threadfence();
@@ -148,33 +155,125 @@ __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
     if (threadIdx.x == 0) *a.loss = static_cast<float>((red[0][0] + red[0][1]) + (red[0][2] + red[0][3]));
 }
 
-__global__ void clear_kernel(int32_t* head) { *head = 0; }
+// head of a call whose tokens all count
+__global__ void head_kernel(int T, int32_t* head) {
+    head[0] = T;
+    head[1] = (T + kBK - 1) / kBK * kBK;
+    head[2] = 0;
+}
 
-constexpr int kDzWaves = 4;
+// v as a sum of three bf16 numbers, largest first
+__device__ __forceinline__ void split3(float v, uint16_t (&part)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        part[i] = f32_to_bf16(v);
+        v -= bf16_to_f32(part[i]);
+    }
+}
+
+struct PrepArgs {
+    const float* prob;
+    const uint8_t* valid;
+    const int32_t* rows;       // tokens that count, or null: all (valid null, or dz in token order alone)
+    const int32_t* head;
+    int T, E, d;
+    const float* q;
+    float* dz;                 // [T][E], or null
+    uint16_t* dzs;             // [list row][group][4][64] parts, or null
+    void* dx;                  // rows to clear where the token does not count, or null
+    int row_bytes;             // of dx
+    const float* w;            // [E][d]
+    uint16_t* ws;              // dx's stack of w's parts ([group][segs][64][d]), or null
+    int segs, map;             // part of w in each
+    const float* x;            // fp32 x to split
+    uint16_t* xs;              // [list row][3][d], or null
+    int blocks_z, blocks_w;    // workgroups of each kind of work
+};
+
+constexpr int kPrepWaves = 4;
+constexpr int kPrepThreads = kPrepWaves * kWave;
 template <int J>
-__global__ __launch_bounds__(kDzWaves * kWave) void dz_kernel(const float* prob, const uint8_t* __restrict__ valid,
-                                                              int T, int E, const float* __restrict__ q, float* dz) {
-    const int lane = lane_id();
+__global__ __launch_bounds__(kPrepThreads) void prep_kernel(PrepArgs a) {
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int E = a.E;
+    const int block = blockIdx.x;
+    if (block >= a.blocks_z + a.blocks_w) {               // x: a list row per workgroup
+        const int i = block - a.blocks_z - a.blocks_w;
+        if (i >= a.head[1]) return;
+        const bool live = i < a.head[0];
+        const int t = live && a.rows ? a.rows[i] : i;
+        for (int c = 4 * threadIdx.x; c < a.d; c += 4 * kPrepThreads) {
+            f32x4 v{};
+            if (live) v = *reinterpret_cast<const f32x4*>(a.x + static_cast<size_t>(t) * a.d + c);
+            uint16_t p[4][3];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split3(v[e], p[e]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+                *reinterpret_cast<uint2*>(a.xs + (static_cast<size_t>(i) * 3 + k) * a.d + c) =
+                    uint2{p[0][k] | static_cast<uint32_t>(p[1][k]) << 16, p[2][k] | static_cast<uint32_t>(p[3][k]) << 16};
+        }
+        return;
+    }
+    if (block >= a.blocks_z) {                            // w: an expert (or a row of zeros) per workgroup
+        const int e = block - a.blocks_z, grp = e / 64;
+        for (int c = 4 * threadIdx.x; c < a.d; c += 4 * kPrepThreads) {
+            f32x4 v{};
+            if (e < E) v = *reinterpret_cast<const f32x4*>(a.w + static_cast<size_t>(e) * a.d + c);
+            uint16_t p[4][3];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) split3(v[k], p[k]);
+            for (int sg = 0; sg < a.segs; ++sg) {
+                const int k = (a.map >> (4 * sg)) & 15;
+                auto pick = [&](int u) { return k == 0 ? p[u][0] : k == 1 ? p[u][1] : p[u][2]; };
+                *reinterpret_cast<uint2*>(a.ws + ((static_cast<size_t>(grp) * a.segs + sg) * 64 + e % 64) * a.d + c) =
+                    uint2{pick(0) | static_cast<uint32_t>(pick(1)) << 16, pick(2) | static_cast<uint32_t>(pick(3)) << 16};
+            }
+        }
+        return;
+    }
+    // lane l: experts l % EP + 64 j of row l / EP of the wave's
     int ep = 1;
     while (ep < min(E, 64)) ep *= 2;
     const int sub = lane / ep, e0 = lane % ep, tpw = kWave / ep;
-    const int t = (blockIdx.x * kDzWaves + threadIdx.x / kWave) * tpw + sub;
-    const bool live = t < T && (!valid || valid[t < T ? t : 0]);
+    const int i = (block * kPrepWaves + wave) * tpw + sub;
+    // the token at this place: cleared where it does not count
+    if (i < a.T && a.valid && !a.valid[i]) {
+        if (a.dz)
+            for (int e = e0; e < E; e += ep) a.dz[static_cast<size_t>(i) * E + e] = 0.f;
+        if (a.dx)
+            for (int c = 16 * e0; c < a.row_bytes; c += 16 * ep)
+                *reinterpret_cast<uint4*>(static_cast<char*>(a.dx) + static_cast<size_t>(i) * a.row_bytes + c) = uint4{};
+    }
+    // the row of the list at this place (without a list: the token)
+    const int n = a.rows ? a.head[0] : a.T, pad = a.dzs ? a.head[1] : n;
+    const int t = a.rows ? (i < n ? a.rows[i] : 0) : i;
+    const bool live = i < n && (a.rows || !a.valid || a.valid[t]);
     float p[J], qe[J];
     double s = 0.0;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int e = 64 * j + e0;
-        p[j] = live && e < E ? prob[static_cast<size_t>(t) * E + e] : 0.f;
-        qe[j] = e < E ? q[e] : 0.f;
+        p[j] = live && e < E ? a.prob[static_cast<size_t>(t) * E + e] : 0.f;
+        qe[j] = e < E ? a.q[e] : 0.f;
         s += static_cast<double>(qe[j]) * p[j];
     }
     for (int o = ep / 2; o >= 1; o /= 2) s += __shfl_xor(s, o, kWave);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int e = 64 * j + e0;
-        if (t < T && e < E)
-            dz[static_cast<size_t>(t) * E + e] = live ? p[j] * static_cast<float>(qe[j] - s) : 0.f;
+        const float v = live && e < E ? p[j] * static_cast<float>(qe[j] - s) : 0.f;
+        if (a.dz && live && e < E) a.dz[static_cast<size_t>(t) * E + e] = v;
+        if (a.dzs && i < pad) {
+            uint16_t part[3];
+            split3(v, part);
+            uint16_t* const o = a.dzs + (static_cast<size_t>(i) * J + j) * 256;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                o[64 * k + e0] = part[k];
+                for (int z = e0 + ep; z < 64; z += ep) o[64 * k + z] = 0;
+            }
+        }
     }
 }
 
@@ -244,25 +343,31 @@ __global__ __launch_bounds__(256) void dw_kernel(const float* __restrict__ dz, c
         }
 }
 
-__global__ __launch_bounds__(256) void dw_join_kernel(const float* __restrict__ part, int splits, int64_t n, float scale,
-                                                      float* dw) {
-    const int64_t i = 4 * (blockIdx.x * int64_t(256) + threadIdx.x);
+// dW_r: the slices' rows of `parts` blocks of d added in order, times scale.
+__global__ __launch_bounds__(256) void dw_join_kernel(const float* __restrict__ part, int splits, int parts, int E, int d,
+                                                      float scale, float* dw) {
+    const int64_t i = 4 * (blockIdx.x * int64_t(256) + threadIdx.x), n = static_cast<int64_t>(E) * d;
     if (i >= n) return;
-    f32x4 s = *reinterpret_cast<const f32x4*>(part + i);
-    for (int k = 1; k < splits; ++k) s += *reinterpret_cast<const f32x4*>(part + k * n + i);
+    const int64_t e = i / d, c = i % d;
+    f32x4 s{};
+    for (int k = 0; k < splits; ++k)
+        for (int u = 0; u < parts; ++u)
+            s += *reinterpret_cast<const f32x4*>(part + (k * static_cast<int64_t>(E) + e) * parts * d + u * static_cast<int64_t>(d) + c);
     *reinterpret_cast<f32x4*>(dw + i) = s * scale;
 }
 
+using Fold = Tile<256, 256, 4, 2, 2>;
+
+// Products on the split operands from here on, on fp32 instructions below.
+bool split_products(const eat_params_t& p, int32_t T) {
+    return static_cast<int64_t>(T) * p.E * p.d_model >= (int64_t{1} << 27);
+}
+
 template <int J>
-hipError_t launch_rows(const eat_params_t& p, const BalancePlan& b, const BalanceCall& c, const StatArgs& a, float* dz,
-                       bool grads, hipStream_t s) {
+hipError_t launch_rows(const eat_params_t& p, const BalancePlan& b, const StatArgs& a, const PrepArgs* prep, int blocks,
+                       hipStream_t s) {
     stat_kernel<J><<<b.blocks, kStatThreads, 0, s>>>(a);
-    if (grads && c.T > 0) {
-        int ep = 1;
-        while (ep < std::min(p.E, 64)) ep *= 2;
-        const int per = kDzWaves * (kWave / ep);
-        dz_kernel<J><<<(c.T + per - 1) / per, kDzWaves * kWave, 0, s>>>(c.prob, c.valid, c.T, p.E, a.q, dz);
-    }
+    if (prep && blocks) prep_kernel<J><<<blocks, kPrepThreads, 0, s>>>(*prep);
     return hipGetLastError();
 }
 
@@ -273,13 +378,59 @@ hipError_t launch_products(const eat_params_t& p, const BalancePlan& b, const Ba
     if (c.dw) {
         dw_kernel<XT><<<dim3((E + 63) / 64, d / 64, b.splits), 256, 0, s>>>(dz, static_cast<const XT*>(c.x), c.valid, c.T, E,
                                                                            d, dwp);
-        const int64_t n = static_cast<int64_t>(E) * d;
-        dw_join_kernel<<<static_cast<int>((n / 4 + 255) / 256), 256, 0, s>>>(dwp, b.splits, n, p.inv_temperature, c.dw);
+        dw_join_kernel<<<static_cast<int>((static_cast<int64_t>(E) * d / 4 + 255) / 256), 256, 0, s>>>(
+            dwp, b.splits, 1, E, d, p.inv_temperature, c.dw);
     }
     if (c.dx && c.T > 0)
         dx_kernel<XT><<<dim3((c.T + 63) / 64, d / 64), 256, 0, s>>>(dz, c.w_router, c.T, E, d, p.inv_temperature,
                                                                      static_cast<XT*>(c.dx));
     return hipGetLastError();
+}
+
+// Parts of dz (low nibble first) and of the router weights that meet in dx:
+// bf16 rows keep 2^-8, so the products of parts down to 2^-16 of the largest do;
+// fp32 rows take those down to 2^-24.
+constexpr int kSegs16 = 3, kDz16 = 0x010, kW16 = 0x100;
+constexpr int kSegs32 = 6, kDz32 = 0x211000, kW32 = 0x010210;
+
+hipError_t launch_split(const eat_params_t& p, const BalancePlan& b, const BalanceCall& c, const int32_t* rows,
+                        const int32_t* head, char* ws, hipStream_t s) {
+    const int E = p.E, d = p.d_model, groups = (E + 63) / 64;
+    const bool bf16 = p.act_dtype == EAT_BF16;
+    const uint16_t* const dzs = reinterpret_cast<const uint16_t*>(ws + b.dzs);
+    hipError_t e = hipSuccess;
+    if (c.dw) {
+        float* const dwp = reinterpret_cast<float*>(ws + b.dwp);
+        const int parts = bf16 ? 1 : 3;
+        GemmArgs g{};
+        g.a = bf16 ? static_cast<const uint16_t*>(c.x) : reinterpret_cast<const uint16_t*>(ws + b.xs);
+        g.lda = g.na = parts * d;
+        g.a_rows = bf16 ? c.T : 1 << 30;
+        g.k_rows = rows;
+        g.b = dzs; g.ldb = 256 * groups; g.nb = E;
+        g.K = (c.T + kBK - 1) / kBK * kBK; g.k_dev = head + 1;
+        g.splits = b.splits;
+        g.out = dwp; g.ldo = parts * d; g.split_stride = static_cast<int64_t>(E) * parts * d;
+        e = bf16 && rows ? launch_gemm<Fold, true, true, PART, true, true>(g, s)
+                         : launch_gemm<Fold, true, true, PART, true, false>(g, s);
+        if (e == hipSuccess) {
+            dw_join_kernel<<<static_cast<int>((static_cast<int64_t>(E) * d / 4 + 255) / 256), 256, 0, s>>>(
+                dwp, b.splits, parts, E, d, p.inv_temperature, c.dw);
+            e = hipGetLastError();
+        }
+    }
+    if (c.dx && e == hipSuccess) {
+        GemmArgs g{};
+        g.segs = bf16 ? kSegs16 : kSegs32;
+        g.map = bf16 ? kDz16 : kDz32;
+        g.K = g.a_rows = groups * g.segs * 64;
+        g.a = reinterpret_cast<const uint16_t*>(ws + b.ws); g.lda = g.na = d;
+        g.b = dzs; g.ldb = 256 * groups; g.nb = c.T; g.nb_dev = head;
+        g.splits = 1;
+        g.out = c.dx; g.ldo = d; g.rows = rows; g.factor = p.inv_temperature;
+        e = bf16 ? launch_gemm<Fold, true, false, ROWS, true>(g, s) : launch_gemm<Fold, true, false, ROWS32, true>(g, s);
+    }
+    return e;
 }
 
 }  // namespace
@@ -289,38 +440,80 @@ BalancePlan plan_balance(const eat_params_t& p, int32_t T) {
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += (bytes + 255) & ~size_t(255); return at; };
     b.blocks = std::max(1, std::min(kStatBlocks, (T + 63) / 64));
-    const int64_t items = static_cast<int64_t>((p.E + 63) / 64) * (p.d_model / 64);
+    b.split = split_products(p, T);
+    const size_t groups = (p.E + 63) / 64, d = p.d_model, pad = (static_cast<size_t>(T) + 255) / 256 * 256;
+    const int parts = b.split && p.act_dtype != EAT_BF16 ? 3 : 1;
+    // dw_router: slices of the tokens until the CUs have an item each (four
+    // small ones of the fp32 kernel), none under 4 chunks (64 tokens)
+    const int64_t items = b.split ? groups * ((parts * d + Fold::NA - 1) / Fold::NA) : groups * (d / 64);
     b.splits = 1;
-    while (items * b.splits * 2 <= 1024 && T / (b.splits * 2) >= 64) b.splits *= 2;
-    b.head = take(4);
+    while (items * b.splits * 2 <= (b.split ? 256 : 1024) && T / (b.splits * 2) >= (b.split ? 4 * kBK : 64)) b.splits *= 2;
+    b.head = take(12);
+    b.rows = take(b.split ? pad * 4 : 0);
     b.q = take(static_cast<size_t>(p.E) * 4);
     b.sum = take(static_cast<size_t>(b.blocks) * p.E * 8);
     b.cnt = take(static_cast<size_t>(b.blocks) * (p.E + 1) * 4);
-    b.dz = take(static_cast<size_t>(T) * p.E * 4);
-    b.dwp = take(static_cast<size_t>(b.splits) * p.E * p.d_model * 4);
+    b.dz = take(b.split ? 0 : static_cast<size_t>(T) * p.E * 4);
+    b.dzs = take(b.split ? pad * groups * 256 * 2 : 0);
+    b.ws = take(b.split ? groups * (p.act_dtype == EAT_BF16 ? kSegs16 : kSegs32) * 64 * d * 2 : 0);
+    b.xs = take(parts == 3 ? pad * 3 * d * 2 : 0);
+    b.dwp = take(static_cast<size_t>(b.splits) * parts * p.E * d * 4);
     b.total = off;
     return b;
 }
 
 hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const BalanceCall& c, char* ws, hipStream_t s) {
-    const StatArgs a{c.prob, c.mask, c.valid, c.T, p.E, c.coef, c.entropy_coef, reinterpret_cast<int32_t*>(ws + b.head),
-                     reinterpret_cast<float*>(ws + b.q), reinterpret_cast<double*>(ws + b.sum),
-                     reinterpret_cast<int32_t*>(ws + b.cnt), c.loss, c.count, c.mean_prob};
-    float* const dz = c.dlogits ? c.dlogits : reinterpret_cast<float*>(ws + b.dz);
-    const bool grads = c.dlogits || c.dx || c.dw;
-    clear_kernel<<<1, 1, 0, s>>>(a.head);
+    int32_t* const head = reinterpret_cast<int32_t*>(ws + b.head);
+    float* const q = reinterpret_cast<float*>(ws + b.q);
+    const StatArgs a{c.prob, c.mask, c.valid, c.T, p.E, c.coef, c.entropy_coef, head, q,
+                     reinterpret_cast<double*>(ws + b.sum), reinterpret_cast<int32_t*>(ws + b.cnt), c.loss, c.count,
+                     c.mean_prob};
+    const bool products = c.dx || c.dw, split = b.split && products;
+    const bool bf16 = p.act_dtype == EAT_BF16;
+    int32_t* const list = split && c.valid ? reinterpret_cast<int32_t*>(ws + b.rows) : nullptr;
+    if (list) list_kernel<uint8_t><<<1, kListThreads, 0, s>>>(c.valid, c.T, 0, list, head);
+    else if (b.blocks > 1 || split) head_kernel<<<1, 1, 0, s>>>(c.T, head);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    switch ((p.E + 63) / 64) {
-        case 1: e = launch_rows<1>(p, b, c, a, dz, grads, s); break;
-        case 2: e = launch_rows<2>(p, b, c, a, dz, grads, s); break;
-        case 3: e = launch_rows<3>(p, b, c, a, dz, grads, s); break;
-        default: e = launch_rows<4>(p, b, c, a, dz, grads, s); break;
+    float* const dz = c.dlogits ? c.dlogits : products && !split ? reinterpret_cast<float*>(ws + b.dz) : nullptr;
+    PrepArgs r{};
+    r.prob = c.prob; r.valid = c.valid; r.rows = list; r.head = head;
+    r.T = c.T; r.E = p.E; r.d = p.d_model;
+    r.q = q; r.dz = dz;
+    int ep = 1;
+    while (ep < std::min(p.E, 64)) ep *= 2;
+    const int per = kPrepWaves * (kWave / ep);
+    const int places = split ? (c.T + kBK - 1) / kBK * kBK : c.T;      // rows of dz there are
+    r.blocks_z = dz || split ? (places + per - 1) / per : 0;
+    int blocks = r.blocks_z;
+    if (split) {
+        r.dzs = reinterpret_cast<uint16_t*>(ws + b.dzs);
+        if (c.dx) {
+            r.dx = c.dx; r.row_bytes = p.d_model * (bf16 ? 2 : 4);
+            r.w = c.w_router;
+            r.ws = reinterpret_cast<uint16_t*>(ws + b.ws);
+            r.segs = bf16 ? kSegs16 : kSegs32;
+            r.map = bf16 ? kW16 : kW32;
+            r.blocks_w = (p.E + 63) / 64 * 64;
+            blocks += r.blocks_w;
+        }
+        if (c.dw && !bf16) {
+            r.x = static_cast<const float*>(c.x);
+            r.xs = reinterpret_cast<uint16_t*>(ws + b.xs);
+            blocks += places;
+        }
     }
-    if (e != hipSuccess || (!c.dx && !c.dw)) return e;
+    const PrepArgs* const rp = dz || split ? &r : nullptr;
+    switch ((p.E + 63) / 64) {
+        case 1: e = launch_rows<1>(p, b, a, rp, blocks, s); break;
+        case 2: e = launch_rows<2>(p, b, a, rp, blocks, s); break;
+        case 3: e = launch_rows<3>(p, b, a, rp, blocks, s); break;
+        default: e = launch_rows<4>(p, b, a, rp, blocks, s); break;
+    }
+    if (e != hipSuccess || !products) return e;
+    if (split) return launch_split(p, b, c, list, head, ws, s);
     float* const dwp = reinterpret_cast<float*>(ws + b.dwp);
-    return p.act_dtype == EAT_BF16 ? launch_products<uint16_t>(p, b, c, dz, dwp, s)
-                                   : launch_products<float>(p, b, c, dz, dwp, s);
+    return bf16 ? launch_products<uint16_t>(p, b, c, dz, dwp, s) : launch_products<float>(p, b, c, dz, dwp, s);
 }
 
 }  // namespace eat

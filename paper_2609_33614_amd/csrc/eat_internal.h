@@ -269,8 +269,9 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s);
 
 // The router's balance loss with gradients (balance.hip).
 struct BalancePlan {
-    size_t head, q, sum, cnt, dz, dwp, total;
+    size_t head, rows, q, sum, cnt, dz, dzs, ws, xs, dwp, total;
     int blocks;              // workgroups of the column sums
+    bool split;              // products on bf16 parts (else on fp32 instructions)
     int splits;              // token slices of dw_router
 };
 struct BalanceCall {

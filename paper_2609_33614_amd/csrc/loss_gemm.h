@@ -1,0 +1,550 @@
+// The products of the losses' gradients (gfx950):
+//   C[b][a] = sum_k A[a][k] B[b][k]
+// in bf16 with fp32 accumulation on v_mfma_f32_32x32x16_bf16 (a lane ends with
+// 4 consecutive columns a of one row b).  Either operand may be stored with
+// its reduction index as the row ("columns": the head for dh; G and h for dW):
+// its LDS tile is then [k][index], and the fragments come out of transposing
+// LDS reads (ds_read_b64_tr_b16: the 16 lanes of a group read a 4 x 16 block, 4
+// lanes a row, and each gets a column of it), so no operand is transposed in
+// memory.  The kernel's output side is one of Out: the cross entropy's first
+// pass (LSE) and its recomputed pieces (GRAD), fp32 slices of a split reduction
+// (PART), finished rows (ROWS).
+//
+// The header's kernels are instantiated by ce.hip and balance.hip.
+#pragma once
+#include <algorithm>
+
+#include "eat_device.h"
+#include "eat_internal.h"
+
+namespace eat {
+namespace {
+
+constexpr int kBK = 64;                   // reduction chunk (bf16 elements)
+constexpr float kLog2e = 1.44269504088896340736f;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// NA x NB outputs per workgroup, WA x WB waves over them, a ring of STAGES
+// chunks in LDS.
+template <int NA_, int NB_, int WA_, int WB_, int STAGES_>
+struct Tile {
+    static constexpr int NA = NA_, NB = NB_, WA = WA_, WB = WB_, STAGES = STAGES_;
+    static constexpr int kWaves = WA * WB;
+    static constexpr int kThreads = kWaves * kWave;
+    static constexpr int FA = NA / (32 * WA), FB = NB / (32 * WB);    // 32-wide fragments per wave
+    static constexpr int kA = NA * kBK * 2, kB = NB * kBK * 2;        // bytes of a stage's operands
+    static constexpr int kStage = kA + kB;
+    static constexpr int kLA = kA / 1024 / kWaves, kLB = kB / 1024 / kWaves;   // 1 KB loads per wave
+    static constexpr int kLoads = kLA + kLB;
+    static constexpr int kP = STAGES - 1;     // chunks in flight ahead of the one computed
+    static_assert(kLA * 1024 * kWaves == kA && kLB * 1024 * kWaves == kB, "loads split evenly over the waves");
+    static_assert(FA * 32 * WA == NA && FB * 32 * WB == NB, "fragments cover the tile");
+    static_assert(kP >= 1 && kP <= 3, "wait counts cover up to three chunks in flight");
+};
+using Big = Tile<256, 256, 4, 2, 2>;
+using Small = Tile<128, 64, 4, 2, 4>;
+
+enum Out { LSE, GRAD, PART, ROWS, ROWS32 };
+
+struct GemmArgs {
+    const uint16_t* a;
+    const uint16_t* b;
+    int lda, ldb;              // elements between stored rows
+    int na, nb, K;             // output columns and rows, reduction length (nb, K: upper bounds where *_dev is set)
+    const int32_t* nb_dev;     // rows of the output, on the device (or null)
+    const int32_t* k_dev;      // reduction length, on the device (or null)
+    int a_rows;                // stored rows of a "columns" A operand (later ones read the last)
+    const int32_t* k_rows;     // GATHER: the stored row of A of each reduction element (whole chunks of them)
+    int segs, map;             // FOLD, B by rows: see loss_gemm
+    int splits;                // slices of the reduction (PART)
+    int col0;                  // LSE, GRAD: vocabulary index of column 0
+    int xcds;
+    void* out;                 // GRAD, ROWS, LSE: bf16; ROWS32: fp32; PART: fp32 slices
+    int64_t ldo, split_stride;
+    int kept;                  // LSE: columns below it leave exp(z - the tile's maximum) in out
+    const int32_t* rows;       // ROWS, ROWS32: destination of each output row (or null: itself)
+    const float* coef;         // ROWS: factor c on the device, or null: factor
+    float factor;
+    int add;                   // PART: add to what the slices hold
+    float2* part;              // LSE: [column tile][ldpart] (maximum, sum) pairs
+    int ldpart;
+    const int32_t* target;     // LSE, GRAD: column that is the row's target
+    const float2* stats;       // GRAD: (lse log2 e, G at the target) of a row
+};
+
+// Operands stored row by row: LDS rows of 128 bytes (64 k), 16-byte slots XORed
+// with the row's 256-byte line, so that an MFMA operand read of 16 rows covers
+// every bank.
+__device__ __forceinline__ int swz_row(int r) { return (static_cast<unsigned>(r) >> 1) & 7; }
+// Operands stored by columns: LDS rows of N indices for each of the 64 k.  A
+// transposing read takes 64 bytes of each of 4 consecutive k: XORing the slot
+// with 4 (k % 4) puts them on different banks.
+__device__ __forceinline__ int swz_col(int k) { return (k & 3) << 2; }
+
+// Loads of one operand's part of a chunk: where lane l of load j gets the 16
+// bytes that belong at LDS byte 1024 (wave + kWaves j) + 16 l.
+template <int N, int L, int WAVES, bool COLS, bool GATHER = false>
+struct Operand {
+    const char* base;          // uniform: the item's first chunk
+    uint32_t ldbytes;
+    uint32_t off[L];           // rows: byte offset; columns: that of the index
+    int k_last;                // columns: last stored row, from the item's first chunk (for the clamp)
+    const int32_t* rows;       // GATHER: where the item's reduction rows are stored
+    int at[GATHER ? L : 1];    // GATHER: those of the chunk issued next
+
+    // first: the tile's first index, count: indices there are (>= 1), k0: the
+    // slice's first k, k_rows: stored rows of a columns operand
+    __device__ __forceinline__ void set(const uint16_t* p, int ld, int first, int count, int k0, int k_rows) {
+        const int lane = lane_id(), wave = threadIdx.x / kWave;
+        ldbytes = static_cast<uint32_t>(ld) * 2;
+        if constexpr (COLS) {
+            base = reinterpret_cast<const char*>(p) + static_cast<size_t>(k0) * ldbytes;
+            k_last = k_rows - 1 - k0;
+            constexpr int VPR = N / 8;         // 16-byte slots per LDS row
+#pragma unroll
+            for (int j = 0; j < L; ++j) {
+                const int g = (wave + WAVES * j) * 64 + lane;
+                const int k = g / VPR, v = (g % VPR) ^ swz_col(k);
+                off[j] = static_cast<uint32_t>(min(first + 8 * v, count - 8)) * 2;
+            }
+        } else {
+            base = reinterpret_cast<const char*>(p) + static_cast<size_t>(first) * ldbytes + 2 * static_cast<size_t>(k0);
+            k_last = 0;
+#pragma unroll
+            for (int j = 0; j < L; ++j) {
+                const int r = (wave + WAVES * j) * 8 + lane / 8, v = (lane & 7) ^ swz_row(r);
+                off[j] = static_cast<uint32_t>(min(r, count - 1 - first)) * ldbytes + 16 * v;
+            }
+        }
+    }
+    __device__ __forceinline__ void look_up(int c) {
+        const int lane = lane_id(), wave = threadIdx.x / kWave;
+        if constexpr (GATHER) {
+#pragma unroll
+            for (int j = 0; j < L; ++j) at[j] = rows[c * kBK + ((wave + WAVES * j) * 64 + lane) / (N / 8)];
+        }
+    }
+    // chunk c into LDS at `st` (a load is waited for by count: the compiler
+    // adds no waits of its own for asm).  GATHER: after look_up(c).
+    __device__ __forceinline__ void issue(uint8_t* st, int c) const {
+        const int lane = lane_id(), wave = threadIdx.x / kWave;
+        const uint64_t at64 = reinterpret_cast<uint64_t>(base) + static_cast<uint64_t>(c) * (COLS ? kBK * ldbytes : kBK * 2);
+        const uint64_t src = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at64 >> 32)))) << 32 |
+                             static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at64)));
+#pragma unroll
+        for (int j = 0; j < L; ++j) {
+            uint32_t o = off[j];
+            if constexpr (GATHER) {
+                const char* p = base + static_cast<size_t>(at[j]) * ldbytes + o;
+                const uint32_t lds = __builtin_amdgcn_readfirstlane(
+                    static_cast<uint32_t>(reinterpret_cast<uintptr_t>(st + 1024 * (wave + WAVES * j))));
+                asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(p), "s"(lds) : "memory", "m0");
+                continue;
+            }
+            if constexpr (COLS) {
+                const int k = ((wave + WAVES * j) * 64 + lane) / (N / 8);
+                o += static_cast<uint32_t>(min(k, k_last - c * kBK)) * ldbytes;
+            }
+            const uint32_t lds = __builtin_amdgcn_readfirstlane(
+                static_cast<uint32_t>(reinterpret_cast<uintptr_t>(st + 1024 * (wave + WAVES * j))));
+            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+                         :: "v"(o), "s"(src), "s"(lds) : "memory", "m0");
+        }
+    }
+};
+
+// The operand fragment of indices i0 .. i0 + 31 and reduction elements 16 s ..
+// 16 s + 15 of a stage: lane l holds index i0 + l % 32, elements 8 (l / 32) ..
+// + 7.
+template <int N, bool COLS>
+__device__ __forceinline__ bf16x8 fragment(const uint8_t* st, int i0, int s) {
+    const int lane = lane_id();
+    if constexpr (COLS) {
+        const int g = lane >> 4, j = lane & 15;
+        const int k = 16 * s + 8 * (g >> 1) + (j >> 2);
+        const int slot = ((i0 >> 3) + 2 * (g & 1) + ((j & 3) >> 1)) ^ ((j >> 2) << 2);
+        const uint8_t* p = st + k * (2 * N) + 16 * slot + 8 * (j & 1);
+        typedef __attribute__((address_space(3))) s16x4* lds_t;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(p));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(p + 4 * (2 * N)));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+        const int r = i0 + (lane & 31);
+        return *reinterpret_cast<const bf16x8*>(st + r * 128 + (((2 * s + (lane >> 5)) ^ swz_row(r)) << 4));
+    }
+}
+
+struct Item {
+    int a0, b0, sp;
+};
+
+// The reference of a row's exponentials over a tile with maximum m (infinite
+// where all are -inf, whose sum is 0, or some +inf: then 0).
+__device__ __forceinline__ float tile_ref(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
+
+__device__ __forceinline__ float swap_halves(float v) { return __shfl_xor(v, 32, kWave); }
+
+// FOLD: B holds numbers of more than bf16's digits as sums of bf16 parts, in
+// groups of 64 indices of 4 parts each ([stored row][group][part][64], part 3
+// unused).  B by columns: a tile of 256 is a group, and the products with its
+// first three parts are added into one output row per index.  B by rows: the
+// reduction runs over the groups, `segs` chunks of 64 each: chunk i of a group
+// is its part (map >> 4 i) & 15 (A holds the matching rows, chunk by chunk).
+template <class C, bool ACOLS, bool BCOLS, int OUT, bool FOLD = false, bool GATHER = false>
+__global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
+    constexpr bool kFoldRows = FOLD && BCOLS;
+    static_assert(!kFoldRows || (C::NB == 256 && C::WB == 2), "a group per tile, 32 indices per wave");
+    constexpr int FA = C::FA, FB = kFoldRows ? 1 : C::FB, FL = kFoldRows ? 3 : C::FB;   // fragments of B: held, read
+    constexpr int NBO = kFoldRows ? 64 : C::NB;        // output rows per tile
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[C::STAGES * C::kStage];
+    const int nb = g.nb_dev ? min(*g.nb_dev, g.nb) : g.nb;
+    const int K = g.k_dev ? min(*g.k_dev, g.K) : g.K;
+    const int nta = (g.na + C::NA - 1) / C::NA, ntb = (nb + NBO - 1) / NBO;
+    const int splits = OUT == PART ? g.splits : 1;
+    const int chunks = (K + kBK - 1) / kBK;
+    const int work = nta * ntb * splits;
+    // contiguous parts of the work list per XCD (workgroups are dealt to XCDs
+    // round-robin), in it groups of 8 row tiles, column tile by column tile:
+    // the workgroups of an XCD that run together share both operands in its L2
+    const int xcd = blockIdx.x % g.xcds, slot = blockIdx.x / g.xcds, per_xcd = gridDim.x / g.xcds;
+    const int part = (work + g.xcds - 1) / g.xcds;
+    const int wbeg = xcd * part, wend = min(work, wbeg + part);
+    auto item_at = [&](int wid) __attribute__((always_inline)) {
+        const int sp = wid / (nta * ntb);
+        int r = wid - sp * nta * ntb;
+        const int grp = r / (8 * nta);
+        const int gb = min(8, ntb - 8 * grp);
+        r -= grp * 8 * nta;
+        Item it;
+        it.sp = __builtin_amdgcn_readfirstlane(sp);
+        it.a0 = __builtin_amdgcn_readfirstlane(r / gb * C::NA);
+        it.b0 = __builtin_amdgcn_readfirstlane((8 * grp + r % gb) * NBO);
+        return it;
+    };
+    int wid = wbeg + slot;
+    if (wid >= wend) return;                  // uniform over the workgroup
+
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int l32 = lane & 31, lh = lane >> 5;
+    const int arow = 32 * FA * (wave % C::WA), brow = 32 * FB * (wave / C::WA);
+    const float coef = (OUT == ROWS || OUT == ROWS32) ? (g.coef ? *g.coef : g.factor) : 1.f;
+
+    Operand<C::NA, C::kLA, C::kWaves, ACOLS, GATHER> oa;
+    Operand<C::NB, C::kLB, C::kWaves, BCOLS> ob;
+    int nch = 0;
+    auto slice = [&](int sp) { return chunks * sp / splits; };     // first chunk of a slice
+    auto setup = [&](const Item& it) __attribute__((always_inline)) {
+        const int c0 = slice(it.sp);
+        oa.set(g.a, g.lda, it.a0, g.na, GATHER ? 0 : c0 * kBK, g.a_rows);
+        if constexpr (GATHER) oa.rows = g.k_rows + c0 * kBK;
+        // (every stored row and column of B there is up to whole tiles)
+        ob.set(g.b, g.ldb, it.b0 / NBO * C::NB, 1 << 30, c0 * kBK, 1 << 30);
+    };
+    auto issue = [&](int stage, int c) __attribute__((always_inline)) {
+        uint8_t* st = ring + stage * C::kStage;
+        oa.issue(st, c);
+        if constexpr (GATHER) oa.look_up(min(c + 1, nch - 1));
+        ob.issue(st + C::kA, FOLD && !BCOLS ? c / g.segs * 4 + ((g.map >> (4 * (c % g.segs))) & 15) : c);
+    };
+    Item cur = item_at(wid);
+    setup(cur);
+    nch = slice(cur.sp + 1) - slice(cur.sp);
+    if constexpr (GATHER)
+        if (nch > 0) oa.look_up(0);
+#pragma unroll
+    for (int c = 0; c < C::kP; ++c)
+        if (c < nch) issue(c, c);
+    int sc = 0;                               // stage of the chunk computed next
+
+    for (;;) {
+        const int nwid = wid + per_xcd;
+        const bool more = nwid < wend;        // uniform
+        const Item nxt = more ? item_at(nwid) : cur;
+        const bool active = cur.b0 + brow < (OUT == GRAD ? (nb + kBK - 1) / kBK * kBK : nb);
+        f32x16 acc[FA][FB];
+#pragma unroll
+        for (int i = 0; i < FA; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j) acc[i][j] = f32x16{};
+
+        // one step of the ring: wait for this wave's loads of chunk c, barrier
+        // (every wave's have landed, and every wave is done with the stage
+        // before), refill that stage, compute
+        for (int c = 0; c < nch; ++c) {
+            const int after = min(C::kP - 1, nch - 1 - c);
+            if (C::kP >= 3 && after >= 2) wait_vm<(C::kP >= 3 ? 2 : 0) * C::kLoads>();
+            else if (C::kP >= 2 && after >= 1) wait_vm<(C::kP >= 2 ? 1 : 0) * C::kLoads>();
+            else wait_vm<0>();
+            lds_barrier();
+            const int si = sc == 0 ? C::STAGES - 1 : sc - 1;
+            if (c + C::kP < nch) issue(si, c + C::kP);
+            const uint8_t* st = ring + sc * C::kStage;
+            sc = sc + 1 == C::STAGES ? 0 : sc + 1;
+            if (!active) continue;
+#pragma unroll
+            for (int s = 0; s < kBK / 16; ++s) {
+                bf16x8 A[FA], B[FL];
+#pragma unroll
+                for (int j = 0; j < FL; ++j)
+                    B[j] = fragment<C::NB, BCOLS>(st + C::kA, brow + (kFoldRows ? 64 : 32) * j, s);
+#pragma unroll
+                for (int i = 0; i < FA; ++i) A[i] = fragment<C::NA, ACOLS>(st, arow + 32 * i, s);
+#pragma unroll
+                for (int j = 0; j < FL; ++j)
+#pragma unroll
+                    for (int i = 0; i < FA; ++i) {
+                        f32x16& c16 = acc[i][kFoldRows ? 0 : j];
+                        c16 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[i], B[j], c16, 0, 0, 0);
+                    }
+            }
+        }
+        lds_barrier();                        // every wave is done with the ring
+        // lane: row cur.b0 + brow + 32 j + l32, columns cur.a0 + arow + 32 i + 8 (q / 4) + 4 lh + q % 4
+        uint8_t* const tb = ring + wave * (C::STAGES * C::kStage / C::kWaves);
+        static_assert(C::STAGES * C::kStage / C::kWaves >= 4096, "a fragment's rows fit a wave's share of the ring");
+        // FA fragments' 32 rows of 64 FA bytes, turned around through the
+        // wave's share of LDS so that adjacent lanes store adjacent pieces
+        auto store16 = [&](int j, auto val, auto dst, int nv) __attribute__((always_inline)) {
+            constexpr int V = 4 * FA;         // 16-byte pieces per row
+            auto at = [&](int r, int v) { return r * (64 * FA) + ((v ^ (FA == 2 ? r & 7 : (r >> 1) & 3)) << 4); };
+#pragma unroll
+            for (int i = 0; i < FA; ++i)
+#pragma unroll
+                for (int qb = 0; qb < 4; ++qb)
+                    *reinterpret_cast<uint2*>(tb + at(l32, 4 * i + qb) + 8 * lh) =
+                        uint2{pack_bf16x2(val(i, 4 * qb), val(i, 4 * qb + 1)),
+                              pack_bf16x2(val(i, 4 * qb + 2), val(i, 4 * qb + 3))};
+            wave_lds_sync();
+#pragma unroll
+            for (int k = 0; k < 32 * V / 64; ++k) {
+                const int r = (64 / V) * k + lane / V, v = lane % V;
+                const u32x4 d = *reinterpret_cast<const u32x4*>(tb + at(r, v));
+                if (r < nv) *reinterpret_cast<u32x4*>(dst(r) + 8 * v) = d;
+            }
+            wave_lds_sync();
+        };
+        if constexpr (OUT == LSE) {
+            // the waves' maxima of a row, then its exponentials over the tile's
+            // maximum and their sum: the tile's first columns may be kept
+            float* const redm = reinterpret_cast<float*>(ring + 4096);       // [WA][NB], beside wave 0's rows
+            float* const reds = redm + C::WA * C::NB;
+            static_assert(4096 + 8 * C::WA * C::NB <= C::STAGES * C::kStage / C::kWaves, "within wave 0's share");
+            const int v0 = cur.a0 + arow + 4 * lh;
+            const bool tail = cur.a0 + C::NA > g.na;
+            const bool kept = cur.a0 < g.kept;
+            const int at = (wave % C::WA) * C::NB + brow + l32;
+#pragma unroll
+            for (int j = 0; j < FB; ++j) {
+                const int row = cur.b0 + brow + 32 * j + l32;
+                const int rel = row < nb ? g.target[row] - g.col0 - v0 : -1;      // the target counts as no column
+                if (ballot(rel >= 0 && rel < 32 * FA) || tail) {
+#pragma unroll
+                    for (int i = 0; i < FA; ++i)
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) {
+                            const int v = 32 * i + 8 * (q / 4) + q % 4;
+                            if (v == rel || v0 + v >= g.na) acc[i][j][q] = -INFINITY;
+                        }
+                }
+                float m = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < FA; ++i)
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) m = fmaxf(m, acc[i][j][q]);
+                m = fmaxf(m, swap_halves(m));
+                if (lh == 0) redm[at + 32 * j] = m;
+            }
+            lds_barrier();
+#pragma unroll
+            for (int j = 0; j < FB; ++j) {
+                float m = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < C::WA; ++w) m = fmaxf(m, redm[w * C::NB + brow + 32 * j + l32]);
+                const float ref = tile_ref(m);
+                float s = 0.f;
+#pragma unroll
+                for (int i = 0; i < FA; ++i)
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        acc[i][j][q] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], kLog2e, -ref * kLog2e));
+                        s += acc[i][j][q];
+                    }
+                s += swap_halves(s);
+                if (lh == 0) reds[at + 32 * j] = s;
+                const int row0 = cur.b0 + brow + 32 * j;
+                if (kept && row0 < nb)
+                    store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q]; },
+                            [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; },
+                            nb - row0);
+            }
+            lds_barrier();
+            for (int r = threadIdx.x; r < C::NB; r += C::kThreads) {
+                float m = -INFINITY, s = 0.f;
+#pragma unroll
+                for (int w = 0; w < C::WA; ++w) {
+                    m = fmaxf(m, redm[w * C::NB + r]);
+                    s += reds[w * C::NB + r];
+                }
+                if (m == INFINITY && s == s) s = 1.f;      // (some are +inf: the row's NLL is)
+                if (cur.b0 + r < nb) g.part[static_cast<size_t>(cur.a0 / C::NA) * g.ldpart + cur.b0 + r] = float2{m, s};
+            }
+        } else if (active) {
+            const int nrow = OUT == GRAD ? (nb + kBK - 1) / kBK * kBK : nb;
+#pragma unroll
+            for (int j = 0; j < FB; ++j) {
+                const int row0 = cur.b0 + brow + 32 * j;
+                const int nv = min(32, nrow - row0);
+                if (nv <= 0) break;
+                if constexpr (OUT == GRAD) {
+                    const int row = row0 + l32;
+                    const bool live = row < nb;
+                    const float2 st = live ? g.stats[row] : float2{0.f, 0.f};
+                    const int rel = (live ? g.target[row] : -1) - (g.col0 + cur.a0 + arow + 4 * lh);
+                    const int end = live ? g.na - (cur.a0 + arow + 4 * lh) : 0;     // columns of the piece from here on
+                    store16(j, [&](int i, int q) __attribute__((always_inline)) {
+                        const int v = 32 * i + 8 * (q / 4) + q % 4;
+                        float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], kLog2e, -st.x));
+                        p = v == rel ? st.y : p;
+                        return v < end ? p : 0.f;
+                    }, [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; }, nv);
+                } else if constexpr (OUT == ROWS) {
+                    if (cur.a0 + arow >= g.na) break;      // (columns come in multiples of 64)
+                    store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q] * coef; },
+                            [&](int r) {
+                                const int64_t to = g.rows && r < nv ? g.rows[row0 + r] : row0 + r;
+                                return static_cast<uint16_t*>(g.out) + to * g.ldo + cur.a0 + arow;
+                            }, nv);
+                } else {
+                    auto at = [&](int r, int v) { return r * 128 + ((v ^ (r & 7)) << 4); };
+#pragma unroll
+                    for (int i = 0; i < FA; ++i) {
+                        const int col = cur.a0 + arow + 32 * i;
+                        if (col >= g.na) break;
+#pragma unroll
+                        for (int qb = 0; qb < 4; ++qb)
+                            *reinterpret_cast<f32x4*>(tb + at(l32, 2 * qb + lh)) =
+                                f32x4{acc[i][j][4 * qb], acc[i][j][4 * qb + 1], acc[i][j][4 * qb + 2], acc[i][j][4 * qb + 3]};
+                        wave_lds_sync();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int r = 8 * k + lane / 8, v = lane % 8;
+                            f32x4 d = *reinterpret_cast<const f32x4*>(tb + at(r, v));
+                            if (r < nv && OUT == ROWS32) {
+                                const int64_t to = g.rows ? g.rows[row0 + r] : row0 + r;
+                                *reinterpret_cast<f32x4*>(static_cast<float*>(g.out) + to * g.ldo + col + 4 * v) = d * coef;
+                            } else if (r < nv) {
+                                float* const p = static_cast<float*>(g.out) + cur.sp * g.split_stride +
+                                                 (row0 + r) * g.ldo + col + 4 * v;
+                                if (g.add) d += *reinterpret_cast<const f32x4*>(p);
+                                *reinterpret_cast<f32x4*>(p) = d;
+                            }
+                        }
+                        wave_lds_sync();
+                    }
+                }
+            }
+        }
+        if (!more) break;
+        cur = nxt;
+        wid = nwid;
+        __syncthreads();
+        setup(cur);
+        nch = slice(cur.sp + 1) - slice(cur.sp);
+        sc = 0;
+        if constexpr (GATHER)
+            if (nch > 0) oa.look_up(0);
+#pragma unroll
+        for (int c = 0; c < C::kP; ++c)
+            if (c < nch) issue(c, c);
+    }
+}
+
+// rows[0 .. n): the indices t < T whose key is not `skip`, in order, and the
+// last of them again up to a whole reduction chunk; head: {n, n rounded up to
+// whole chunks, 0}.  One workgroup: the list is a running count over the call.
+constexpr int kListThreads = 1024, kListLoads = 8;
+template <typename Key>
+__global__ __launch_bounds__(kListThreads) void list_kernel(const Key* __restrict__ key, int T, Key skip, int32_t* rows,
+                                                            int32_t* head) {
+    constexpr int NW = kListThreads / kWave;
+    __shared__ int cnt[kListLoads][NW];
+    __shared__ int lastrow;
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const uint64_t below = lane == 0 ? 0ull : ~0ull >> (kWave - lane);
+    int base = 0;
+    for (int t0 = 0; t0 < T; t0 += kListThreads * kListLoads) {
+        bool keep[kListLoads];
+        uint64_t m[kListLoads];
+#pragma unroll
+        for (int i = 0; i < kListLoads; ++i) {
+            const int t = t0 + i * kListThreads + threadIdx.x;
+            keep[i] = t < T && key[t < T ? t : 0] != skip;
+        }
+#pragma unroll
+        for (int i = 0; i < kListLoads; ++i) {
+            m[i] = ballot(keep[i]);
+            if (lane == 0) cnt[i][wave] = __popcll(m[i]);
+        }
+        __syncthreads();
+        int pos[kListLoads];
+#pragma unroll
+        for (int i = 0; i < kListLoads; ++i) {
+            pos[i] = base + __popcll(m[i] & below);
+            for (int w = 0; w < NW; ++w) {
+                const int c = cnt[i][w];
+                pos[i] += w < wave ? c : 0;
+                base += c;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kListLoads; ++i)
+            if (keep[i]) {
+                const int t = t0 + i * kListThreads + threadIdx.x;
+                rows[pos[i]] = t;
+                if (pos[i] == base - 1) lastrow = t;
+            }
+        __syncthreads();
+    }
+    const int pad = (base + kBK - 1) / kBK * kBK;
+    for (int i = base + threadIdx.x; i < pad; i += kListThreads) rows[i] = lastrow;
+    if (threadIdx.x == 0) {
+        head[0] = base;
+        head[1] = pad;
+        head[2] = 0;
+    }
+}
+
+struct Geometry {
+    int cus, xcds;
+};
+const Geometry& geometry() {
+    static const Geometry g = [] {
+        int dev = 0, cus = 0, xccs = 0;
+        if (hipGetDevice(&dev) != hipSuccess ||
+            hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1)
+            cus = 256;
+        if (hipDeviceGetAttribute(&xccs, hipDeviceAttributeNumberOfXccs, dev) != hipSuccess || xccs < 1 || xccs > cus)
+            xccs = 1;
+        return Geometry{cus, xccs};
+    }();
+    return g;
+}
+
+// Persistent: a workgroup per CU (the ring fills its LDS) or per item, a
+// multiple of the XCD count.
+template <class C, bool ACOLS, bool BCOLS, int OUT, bool FOLD = false, bool GATHER = false>
+hipError_t launch_gemm(GemmArgs g, hipStream_t s) {
+    constexpr int kRows = FOLD && BCOLS ? 64 : C::NB;
+    g.xcds = geometry().xcds;
+    const int64_t work = static_cast<int64_t>((g.na + C::NA - 1) / C::NA) * ((g.nb + kRows - 1) / kRows) * g.splits;
+    if (work == 0) return hipSuccess;
+    int64_t blocks = std::min<int64_t>(work, geometry().cus);
+    blocks = std::max<int64_t>(g.xcds, (blocks + g.xcds - 1) / g.xcds * g.xcds);
+    loss_gemm<C, ACOLS, BCOLS, OUT, FOLD, GATHER><<<static_cast<int>(blocks), C::kThreads, 0, s>>>(g);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace eat

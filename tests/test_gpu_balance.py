@@ -125,14 +125,18 @@ def routed(E, d, bf16, T, mode="topk", k=2, seed=0, **kw):
 @pytest.mark.parametrize("bf16", [True, False])
 @pytest.mark.parametrize("T,E,d,k", [(1, 1, 64, 1), (1, 8, 128, 2), (3, 5, 64, 2), (32, 8, 128, 2), (63, 64, 192, 8),
                                      (65, 60, 128, 4), (100, 65, 64, 3), (200, 100, 320, 8), (257, 128, 256, 8),
-                                     (1000, 200, 128, 8), (777, 256, 512, 8), (2049, 16, 64, 1), (5000, 33, 128, 2)])
+                                     (1000, 200, 128, 8), (777, 256, 512, 8), (2049, 16, 64, 1), (5000, 33, 128, 2),
+                                     (2111, 64, 1024, 8), (1030, 256, 576, 8), (4111, 130, 320, 4), (20000, 7, 1024, 2),
+                                     (257, 256, 2112, 2), (64, 250, 8640, 8)])
 def test_loss_counts_gradients(T, E, d, k, bf16):
     layer, x, prob, mask = routed(E, d, bf16, T, k=k)
     check(f"bal {T} {E} {d}", call(layer, x, prob, mask, None), reference(layer, x, prob, mask, None, 0.01, 0.002))
 
 
 @pytest.mark.parametrize("kind", ["some", "none", "one", "tail"])
-@pytest.mark.parametrize("T,E,d,bf16", [(1, 8, 64, False), (70, 60, 128, True), (600, 130, 192, True), (600, 12, 64, False)])
+@pytest.mark.parametrize("T,E,d,bf16", [(1, 8, 64, False), (70, 60, 128, True), (600, 130, 192, True), (600, 12, 64, False),
+                                        (2300, 60, 1024, True), (2300, 60, 1024, False), (1100, 200, 640, True),
+                                        (1100, 200, 640, False)])
 def test_tokens_that_do_not_count(T, E, d, bf16, kind):
     layer, x, prob, mask = routed(E, d, bf16, T)
     valid = make_valid(T, kind)
@@ -221,9 +225,9 @@ def test_gradients_against_differences():
         assert (mine - slope).abs() <= bound, (name, float(mine), float(slope))
 
 
-@pytest.mark.parametrize("T,E", [(40, 8), (500, 128)])
-def test_every_choice_of_outputs_and_aliases(T, E):
-    layer, x, prob, mask = routed(E, 192, True, T)
+@pytest.mark.parametrize("T,E,d,bf16", [(40, 8, 192, True), (500, 128, 192, True), (2200, 128, 512, True), (2200, 128, 512, False)])
+def test_every_choice_of_outputs_and_aliases(T, E, d, bf16):
+    layer, x, prob, mask = routed(E, d, bf16, T)
     valid = make_valid(T, "some")
     full = call(layer, x, prob, mask, valid)
     for bits in range(8):
@@ -246,8 +250,8 @@ def test_empty_call():
     assert loss.item() == 0 and (count == 0).all() and (mean == 0).all() and (dw == 0).all()
 
 
-def test_other_stream_and_graph_replays():
-    T, E, d = 700, 60, 128
+@pytest.mark.parametrize("T,E,d", [(700, 60, 128), (2200, 128, 512)])
+def test_other_stream_and_graph_replays(T, E, d):
     layer, x, prob, mask = routed(E, d, True, T)
     valid = make_valid(T, "some")
     ref = call(layer, x, prob, mask, valid)
