@@ -35,7 +35,7 @@ struct StatArgs {
     float coef, entropy_coef;
     int32_t* head;             // {., ., workgroups done}
     float* q;                  // [E] dloss / dP_e / max(n, 1)
-    double* sum;               // [blocks][E]
+    double* sum;               // [blocks][E] (unused by one workgroup)
     int32_t* cnt;              // [blocks][E + 1]: selections, then valid tokens
     float* loss;
     int64_t* count;
@@ -43,116 +43,157 @@ struct StatArgs {
 };
 
 // Lane l holds experts l % EP + 64 j of token l / EP of a group of 64 / EP
-// tokens (EP: E rounded up to a power of two, 64 at most).
+// tokens (EP: E rounded up to a power of two, 64 at most); a wave has kStatRows
+// groups' loads in flight.
+constexpr int kStatRows = 4;
 template <int J>
 __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
-    __shared__ double red[kStatWaves][kWave];
-    __shared__ int redc[kStatWaves][kWave];
-    __shared__ double fin[4][kMaxExperts];
-    __shared__ int finc[4][kMaxExperts];
+    __shared__ double red[kStatWaves][kWave * J];
+    __shared__ int redc[kStatWaves][kWave * J];
     __shared__ int redn[kStatWaves];
     __shared__ int last;
-    const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int E = a.E;
+    const int lane = lane_id(), wave = threadIdx.x / kWave, tid = threadIdx.x;
+    const int E = a.E, blocks = gridDim.x;
     int ep = 1;
     while (ep < min(E, 64)) ep *= 2;
     const int sub = lane / ep, e0 = lane % ep, tpw = kWave / ep;
-    const int per = (a.T + gridDim.x - 1) / gridDim.x;
+    const int per = (a.T + blocks - 1) / blocks;
     const int tbeg = min(a.T, static_cast<int>(blockIdx.x) * per), tend = min(a.T, tbeg + per);
     double s[J];
     int c[J], n = 0;
 #pragma unroll
     for (int j = 0; j < J; ++j) { s[j] = 0.0; c[j] = 0; }
-    for (int t0 = tbeg + wave * tpw; t0 < tend; t0 += kStatWaves * tpw) {
-        const int t = t0 + sub;
-        if (t < tend && (!a.valid || a.valid[t])) {
-            n += e0 == 0;
+    for (int t0 = tbeg + wave * tpw * kStatRows; t0 < tend; t0 += kStatWaves * tpw * kStatRows) {
+        float p[kStatRows][J];
+        uint64_t m[kStatRows][J];
+        bool live[kStatRows];
+        // (every load is unconditional, of a token and an expert that exist)
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-                if (64 * j + e0 < E) {
-                    s[j] += static_cast<double>(a.prob[static_cast<size_t>(t) * E + 64 * j + e0]);
-                    c[j] += static_cast<int>((a.mask[static_cast<size_t>(t) * J + j] >> e0) & 1);
-                }
+        for (int u = 0; u < kStatRows; ++u) {
+            const int t = t0 + u * tpw + sub, ts = min(t, tend - 1);
+            live[u] = t < tend && (!a.valid || a.valid[ts]);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                p[u][j] = a.prob[static_cast<size_t>(ts) * E + min(64 * j + e0, E - 1)];
+                m[u][j] = a.mask[static_cast<size_t>(ts) * J + j];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kStatRows; ++u) {
+            n += live[u] && e0 == 0;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const bool on = live[u] && 64 * j + e0 < E;
+                s[j] += on ? static_cast<double>(p[u][j]) : 0.0;
+                c[j] += on ? static_cast<int>((m[u][j] >> e0) & 1) : 0;
+            }
         }
     }
+    for (int o = ep; o < kWave; o *= 2)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            s[j] += __shfl_xor(s[j], o, kWave);
+            c[j] += __shfl_xor(c[j], o, kWave);
+        }
     n = wave_sum(n);
     if (lane == 0) redn[wave] = n;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        red[wave][lane] = s[j];
-        redc[wave][lane] = c[j];
-        __syncthreads();
-        const int e = 64 * j + threadIdx.x;
-        if (static_cast<int>(threadIdx.x) < ep && e < E) {
-            double t = 0.0;
-            int k = 0;
-            for (int w = 0; w < kStatWaves; ++w)
-                for (int u = 0; u < tpw; ++u) {
-                    t += red[w][u * ep + threadIdx.x];
-                    k += redc[w][u * ep + threadIdx.x];
-                }
-            a.sum[static_cast<size_t>(blockIdx.x) * E + e] = t;
-            a.cnt[static_cast<size_t>(blockIdx.x) * (E + 1) + e] = k;
-        }
-        __syncthreads();
+        red[wave][64 * j + lane] = s[j];
+        redc[wave][64 * j + lane] = c[j];
     }
-    if (threadIdx.x == 0) {
-        int k = 0;
-        for (int w = 0; w < kStatWaves; ++w) k += redn[w];
-        a.cnt[static_cast<size_t>(blockIdx.x) * (E + 1) + E] = k;
-    }
-    __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0)
-        last = gridDim.x == 1 || __hip_atomic_fetch_add(a.head + 2, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
-                                     static_cast<int>(gridDim.x) - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    // the shares in order: quarter g of them per thread and expert, then the quarters
-    const int blocks = gridDim.x;
-    const int g = threadIdx.x >> 8, e = threadIdx.x & 255;
+    // an expert per thread: the waves' sums in order
     double t = 0.0;
     int k = 0, nn = 0;
-    if (e < E)
-        for (int b = blocks * g / 4; b < blocks * (g + 1) / 4; ++b) {
-            t += __hip_atomic_load(a.sum + static_cast<size_t>(b) * E + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            k += __hip_atomic_load(a.cnt + static_cast<size_t>(b) * (E + 1) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-    fin[g][e] = t;
-    finc[g][e] = k;
-    if (wave == 0) {
-        for (int b = lane; b < blocks; b += kWave)
-            nn += __hip_atomic_load(a.cnt + static_cast<size_t>(b) * (E + 1) + E, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        nn = wave_sum(nn);
-        if (lane == 0) redn[0] = nn;
-    }
-    __syncthreads();
-    // one thread per expert from here on (waves 0 to 3)
-    const double inv = 1.0 / max(redn[0], 1);
-    double p = 0.0;
-    if (wave < 4) {
-        k = finc[0][e] + finc[1][e] + finc[2][e] + finc[3][e];
-        p = (fin[0][e] + fin[1][e] + fin[2][e] + fin[3][e]) * inv;
-        // (a call's selections are below 2^31: max_tokens times the most experts of a token is)
-        const int sel = wave_sum(e < E ? k : 0);
-        if (lane == 0) redc[0][wave] = sel;
-    }
-    __syncthreads();
-    if (wave < 4) {
-        const int total = redc[0][0] + redc[0][1] + redc[0][2] + redc[0][3];
-        const double f = static_cast<double>(k) / max(total, 1);
-        const double lg = p > 0.0 ? log(p) : p == 0.0 ? 0.0 : p;      // (NaN stays)
-        const double l = wave_sum(e < E ? a.coef * E * f * p + a.entropy_coef * p * lg : 0.0);
-        if (lane == 0) red[0][wave] = l;
-        if (e < E) {
-            a.q[e] = static_cast<float>((a.coef * E * f + a.entropy_coef * (lg + 1.0)) * inv);
-            if (a.count) a.count[e] = k;
-            if (a.mean_prob) a.mean_prob[e] = static_cast<float>(p);
+    if (tid < E) {
+#pragma unroll
+        for (int w = 0; w < kStatWaves; ++w) {
+            t += red[w][tid];
+            k += redc[w][tid];
         }
     }
+    if (wave == 0) nn = wave_sum(lane < kStatWaves ? redn[lane] : 0);
+    if (blocks > 1) {
+        // the share to memory past this XCD's cache; the last workgroup reads all
+        if (tid < E) {
+            __hip_atomic_store(a.sum + static_cast<size_t>(blockIdx.x) * E + tid, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(a.cnt + static_cast<size_t>(blockIdx.x) * (E + 1) + tid, k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        if (tid == 0)
+            __hip_atomic_store(a.cnt + static_cast<size_t>(blockIdx.x) * (E + 1) + E, nn, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (tid == 0)
+            last = __hip_atomic_fetch_add(a.head + 2, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
+        __syncthreads();
+        if (!last) return;
+        // a wave takes the shares of its residue, in order, a lane per expert
+        double sj[J];
+        int cj[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) { sj[j] = 0.0; cj[j] = 0; }
+        for (int b0 = wave; b0 < blocks; b0 += 4 * kStatWaves) {
+            double v[4][J];
+            int w[4][J];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int bs = min(b0 + u * kStatWaves, blocks - 1);
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int e = min(64 * j + lane, E - 1);
+                    v[u][j] = __hip_atomic_load(a.sum + static_cast<size_t>(bs) * E + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    w[u][j] = __hip_atomic_load(a.cnt + static_cast<size_t>(bs) * (E + 1) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const bool on = b0 + u * kStatWaves < blocks;
+                    sj[j] += on ? v[u][j] : 0.0;
+                    cj[j] += on ? w[u][j] : 0;
+                }
+        }
+        nn = 0;
+        if (wave == 0) {
+            for (int b = lane; b < blocks; b += kWave)
+                nn += __hip_atomic_load(a.cnt + static_cast<size_t>(b) * (E + 1) + E, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            nn = wave_sum(nn);
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            red[wave][64 * j + lane] = sj[j];
+            redc[wave][64 * j + lane] = cj[j];
+        }
+        __syncthreads();
+        t = 0.0;
+        k = 0;
+        if (tid < E) {
+#pragma unroll
+            for (int w = 0; w < kStatWaves; ++w) {
+                t += red[w][tid];
+                k += redc[w][tid];
+            }
+        }
+    }
+    // (a call's selections are below 2^31: max_tokens times the most experts of a token is)
+    const int sel = wave_sum(tid < E ? k : 0);
     __syncthreads();
-    if (threadIdx.x == 0) *a.loss = static_cast<float>((red[0][0] + red[0][1]) + (red[0][2] + red[0][3]));
+    if (tid == 0) redn[15] = nn;
+    if (lane == 0 && wave < 4) redn[wave] = sel;
+    __syncthreads();
+    const double inv = 1.0 / max(redn[15], 1), p = t * inv;
+    const double f = static_cast<double>(k) / max(redn[0] + redn[1] + redn[2] + redn[3], 1);
+    const double lg = p > 0.0 ? log(p) : p == 0.0 ? 0.0 : p;      // (NaN stays)
+    if (tid < E) {
+        a.q[tid] = static_cast<float>((a.coef * E * f + a.entropy_coef * (lg + 1.0)) * inv);
+        if (a.count) a.count[tid] = k;
+        if (a.mean_prob) a.mean_prob[tid] = static_cast<float>(p);
+    }
+    const double l = wave_sum(tid < E ? a.coef * E * f * p + a.entropy_coef * p * lg : 0.0);
+    if (lane == 0) red[0][wave] = l;
+    __syncthreads();
+    if (tid == 0) *a.loss = static_cast<float>((red[0][0] + red[0][1]) + (red[0][2] + red[0][3]));
 }
 
 // head of a call whose tokens all count

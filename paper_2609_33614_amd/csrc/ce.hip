@@ -27,14 +27,37 @@ namespace {
 // One wave per row.  Row t of the call, where it is ignored: its NLL and its
 // dh are zero.  Row i of the list: its hidden row, its target and the target's
 // logit in fp64 (the NLL would depend most on that logit's rounding); rows
-// behind the list up to whole tiles: zeros.
-constexpr int kGatherWaves = 4;
+// behind the list up to whole tiles: zeros.  LIST (calls of up to kListedRows
+// rows): every workgroup works the list out for itself, a lane per row, instead of a
+// launch before this one (~5 us).
+constexpr int kGatherWaves = 4, kListedRows = kGatherWaves * kWave;
+template <bool LIST>
 __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
     const uint16_t* __restrict__ h, const uint16_t* __restrict__ w, const int32_t* __restrict__ target, int T, int Tpad,
-    int d, int V, int ignore, const int32_t* __restrict__ rows, const int32_t* __restrict__ head, uint16_t* hc,
-    int32_t* tc, double* zt, float* nll, uint16_t* dh) {
-    const int lane = lane_id(), i = blockIdx.x * kGatherWaves + threadIdx.x / kWave;
-    const int n = head[0];
+    int d, int V, int ignore, int32_t* rows, int32_t* head, uint16_t* hc, int32_t* tc, double* zt, float* nll,
+    uint16_t* dh) {
+    __shared__ uint64_t keep[kGatherWaves];
+    const int lane = lane_id(), i = blockIdx.x * kGatherWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    int n, t = 0;
+    if constexpr (LIST) {
+        const int at = threadIdx.x;
+        const uint64_t b = ballot(at < T && target[at < T ? at : 0] != ignore);
+        if (lane == 0) keep[at / kWave] = b;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int k = 0; k < kGatherWaves; ++k) n += __popcll(keep[k]);
+        if (i < n) t = nth_token<kGatherWaves>(keep, i);
+        if (i < n && lane == 0) rows[i] = t;
+        if (i == 0 && lane == 0) {
+            head[0] = n;
+            head[1] = (n + kBK - 1) / kBK * kBK;
+            head[2] = 0;
+        }
+    } else {
+        n = head[0];
+        if (i < n) t = rows[i];
+    }
     if (i < T && target[i] == ignore) {
         if (nll && lane == 0) nll[i] = 0.f;
         if (dh)
@@ -42,7 +65,6 @@ __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
                 *reinterpret_cast<uint4*>(dh + static_cast<size_t>(i) * d + k) = uint4{};
     }
     if (i >= Tpad || i >= (n + 255) / 256 * 256) return;
-    const int t = i < n ? rows[i] : 0;
     const int y = i < n ? target[t] : 0;
     const bool known = y >= 0 && y < V;
     double z = 0.0;
@@ -68,7 +90,7 @@ __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
 // The row's (maximum, sum) over the column tiles, a lane per row and a wave
 // per share of the tiles; then its NLL, its softmax denominator and G at its
 // target.  The last workgroup to finish adds up the loss, in row order.
-constexpr int kRowWaves = 8;
+constexpr int kRowWaves = 16, kRowLoads = 8;
 __global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(const float2* __restrict__ part, int ntiles, int ldpart,
                                                                 int32_t* head, const int32_t* __restrict__ rows,
                                                                 const int32_t* __restrict__ tc,
@@ -81,33 +103,35 @@ __global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(const float2* __
     const int lane = lane_id(), wave = threadIdx.x / kWave;
     const int n = head[0], blocks = max(1, (n + kWave - 1) / kWave);
     if (static_cast<int>(blockIdx.x) >= blocks) return;
-    const int i = blockIdx.x * kWave + lane;
+    const int i = blockIdx.x * kWave + lane, is = max(0, min(i, n - 1));
     float m = -INFINITY, s = 0.f;
     auto merge = [&](float2 p) __attribute__((always_inline)) {
         const float hi = fmaxf(m, p.x);
         s = (m == hi ? s : s * __expf(m - hi)) + (p.x == hi ? p.y : p.y * __expf(p.x - hi));
         m = hi;
     };
-    if (i < n) {
-        for (int t0 = wave; t0 < ntiles; t0 += 8 * kRowWaves) {
-            float2 p[8];
+    // (loads of a row and a tile that exist, all issued before the first use)
+    const double z = wave == 0 && n > 0 ? zt[is] : 0.0;
+    const int y = wave == 0 && n > 0 ? tc[is] : 0;
+    if (n > 0)
+        for (int t0 = wave; t0 < ntiles; t0 += kRowLoads * kRowWaves) {
+            float2 p[kRowLoads];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int t = t0 + u * kRowWaves;
-                p[u] = part[static_cast<size_t>(t < ntiles ? t : t0) * ldpart + i];
-            }
+            for (int u = 0; u < kRowLoads; ++u)
+                p[u] = part[static_cast<size_t>(min(t0 + u * kRowWaves, ntiles - 1)) * ldpart + is];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
+            for (int u = 0; u < kRowLoads; ++u)
                 if (t0 + u * kRowWaves < ntiles) merge(p[u]);
         }
-    }
     red[wave][lane] = float2{m, s};
     __syncthreads();
+    double v = 0.0;
     if (wave == 0 && i < n) {
+#pragma unroll
         for (int w = 1; w < kRowWaves; ++w) merge(red[w][lane]);
-        // (zt - zt is NaN for an infinite target, as its row's logsumexp less itself)
-        const double md = m, rest = s, z = zt[i];
-        double v, lse;
+        // (z - z is NaN for an infinite target, as its row's logsumexp less itself)
+        const double md = m, rest = s;
+        double lse;
         if (z >= md) {
             v = log1p(rest * exp(md - z)) + (z - z);
             lse = z + v;
@@ -115,21 +139,21 @@ __global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(const float2* __
             lse = md + log(rest + exp(z - md));
             v = lse - z;
         }
-        if (tc[i] < 0) v = lse = NAN;
-        nllc[i] = v;
+        if (y < 0) v = lse = NAN;
         stats[i] = float2{static_cast<float>(lse * 1.4426950408889634), static_cast<float>(expm1(-v))};
         if (nll) nll[rows[i]] = static_cast<float>(v);
+        if (blocks > 1) __hip_atomic_store(nllc + i, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    if (threadIdx.x == 0) {
-        __threadfence();
-        last = __hip_atomic_fetch_add(head + 2, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
+    double a = v;
+    if (blocks > 1) {
+        if (threadIdx.x == 0)
+            last = __hip_atomic_fetch_add(head + 2, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
+        __syncthreads();
+        if (!last) return;
+        a = 0.0;
+        for (int r = threadIdx.x; r < n; r += kRowWaves * kWave)
+            a += __hip_atomic_load(nllc + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    double a = 0.0;
-    for (int r = threadIdx.x; r < n; r += kRowWaves * kWave)
-        a += __hip_atomic_load(nllc + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     a = wave_sum(a);
     if (lane == 0) sums[wave] = a;
     __syncthreads();
@@ -215,8 +239,32 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restr
     }
 }
 
-// Calls of few rows take the tile of 64 rows, which streams the head.
-bool small_call(int T) { return T <= Small::NB; }
+// The tile of a product of `rows` x `cols` outputs with one reduction slice:
+// Small up to its 64 rows (the operand of `cols` streams past), else the larger
+// one of Big and Mid whose rounds over the CUs take less time.  (A chunk costs a
+// Big workgroup kBigNs, a Mid one kMidNs.)
+enum Size { kSmall, kMid, kBig };
+constexpr int kBigNs = 1900, kMidNs = 900, kCus = 256;
+int64_t tiles_of(int64_t rows, int64_t cols, int nb, int na) { return ((rows + nb - 1) / nb) * ((cols + na - 1) / na); }
+Size pick_tile(int64_t rows, int64_t cols) {
+    if (rows <= Small::NB) return kSmall;
+    const int64_t big = (tiles_of(rows, cols, Big::NB, Big::NA) + kCus - 1) / kCus * kBigNs;
+    const int64_t mid = (tiles_of(rows, cols, Mid::NB, Mid::NA) + kCus - 1) / kCus * kMidNs;
+    return mid < big ? kMid : kBig;
+}
+constexpr int tile_cols(Size z) { return z == kBig ? Big::NA : Mid::NA; }
+static_assert(Mid::NA == Small::NA, "column tiles of 128 or 256");
+
+// dh, whose reduction is split over what CUs its tiles leave: by the rows alone.
+Size dh_tile(int64_t rows) { return rows <= Small::NB ? kSmall : rows <= Mid::NB ? kMid : kBig; }
+
+template <bool ACOLS, bool BCOLS, int OUT>
+hipError_t launch_sized(Size z, const GemmArgs& g, hipStream_t s) {
+    if (z == kBig) return launch_gemm<Big, ACOLS, BCOLS, OUT>(g, s);
+    if (z == kMid) return launch_gemm<Mid, ACOLS, BCOLS, OUT>(g, s);
+    if constexpr (BCOLS) return launch_gemm<Mid, ACOLS, BCOLS, OUT>(g, s);      // (few entries, not few rows)
+    else return launch_gemm<Small, ACOLS, BCOLS, OUT>(g, s);
+}
 
 // G held at a time: a piece of the vocabulary whose G takes kPieceBytes at
 // most (1.4% of the card's memory) and, with a smaller workspace, what fits,
@@ -229,9 +277,9 @@ constexpr int kMinPiece = 4096;
 
 CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) {
     CePlan p{};
-    p.rows_pad = small_call(T) ? Small::NB : (T + Big::NB - 1) / Big::NB * Big::NB;
+    p.rows_pad = T <= Small::NB ? Small::NB : (T + Big::NB - 1) / Big::NB * Big::NB;
     const size_t tp = p.rows_pad;
-    p.tile = small_call(T) ? Small::NA : Big::NA;
+    p.tile = tile_cols(pick_tile(T, V));
     p.tiles = (V + p.tile - 1) / p.tile;
     const int vpad = (V + 255) / 256 * 256;
     const int least = std::min(vpad, kMinPiece);
@@ -239,10 +287,10 @@ CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) 
         return static_cast<int>(std::max<size_t>(least, std::min<size_t>(vpad, room / (2 * tp) / 256 * 256)));
     };
     // dh: slices of the reduction until the CUs have an item each, none under 4 chunks
-    const int nb = small_call(T) ? Small::NB : Big::NB;
-    const int64_t items = static_cast<int64_t>((T + nb - 1) / nb) * ((d + p.tile - 1) / p.tile);
+    const Size zh = dh_tile(T);
+    const int64_t items = tiles_of(T, d, zh == kSmall ? Small::NB : zh == kMid ? Mid::NB : Big::NB, tile_cols(zh));
     p.splits = 1;
-    while (dh && items * p.splits * 2 <= 256 && vpad / kBK / (p.splits * 2) >= 4) p.splits *= 2;
+    while (dh && items * p.splits * 2 <= kCus && vpad / kBK / (p.splits * 2) >= 4) p.splits *= 2;
     auto layout = [&](int piece) {
         size_t off = 0;
         auto take = [&](size_t n) { const size_t at = off; off += (n + 255) & ~size_t(255); return at; };
@@ -281,11 +329,17 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
     uint16_t* const gbuf = reinterpret_cast<uint16_t*>(ws + p.g);
     float* const dhp = reinterpret_cast<float*>(ws + p.dhp);
     const int T = c.T, d = c.d, V = c.V;
-    const bool small = small_call(T);
+    const Size zz = pick_tile(T, V), zh = dh_tile(T);
 
-    list_kernel<<<1, kListThreads, 0, s>>>(c.target, T, c.ignore, rows, head);
-    gather_kernel<<<(p.rows_pad + kGatherWaves - 1) / kGatherWaves, kGatherWaves * kWave, 0, s>>>(
-        c.h, c.w, c.target, T, p.rows_pad, d, V, c.ignore, rows, head, hc, tc, zt, c.nll, c.dh);
+    const int rb = (p.rows_pad + kGatherWaves - 1) / kGatherWaves;
+    if (T <= kListedRows) {
+        gather_kernel<true><<<rb, kGatherWaves * kWave, 0, s>>>(c.h, c.w, c.target, T, p.rows_pad, d, V, c.ignore, rows,
+                                                                head, hc, tc, zt, c.nll, c.dh);
+    } else {
+        list_kernel<int32_t><<<1, kListThreads, 0, s>>>(c.target, T, c.ignore, rows, head);
+        gather_kernel<false><<<rb, kGatherWaves * kWave, 0, s>>>(c.h, c.w, c.target, T, p.rows_pad, d, V, c.ignore, rows,
+                                                                 head, hc, tc, zt, c.nll, c.dh);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     GemmArgs z{};
@@ -294,7 +348,7 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
     z.K = d; z.splits = 1;
     z.part = part; z.ldpart = p.rows_pad; z.target = tc;
     z.out = gbuf; z.ldo = p.piece; z.kept = c.dh || c.dw ? p.piece : 0;
-    e = small ? launch_gemm<Small, false, false, LSE>(z, s) : launch_gemm<Big, false, false, LSE>(z, s);
+    e = launch_sized<false, false, LSE>(zz, z, s);
     if (e != hipSuccess) return e;
     row_kernel<<<std::max(1, (T + kWave - 1) / kWave), kRowWaves * kWave, 0, s>>>(part, p.tiles, p.rows_pad, head, rows, tc, zt, c.scale,
                                                                     c.mean, stats, nllc, c.nll, c.loss, coef, c.count);
@@ -305,14 +359,14 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
         const uint16_t* w = c.w + static_cast<size_t>(v0) * d;
         if (v0 == 0) {
             const dim3 grid((nv + p.tile - 1) / p.tile, p.rows_pad / kScaleRows);
-            if (small) scale_kernel<Small::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
+            if (p.tile == Mid::NA) scale_kernel<Mid::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
             else scale_kernel<Big::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
             e = hipGetLastError();
         } else {
             GemmArgs q = z;
             q.a = w; q.na = nv; q.col0 = v0;
             q.stats = stats;
-            e = small ? launch_gemm<Small, false, false, GRAD>(q, s) : launch_gemm<Big, false, false, GRAD>(q, s);
+            e = launch_sized<false, false, GRAD>(zz, q, s);
         }
         if (e == hipSuccess && c.dh) {
             GemmArgs a{};
@@ -321,10 +375,10 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
             a.K = nv; a.splits = p.splits;
             if (p.parts) {
                 a.out = dhp; a.ldo = d; a.split_stride = static_cast<int64_t>(p.rows_pad) * d; a.add = v0 > 0;
-                e = small ? launch_gemm<Small, true, false, PART>(a, s) : launch_gemm<Big, true, false, PART>(a, s);
+                e = launch_sized<true, false, PART>(zh, a, s);
             } else {
                 a.out = c.dh; a.ldo = d; a.rows = rows; a.coef = coef;
-                e = small ? launch_gemm<Small, true, false, ROWS>(a, s) : launch_gemm<Big, true, false, ROWS>(a, s);
+                e = launch_sized<true, false, ROWS>(zh, a, s);
             }
         }
         if (e == hipSuccess && c.dw) {
@@ -333,7 +387,7 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
             a.b = gbuf; a.ldb = p.piece; a.nb = nv;
             a.K = p.rows_pad; a.k_dev = head + 1; a.splits = 1;
             a.out = c.dw + static_cast<size_t>(v0) * d; a.ldo = d; a.coef = coef;
-            e = launch_gemm<Big, true, true, ROWS>(a, s);
+            e = launch_sized<true, true, ROWS>(pick_tile(nv, d), a, s);
         }
     }
     if (e == hipSuccess && p.parts) {

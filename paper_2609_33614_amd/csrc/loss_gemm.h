@@ -43,6 +43,7 @@ struct Tile {
     static_assert(kP >= 1 && kP <= 3, "wait counts cover up to three chunks in flight");
 };
 using Big = Tile<256, 256, 4, 2, 2>;
+using Mid = Tile<128, 128, 4, 2, 4>;
 using Small = Tile<128, 64, 4, 2, 4>;
 
 enum Out { LSE, GRAD, PART, ROWS, ROWS32 };
@@ -464,49 +465,45 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
 // rows[0 .. n): the indices t < T whose key is not `skip`, in order, and the
 // last of them again up to a whole reduction chunk; head: {n, n rounded up to
 // whole chunks, 0}.  One workgroup: the list is a running count over the call.
-constexpr int kListThreads = 1024, kListLoads = 8;
+// A thread takes 16 bytes of keys at a time, so that 4096 fp32-sized keys are
+// one round of loads and one scan.
+constexpr int kListThreads = 1024;
 template <typename Key>
 __global__ __launch_bounds__(kListThreads) void list_kernel(const Key* __restrict__ key, int T, Key skip, int32_t* rows,
                                                             int32_t* head) {
-    constexpr int NW = kListThreads / kWave;
-    __shared__ int cnt[kListLoads][NW];
+    constexpr int NW = kListThreads / kWave, N = 16 / sizeof(Key);
+    __shared__ int cnt[2][NW];
     __shared__ int lastrow;
     const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const uint64_t below = lane == 0 ? 0ull : ~0ull >> (kWave - lane);
-    int base = 0;
-    for (int t0 = 0; t0 < T; t0 += kListThreads * kListLoads) {
-        bool keep[kListLoads];
-        uint64_t m[kListLoads];
+    const bool wide = reinterpret_cast<uintptr_t>(key) % 16 == 0;
+    int base = 0, flip = 0;
+    for (int t0 = 0; t0 < T; t0 += kListThreads * N, flip ^= 1) {
+        const int t = t0 + threadIdx.x * N;
+        alignas(16) Key k[N];
+        if (wide && t + N <= T) {
+            *reinterpret_cast<uint4*>(k) = *reinterpret_cast<const uint4*>(key + t);
+        } else {
 #pragma unroll
-        for (int i = 0; i < kListLoads; ++i) {
-            const int t = t0 + i * kListThreads + threadIdx.x;
-            keep[i] = t < T && key[t < T ? t : 0] != skip;
+            for (int i = 0; i < N; ++i) k[i] = t + i < T ? key[t + i] : skip;
         }
+        int c = 0;
 #pragma unroll
-        for (int i = 0; i < kListLoads; ++i) {
-            m[i] = ballot(keep[i]);
-            if (lane == 0) cnt[i][wave] = __popcll(m[i]);
-        }
-        __syncthreads();
-        int pos[kListLoads];
+        for (int i = 0; i < N; ++i) c += k[i] != skip;
+        const int upto = wave_scan(c);
+        if (lane == kWave - 1) cnt[flip][wave] = upto;
+        __syncthreads();               // (the other half of cnt was last read before the round before's barrier)
+        int sum = wave_scan(lane < NW ? cnt[flip][lane] : 0);
+        const int total = __builtin_amdgcn_readlane(sum, NW - 1);
+        int at = base + upto - c + (wave ? __builtin_amdgcn_readlane(sum, wave - 1) : 0);
+        base += total;
 #pragma unroll
-        for (int i = 0; i < kListLoads; ++i) {
-            pos[i] = base + __popcll(m[i] & below);
-            for (int w = 0; w < NW; ++w) {
-                const int c = cnt[i][w];
-                pos[i] += w < wave ? c : 0;
-                base += c;
+        for (int i = 0; i < N; ++i)
+            if (k[i] != skip) {
+                rows[at] = t + i;
+                if (++at == base) lastrow = t + i;
             }
-        }
-#pragma unroll
-        for (int i = 0; i < kListLoads; ++i)
-            if (keep[i]) {
-                const int t = t0 + i * kListThreads + threadIdx.x;
-                rows[pos[i]] = t;
-                if (pos[i] == base - 1) lastrow = t;
-            }
-        __syncthreads();
     }
+    __syncthreads();
     const int pad = (base + kBK - 1) / kBK * kBK;
     for (int i = base + threadIdx.x; i < pad; i += kListThreads) rows[i] = lastrow;
     if (threadIdx.x == 0) {
