@@ -397,7 +397,7 @@ __global__ __launch_bounds__(256) void dw_join_kernel(const float* __restrict__ 
     *reinterpret_cast<f32x4*>(dw + i) = s * scale;
 }
 
-using Fold = Tile<256, 256, 4, 2, 2>;
+using Fold = Big;
 
 // Products on the split operands from here on, on fp32 instructions below.
 bool split_products(const eat_params_t& p, int32_t T) {

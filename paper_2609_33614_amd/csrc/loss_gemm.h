@@ -25,26 +25,31 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// NA x NB outputs per workgroup, WA x WB waves over them, a ring of STAGES
-// chunks in LDS.
-template <int NA_, int NB_, int WA_, int WB_, int STAGES_>
+// NA x NB outputs per workgroup, WA x WB waves over them.  A chunk is two
+// parts, A's and B's, and LDS a ring of SLOTS parts: the two computed and
+// kAhead loaded or on their way.
+template <int NA_, int NB_, int WA_, int WB_>
 struct Tile {
-    static constexpr int NA = NA_, NB = NB_, WA = WA_, WB = WB_, STAGES = STAGES_;
+    static constexpr int NA = NA_, NB = NB_, WA = WA_, WB = WB_;
     static constexpr int kWaves = WA * WB;
     static constexpr int kThreads = kWaves * kWave;
     static constexpr int FA = NA / (32 * WA), FB = NB / (32 * WB);    // 32-wide fragments per wave
-    static constexpr int kA = NA * kBK * 2, kB = NB * kBK * 2;        // bytes of a stage's operands
-    static constexpr int kStage = kA + kB;
+    static constexpr int kA = NA * kBK * 2, kB = NB * kBK * 2;        // bytes of a chunk's parts
+    static constexpr int kSlot = kA > kB ? kA : kB;
+    static constexpr int SLOTS = (160 * 1024 / kSlot - 1) | 1;        // odd
+    static constexpr int kAhead = SLOTS - 2;
     static constexpr int kLA = kA / 1024 / kWaves, kLB = kB / 1024 / kWaves;   // 1 KB loads per wave
-    static constexpr int kLoads = kLA + kLB;
-    static constexpr int kP = STAGES - 1;     // chunks in flight ahead of the one computed
+    static constexpr int kShare = 2 * kSlot / kWaves;                 // a wave's bytes of two slots
     static_assert(kLA * 1024 * kWaves == kA && kLB * 1024 * kWaves == kB, "loads split evenly over the waves");
     static_assert(FA * 32 * WA == NA && FB * 32 * WB == NB, "fragments cover the tile");
-    static_assert(kP >= 1 && kP <= 3, "wait counts cover up to three chunks in flight");
+    static_assert(kAhead >= 3, "a chunk and the next one's first part");
+    static_assert(kShare >= 4096 && kShare >= 2048 * FA + 256 * FB, "a fragment's rows and sums fit a wave's share");
+    // loads of `parts` parts in a row, the first of them A's
+    static constexpr int loads(int parts) { return (parts + 1) / 2 * kLA + parts / 2 * kLB; }
 };
-using Big = Tile<256, 256, 4, 2, 2>;
-using Mid = Tile<128, 128, 4, 2, 4>;
-using Small = Tile<128, 64, 4, 2, 4>;
+using Big = Tile<256, 256, 4, 2>;
+using Mid = Tile<128, 128, 4, 2>;
+using Small = Tile<128, 64, 4, 2>;
 
 enum Out { LSE, GRAD, PART, ROWS, ROWS32 };
 
@@ -74,6 +79,9 @@ struct GemmArgs {
     const float2* stats;       // GRAD: (lse log2 e, G at the target) of a row
 };
 
+// (uniform: what depends on it branches on scalars)
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave); }
+
 // Operands stored row by row: LDS rows of 128 bytes (64 k), 16-byte slots XORed
 // with the row's 256-byte line, so that an MFMA operand read of 16 rows covers
 // every bank.
@@ -97,7 +105,7 @@ struct Operand {
     // first: the tile's first index, count: indices there are (>= 1), k0: the
     // slice's first k, k_rows: stored rows of a columns operand
     __device__ __forceinline__ void set(const uint16_t* p, int ld, int first, int count, int k0, int k_rows) {
-        const int lane = lane_id(), wave = threadIdx.x / kWave;
+        const int lane = lane_id(), wave = wave_id();
         ldbytes = static_cast<uint32_t>(ld) * 2;
         if constexpr (COLS) {
             base = reinterpret_cast<const char*>(p) + static_cast<size_t>(k0) * ldbytes;
@@ -120,37 +128,41 @@ struct Operand {
         }
     }
     __device__ __forceinline__ void look_up(int c) {
-        const int lane = lane_id(), wave = threadIdx.x / kWave;
+        const int lane = lane_id(), wave = wave_id();
         if constexpr (GATHER) {
 #pragma unroll
             for (int j = 0; j < L; ++j) at[j] = rows[c * kBK + ((wave + WAVES * j) * 64 + lane) / (N / 8)];
         }
     }
-    // chunk c into LDS at `st` (a load is waited for by count: the compiler
-    // adds no waits of its own for asm).  GATHER: after look_up(c).
-    __device__ __forceinline__ void issue(uint8_t* st, int c) const {
-        const int lane = lane_id(), wave = threadIdx.x / kWave;
+    __device__ __forceinline__ uint64_t source(int c) const {      // uniform: chunk c (not GATHER)
         const uint64_t at64 = reinterpret_cast<uint64_t>(base) + static_cast<uint64_t>(c) * (COLS ? kBK * ldbytes : kBK * 2);
-        const uint64_t src = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at64 >> 32)))) << 32 |
-                             static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at64)));
-#pragma unroll
-        for (int j = 0; j < L; ++j) {
-            uint32_t o = off[j];
-            if constexpr (GATHER) {
-                const char* p = base + static_cast<size_t>(at[j]) * ldbytes + o;
-                const uint32_t lds = __builtin_amdgcn_readfirstlane(
-                    static_cast<uint32_t>(reinterpret_cast<uintptr_t>(st + 1024 * (wave + WAVES * j))));
-                asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(p), "s"(lds) : "memory", "m0");
-                continue;
-            }
+        return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at64 >> 32)))) << 32 |
+               static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at64)));
+    }
+    // load j of chunk c (src: source(c)) into LDS at `st`; a load is waited for
+    // by count: the compiler adds no waits of its own for asm.  GATHER: after look_up(c).
+    // `on`: lanes that load, all or none (an instruction without lanes still
+    // counts as a load of the wave, so that the waits are constants).
+    __device__ __forceinline__ void load(uint8_t* st, uint64_t src, int c, int j, uint64_t on) const {
+        const int lane = lane_id(), wave = wave_id();
+        const uint32_t lds = __builtin_amdgcn_readfirstlane(
+            static_cast<uint32_t>(reinterpret_cast<uintptr_t>(st + 1024 * (wave + WAVES * j))));
+        uint32_t o = off[j];
+        if constexpr (GATHER) {
+            const char* p = base + static_cast<size_t>(at[j]) * ldbytes + o;
+            uint64_t save;
+            asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\t"
+                         "global_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, %0"
+                         : "=&s"(save) : "v"(p), "s"(lds), "s"(on) : "memory", "m0");
+        } else {
             if constexpr (COLS) {
                 const int k = ((wave + WAVES * j) * 64 + lane) / (N / 8);
-                o += static_cast<uint32_t>(min(k, k_last - c * kBK)) * ldbytes;
+                o += __umul24(min(k, k_last - c * kBK), ldbytes);
             }
-            const uint32_t lds = __builtin_amdgcn_readfirstlane(
-                static_cast<uint32_t>(reinterpret_cast<uintptr_t>(st + 1024 * (wave + WAVES * j))));
-            asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-                         :: "v"(o), "s"(src), "s"(lds) : "memory", "m0");
+            uint64_t save;
+            asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %4\n\ts_mov_b32 m0, %3\n\t"
+                         "global_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, %0"
+                         : "=&s"(save) : "v"(o), "s"(src), "s"(lds), "s"(on) : "memory", "m0");
         }
     }
 };
@@ -199,7 +211,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
     static_assert(!kFoldRows || (C::NB == 256 && C::WB == 2), "a group per tile, 32 indices per wave");
     constexpr int FA = C::FA, FB = kFoldRows ? 1 : C::FB, FL = kFoldRows ? 3 : C::FB;   // fragments of B: held, read
     constexpr int NBO = kFoldRows ? 64 : C::NB;        // output rows per tile
-    __shared__ __attribute__((aligned(1024))) uint8_t ring[C::STAGES * C::kStage];
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[C::SLOTS * C::kSlot];
     const int nb = g.nb_dev ? min(*g.nb_dev, g.nb) : g.nb;
     const int K = g.k_dev ? min(*g.k_dev, g.K) : g.K;
     const int nta = (g.na + C::NA - 1) / C::NA, ntb = (nb + NBO - 1) / NBO;
@@ -227,84 +239,206 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
     int wid = wbeg + slot;
     if (wid >= wend) return;                  // uniform over the workgroup
 
-    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int lane = lane_id(), wave = wave_id();
     const int l32 = lane & 31, lh = lane >> 5;
     const int arow = 32 * FA * (wave % C::WA), brow = 32 * FB * (wave / C::WA);
     const float coef = (OUT == ROWS || OUT == ROWS32) ? (g.coef ? *g.coef : g.factor) : 1.f;
 
+    auto slice = [&](int sp) { return chunks * sp / splits; };     // first chunk of a slice
+
+    // The stream of loads: the parts A, B, A, B, ... of the chunks of this
+    // workgroup's items, on into the next item while the last chunks of one are
+    // computed and stored.  After the first A it goes by pairs, the B of the last
+    // A and the A after it; behind the last chunk the pairs load nothing.
     Operand<C::NA, C::kLA, C::kWaves, ACOLS, GATHER> oa;
     Operand<C::NB, C::kLB, C::kWaves, BCOLS> ob;
-    int nch = 0;
-    auto slice = [&](int sp) { return chunks * sp / splits; };     // first chunk of a slice
-    auto setup = [&](const Item& it) __attribute__((always_inline)) {
-        const int c0 = slice(it.sp);
-        oa.set(g.a, g.lda, it.a0, g.na, GATHER ? 0 : c0 * kBK, g.a_rows);
-        if constexpr (GATHER) oa.rows = g.k_rows + c0 * kBK;
-        // (every stored row and column of B there is up to whole tiles)
-        ob.set(g.b, g.ldb, it.b0 / NBO * C::NB, 1 << 30, c0 * kBK, 1 << 30);
+    int iwid = wid - per_xcd, ich = -1, inch = 0;     // the last A's item and chunk, the item's chunks
+    Item item{};
+    uint64_t aon = 0, bon = 0, srca = 0, srcb = 0;
+    int cb = 0, islot = 0;                    // islot: the slot loaded next
+    auto next_a = [&]() __attribute__((always_inline)) {
+        if (++ich < inch) {
+            srca = GATHER ? 0 : oa.source(ich);
+            return;
+        }
+        for (iwid += per_xcd; iwid < wend; iwid += per_xcd) {          // the next item that has chunks
+            item = item_at(iwid);
+            const int c0 = slice(item.sp);
+            inch = slice(item.sp + 1) - c0;
+            if (inch == 0) continue;
+            oa.set(g.a, g.lda, item.a0, g.na, GATHER ? 0 : c0 * kBK, g.a_rows);
+            if constexpr (GATHER) {
+                oa.rows = g.k_rows + c0 * kBK;
+                oa.look_up(0);
+            }
+            ich = 0;
+            srca = GATHER ? 0 : oa.source(0);
+            aon = ~0ull;
+            return;
+        }
+        aon = 0;
+        ich = -1;
+        inch = 0;
     };
-    auto issue = [&](int stage, int c) __attribute__((always_inline)) {
-        uint8_t* st = ring + stage * C::kStage;
-        oa.issue(st, c);
-        if constexpr (GATHER) oa.look_up(min(c + 1, nch - 1));
-        ob.issue(st + C::kA, FOLD && !BCOLS ? c / g.segs * 4 + ((g.map >> (4 * (c % g.segs))) & 15) : c);
+    auto next_pair = [&]() __attribute__((always_inline)) {
+        bon = aon;
+        if (bon) {
+            // (every stored row and column of B there is up to whole tiles)
+            if (ich == 0) ob.set(g.b, g.ldb, item.b0 / NBO * C::NB, 1 << 30, slice(item.sp) * kBK, 1 << 30);
+            cb = FOLD && !BCOLS ? ich / g.segs * 4 + ((g.map >> (4 * (ich % g.segs))) & 15) : ich;
+            srcb = ob.source(cb);
+            next_a();
+        }
     };
-    Item cur = item_at(wid);
-    setup(cur);
-    nch = slice(cur.sp + 1) - slice(cur.sp);
-    if constexpr (GATHER)
-        if (nch > 0) oa.look_up(0);
+    auto slot_at = [&](int ahead) __attribute__((always_inline)) {
+        const int sl = islot + ahead;
+        return ring + (sl >= C::SLOTS ? sl - C::SLOTS : sl) * C::kSlot;
+    };
+    auto advance = [&](int parts) __attribute__((always_inline)) {
+        islot += parts;
+        if (islot >= C::SLOTS) islot -= C::SLOTS;
+    };
+    // load q of a pair: B's, then A's
+    auto pair_load = [&](int q) __attribute__((always_inline)) {
+        if (q < C::kLB) ob.load(slot_at(0), srcb, cb, q, bon);
+        else oa.load(slot_at(1), srca, ich, q - C::kLB, aon);
+    };
+    auto pair_done = [&]() __attribute__((always_inline)) {
+        if constexpr (GATHER)
+            if (aon) oa.look_up(min(ich + 1, inch - 1));
+        advance(2);
+    };
+    // Waits until at most the loads of the parts behind the chunk met next, and
+    // `stores` output stores issued since, are still in flight (vector memory operations complete
+    // in issue order for this counter; counting fewer only waits longer).
+    auto wait_parts = [&](int stores) __attribute__((always_inline)) {
+        constexpr int N = C::loads(C::kAhead - 2);
+        if (stores == 0) wait_vm<N>();
+        else if (stores < 8) wait_vm<N + 1>();
+        else if (stores < 16) wait_vm<N + 8>();
+        else wait_vm<N + 16>();
+    };
+    next_a();
 #pragma unroll
-    for (int c = 0; c < C::kP; ++c)
-        if (c < nch) issue(c, c);
-    int sc = 0;                               // stage of the chunk computed next
+    for (int j = 0; j < C::kLA; ++j) oa.load(slot_at(0), srca, ich, j, aon);
+    if constexpr (GATHER)
+        if (aon) oa.look_up(min(ich + 1, inch - 1));
+    advance(1);
+#pragma unroll 1
+    for (int i = 0; i < (C::kAhead - 1) / 2; ++i) {
+        next_pair();
+#pragma unroll
+        for (int q = 0; q < C::kLA + C::kLB; ++q) pair_load(q);
+        pair_done();
+    }
+    int slot0 = 0;                            // slot of the chunk met next
+    int stored = 0;                           // output stores since the loads it awaits
 
     for (;;) {
-        const int nwid = wid + per_xcd;
-        const bool more = nwid < wend;        // uniform
-        const Item nxt = more ? item_at(nwid) : cur;
+        const Item cur = item_at(wid);
+        const int nch = slice(cur.sp + 1) - slice(cur.sp);
         const bool active = cur.b0 + brow < (OUT == GRAD ? (nb + kBK - 1) / kBK * kBK : nb);
+        // what the epilogue needs of the rows, before the loads it would wait behind
+        int target[FB];
+        float2 stats[FB];
+#pragma unroll
+        for (int j = 0; j < FB; ++j) {
+            const int row = cur.b0 + brow + 32 * j + l32;
+            if constexpr (OUT == LSE || OUT == GRAD) target[j] = nb > 0 ? g.target[min(row, nb - 1)] : 0;
+            if constexpr (OUT == GRAD) stats[j] = nb > 0 ? g.stats[min(row, nb - 1)] : float2{};
+        }
         f32x16 acc[FA][FB];
 #pragma unroll
         for (int i = 0; i < FA; ++i)
 #pragma unroll
             for (int j = 0; j < FB; ++j) acc[i][j] = f32x16{};
 
-        // one step of the ring: wait for this wave's loads of chunk c, barrier
-        // (every wave's have landed, and every wave is done with the stage
-        // before), refill that stage, compute
-        for (int c = 0; c < nch; ++c) {
-            const int after = min(C::kP - 1, nch - 1 - c);
-            if (C::kP >= 3 && after >= 2) wait_vm<(C::kP >= 3 ? 2 : 0) * C::kLoads>();
-            else if (C::kP >= 2 && after >= 1) wait_vm<(C::kP >= 2 ? 1 : 0) * C::kLoads>();
-            else wait_vm<0>();
-            lds_barrier();
-            const int si = sc == 0 ? C::STAGES - 1 : sc - 1;
-            if (c + C::kP < nch) issue(si, c + C::kP);
-            const uint8_t* st = ring + sc * C::kStage;
-            sc = sc + 1 == C::STAGES ? 0 : sc + 1;
-            if (!active) continue;
+        // The ring's step to a chunk: wait for this wave's loads of it, barrier
+        // (every wave's have landed, and every wave has read the chunk before),
+        // refill that one's slots.  It comes before the last of the 4 products of the
+        // chunk before, whose fragments are in registers, so the matrix cores
+        // have work while the waves meet and read on; inside a chunk the
+        // fragments of a product are read during the one before.
+        bf16x8 A[2][FA], B[2][FL];
+        const uint8_t *sa = ring, *sb = ring;
+        auto read = [&](int p, int s) __attribute__((always_inline)) {
 #pragma unroll
-            for (int s = 0; s < kBK / 16; ++s) {
-                bf16x8 A[FA], B[FL];
+            for (int j = 0; j < FL; ++j) B[p][j] = fragment<C::NB, BCOLS>(sb, brow + (kFoldRows ? 64 : 32) * j, s);
 #pragma unroll
-                for (int j = 0; j < FL; ++j)
-                    B[j] = fragment<C::NB, BCOLS>(st + C::kA, brow + (kFoldRows ? 64 : 32) * j, s);
+            for (int i = 0; i < FA; ++i) A[p][i] = fragment<C::NA, ACOLS>(sa, arow + 32 * i, s);
+        };
+        auto product = [&](int p, int j, int i) __attribute__((always_inline)) {
+            f32x16& c16 = acc[i][kFoldRows ? 0 : j];
+            c16 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[p][i], B[p][j], c16, 0, 0, 0);
+        };
+        auto products = [&](int p) __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < FA; ++i) A[i] = fragment<C::NA, ACOLS>(st, arow + 32 * i, s);
+            for (int j = 0; j < FL; ++j)
 #pragma unroll
-                for (int j = 0; j < FL; ++j)
+                for (int i = 0; i < FA; ++i) product(p, j, i);
+        };
+        constexpr int kReads = FA * (ACOLS ? 2 : 1) + FL * (BCOLS ? 2 : 1), kProducts = FA * FL;
+        constexpr int kPerProduct = (kReads + kProducts - 1) / kProducts;
+        auto spread = [&]() __attribute__((always_inline)) {      // reads evenly between the products
 #pragma unroll
-                    for (int i = 0; i < FA; ++i) {
-                        f32x16& c16 = acc[i][kFoldRows ? 0 : j];
-                        c16 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[i], B[j], c16, 0, 0, 0);
-                    }
+            for (int m = 0; m < kProducts; ++m) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, kPerProduct, 0);
             }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto meet = [&](int stores) __attribute__((always_inline)) {
+            wait_parts(stores);
+            lds_barrier();
+            sa = ring + slot0 * C::kSlot;
+            slot0 = slot0 + 1 == C::SLOTS ? 0 : slot0 + 1;
+            sb = ring + slot0 * C::kSlot;
+            slot0 = slot0 + 1 == C::SLOTS ? 0 : slot0 + 1;
+            next_pair();
+        };
+        auto first_three = [&]() __attribute__((always_inline)) {
+            read(1, 1);
+            products(0);
+            spread();
+            read(0, 2);
+            products(1);
+            spread();
+            read(1, 3);
+            products(0);
+            spread();
+        };
+        constexpr int kPair = C::kLA + C::kLB;
+        if (nch > 0) {
+            meet(stored);
+            read(0, 0);
+#pragma unroll
+            for (int q = 0; q < kPair; ++q) pair_load(q);
+            pair_done();
+            for (int c = 1; c < nch; ++c) {
+                first_three();
+                meet(0);
+                read(0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int m = 0; m < kProducts; ++m) {
+                    product(1, m / FA, m % FA);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int q = m * kPair / kProducts; q < (m + 1) * kPair / kProducts; ++q) pair_load(q);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                pair_done();
+            }
+            first_three();
+            products(1);
         }
-        lds_barrier();                        // every wave is done with the ring
+        lds_barrier();                        // every wave is done with the ring's two next slots
+        stored = 0;
         // lane: row cur.b0 + brow + 32 j + l32, columns cur.a0 + arow + 32 i + 8 (q / 4) + 4 lh + q % 4
-        uint8_t* const tb = ring + wave * (C::STAGES * C::kStage / C::kWaves);
-        static_assert(C::STAGES * C::kStage / C::kWaves >= 4096, "a fragment's rows fit a wave's share of the ring");
+        auto share = [&](int w) __attribute__((always_inline)) {      // wave w's bytes of those slots
+            return slot_at(w >= C::kWaves / 2) + w % (C::kWaves / 2) * C::kShare;
+        };
+        uint8_t* const tb = share(wave);
         // FA fragments' 32 rows of 64 FA bytes, turned around through the
         // wave's share of LDS so that adjacent lanes store adjacent pieces
         auto store16 = [&](int j, auto val, auto dst, int nv) __attribute__((always_inline)) {
@@ -320,26 +454,25 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
             wave_lds_sync();
 #pragma unroll
             for (int k = 0; k < 32 * V / 64; ++k) {
+                if ((64 / V) * k >= nv) break;
                 const int r = (64 / V) * k + lane / V, v = lane % V;
                 const u32x4 d = *reinterpret_cast<const u32x4*>(tb + at(r, v));
                 if (r < nv) *reinterpret_cast<u32x4*>(dst(r) + 8 * v) = d;
+                ++stored;
             }
             wave_lds_sync();
         };
         if constexpr (OUT == LSE) {
             // the waves' maxima of a row, then its exponentials over the tile's
             // maximum and their sum: the tile's first columns may be kept
-            float* const redm = reinterpret_cast<float*>(ring + 4096);       // [WA][NB], beside wave 0's rows
-            float* const reds = redm + C::WA * C::NB;
-            static_assert(4096 + 8 * C::WA * C::NB <= C::STAGES * C::kStage / C::kWaves, "within wave 0's share");
+            auto sums = [&](int w) { return reinterpret_cast<float*>(share(w) + 2048 * FA); };   // [2][32 FB] of wave w
+            const int wb = wave / C::WA;
             const int v0 = cur.a0 + arow + 4 * lh;
             const bool tail = cur.a0 + C::NA > g.na;
             const bool kept = cur.a0 < g.kept;
-            const int at = (wave % C::WA) * C::NB + brow + l32;
 #pragma unroll
             for (int j = 0; j < FB; ++j) {
-                const int row = cur.b0 + brow + 32 * j + l32;
-                const int rel = row < nb ? g.target[row] - g.col0 - v0 : -1;      // the target counts as no column
+                const int rel = target[j] - g.col0 - v0;                // the target counts as no column
                 if (ballot(rel >= 0 && rel < 32 * FA) || tail) {
 #pragma unroll
                     for (int i = 0; i < FA; ++i)
@@ -355,14 +488,14 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
 #pragma unroll
                     for (int q = 0; q < 16; ++q) m = fmaxf(m, acc[i][j][q]);
                 m = fmaxf(m, swap_halves(m));
-                if (lh == 0) redm[at + 32 * j] = m;
+                if (lh == 0) sums(wave)[32 * j + l32] = m;
             }
             lds_barrier();
 #pragma unroll
             for (int j = 0; j < FB; ++j) {
                 float m = -INFINITY;
 #pragma unroll
-                for (int w = 0; w < C::WA; ++w) m = fmaxf(m, redm[w * C::NB + brow + 32 * j + l32]);
+                for (int w = 0; w < C::WA; ++w) m = fmaxf(m, sums(C::WA * wb + w)[32 * j + l32]);
                 const float ref = tile_ref(m);
                 float s = 0.f;
 #pragma unroll
@@ -373,7 +506,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                         s += acc[i][j][q];
                     }
                 s += swap_halves(s);
-                if (lh == 0) reds[at + 32 * j] = s;
+                if (lh == 0) sums(wave)[32 * (FB + j) + l32] = s;
                 const int row0 = cur.b0 + brow + 32 * j;
                 if (kept && row0 < nb)
                     store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q]; },
@@ -382,11 +515,12 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
             }
             lds_barrier();
             for (int r = threadIdx.x; r < C::NB; r += C::kThreads) {
+                const int rb = r / (32 * FB), at = r % (32 * FB);
                 float m = -INFINITY, s = 0.f;
 #pragma unroll
                 for (int w = 0; w < C::WA; ++w) {
-                    m = fmaxf(m, redm[w * C::NB + r]);
-                    s += reds[w * C::NB + r];
+                    m = fmaxf(m, sums(C::WA * rb + w)[at]);
+                    s += sums(C::WA * rb + w)[32 * FB + at];
                 }
                 if (m == INFINITY && s == s) s = 1.f;      // (some are +inf: the row's NLL is)
                 if (cur.b0 + r < nb) g.part[static_cast<size_t>(cur.a0 / C::NA) * g.ldpart + cur.b0 + r] = float2{m, s};
@@ -401,8 +535,8 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                 if constexpr (OUT == GRAD) {
                     const int row = row0 + l32;
                     const bool live = row < nb;
-                    const float2 st = live ? g.stats[row] : float2{0.f, 0.f};
-                    const int rel = (live ? g.target[row] : -1) - (g.col0 + cur.a0 + arow + 4 * lh);
+                    const float2 st = stats[j];
+                    const int rel = target[j] - (g.col0 + cur.a0 + arow + 4 * lh);
                     const int end = live ? g.na - (cur.a0 + arow + 4 * lh) : 0;     // columns of the piece from here on
                     store16(j, [&](int i, int q) __attribute__((always_inline)) {
                         const int v = 32 * i + 8 * (q / 4) + q % 4;
@@ -430,6 +564,8 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                         wave_lds_sync();
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
+                            if (8 * k >= nv) break;
+                            ++stored;
                             const int r = 8 * k + lane / 8, v = lane % 8;
                             f32x4 d = *reinterpret_cast<const f32x4*>(tb + at(r, v));
                             if (r < nv && OUT == ROWS32) {
@@ -447,18 +583,8 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                 }
             }
         }
-        if (!more) break;
-        cur = nxt;
-        wid = nwid;
-        __syncthreads();
-        setup(cur);
-        nch = slice(cur.sp + 1) - slice(cur.sp);
-        sc = 0;
-        if constexpr (GATHER)
-            if (nch > 0) oa.look_up(0);
-#pragma unroll
-        for (int c = 0; c < C::kP; ++c)
-            if (c < nch) issue(c, c);
+        wid += per_xcd;
+        if (wid >= wend) break;
     }
 }
 
