@@ -27,6 +27,18 @@ constexpr int kStatWaves = 16;
 constexpr int kStatThreads = kStatWaves * kWave;
 constexpr int kStatBlocks = 64;           // most shares of the tokens
 
+// dz of a row whose lanes (EP of them, E rounded up to a power of two up to 64)
+// hold experts e0 + 64 j: p (q - <q, p>), <q, p> in fp64.
+template <int J>
+__device__ __forceinline__ void score_grad(const float (&p)[J], const float (&q)[J], int ep, float (&dz)[J]) {
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) s += static_cast<double>(q[j]) * p[j];
+    for (int o = ep / 2; o >= 1; o /= 2) s += __shfl_xor(s, o, kWave);
+#pragma unroll
+    for (int j = 0; j < J; ++j) dz[j] = p[j] * static_cast<float>(q[j] - s);
+}
+
 struct StatArgs {
     const float* prob;
     const uint64_t* mask;
@@ -40,6 +52,7 @@ struct StatArgs {
     float* loss;
     int64_t* count;
     float* mean_prob;
+    float* dz;                 // one workgroup: [T][E], made here too (or null)
 };
 
 // Lane l holds experts l % EP + 64 j of token l / EP of a group of 64 / EP
@@ -194,6 +207,36 @@ __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
     if (lane == 0) red[0][wave] = l;
     __syncthreads();
     if (tid == 0) *a.loss = static_cast<float>((red[0][0] + red[0][1]) + (red[0][2] + red[0][3]));
+    if (!a.dz || blocks > 1) return;
+    // small calls: the scores' gradient without a launch of its own
+    float* const qs = reinterpret_cast<float*>(redc);
+    if (tid < E) qs[tid] = static_cast<float>((a.coef * E * f + a.entropy_coef * (lg + 1.0)) * inv);
+    __syncthreads();
+    float q[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) q[j] = 64 * j + e0 < E ? qs[64 * j + e0] : 0.f;
+    for (int t0 = wave * tpw * kStatRows; t0 < a.T; t0 += kStatWaves * tpw * kStatRows) {
+        float p[kStatRows][J];
+#pragma unroll
+        for (int u = 0; u < kStatRows; ++u) {
+            const int t = t0 + u * tpw + sub, ts = min(t, a.T - 1);
+            const bool live = t < a.T && (!a.valid || a.valid[ts]);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const float v = a.prob[static_cast<size_t>(ts) * E + min(64 * j + e0, E - 1)];
+                p[u][j] = live && 64 * j + e0 < E ? v : 0.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kStatRows; ++u) {
+            const int t = t0 + u * tpw + sub;
+            float dz[J];
+            score_grad<J>(p[u], q, ep, dz);
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (t < a.T && 64 * j + e0 < E) a.dz[static_cast<size_t>(t) * E + 64 * j + e0] = dz[j];
+        }
+    }
 }
 
 // head of a call whose tokens all count
@@ -290,20 +333,18 @@ __global__ __launch_bounds__(kPrepThreads) void prep_kernel(PrepArgs a) {
     const int n = a.rows ? a.head[0] : a.T, pad = a.dzs ? a.head[1] : n;
     const int t = a.rows ? (i < n ? a.rows[i] : 0) : i;
     const bool live = i < n && (a.rows || !a.valid || a.valid[t]);
-    float p[J], qe[J];
-    double s = 0.0;
+    float p[J], qe[J], dz[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int e = 64 * j + e0;
         p[j] = live && e < E ? a.prob[static_cast<size_t>(t) * E + e] : 0.f;
         qe[j] = e < E ? a.q[e] : 0.f;
-        s += static_cast<double>(qe[j]) * p[j];
     }
-    for (int o = ep / 2; o >= 1; o /= 2) s += __shfl_xor(s, o, kWave);
+    score_grad<J>(p, qe, ep, dz);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int e = 64 * j + e0;
-        const float v = live && e < E ? p[j] * static_cast<float>(qe[j] - s) : 0.f;
+        const float v = dz[j];
         if (a.dz && live && e < E) a.dz[static_cast<size_t>(t) * E + e] = v;
         if (a.dzs && i < pad) {
             uint16_t part[3];
@@ -323,64 +364,76 @@ __device__ __forceinline__ float load_f32(const uint16_t* p) { return bf16_to_f3
 __device__ __forceinline__ void store_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_f32(uint16_t* p, float v) { *p = f32_to_bf16(v); }
 
-// 64 tokens x 64 columns per workgroup, 16 tokens per wave.
+// The products of small calls, fp32 matrix instructions on operands straight
+// from memory, kSteps of 4 reduction elements' loads in flight: 64 columns and
+// 16 rows per wave, 64 rows per workgroup.  Workgroups below blocks_w make
+// dW_r (rows: experts; reduction: a slice of the tokens, those that are not
+// valid read as zeros), the others dx (rows: tokens; reduction: experts).
+constexpr int kSteps = 8;
+struct ProductArgs {
+    const float* dz;
+    const void* x;
+    const float* w;
+    const uint8_t* valid;
+    int T, E, d, splits, blocks_w;
+    float scale;
+    float* dw;                 // dW_r where splits is 1
+    float* dwp;                // else its slices [splits][E][d], unscaled
+    void* dx;
+};
 template <typename XT>
-__global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ dz, const float* __restrict__ w, int T, int E,
-                                                 int d, float scale, XT* dx) {
+__global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
     const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int t0 = blockIdx.x * 64 + 16 * wave, c0 = blockIdx.y * 64;
-    const int l16 = lane & 15, lk = lane >> 4;
+    const int l16 = lane & 15, lk = lane >> 4, cols = a.d / 64;
+    const bool dw = static_cast<int>(blockIdx.x) < a.blocks_w;
+    int b = dw ? blockIdx.x : blockIdx.x - a.blocks_w;
+    const int c0 = b % cols * 64;
+    b /= cols;
+    const int rows = dw ? a.E : a.T, tiles = (rows + 63) / 64;
+    const int r0 = b % tiles * 64 + 16 * wave, sp = b / tiles;
+    const int row = min(r0 + l16, rows - 1);
+    int kbeg = 0, kend = a.E;
+    if (dw) {
+        const int per = ((a.T + a.splits - 1) / a.splits + 3) / 4 * 4;
+        kbeg = min(a.T, sp * per);
+        kend = min(a.T, kbeg + per);
+    }
     f32x4 acc[4] = {};
-    const int t = min(t0 + l16, T - 1);
-    for (int e = 0; e < E; e += 4) {
-        const int k = min(e + lk, E - 1);
-        const float z = dz[static_cast<size_t>(t) * E + k];
-        const float a = e + lk < E ? z : 0.f;
+    for (int k0 = kbeg; k0 < kend; k0 += 4 * kSteps) {
+        float z[kSteps], v[kSteps][4];
+        bool on[kSteps];
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            const float wv = w[static_cast<size_t>(k) * d + c0 + 16 * f + l16];
-            acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, e + lk < E ? wv : 0.f, acc[f], 0, 0, 0);
+        for (int s = 0; s < kSteps; ++s) {
+            const int k = min(k0 + 4 * s + lk, kend - 1);
+            on[s] = k0 + 4 * s + lk < kend;
+            if (dw) {
+                if (a.valid) on[s] = on[s] && a.valid[k];
+                z[s] = a.dz[static_cast<size_t>(k) * a.E + row];
+            } else {
+                z[s] = a.dz[static_cast<size_t>(row) * a.E + k];
+            }
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                const size_t at = static_cast<size_t>(k) * a.d + c0 + 16 * f + l16;
+                v[s][f] = dw ? load_f32(static_cast<const XT*>(a.x) + at) : a.w[at];
+            }
         }
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+                acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(on[s] ? z[s] : 0.f, on[s] ? v[s][f] : 0.f, acc[f], 0, 0, 0);
     }
 #pragma unroll
     for (int f = 0; f < 4; ++f)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = t0 + 4 * lk + i;
-            if (row < T) store_f32(dx + static_cast<size_t>(row) * d + c0 + 16 * f + l16, acc[f][i] * scale);
-        }
-}
-
-// 64 experts x 64 columns per workgroup, 16 experts per wave, over slice
-// blockIdx.z of the tokens; tokens that are not valid read as zeros.
-template <typename XT>
-__global__ __launch_bounds__(256) void dw_kernel(const float* __restrict__ dz, const XT* __restrict__ x,
-                                                 const uint8_t* __restrict__ valid, int T, int E, int d, float* out) {
-    const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int e0 = blockIdx.x * 64 + 16 * wave, c0 = blockIdx.y * 64;
-    const int l16 = lane & 15, lk = lane >> 4;
-    const int per = ((T + static_cast<int>(gridDim.z) - 1) / static_cast<int>(gridDim.z) + 3) / 4 * 4;
-    const int tbeg = min(T, static_cast<int>(blockIdx.z) * per), tend = min(T, tbeg + per);
-    f32x4 acc[4] = {};
-    const int e = min(e0 + l16, E - 1);
-    for (int t0 = tbeg; t0 < tend; t0 += 4) {
-        const int t = min(t0 + lk, tend - 1);
-        const bool live = t0 + lk < tend && (!valid || valid[t]);
-        const float z = dz[static_cast<size_t>(t) * E + e];
-        const float a = live ? z : 0.f;
-#pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            const float xv = load_f32(x + static_cast<size_t>(t) * d + c0 + 16 * f + l16);
-            acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, live ? xv : 0.f, acc[f], 0, 0, 0);
-        }
-    }
-    float* const o = out + static_cast<size_t>(blockIdx.z) * E * d;
-#pragma unroll
-    for (int f = 0; f < 4; ++f)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = e0 + 4 * lk + i;
-            if (row < E) o[static_cast<size_t>(row) * d + c0 + 16 * f + l16] = acc[f][i];
+            const int r = r0 + 4 * lk + i;
+            if (r >= rows) continue;
+            const size_t at = static_cast<size_t>(r) * a.d + c0 + 16 * f + l16;
+            if (!dw) store_f32(static_cast<XT*>(a.dx) + at, acc[f][i] * a.scale);
+            else if (a.splits == 1) a.dw[at] = acc[f][i] * a.scale;
+            else a.dwp[static_cast<size_t>(sp) * a.E * a.d + at] = acc[f][i];
         }
 }
 
@@ -399,6 +452,9 @@ __global__ __launch_bounds__(256) void dw_join_kernel(const float* __restrict__ 
 
 using Fold = Big;
 
+constexpr int kOneBlock = 16384;          // most probabilities one workgroup sums up
+constexpr int kOneSlice = 256;            // most tokens that dW_r of a small call takes in one slice
+
 // Products on the split operands from here on, on fp32 instructions below.
 bool split_products(const eat_params_t& p, int32_t T) {
     return static_cast<int64_t>(T) * p.E * p.d_model >= (int64_t{1} << 27);
@@ -416,15 +472,12 @@ template <typename XT>
 hipError_t launch_products(const eat_params_t& p, const BalancePlan& b, const BalanceCall& c, const float* dz, float* dwp,
                            hipStream_t s) {
     const int E = p.E, d = p.d_model;
-    if (c.dw) {
-        dw_kernel<XT><<<dim3((E + 63) / 64, d / 64, b.splits), 256, 0, s>>>(dz, static_cast<const XT*>(c.x), c.valid, c.T, E,
-                                                                           d, dwp);
+    const int bw = c.dw ? (E + 63) / 64 * (d / 64) * b.splits : 0, bx = c.dx ? (c.T + 63) / 64 * (d / 64) : 0;
+    const ProductArgs a{dz, c.x, c.w_router, c.valid, c.T, E, d, b.splits, bw, p.inv_temperature, c.dw, dwp, c.dx};
+    if (bw + bx > 0) product_kernel<XT><<<bw + bx, 256, 0, s>>>(a);
+    if (c.dw && b.splits > 1)
         dw_join_kernel<<<static_cast<int>((static_cast<int64_t>(E) * d / 4 + 255) / 256), 256, 0, s>>>(
             dwp, b.splits, 1, E, d, p.inv_temperature, c.dw);
-    }
-    if (c.dx && c.T > 0)
-        dx_kernel<XT><<<dim3((c.T + 63) / 64, d / 64), 256, 0, s>>>(dz, c.w_router, c.T, E, d, p.inv_temperature,
-                                                                     static_cast<XT*>(c.dx));
     return hipGetLastError();
 }
 
@@ -480,7 +533,8 @@ BalancePlan plan_balance(const eat_params_t& p, int32_t T) {
     BalancePlan b{};
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += (bytes + 255) & ~size_t(255); return at; };
-    b.blocks = std::max(1, std::min(kStatBlocks, (T + 63) / 64));
+    // (one workgroup needs no meeting of several, and makes dz of a small call as well)
+    b.blocks = static_cast<int64_t>(T) * p.E <= kOneBlock ? 1 : std::min(kStatBlocks, (T + 63) / 64);
     b.split = split_products(p, T);
     const size_t groups = (p.E + 63) / 64, d = p.d_model, pad = (static_cast<size_t>(T) + 255) / 256 * 256;
     const int parts = b.split && p.act_dtype != EAT_BF16 ? 3 : 1;
@@ -488,7 +542,9 @@ BalancePlan plan_balance(const eat_params_t& p, int32_t T) {
     // small ones of the fp32 kernel), none under 4 chunks (64 tokens)
     const int64_t items = b.split ? groups * ((parts * d + Fold::NA - 1) / Fold::NA) : groups * (d / 64);
     b.splits = 1;
-    while (items * b.splits * 2 <= (b.split ? 256 : 1024) && T / (b.splits * 2) >= (b.split ? 4 * kBK : 64)) b.splits *= 2;
+    if (b.split || T > kOneSlice)
+        while (items * b.splits * 2 <= (b.split ? 256 : 1024) && T / (b.splits * 2) >= (b.split ? 4 * kBK : 64))
+            b.splits *= 2;
     b.head = take(12);
     b.rows = take(b.split ? pad * 4 : 0);
     b.q = take(static_cast<size_t>(p.E) * 4);
@@ -506,9 +562,6 @@ BalancePlan plan_balance(const eat_params_t& p, int32_t T) {
 hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const BalanceCall& c, char* ws, hipStream_t s) {
     int32_t* const head = reinterpret_cast<int32_t*>(ws + b.head);
     float* const q = reinterpret_cast<float*>(ws + b.q);
-    const StatArgs a{c.prob, c.mask, c.valid, c.T, p.E, c.coef, c.entropy_coef, head, q,
-                     reinterpret_cast<double*>(ws + b.sum), reinterpret_cast<int32_t*>(ws + b.cnt), c.loss, c.count,
-                     c.mean_prob};
     const bool products = c.dx || c.dw, split = b.split && products;
     const bool bf16 = p.act_dtype == EAT_BF16;
     int32_t* const list = split && c.valid ? reinterpret_cast<int32_t*>(ws + b.rows) : nullptr;
@@ -517,6 +570,10 @@ hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const Bal
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     float* const dz = c.dlogits ? c.dlogits : products && !split ? reinterpret_cast<float*>(ws + b.dz) : nullptr;
+    const bool fused = b.blocks == 1 && !split;            // dz by the sums' workgroup
+    const StatArgs a{c.prob, c.mask, c.valid, c.T, p.E, c.coef, c.entropy_coef, head, q,
+                     reinterpret_cast<double*>(ws + b.sum), reinterpret_cast<int32_t*>(ws + b.cnt), c.loss, c.count,
+                     c.mean_prob, fused ? dz : nullptr};
     PrepArgs r{};
     r.prob = c.prob; r.valid = c.valid; r.rows = list; r.head = head;
     r.T = c.T; r.E = p.E; r.d = p.d_model;
@@ -544,7 +601,7 @@ hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const Bal
             blocks += places;
         }
     }
-    const PrepArgs* const rp = dz || split ? &r : nullptr;
+    const PrepArgs* const rp = (dz && !fused) || split ? &r : nullptr;
     switch ((p.E + 63) / 64) {
         case 1: e = launch_rows<1>(p, b, a, rp, blocks, s); break;
         case 2: e = launch_rows<2>(p, b, a, rp, blocks, s); break;

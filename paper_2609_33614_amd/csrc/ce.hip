@@ -216,13 +216,15 @@ __global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __re
     }
 }
 
-// dh of the listed rows: its slices added in order, times c.
+// dh of the listed rows: its slices (head[3] of them) added in order, times c.
 constexpr int kJoinThreads = 256;
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int splits, int64_t stride,
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int tile_rows, int direct,
                                                             const int32_t* __restrict__ head,
                                                             const int32_t* __restrict__ rows, int d,
                                                             const float* __restrict__ coef, uint16_t* dh) {
-    const int n = head[0];
+    const int n = head[0], splits = head[3];
+    if (splits == 1 && direct) return;                     // (written as it was finished)
+    const int64_t stride = static_cast<int64_t>((n + tile_rows - 1) / tile_rows) * tile_rows * d;
     const float c = *coef;
     const int64_t total = static_cast<int64_t>(n) * (d / 8);
     for (int64_t at = blockIdx.x * int64_t(kJoinThreads) + threadIdx.x; at < total; at += int64_t(gridDim.x) * kJoinThreads) {
@@ -244,7 +246,6 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restr
 // one of Big and Mid whose rounds over the CUs take less time.  (A chunk costs a
 // Big workgroup kBigNs, a Mid one kMidNs.)
 enum Size { kSmall, kMid, kBig };
-constexpr int kBigNs = 1900, kMidNs = 900, kCus = 256;
 int64_t tiles_of(int64_t rows, int64_t cols, int nb, int na) { return ((rows + nb - 1) / nb) * ((cols + na - 1) / na); }
 Size pick_tile(int64_t rows, int64_t cols) {
     if (rows <= Small::NB) return kSmall;
@@ -286,16 +287,14 @@ CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) 
     auto fit = [&](size_t room) {
         return static_cast<int>(std::max<size_t>(least, std::min<size_t>(vpad, room / (2 * tp) / 256 * 256)));
     };
-    // dh: slices of the reduction until the CUs have an item each, none under 4 chunks
-    const Size zh = dh_tile(T);
-    const int64_t items = tiles_of(T, d, zh == kSmall ? Small::NB : zh == kMid ? Mid::NB : Big::NB, tile_cols(zh));
-    p.splits = 1;
-    while (dh && items * p.splits * 2 <= kCus && vpad / kBK / (p.splits * 2) >= 4) p.splits *= 2;
+    // dh: room for its slices, a few of many rows (how many there are is chosen on
+    // the device, by the rows that count)
+    const size_t pool = dh ? std::max<size_t>(tp, std::min<size_t>(16 * tp, 16384)) : 0;
+    p.pool_rows = static_cast<int>(pool);
     auto layout = [&](int piece) {
         size_t off = 0;
         auto take = [&](size_t n) { const size_t at = off; off += (n + 255) & ~size_t(255); return at; };
         p.piece = piece;
-        p.parts = dh && (p.splits > 1 || piece < vpad) ? p.splits : 0;
         p.head = take(16);
         p.coef = take(4);
         p.rows = take(tp * 4);
@@ -305,7 +304,7 @@ CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) 
         p.stats = take(tp * 8);
         p.hc = take(tp * d * 2);
         p.part = take(tp * p.tiles * 8);
-        p.dhp = take(static_cast<size_t>(p.parts) * tp * d * 4);
+        p.dhp = take(pool * d * 4);
         p.g = off;
         p.total = off + (dh || dw ? tp * piece * 2 : 0);
     };
@@ -372,14 +371,11 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
             GemmArgs a{};
             a.a = w; a.lda = d; a.na = d; a.a_rows = nv;
             a.b = gbuf; a.ldb = p.piece; a.nb = T; a.nb_dev = head;
-            a.K = nv; a.splits = p.splits;
-            if (p.parts) {
-                a.out = dhp; a.ldo = d; a.split_stride = static_cast<int64_t>(p.rows_pad) * d; a.add = v0 > 0;
-                e = launch_sized<true, false, PART>(zh, a, s);
-            } else {
-                a.out = c.dh; a.ldo = d; a.rows = rows; a.coef = coef;
-                e = launch_sized<true, false, ROWS>(zh, a, s);
-            }
+            a.K = nv; a.splits = 0;
+            a.pool_rows = p.pool_rows; a.slice_chunks = std::min(p.piece, V + kBK - 1) / kBK; a.slices_out = head + 3;
+            a.direct = p.piece < V ? nullptr : c.dh;
+            a.out = dhp; a.ldo = d; a.add = v0 > 0; a.rows = rows; a.coef = coef;
+            e = launch_sized<true, false, PART>(zh, a, s);
         }
         if (e == hipSuccess && c.dw) {
             GemmArgs a{};
@@ -390,10 +386,11 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
             e = launch_sized<true, true, ROWS>(pick_tile(nv, d), a, s);
         }
     }
-    if (e == hipSuccess && p.parts) {
+    if (e == hipSuccess && c.dh) {
         const int64_t n8 = static_cast<int64_t>(T) * (d / 8);
-        join_kernel<<<static_cast<int>(std::min<int64_t>((n8 + kJoinThreads - 1) / kJoinThreads, 2048)), kJoinThreads, 0, s>>>(
-            dhp, p.splits, static_cast<int64_t>(p.rows_pad) * d, head, rows, d, coef, c.dh);
+        if (n8 > 0)
+            join_kernel<<<static_cast<int>(std::min<int64_t>((n8 + kJoinThreads - 1) / kJoinThreads, 2048)), kJoinThreads, 0, s>>>(
+                dhp, zh == kSmall ? Small::NB : zh == kMid ? Mid::NB : Big::NB, p.piece < V ? 0 : 1, head, rows, d, coef, c.dh);
         e = hipGetLastError();
     }
     return e;

@@ -247,8 +247,7 @@ struct CePlan {
     int rows_pad;            // rows of the row arrays: T rounded up to whole tiles
     int tile, tiles;         // head rows per column tile of the first pass, and their number
     int piece;               // head rows whose G is held at a time
-    int splits;              // reduction slices of dh
-    int parts;               // fp32 slices of dh held (0: it is written directly)
+    int pool_rows;           // fp32 rows of dh's slices there is room for
 };
 struct CeCall {
     const uint16_t* h;       // [T][d]

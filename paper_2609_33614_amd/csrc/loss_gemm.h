@@ -63,11 +63,15 @@ struct GemmArgs {
     int a_rows;                // stored rows of a "columns" A operand (later ones read the last)
     const int32_t* k_rows;     // GATHER: the stored row of A of each reduction element (whole chunks of them)
     int segs, map;             // FOLD, B by rows: see loss_gemm
-    int splits;                // slices of the reduction (PART)
+    int splits;                // slices of the reduction (PART); 0: chosen on the device (pick_slices)
+    int pool_rows, slice_chunks;   // ... by the rows the slices may take and the reduction's chunks
+    int32_t* slices_out;       // ... and written there
+    void* direct;              // ... and one slice goes there as ROWS (or null)
     int col0;                  // LSE, GRAD: vocabulary index of column 0
     int xcds;
     void* out;                 // GRAD, ROWS, LSE: bf16; ROWS32: fp32; PART: fp32 slices
-    int64_t ldo, split_stride;
+    int64_t ldo;
+    int64_t split_stride;      // PART: between slices (0: the output's whole tiles of rows)
     int kept;                  // LSE: columns below it leave exp(z - the tile's maximum) in out
     const int32_t* rows;       // ROWS, ROWS32: destination of each output row (or null: itself)
     const float* coef;         // ROWS: factor c on the device, or null: factor
@@ -91,16 +95,22 @@ __device__ __forceinline__ int swz_row(int r) { return (static_cast<unsigned>(r)
 // with 4 (k % 4) puts them on different banks.
 __device__ __forceinline__ int swz_col(int k) { return (k & 3) << 2; }
 
+__device__ __forceinline__ uint64_t uniform(uint64_t v) {
+    return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32)))) << 32 |
+           static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
+}
+
 // Loads of one operand's part of a chunk: where lane l of load j gets the 16
-// bytes that belong at LDS byte 1024 (wave + kWaves j) + 16 l.
+// bytes that belong at LDS byte 1024 (wave + WAVES j) + 16 l of the part.
 template <int N, int L, int WAVES, bool COLS, bool GATHER = false>
 struct Operand {
-    const char* base;          // uniform: the item's first chunk
+    uint64_t src;              // uniform: where the chunk begins
+    uint32_t step;             // to the next chunk's
     uint32_t ldbytes;
-    uint32_t off[L];           // rows: byte offset; columns: that of the index
-    int k_last;                // columns: last stored row, from the item's first chunk (for the clamp)
-    const int32_t* rows;       // GATHER: where the item's reduction rows are stored
-    int at[GATHER ? L : 1];    // GATHER: those of the chunk issued next
+    uint32_t off[L];           // byte offset of the lane's 16 bytes from there (GATHER: from their row)
+    int k_last;                // columns: last stored row, from the chunk's first
+    const int32_t* rows;       // GATHER: where the reduction rows of the next chunk are stored
+    int at[GATHER ? L : 1];    // GATHER: those of the chunk
 
     // first: the tile's first index, count: indices there are (>= 1), k0: the
     // slice's first k, k_rows: stored rows of a columns operand
@@ -108,7 +118,8 @@ struct Operand {
         const int lane = lane_id(), wave = wave_id();
         ldbytes = static_cast<uint32_t>(ld) * 2;
         if constexpr (COLS) {
-            base = reinterpret_cast<const char*>(p) + static_cast<size_t>(k0) * ldbytes;
+            src = uniform(reinterpret_cast<uint64_t>(p) + static_cast<uint64_t>(k0) * ldbytes);
+            step = kBK * ldbytes;
             k_last = k_rows - 1 - k0;
             constexpr int VPR = N / 8;         // 16-byte slots per LDS row
 #pragma unroll
@@ -116,9 +127,11 @@ struct Operand {
                 const int g = (wave + WAVES * j) * 64 + lane;
                 const int k = g / VPR, v = (g % VPR) ^ swz_col(k);
                 off[j] = static_cast<uint32_t>(min(first + 8 * v, count - 8)) * 2;
+                if constexpr (!GATHER) off[j] += __umul24(min(k, k_last), ldbytes);
             }
         } else {
-            base = reinterpret_cast<const char*>(p) + static_cast<size_t>(first) * ldbytes + 2 * static_cast<size_t>(k0);
+            src = uniform(reinterpret_cast<uint64_t>(p) + static_cast<uint64_t>(first) * ldbytes + 2 * static_cast<uint64_t>(k0));
+            step = kBK * 2;
             k_last = 0;
 #pragma unroll
             for (int j = 0; j < L; ++j) {
@@ -127,42 +140,37 @@ struct Operand {
             }
         }
     }
-    __device__ __forceinline__ void look_up(int c) {
-        const int lane = lane_id(), wave = wave_id();
-        if constexpr (GATHER) {
+    __device__ __forceinline__ void next() {
+        src += step;
+        if constexpr (COLS && !GATHER) {
+            k_last -= kBK;
+            if (k_last < kBK - 1) {            // the last chunk, not a whole one: its last row again
 #pragma unroll
-            for (int j = 0; j < L; ++j) at[j] = rows[c * kBK + ((wave + WAVES * j) * 64 + lane) / (N / 8)];
+                for (int j = 0; j < L; ++j) {
+                    const int k = ((wave_id() + WAVES * j) * 64 + lane_id()) / (N / 8);
+                    off[j] -= __umul24(max(k - k_last, 0), ldbytes);
+                }
+            }
         }
     }
-    __device__ __forceinline__ uint64_t source(int c) const {      // uniform: chunk c (not GATHER)
-        const uint64_t at64 = reinterpret_cast<uint64_t>(base) + static_cast<uint64_t>(c) * (COLS ? kBK * ldbytes : kBK * 2);
-        return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at64 >> 32)))) << 32 |
-               static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at64)));
-    }
-    // load j of chunk c (src: source(c)) into LDS at `st`; a load is waited for
-    // by count: the compiler adds no waits of its own for asm.  GATHER: after look_up(c).
-    // `on`: lanes that load, all or none (an instruction without lanes still
-    // counts as a load of the wave, so that the waits are constants).
-    __device__ __forceinline__ void load(uint8_t* st, uint64_t src, int c, int j, uint64_t on) const {
-        const int lane = lane_id(), wave = wave_id();
-        const uint32_t lds = __builtin_amdgcn_readfirstlane(
-            static_cast<uint32_t>(reinterpret_cast<uintptr_t>(st + 1024 * (wave + WAVES * j))));
-        uint32_t o = off[j];
+    // the stored rows of the chunk at `rows`
+    __device__ __forceinline__ void look_up() {
         if constexpr (GATHER) {
-            const char* p = base + static_cast<size_t>(at[j]) * ldbytes + o;
-            uint64_t save;
-            asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\t"
-                         "global_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, %0"
-                         : "=&s"(save) : "v"(p), "s"(lds), "s"(on) : "memory", "m0");
+#pragma unroll
+            for (int j = 0; j < L; ++j) at[j] = rows[((wave_id() + WAVES * j) * 64 + lane_id()) / (N / 8)];
+        }
+    }
+    // load j of the chunk (at: src, in scalar registers) into the part at LDS byte `lds` (+ 1024
+    // wave); a load is waited for by count: the compiler adds no waits of its own for asm
+    __device__ __forceinline__ void load(uint32_t lds, uint64_t from, int j) const {
+        const uint32_t o = off[j];
+        if constexpr (GATHER) {
+            const uint64_t p = from + static_cast<uint64_t>(at[j]) * ldbytes + o;
+            asm volatile("s_add_u32 m0, %1, %2\n\tglobal_load_lds_dwordx4 %0, off"
+                         :: "v"(p), "s"(lds), "n"(1024 * WAVES * j) : "memory", "m0", "scc");
         } else {
-            if constexpr (COLS) {
-                const int k = ((wave + WAVES * j) * 64 + lane) / (N / 8);
-                o += __umul24(min(k, k_last - c * kBK), ldbytes);
-            }
-            uint64_t save;
-            asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %4\n\ts_mov_b32 m0, %3\n\t"
-                         "global_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, %0"
-                         : "=&s"(save) : "v"(o), "s"(src), "s"(lds), "s"(on) : "memory", "m0");
+            asm volatile("s_add_u32 m0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %1"
+                         :: "v"(o), "s"(from), "s"(lds), "n"(1024 * WAVES * j) : "memory", "m0", "scc");
         }
     }
 };
@@ -193,6 +201,25 @@ struct Item {
     int a0, b0, sp;
 };
 
+// Slices of a reduction of `chunks` over `items` tiles whose every slice holds
+// `rows` fp32 rows of `cols`, `pool_rows` of them at most: the count that takes
+// least time, by its rounds over the CUs (about 1650 ns a chunk of the 256 x 256
+// tile, 800 of the smaller ones) and the slices' rows written and read again
+// (about 4.5 TB/s).  A slice keeps four chunks.  (The times and the CU count
+// only steer the choice.)
+constexpr int kCus = 256;
+constexpr int kBigNs = 1650, kMidNs = 800;
+__device__ inline int pick_slices(int items, int chunks, int rows, int cols, int pool_rows, int chunk_ns) {
+    int best = 1;
+    int64_t least = static_cast<int64_t>((items + kCus - 1) / kCus) * chunks * chunk_ns;
+    for (int s = 2; s <= 32 && s * rows <= pool_rows && chunks / s >= 4; ++s) {
+        const int64_t cost = static_cast<int64_t>((items * s + kCus - 1) / kCus) * ((chunks + s - 1) / s) * chunk_ns +
+                             static_cast<int64_t>(s) * rows * cols / 562;
+        if (cost < least) { best = s; least = cost; }
+    }
+    return best;
+}
+
 // The reference of a row's exponentials over a tile with maximum m (infinite
 // where all are -inf, whose sum is 0, or some +inf: then 0).
 __device__ __forceinline__ float tile_ref(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
@@ -215,8 +242,18 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
     const int nb = g.nb_dev ? min(*g.nb_dev, g.nb) : g.nb;
     const int K = g.k_dev ? min(*g.k_dev, g.K) : g.K;
     const int nta = (g.na + C::NA - 1) / C::NA, ntb = (nb + NBO - 1) / NBO;
-    const int splits = OUT == PART ? g.splits : 1;
     const int chunks = (K + kBK - 1) / kBK;
+    int splits = 1;
+    if constexpr (OUT == PART) {
+        splits = g.splits;
+        if (splits == 0) {
+            splits = __builtin_amdgcn_readfirstlane(pick_slices(nta * ntb, g.slice_chunks, ntb * NBO, g.na, g.pool_rows,
+                                                                C::NA == 256 ? kBigNs : kMidNs));
+            if (blockIdx.x == 0 && threadIdx.x == 0) *g.slices_out = splits;
+        }
+    }
+    const bool direct = OUT == PART && splits == 1 && g.direct;
+    const int64_t split_stride = g.split_stride ? g.split_stride : static_cast<int64_t>(ntb) * NBO * g.ldo;
     const int work = nta * ntb * splits;
     // contiguous parts of the work list per XCD (workgroups are dealt to XCDs
     // round-robin), in it groups of 8 row tiles, column tile by column tile:
@@ -242,71 +279,92 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
     const int lane = lane_id(), wave = wave_id();
     const int l32 = lane & 31, lh = lane >> 5;
     const int arow = 32 * FA * (wave % C::WA), brow = 32 * FB * (wave / C::WA);
-    const float coef = (OUT == ROWS || OUT == ROWS32) ? (g.coef ? *g.coef : g.factor) : 1.f;
+    const float coef = (OUT == ROWS || OUT == ROWS32 || OUT == PART) ? (g.coef ? *g.coef : g.factor) : 1.f;
 
     auto slice = [&](int sp) { return chunks * sp / splits; };     // first chunk of a slice
 
     // The stream of loads: the parts A, B, A, B, ... of the chunks of this
     // workgroup's items, on into the next item while the last chunks of one are
     // computed and stored.  After the first A it goes by pairs, the B of the last
-    // A and the A after it; behind the last chunk the pairs load nothing.
+    // A and the A after it.  Behind the last chunk (`ended`) the pairs load that one
+    // again, into slots nothing reads, so that the waits are constants; a workgroup
+    // whose items have no chunks never loads (nor meets).
     Operand<C::NA, C::kLA, C::kWaves, ACOLS, GATHER> oa;
     Operand<C::NB, C::kLB, C::kWaves, BCOLS> ob;
-    int iwid = wid - per_xcd, ich = -1, inch = 0;     // the last A's item and chunk, the item's chunks
+    int iwid = wid - per_xcd, left = 1;       // the last A's item, chunks from it on
+    int cb = 0, bfirst = 0;                   // FOLD by rows: B's chunk and first row
     Item item{};
-    uint64_t aon = 0, bon = 0, srca = 0, srcb = 0;
-    int cb = 0, islot = 0;                    // islot: the slot loaded next
+    bool fresh = false, ended = false;        // the last A is its item's first; there is none after it
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring)) + 1024 * wave;
+    int islot = 0;                            // the slot loaded next
     auto next_a = [&]() __attribute__((always_inline)) {
-        if (++ich < inch) {
-            srca = GATHER ? 0 : oa.source(ich);
+        fresh = false;
+        if (--left > 0) {
+            oa.next();
             return;
         }
         for (iwid += per_xcd; iwid < wend; iwid += per_xcd) {          // the next item that has chunks
             item = item_at(iwid);
             const int c0 = slice(item.sp);
-            inch = slice(item.sp + 1) - c0;
-            if (inch == 0) continue;
+            left = slice(item.sp + 1) - c0;
+            if (left == 0) continue;
             oa.set(g.a, g.lda, item.a0, g.na, GATHER ? 0 : c0 * kBK, g.a_rows);
             if constexpr (GATHER) {
+                oa.step = 0;
                 oa.rows = g.k_rows + c0 * kBK;
-                oa.look_up(0);
+                oa.look_up();
             }
-            ich = 0;
-            srca = GATHER ? 0 : oa.source(0);
-            aon = ~0ull;
+            fresh = true;
             return;
         }
-        aon = 0;
-        ich = -1;
-        inch = 0;
+        ended = true;
+    };
+    auto looked_up = [&]() __attribute__((always_inline)) {   // after A's loads: the next chunk's rows
+        if constexpr (GATHER) {
+            if (!ended && left > 1) {
+                oa.rows += kBK;
+                oa.look_up();
+            }
+        }
     };
     auto next_pair = [&]() __attribute__((always_inline)) {
-        bon = aon;
-        if (bon) {
+        if (ended) return;
+        if (fresh) {
             // (every stored row and column of B there is up to whole tiles)
-            if (ich == 0) ob.set(g.b, g.ldb, item.b0 / NBO * C::NB, 1 << 30, slice(item.sp) * kBK, 1 << 30);
-            cb = FOLD && !BCOLS ? ich / g.segs * 4 + ((g.map >> (4 * (ich % g.segs))) & 15) : ich;
-            srcb = ob.source(cb);
-            next_a();
+            ob.set(g.b, g.ldb, item.b0 / NBO * C::NB, 1 << 30, slice(item.sp) * kBK, 1 << 30);
+            cb = 0;
+            bfirst = item.b0;
+        } else {
+            ob.next();
+            ++cb;
         }
+        next_a();
     };
     auto slot_at = [&](int ahead) __attribute__((always_inline)) {
         const int sl = islot + ahead;
-        return ring + (sl >= C::SLOTS ? sl - C::SLOTS : sl) * C::kSlot;
+        return (sl >= C::SLOTS ? sl - C::SLOTS : sl) * C::kSlot;
     };
     auto advance = [&](int parts) __attribute__((always_inline)) {
         islot += parts;
         if (islot >= C::SLOTS) islot -= C::SLOTS;
     };
+    uint32_t ldsa = lds0, ldsb = 0;           // the pair's slots and sources
+    uint64_t srca = 0, srcb = 0;
+    auto pair_slots = [&]() __attribute__((always_inline)) {
+        ldsb = lds0 + slot_at(0);
+        ldsa = lds0 + slot_at(1);
+        advance(2);
+        srca = uniform(oa.src);
+        srcb = uniform(ob.src);
+        if constexpr (FOLD && !BCOLS) {        // the group's part that meets A's chunk (splits is 1: chunks from 0 on)
+            const int c = cb / g.segs * 4 + ((g.map >> (4 * (cb % g.segs))) & 15);
+            srcb = uniform(reinterpret_cast<uint64_t>(g.b + static_cast<size_t>(bfirst) * g.ldb) + c * (kBK * 2));
+        }
+    };
     // load q of a pair: B's, then A's
     auto pair_load = [&](int q) __attribute__((always_inline)) {
-        if (q < C::kLB) ob.load(slot_at(0), srcb, cb, q, bon);
-        else oa.load(slot_at(1), srca, ich, q - C::kLB, aon);
-    };
-    auto pair_done = [&]() __attribute__((always_inline)) {
-        if constexpr (GATHER)
-            if (aon) oa.look_up(min(ich + 1, inch - 1));
-        advance(2);
+        if (q < C::kLB) ob.load(ldsb, srcb, q);
+        else oa.load(ldsa, srca, q - C::kLB);
     };
     // Waits until at most the loads of the parts behind the chunk met next, and
     // `stores` output stores issued since, are still in flight (vector memory operations complete
@@ -319,17 +377,20 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
         else wait_vm<N + 16>();
     };
     next_a();
+    if (!ended) {
+        srca = uniform(oa.src);
 #pragma unroll
-    for (int j = 0; j < C::kLA; ++j) oa.load(slot_at(0), srca, ich, j, aon);
-    if constexpr (GATHER)
-        if (aon) oa.look_up(min(ich + 1, inch - 1));
-    advance(1);
+        for (int j = 0; j < C::kLA; ++j) oa.load(ldsa, srca, j);
+        looked_up();
+        advance(1);
 #pragma unroll 1
-    for (int i = 0; i < (C::kAhead - 1) / 2; ++i) {
-        next_pair();
+        for (int i = 0; i < (C::kAhead - 1) / 2; ++i) {
+            next_pair();
+            pair_slots();
 #pragma unroll
-        for (int q = 0; q < C::kLA + C::kLB; ++q) pair_load(q);
-        pair_done();
+            for (int q = 0; q < C::kLA + C::kLB; ++q) pair_load(q);
+            looked_up();
+        }
     }
     int slot0 = 0;                            // slot of the chunk met next
     int stored = 0;                           // output stores since the loads it awaits
@@ -395,6 +456,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
             sb = ring + slot0 * C::kSlot;
             slot0 = slot0 + 1 == C::SLOTS ? 0 : slot0 + 1;
             next_pair();
+            pair_slots();
         };
         auto first_three = [&]() __attribute__((always_inline)) {
             read(1, 1);
@@ -413,7 +475,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
             read(0, 0);
 #pragma unroll
             for (int q = 0; q < kPair; ++q) pair_load(q);
-            pair_done();
+            looked_up();
             for (int c = 1; c < nch; ++c) {
                 first_three();
                 meet(0);
@@ -427,7 +489,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                     for (int q = m * kPair / kProducts; q < (m + 1) * kPair / kProducts; ++q) pair_load(q);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                pair_done();
+                looked_up();
             }
             first_three();
             products(1);
@@ -436,14 +498,14 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
         stored = 0;
         // lane: row cur.b0 + brow + 32 j + l32, columns cur.a0 + arow + 32 i + 8 (q / 4) + 4 lh + q % 4
         auto share = [&](int w) __attribute__((always_inline)) {      // wave w's bytes of those slots
-            return slot_at(w >= C::kWaves / 2) + w % (C::kWaves / 2) * C::kShare;
+            return ring + slot_at(w >= C::kWaves / 2) + w % (C::kWaves / 2) * C::kShare;
         };
         uint8_t* const tb = share(wave);
         // FA fragments' 32 rows of 64 FA bytes, turned around through the
         // wave's share of LDS so that adjacent lanes store adjacent pieces
         auto store16 = [&](int j, auto val, auto dst, int nv) __attribute__((always_inline)) {
             constexpr int V = 4 * FA;         // 16-byte pieces per row
-            auto at = [&](int r, int v) { return r * (64 * FA) + ((v ^ (FA == 2 ? r & 7 : (r >> 1) & 3)) << 4); };
+            auto at = [&](int r, int v) { return r * (64 * FA) + ((v ^ (FA == 1 ? (r >> 1) & 3 : r & (4 * FA - 1))) << 4); };
 #pragma unroll
             for (int i = 0; i < FA; ++i)
 #pragma unroll
@@ -544,12 +606,12 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                         p = v == rel ? st.y : p;
                         return v < end ? p : 0.f;
                     }, [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; }, nv);
-                } else if constexpr (OUT == ROWS) {
+                } else if (OUT == ROWS || direct) {
                     if (cur.a0 + arow >= g.na) break;      // (columns come in multiples of 64)
                     store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q] * coef; },
                             [&](int r) {
                                 const int64_t to = g.rows && r < nv ? g.rows[row0 + r] : row0 + r;
-                                return static_cast<uint16_t*>(g.out) + to * g.ldo + cur.a0 + arow;
+                                return static_cast<uint16_t*>(direct ? g.direct : g.out) + to * g.ldo + cur.a0 + arow;
                             }, nv);
                 } else {
                     auto at = [&](int r, int v) { return r * 128 + ((v ^ (r & 7)) << 4); };
@@ -572,7 +634,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                                 const int64_t to = g.rows ? g.rows[row0 + r] : row0 + r;
                                 *reinterpret_cast<f32x4*>(static_cast<float*>(g.out) + to * g.ldo + col + 4 * v) = d * coef;
                             } else if (r < nv) {
-                                float* const p = static_cast<float*>(g.out) + cur.sp * g.split_stride +
+                                float* const p = static_cast<float*>(g.out) + cur.sp * split_stride +
                                                  (row0 + r) * g.ldo + col + 4 * v;
                                 if (g.add) d += *reinterpret_cast<const f32x4*>(p);
                                 *reinterpret_cast<f32x4*>(p) = d;
@@ -586,6 +648,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
         wid += per_xcd;
         if (wid >= wend) break;
     }
+    wait_vm<0>();                             // (the last pairs' loads land before the LDS is another's)
 }
 
 // rows[0 .. n): the indices t < T whose key is not `skip`, in order, and the
@@ -661,7 +724,8 @@ template <class C, bool ACOLS, bool BCOLS, int OUT, bool FOLD = false, bool GATH
 hipError_t launch_gemm(GemmArgs g, hipStream_t s) {
     constexpr int kRows = FOLD && BCOLS ? 64 : C::NB;
     g.xcds = geometry().xcds;
-    const int64_t work = static_cast<int64_t>((g.na + C::NA - 1) / C::NA) * ((g.nb + kRows - 1) / kRows) * g.splits;
+    const int64_t work = static_cast<int64_t>((g.na + C::NA - 1) / C::NA) * ((g.nb + kRows - 1) / kRows) *
+                         (g.splits ? g.splits : kCus);
     if (work == 0) return hipSuccess;
     int64_t blocks = std::min<int64_t>(work, geometry().cus);
     blocks = std::max<int64_t>(g.xcds, (blocks + g.xcds - 1) / g.xcds * g.xcds);

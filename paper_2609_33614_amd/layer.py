@@ -17,9 +17,8 @@ def _expect(name: str, t: Optional[torch.Tensor], dtype, shape) -> None:
     """Refuse a tensor (None passes) whose type or shape the library would misread."""
     if t is None:
         return
-    dtypes = dtype if isinstance(dtype, tuple) else (dtype,)
-    if t.dtype not in dtypes or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected {' or '.join(str(v) for v in dtypes)} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)) or t.shape != tuple(shape):
+        raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
 
 
 class EatLayer:
