@@ -58,9 +58,9 @@ struct StatArgs {
 // Lane l holds experts l % EP + 64 j of token l / EP of a group of 64 / EP
 // tokens (EP: E rounded up to a power of two, 64 at most); a wave has kStatRows
 // groups' loads in flight.
-constexpr int kStatRows = 4;
 template <int J>
 __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
+    constexpr int kStatRows = J <= 2 ? 8 : 4;
     __shared__ double red[kStatWaves][kWave * J];
     __shared__ int redc[kStatWaves][kWave * J];
     __shared__ int redn[kStatWaves];
@@ -381,60 +381,65 @@ struct ProductArgs {
     float* dwp;                // else its slices [splits][E][d], unscaled
     void* dx;
 };
-template <typename XT>
-__global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
+// out[r][c] = scale sum_k dz[r rs + k ks] v[k][c] over k in [kbeg, kend), those
+// whose valid[k] is 0 left out, for rows r0 .. r0 + 63 and columns c0 .. c0 + 63.
+template <typename VT, typename OT>
+__device__ __forceinline__ void product_tile(const float* dz, int rs, int ks, const VT* v, const uint8_t* valid, int kbeg,
+                                             int kend, int rows, int r0, int d, int c0, float scale, OT* out) {
     const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int l16 = lane & 15, lk = lane >> 4, cols = a.d / 64;
-    const bool dw = static_cast<int>(blockIdx.x) < a.blocks_w;
-    int b = dw ? blockIdx.x : blockIdx.x - a.blocks_w;
-    const int c0 = b % cols * 64;
-    b /= cols;
-    const int rows = dw ? a.E : a.T, tiles = (rows + 63) / 64;
-    const int r0 = b % tiles * 64 + 16 * wave, sp = b / tiles;
-    const int row = min(r0 + l16, rows - 1);
-    int kbeg = 0, kend = a.E;
-    if (dw) {
-        const int per = ((a.T + a.splits - 1) / a.splits + 3) / 4 * 4;
-        kbeg = min(a.T, sp * per);
-        kend = min(a.T, kbeg + per);
-    }
+    const int l16 = lane & 15, lk = lane >> 4;
+    r0 += 16 * wave;
+    const float* const zr = dz + static_cast<size_t>(min(r0 + l16, rows - 1)) * rs;
     f32x4 acc[4] = {};
     for (int k0 = kbeg; k0 < kend; k0 += 4 * kSteps) {
-        float z[kSteps], v[kSteps][4];
-        bool on[kSteps];
+        float z[kSteps], x[kSteps][4];
+        uint8_t ok[kSteps];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) ok[s] = 1;
+        if (valid) {
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) ok[s] = valid[min(k0 + 4 * s + lk, kend - 1)];
+        }
+        // (every load is unconditional, of a reduction element that exists)
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             const int k = min(k0 + 4 * s + lk, kend - 1);
-            on[s] = k0 + 4 * s + lk < kend;
-            if (dw) {
-                if (a.valid) on[s] = on[s] && a.valid[k];
-                z[s] = a.dz[static_cast<size_t>(k) * a.E + row];
-            } else {
-                z[s] = a.dz[static_cast<size_t>(row) * a.E + k];
-            }
+            z[s] = zr[static_cast<size_t>(k) * ks];
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
-                const size_t at = static_cast<size_t>(k) * a.d + c0 + 16 * f + l16;
-                v[s][f] = dw ? load_f32(static_cast<const XT*>(a.x) + at) : a.w[at];
-            }
+            for (int f = 0; f < 4; ++f) x[s][f] = load_f32(v + static_cast<size_t>(k) * d + c0 + 16 * f + l16);
         }
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+        for (int s = 0; s < kSteps; ++s) {
+            const bool on = k0 + 4 * s + lk < kend && ok[s];
 #pragma unroll
             for (int f = 0; f < 4; ++f)
-                acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(on[s] ? z[s] : 0.f, on[s] ? v[s][f] : 0.f, acc[f], 0, 0, 0);
+                acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(on ? z[s] : 0.f, on ? x[s][f] : 0.f, acc[f], 0, 0, 0);
+        }
     }
 #pragma unroll
     for (int f = 0; f < 4; ++f)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = r0 + 4 * lk + i;
-            if (r >= rows) continue;
-            const size_t at = static_cast<size_t>(r) * a.d + c0 + 16 * f + l16;
-            if (!dw) store_f32(static_cast<XT*>(a.dx) + at, acc[f][i] * a.scale);
-            else if (a.splits == 1) a.dw[at] = acc[f][i] * a.scale;
-            else a.dwp[static_cast<size_t>(sp) * a.E * a.d + at] = acc[f][i];
+            if (r < rows) store_f32(out + static_cast<size_t>(r) * d + c0 + 16 * f + l16, acc[f][i] * scale);
         }
+}
+
+template <typename XT>
+__global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
+    const bool dw = static_cast<int>(blockIdx.x) < a.blocks_w;
+    const int block = dw ? blockIdx.x : blockIdx.x - a.blocks_w, cols = a.d / 64;
+    const int c0 = block % cols * 64, b = block / cols;
+    if (dw) {
+        const int tiles = (a.E + 63) / 64, sp = b / tiles;
+        const int per = ((a.T + a.splits - 1) / a.splits + 3) / 4 * 4;
+        const int kbeg = min(a.T, sp * per), kend = min(a.T, kbeg + per);
+        float* const out = a.splits == 1 ? a.dw : a.dwp + static_cast<size_t>(sp) * a.E * a.d;
+        product_tile(a.dz, 1, a.E, static_cast<const XT*>(a.x), a.valid, kbeg, kend, a.E, b % tiles * 64, a.d, c0,
+                     a.splits == 1 ? a.scale : 1.f, out);
+    } else {
+        product_tile(a.dz, a.E, 1, a.w, nullptr, 0, a.E, a.T, b * 64, a.d, c0, a.scale, static_cast<XT*>(a.dx));
+    }
 }
 
 // dW_r: the slices' rows of `parts` blocks of d added in order, times scale.
@@ -452,8 +457,8 @@ __global__ __launch_bounds__(256) void dw_join_kernel(const float* __restrict__ 
 
 using Fold = Big;
 
-constexpr int kOneBlock = 16384;          // most probabilities one workgroup sums up
-constexpr int kOneSlice = 256;            // most tokens that dW_r of a small call takes in one slice
+constexpr int kOneBlock = 4096;           // most probabilities one workgroup sums up
+constexpr int kOneSlice = 64;             // most tokens that dW_r of a small call takes in one slice
 
 // Products on the split operands from here on, on fp32 instructions below.
 bool split_products(const eat_params_t& p, int32_t T) {

@@ -68,16 +68,27 @@ __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
     const int y = i < n ? target[t] : 0;
     const bool known = y >= 0 && y < V;
     double z = 0.0;
-    for (int k = 8 * lane; k < d; k += 8 * kWave) {
-        const uint4 p = i < n ? *reinterpret_cast<const uint4*>(h + static_cast<size_t>(t) * d + k) : uint4{};
-        const uint4 q = *reinterpret_cast<const uint4*>(w + static_cast<size_t>(known ? y : 0) * d + k);
-        *reinterpret_cast<uint4*>(hc + static_cast<size_t>(i) * d + k) = p;
-        const uint32_t pw[4] = {p.x, p.y, p.z, p.w}, qw[4] = {q.x, q.y, q.z, q.w};
+    constexpr int kLoads = 4;                 // 16-byte pieces of each row a lane has in flight
+    for (int k0 = 8 * lane; k0 < d; k0 += 8 * kWave * kLoads) {
+        uint4 p[kLoads], q[kLoads];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            z = fma(static_cast<double>(__uint_as_float(pw[e] << 16)), static_cast<double>(__uint_as_float(qw[e] << 16)), z);
-            z = fma(static_cast<double>(__uint_as_float(pw[e] & 0xffff0000u)),
-                    static_cast<double>(__uint_as_float(qw[e] & 0xffff0000u)), z);
+        for (int u = 0; u < kLoads; ++u) {    // (pieces past the row load its first)
+            const int k = k0 + 8 * kWave * u < d ? k0 + 8 * kWave * u : k0;
+            p[u] = *reinterpret_cast<const uint4*>(h + static_cast<size_t>(t) * d + k);
+            q[u] = *reinterpret_cast<const uint4*>(w + static_cast<size_t>(known ? y : 0) * d + k);
+        }
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int k = k0 + 8 * kWave * u;
+            if (k >= d) break;
+            *reinterpret_cast<uint4*>(hc + static_cast<size_t>(i) * d + k) = i < n ? p[u] : uint4{};
+            const uint32_t pw[4] = {p[u].x, p[u].y, p[u].z, p[u].w}, qw[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                z = fma(static_cast<double>(__uint_as_float(pw[e] << 16)), static_cast<double>(__uint_as_float(qw[e] << 16)), z);
+                z = fma(static_cast<double>(__uint_as_float(pw[e] & 0xffff0000u)),
+                        static_cast<double>(__uint_as_float(qw[e] & 0xffff0000u)), z);
+            }
         }
     }
     z = wave_sum(z);
@@ -257,7 +268,7 @@ constexpr int tile_cols(Size z) { return z == kBig ? Big::NA : Mid::NA; }
 static_assert(Mid::NA == Small::NA, "column tiles of 128 or 256");
 
 // dh, whose reduction is split over what CUs its tiles leave: by the rows alone.
-Size dh_tile(int64_t rows) { return rows <= Small::NB ? kSmall : rows <= Mid::NB ? kMid : kBig; }
+Size dh_tile(int64_t rows) { return rows <= Small::NB ? kSmall : rows <= 2 * Mid::NB ? kMid : kBig; }
 
 template <bool ACOLS, bool BCOLS, int OUT>
 hipError_t launch_sized(Size z, const GemmArgs& g, hipStream_t s) {

@@ -201,25 +201,26 @@ struct Item {
     int a0, b0, sp;
 };
 
-// Slices of a reduction of `chunks` over `items` tiles whose every slice holds
-// `rows` fp32 rows of `cols`, `pool_rows` of them at most: the count that takes
-// least time, by its rounds over the CUs (about 1650 ns a chunk of the 256 x 256
-// tile, 800 of the smaller ones) and the slices' rows written and read again
+// Slices of a reduction of `chunks` over `items` tiles, every slice's `rows` fp32
+// rows of `cols` taking tile_rows of the pool_rows there are: the count that
+// takes least time, by its rounds over the CUs (about 1650 ns a chunk of the 256 x
+// 256 tile, 800 of the smaller ones) and the slices' rows written and read again
 // (about 4.5 TB/s).  A slice keeps four chunks.  (The times and the CU count
 // only steer the choice.)
-constexpr int kCus = 256;
+constexpr int kCus = 256, kMostSlices = 32;
 constexpr int kBigNs = 1650, kMidNs = 800;
-__device__ inline int pick_slices(int items, int chunks, int rows, int cols, int pool_rows, int chunk_ns) {
+__device__ inline int pick_slices(int items, int chunks, int rows, int cols, int tile_rows, int pool_rows, int chunk_ns) {
     int best = 1;
-    int64_t least = static_cast<int64_t>((items + kCus - 1) / kCus) * chunks * chunk_ns;
-    for (int s = 2; s <= 32 && s * rows <= pool_rows && chunks / s >= 4; ++s) {
-        const int64_t cost = static_cast<int64_t>((items * s + kCus - 1) / kCus) * ((chunks + s - 1) / s) * chunk_ns +
-                             static_cast<int64_t>(s) * rows * cols / 562;
-        if (cost < least) { best = s; least = cost; }
+    float least = 0.f;
+    const float row_ns = static_cast<float>(rows) * static_cast<float>(cols) * (1.f / 562.f);
+    for (int s = 1; s <= kMostSlices && (s == 1 || (s * tile_rows <= pool_rows && 4 * s <= chunks)); ++s) {
+        const int each = static_cast<int>(static_cast<float>(chunks + s - 1) / static_cast<float>(s));
+        const float cost = static_cast<float>((items * s + kCus - 1) / kCus) * static_cast<float>(each * chunk_ns) +
+                           (s > 1 ? static_cast<float>(s) * row_ns : 0.f);
+        if (s == 1 || cost < least) { best = s; least = cost; }
     }
     return best;
 }
-
 // The reference of a row's exponentials over a tile with maximum m (infinite
 // where all are -inf, whose sum is 0, or some +inf: then 0).
 __device__ __forceinline__ float tile_ref(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
@@ -247,8 +248,8 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
     if constexpr (OUT == PART) {
         splits = g.splits;
         if (splits == 0) {
-            splits = __builtin_amdgcn_readfirstlane(pick_slices(nta * ntb, g.slice_chunks, ntb * NBO, g.na, g.pool_rows,
-                                                                C::NA == 256 ? kBigNs : kMidNs));
+            splits = __builtin_amdgcn_readfirstlane(pick_slices(nta * ntb, g.slice_chunks, nb, g.na, ntb * NBO,
+                                                                g.pool_rows, C::NA == 256 ? kBigNs : kMidNs));
             if (blockIdx.x == 0 && threadIdx.x == 0) *g.slices_out = splits;
         }
     }
@@ -725,7 +726,7 @@ hipError_t launch_gemm(GemmArgs g, hipStream_t s) {
     constexpr int kRows = FOLD && BCOLS ? 64 : C::NB;
     g.xcds = geometry().xcds;
     const int64_t work = static_cast<int64_t>((g.na + C::NA - 1) / C::NA) * ((g.nb + kRows - 1) / kRows) *
-                         (g.splits ? g.splits : kCus);
+                         (g.splits ? g.splits : std::max(1, std::min(kMostSlices, g.slice_chunks / 4)));
     if (work == 0) return hipSuccess;
     int64_t blocks = std::min<int64_t>(work, geometry().cus);
     blocks = std::max<int64_t>(g.xcds, (blocks + g.xcds - 1) / g.xcds * g.xcds);
