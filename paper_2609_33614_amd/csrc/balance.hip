@@ -1,9 +1,11 @@
 // The router's balance loss with per-expert counts and gradients (gfx950).
 //
 // stat_kernel sums the probabilities (fp64) and counts the selections of every
-// expert, a share of the tokens per workgroup; the last workgroup to finish
-// adds the shares in order and forms the loss and q = dloss / dP.  prep_kernel
-// makes the scores' gradient dz = p (q - <q, p>) / n row by row.
+// expert, a share of the tokens per workgroup (and lists the tokens that count,
+// in a workgroup beside them); total_kernel adds the shares in order (adding them in
+// every workgroup of prep_kernel took 10 us longer, in the last of stat_kernel's to
+// finish 4 us); prep_kernel makes the scores' gradient dz = p (q - <q, p>) / n
+// row by row, q = dloss / dP.
 //
 // The products of dz with the router weights (dx) and with x (dW_r), small
 // calls: dx_kernel and dw_kernel on fp32 matrix instructions, straight from
@@ -34,7 +36,9 @@ __device__ __forceinline__ void score_grad(const float (&p)[J], const float (&q)
     double s = 0.0;
 #pragma unroll
     for (int j = 0; j < J; ++j) s += static_cast<double>(q[j]) * p[j];
-    for (int o = ep / 2; o >= 1; o /= 2) s += __shfl_xor(s, o, kWave);
+    if (J > 1 || ep == kWave) s = wave_sum(s);
+    else
+        for (int o = ep / 2; o >= 1; o /= 2) s += __shfl_xor(s, o, kWave);
 #pragma unroll
     for (int j = 0; j < J; ++j) dz[j] = p[j] * static_cast<float>(q[j] - s);
 }
@@ -43,17 +47,47 @@ struct StatArgs {
     const float* prob;
     const uint64_t* mask;
     const uint8_t* valid;
-    int T, E;
+    int T, E, blocks;          // blocks: shares of the tokens
     float coef, entropy_coef;
-    int32_t* head;             // {., ., workgroups done}
-    float* q;                  // [E] dloss / dP_e / max(n, 1)
-    double* sum;               // [blocks][E] (unused by one workgroup)
+    float* q;                  // [E] dloss / dP_e / max(n, 1) (of one workgroup)
+    double* sum;               // [blocks][E] (of several)
     int32_t* cnt;              // [blocks][E + 1]: selections, then valid tokens
     float* loss;
     int64_t* count;
     float* mean_prob;
     float* dz;                 // one workgroup: [T][E], made here too (or null)
+    int32_t* rows;             // the valid tokens' list, made by a workgroup more (or null)
+    int32_t* head;             // {n, n in whole chunks, .} of it
 };
+
+// From the totals (a thread per expert: the sum of its probabilities, its
+// selections; `tokens`, thread 0's, those that count) q into qs (LDS) and the
+// call's results out.  Every thread of the workgroup calls it; a thread's q is
+// its own until a barrier.
+struct Totals {
+    double loss[4];
+    int sel[4], tokens;
+};
+__device__ __forceinline__ void finish(const StatArgs& a, double sum, int sel, int tokens, float* qs, Totals& s) {
+    const int tid = threadIdx.x, wave = tid / kWave, E = a.E;
+    // (a call's selections are below 2^31: max_tokens times the most experts of a token is)
+    const int part = wave_sum(tid < E ? sel : 0);
+    if (lane_id() == 0 && wave < 4) s.sel[wave] = part;
+    if (tid == 0) s.tokens = tokens;
+    __syncthreads();
+    const double inv = 1.0 / max(s.tokens, 1), p = sum * inv;
+    const double f = static_cast<double>(sel) / max(s.sel[0] + s.sel[1] + s.sel[2] + s.sel[3], 1);
+    const double lg = p > 0.0 ? log(p) : p == 0.0 ? 0.0 : p;      // (NaN stays)
+    if (tid < E) {
+        qs[tid] = static_cast<float>((a.coef * E * f + a.entropy_coef * (lg + 1.0)) * inv);
+        if (a.count) a.count[tid] = sel;
+        if (a.mean_prob) a.mean_prob[tid] = static_cast<float>(p);
+    }
+    const double l = wave_sum(tid < E ? a.coef * E * f * p + a.entropy_coef * p * lg : 0.0);
+    if (lane_id() == 0 && wave < 4) s.loss[wave] = l;
+    __syncthreads();
+    if (tid == 0) *a.loss = static_cast<float>((s.loss[0] + s.loss[1]) + (s.loss[2] + s.loss[3]));
+}
 
 // Lane l holds experts l % EP + 64 j of token l / EP of a group of 64 / EP
 // tokens (EP: E rounded up to a power of two, 64 at most); a wave has kStatRows
@@ -64,13 +98,17 @@ __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
     __shared__ double red[kStatWaves][kWave * J];
     __shared__ int redc[kStatWaves][kWave * J];
     __shared__ int redn[kStatWaves];
-    __shared__ int last;
+    __shared__ Totals totals;
+    if (static_cast<int>(blockIdx.x) == a.blocks) {
+        list_rows<uint8_t>(a.valid, a.T, 0, a.rows, a.head);
+        return;
+    }
     const int lane = lane_id(), wave = threadIdx.x / kWave, tid = threadIdx.x;
-    const int E = a.E, blocks = gridDim.x;
+    const int E = a.E;
     int ep = 1;
     while (ep < min(E, 64)) ep *= 2;
     const int sub = lane / ep, e0 = lane % ep, tpw = kWave / ep;
-    const int per = (a.T + blocks - 1) / blocks;
+    const int per = (a.T + a.blocks - 1) / a.blocks;
     const int tbeg = min(a.T, static_cast<int>(blockIdx.x) * per), tend = min(a.T, tbeg + per);
     double s[J];
     int c[J], n = 0;
@@ -127,91 +165,21 @@ __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
         }
     }
     if (wave == 0) nn = wave_sum(lane < kStatWaves ? redn[lane] : 0);
-    if (blocks > 1) {
-        // the share to memory past this XCD's cache; the last workgroup reads all
+    if (a.blocks > 1) {                       // (added up by total_kernel)
         if (tid < E) {
-            __hip_atomic_store(a.sum + static_cast<size_t>(blockIdx.x) * E + tid, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(a.cnt + static_cast<size_t>(blockIdx.x) * (E + 1) + tid, k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            a.sum[static_cast<size_t>(blockIdx.x) * E + tid] = t;
+            a.cnt[static_cast<size_t>(blockIdx.x) * (E + 1) + tid] = k;
         }
-        if (tid == 0)
-            __hip_atomic_store(a.cnt + static_cast<size_t>(blockIdx.x) * (E + 1) + E, nn, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __syncthreads();
-        if (tid == 0)
-            last = __hip_atomic_fetch_add(a.head + 2, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
-        __syncthreads();
-        if (!last) return;
-        // a wave takes the shares of its residue, in order, a lane per expert
-        double sj[J];
-        int cj[J];
-#pragma unroll
-        for (int j = 0; j < J; ++j) { sj[j] = 0.0; cj[j] = 0; }
-        for (int b0 = wave; b0 < blocks; b0 += 4 * kStatWaves) {
-            double v[4][J];
-            int w[4][J];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int bs = min(b0 + u * kStatWaves, blocks - 1);
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    const int e = min(64 * j + lane, E - 1);
-                    v[u][j] = __hip_atomic_load(a.sum + static_cast<size_t>(bs) * E + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    w[u][j] = __hip_atomic_load(a.cnt + static_cast<size_t>(bs) * (E + 1) + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    const bool on = b0 + u * kStatWaves < blocks;
-                    sj[j] += on ? v[u][j] : 0.0;
-                    cj[j] += on ? w[u][j] : 0;
-                }
-        }
-        nn = 0;
-        if (wave == 0) {
-            for (int b = lane; b < blocks; b += kWave)
-                nn += __hip_atomic_load(a.cnt + static_cast<size_t>(b) * (E + 1) + E, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            nn = wave_sum(nn);
-        }
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            red[wave][64 * j + lane] = sj[j];
-            redc[wave][64 * j + lane] = cj[j];
-        }
-        __syncthreads();
-        t = 0.0;
-        k = 0;
-        if (tid < E) {
-#pragma unroll
-            for (int w = 0; w < kStatWaves; ++w) {
-                t += red[w][tid];
-                k += redc[w][tid];
-            }
-        }
+        if (tid == 0) a.cnt[static_cast<size_t>(blockIdx.x) * (E + 1) + E] = nn;
+        return;
     }
-    // (a call's selections are below 2^31: max_tokens times the most experts of a token is)
-    const int sel = wave_sum(tid < E ? k : 0);
     __syncthreads();
-    if (tid == 0) redn[15] = nn;
-    if (lane == 0 && wave < 4) redn[wave] = sel;
+    float* const qs = reinterpret_cast<float*>(red);
+    finish(a, t, k, nn, qs, totals);
     __syncthreads();
-    const double inv = 1.0 / max(redn[15], 1), p = t * inv;
-    const double f = static_cast<double>(k) / max(redn[0] + redn[1] + redn[2] + redn[3], 1);
-    const double lg = p > 0.0 ? log(p) : p == 0.0 ? 0.0 : p;      // (NaN stays)
-    if (tid < E) {
-        a.q[tid] = static_cast<float>((a.coef * E * f + a.entropy_coef * (lg + 1.0)) * inv);
-        if (a.count) a.count[tid] = k;
-        if (a.mean_prob) a.mean_prob[tid] = static_cast<float>(p);
-    }
-    const double l = wave_sum(tid < E ? a.coef * E * f * p + a.entropy_coef * p * lg : 0.0);
-    if (lane == 0) red[0][wave] = l;
-    __syncthreads();
-    if (tid == 0) *a.loss = static_cast<float>((red[0][0] + red[0][1]) + (red[0][2] + red[0][3]));
-    if (!a.dz || blocks > 1) return;
+    if (tid < E) a.q[tid] = qs[tid];
+    if (!a.dz) return;
     // small calls: the scores' gradient without a launch of its own
-    float* const qs = reinterpret_cast<float*>(redc);
-    if (tid < E) qs[tid] = static_cast<float>((a.coef * E * f + a.entropy_coef * (lg + 1.0)) * inv);
-    __syncthreads();
     float q[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) q[j] = 64 * j + e0 < E ? qs[64 * j + e0] : 0.f;
@@ -239,11 +207,54 @@ __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
     }
 }
 
-// head of a call whose tokens all count
-__global__ void head_kernel(int T, int32_t* head) {
-    head[0] = T;
-    head[1] = (T + kBK - 1) / kBK * kBK;
-    head[2] = 0;
+// The shares of several workgroups: a wave adds those of its residue, a lane per
+// expert, a thread per expert the waves' in order.
+template <int J>
+__global__ __launch_bounds__(kStatThreads) void total_kernel(StatArgs a) {
+    __shared__ double red[kStatWaves][kWave * J];
+    __shared__ int redc[kStatWaves][kWave * J];
+    __shared__ float qs[kMaxExperts];
+    __shared__ Totals totals;
+    const int lane = lane_id(), wave = threadIdx.x / kWave, tid = threadIdx.x;
+    const int E = a.E;
+    constexpr int N = kStatBlocks / kStatWaves;
+    double v[N][J];
+    int c[N][J];
+    const int tokens = wave_sum(lane < a.blocks ? a.cnt[static_cast<size_t>(min(lane, a.blocks - 1)) * (E + 1) + E] : 0);
+    static_assert(kStatBlocks <= kWave, "a lane per share");
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int b = min(wave + u * kStatWaves, a.blocks - 1), e = min(64 * j + lane, E - 1);
+            v[u][j] = a.sum[static_cast<size_t>(b) * E + e];
+            c[u][j] = a.cnt[static_cast<size_t>(b) * (E + 1) + e];
+        }
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        double s = 0.0;
+        int k = 0;
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            if (wave + u * kStatWaves < a.blocks) {
+                s += v[u][j];
+                k += c[u][j];
+            }
+        red[wave][64 * j + lane] = s;
+        redc[wave][64 * j + lane] = k;
+    }
+    __syncthreads();
+    double t = 0.0;
+    int k = 0;
+    if (tid < E) {
+#pragma unroll
+        for (int w = 0; w < kStatWaves; ++w) {
+            t += red[w][tid];
+            k += redc[w][tid];
+        }
+    }
+    finish(a, t, k, tokens, qs, totals);
+    if (tid < E) a.q[tid] = qs[tid];
 }
 
 // v as a sum of three bf16 numbers, largest first
@@ -256,12 +267,9 @@ __device__ __forceinline__ void split3(float v, uint16_t (&part)[3]) {
 }
 
 struct PrepArgs {
-    const float* prob;
-    const uint8_t* valid;
+    StatArgs stat;
     const int32_t* rows;       // tokens that count, or null: all (valid null, or dz in token order alone)
-    const int32_t* head;
-    int T, E, d;
-    const float* q;
+    int d;
     float* dz;                 // [T][E], or null
     uint16_t* dzs;             // [list row][group][4][64] parts, or null
     void* dx;                  // rows to clear where the token does not count, or null
@@ -279,12 +287,13 @@ constexpr int kPrepThreads = kPrepWaves * kWave;
 template <int J>
 __global__ __launch_bounds__(kPrepThreads) void prep_kernel(PrepArgs a) {
     const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int E = a.E;
+    const int E = a.stat.E, T = a.stat.T;
     const int block = blockIdx.x;
+    const int n = a.rows ? a.stat.head[0] : T, padded = (n + kBK - 1) / kBK * kBK;
     if (block >= a.blocks_z + a.blocks_w) {               // x: a list row per workgroup
         const int i = block - a.blocks_z - a.blocks_w;
-        if (i >= a.head[1]) return;
-        const bool live = i < a.head[0];
+        if (i >= padded) return;
+        const bool live = i < n;
         const int t = live && a.rows ? a.rows[i] : i;
         for (int c = 4 * threadIdx.x; c < a.d; c += 4 * kPrepThreads) {
             f32x4 v{};
@@ -316,39 +325,31 @@ __global__ __launch_bounds__(kPrepThreads) void prep_kernel(PrepArgs a) {
         }
         return;
     }
-    // lane l: experts l % EP + 64 j of row l / EP of the wave's
+    // lane l: experts l % EP + 64 j of row l / EP of a group
     int ep = 1;
     while (ep < min(E, 64)) ep *= 2;
     const int sub = lane / ep, e0 = lane % ep, tpw = kWave / ep;
-    const int i = (block * kPrepWaves + wave) * tpw + sub;
-    // the token at this place: cleared where it does not count
-    if (i < a.T && a.valid && !a.valid[i]) {
-        if (a.dz)
-            for (int e = e0; e < E; e += ep) a.dz[static_cast<size_t>(i) * E + e] = 0.f;
-        if (a.dx)
-            for (int c = 16 * e0; c < a.row_bytes; c += 16 * ep)
-                *reinterpret_cast<uint4*>(static_cast<char*>(a.dx) + static_cast<size_t>(i) * a.row_bytes + c) = uint4{};
-    }
+    float q[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) q[j] = 64 * j + e0 < E ? a.stat.q[64 * j + e0] : 0.f;
     // the row of the list at this place (without a list: the token)
-    const int n = a.rows ? a.head[0] : a.T, pad = a.dzs ? a.head[1] : n;
-    const int t = a.rows ? (i < n ? a.rows[i] : 0) : i;
-    const bool live = i < n && (a.rows || !a.valid || a.valid[t]);
-    float p[J], qe[J], dz[J];
+    const int i = (block * kPrepWaves + wave) * tpw + sub;
+    const bool live = i < n && (a.rows || !a.stat.valid || a.stat.valid[min(i, T - 1)]);
+    const int t = n == 0 ? 0 : a.rows ? a.rows[min(i, n - 1)] : min(i, T - 1);
+    float p[J], dz[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-        const int e = 64 * j + e0;
-        p[j] = live && e < E ? a.prob[static_cast<size_t>(t) * E + e] : 0.f;
-        qe[j] = e < E ? a.q[e] : 0.f;
+        const float v = a.stat.prob[static_cast<size_t>(t) * E + min(64 * j + e0, E - 1)];
+        p[j] = live && 64 * j + e0 < E ? v : 0.f;
     }
-    score_grad<J>(p, qe, ep, dz);
+    score_grad<J>(p, q, ep, dz);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int e = 64 * j + e0;
-        const float v = dz[j];
-        if (a.dz && live && e < E) a.dz[static_cast<size_t>(t) * E + e] = v;
-        if (a.dzs && i < pad) {
+        if (a.dz && live && e < E) a.dz[static_cast<size_t>(t) * E + e] = dz[j];
+        if (a.dzs && i < padded) {
             uint16_t part[3];
-            split3(v, part);
+            split3(dz[j], part);
             uint16_t* const o = a.dzs + (static_cast<size_t>(i) * J + j) * 256;
 #pragma unroll
             for (int k = 0; k < 3; ++k) {
@@ -356,6 +357,14 @@ __global__ __launch_bounds__(kPrepThreads) void prep_kernel(PrepArgs a) {
                 for (int z = e0 + ep; z < 64; z += ep) o[64 * k + z] = 0;
             }
         }
+    }
+    // the token at this place: cleared where it does not count
+    if (i < T && a.stat.valid && !a.stat.valid[i]) {
+        if (a.dz)
+            for (int e = e0; e < E; e += ep) a.dz[static_cast<size_t>(i) * E + e] = 0.f;
+        if (a.dx)
+            for (int c = 16 * e0; c < a.row_bytes; c += 16 * ep)
+                *reinterpret_cast<uint4*>(static_cast<char*>(a.dx) + static_cast<size_t>(i) * a.row_bytes + c) = uint4{};
     }
 }
 
@@ -468,7 +477,8 @@ bool split_products(const eat_params_t& p, int32_t T) {
 template <int J>
 hipError_t launch_rows(const eat_params_t& p, const BalancePlan& b, const StatArgs& a, const PrepArgs* prep, int blocks,
                        hipStream_t s) {
-    stat_kernel<J><<<b.blocks, kStatThreads, 0, s>>>(a);
+    stat_kernel<J><<<b.blocks + (a.rows ? 1 : 0), kStatThreads, 0, s>>>(a);
+    if (b.blocks > 1) total_kernel<J><<<1, kStatThreads, 0, s>>>(a);
     if (prep && blocks) prep_kernel<J><<<blocks, kPrepThreads, 0, s>>>(*prep);
     return hipGetLastError();
 }
@@ -507,7 +517,7 @@ hipError_t launch_split(const eat_params_t& p, const BalancePlan& b, const Balan
         g.a_rows = bf16 ? c.T : 1 << 30;
         g.k_rows = rows;
         g.b = dzs; g.ldb = 256 * groups; g.nb = E;
-        g.K = (c.T + kBK - 1) / kBK * kBK; g.k_dev = head + 1;
+        g.K = (c.T + kBK - 1) / kBK * kBK; g.k_dev = rows ? head + 1 : nullptr;
         g.splits = b.splits;
         g.out = dwp; g.ldo = parts * d; g.split_stride = static_cast<int64_t>(E) * parts * d;
         e = bf16 && rows ? launch_gemm<Fold, true, true, PART, true, true>(g, s)
@@ -524,7 +534,7 @@ hipError_t launch_split(const eat_params_t& p, const BalancePlan& b, const Balan
         g.map = bf16 ? kDz16 : kDz32;
         g.K = g.a_rows = groups * g.segs * 64;
         g.a = reinterpret_cast<const uint16_t*>(ws + b.ws); g.lda = g.na = d;
-        g.b = dzs; g.ldb = 256 * groups; g.nb = c.T; g.nb_dev = head;
+        g.b = dzs; g.ldb = 256 * groups; g.nb = c.T; g.nb_dev = rows ? head : nullptr;
         g.splits = 1;
         g.out = c.dx; g.ldo = d; g.rows = rows; g.factor = p.inv_temperature;
         e = bf16 ? launch_gemm<Fold, true, false, ROWS, true>(g, s) : launch_gemm<Fold, true, false, ROWS32, true>(g, s);
@@ -570,19 +580,16 @@ hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const Bal
     const bool products = c.dx || c.dw, split = b.split && products;
     const bool bf16 = p.act_dtype == EAT_BF16;
     int32_t* const list = split && c.valid ? reinterpret_cast<int32_t*>(ws + b.rows) : nullptr;
-    if (list) list_kernel<uint8_t><<<1, kListThreads, 0, s>>>(c.valid, c.T, 0, list, head);
-    else if (b.blocks > 1 || split) head_kernel<<<1, 1, 0, s>>>(c.T, head);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
     float* const dz = c.dlogits ? c.dlogits : products && !split ? reinterpret_cast<float*>(ws + b.dz) : nullptr;
     const bool fused = b.blocks == 1 && !split;            // dz by the sums' workgroup
-    const StatArgs a{c.prob, c.mask, c.valid, c.T, p.E, c.coef, c.entropy_coef, head, q,
+    const StatArgs a{c.prob, c.mask, c.valid, c.T, p.E, b.blocks, c.coef, c.entropy_coef, q,
                      reinterpret_cast<double*>(ws + b.sum), reinterpret_cast<int32_t*>(ws + b.cnt), c.loss, c.count,
-                     c.mean_prob, fused ? dz : nullptr};
+                     c.mean_prob, fused ? dz : nullptr, list, head};
     PrepArgs r{};
-    r.prob = c.prob; r.valid = c.valid; r.rows = list; r.head = head;
-    r.T = c.T; r.E = p.E; r.d = p.d_model;
-    r.q = q; r.dz = dz;
+    r.stat = a;
+    r.rows = list;
+    r.d = p.d_model;
+    r.dz = dz;
     int ep = 1;
     while (ep < std::min(p.E, 64)) ep *= 2;
     const int per = kPrepWaves * (kWave / ep);
@@ -607,6 +614,7 @@ hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const Bal
         }
     }
     const PrepArgs* const rp = (dz && !fused) || split ? &r : nullptr;
+    hipError_t e;
     switch ((p.E + 63) / 64) {
         case 1: e = launch_rows<1>(p, b, a, rp, blocks, s); break;
         case 2: e = launch_rows<2>(p, b, a, rp, blocks, s); break;

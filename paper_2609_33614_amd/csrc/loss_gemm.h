@@ -654,13 +654,12 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
 
 // rows[0 .. n): the indices t < T whose key is not `skip`, in order, and the
 // last of them again up to a whole reduction chunk; head: {n, n rounded up to
-// whole chunks, 0}.  One workgroup: the list is a running count over the call.
+// whole chunks, 0}.  One workgroup of kListThreads: the list is a running count over the call.
 // A thread takes 16 bytes of keys at a time, so that 4096 fp32-sized keys are
 // one round of loads and one scan.
 constexpr int kListThreads = 1024;
 template <typename Key>
-__global__ __launch_bounds__(kListThreads) void list_kernel(const Key* __restrict__ key, int T, Key skip, int32_t* rows,
-                                                            int32_t* head) {
+__device__ __forceinline__ void list_rows(const Key* __restrict__ key, int T, Key skip, int32_t* rows, int32_t* head) {
     constexpr int NW = kListThreads / kWave, N = 16 / sizeof(Key);
     __shared__ int cnt[2][NW];
     __shared__ int lastrow;
@@ -701,6 +700,11 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(const Key* __restric
         head[1] = pad;
         head[2] = 0;
     }
+}
+template <typename Key>
+__global__ __launch_bounds__(kListThreads) void list_kernel(const Key* __restrict__ key, int T, Key skip, int32_t* rows,
+                                                            int32_t* head) {
+    list_rows(key, T, skip, rows, head);
 }
 
 struct Geometry {
