@@ -14,7 +14,7 @@
 // ones before leave, so three hold 24 bits or more, two 16): dz in three parts, x
 // as it is (bf16) or in three, the router weights in two (dx in bf16) or three.
 // dW_r takes every product of parts, dx those above its precision (loss_gemm's
-// FOLD).  Tokens that do not count are left out of the reduction (loss_gemm's
+// GROUPS).  Tokens that do not count are left out of the reduction (loss_gemm's
 // GATHER), so nothing of theirs is read.
 #include <math.h>
 
@@ -464,7 +464,6 @@ __global__ __launch_bounds__(256) void dw_join_kernel(const float* __restrict__ 
     *reinterpret_cast<f32x4*>(dw + i) = s * scale;
 }
 
-using Fold = Big;
 
 constexpr int kOneBlock = 4096;           // most probabilities one workgroup sums up
 constexpr int kOneSlice = 64;             // most tokens that dW_r of a small call takes in one slice
@@ -517,11 +516,11 @@ hipError_t launch_split(const eat_params_t& p, const BalancePlan& b, const Balan
         g.a_rows = bf16 ? c.T : 1 << 30;
         g.k_rows = rows;
         g.b = dzs; g.ldb = 256 * groups; g.nb = E;
-        g.K = (c.T + kBK - 1) / kBK * kBK; g.k_dev = rows ? head + 1 : nullptr;
+        g.K = (c.T + kBK - 1) / kBK * kBK; g.k_dev = rows ? head + 1 : nullptr; g.k_times = 1;
         g.splits = b.splits;
         g.out = dwp; g.ldo = parts * d; g.split_stride = static_cast<int64_t>(E) * parts * d;
-        e = bf16 && rows ? launch_gemm<Fold, true, true, PART, true, true>(g, s)
-                         : launch_gemm<Fold, true, true, PART, true, false>(g, s);
+        e = bf16 && rows ? launch_gemm<Big, true, true, PART, GROUPS, true>(g, s)
+                         : launch_gemm<Big, true, true, PART, GROUPS, false>(g, s);
         if (e == hipSuccess) {
             dw_join_kernel<<<static_cast<int>((static_cast<int64_t>(E) * d / 4 + 255) / 256), 256, 0, s>>>(
                 dwp, b.splits, parts, E, d, p.inv_temperature, c.dw);
@@ -537,7 +536,7 @@ hipError_t launch_split(const eat_params_t& p, const BalancePlan& b, const Balan
         g.b = dzs; g.ldb = 256 * groups; g.nb = c.T; g.nb_dev = rows ? head : nullptr;
         g.splits = 1;
         g.out = c.dx; g.ldo = d; g.rows = rows; g.factor = p.inv_temperature;
-        e = bf16 ? launch_gemm<Fold, true, false, ROWS, true>(g, s) : launch_gemm<Fold, true, false, ROWS32, true>(g, s);
+        e = bf16 ? launch_gemm<Big, true, false, ROWS, GROUPS>(g, s) : launch_gemm<Big, true, false, ROWS32, GROUPS>(g, s);
     }
     return e;
 }
@@ -555,7 +554,7 @@ BalancePlan plan_balance(const eat_params_t& p, int32_t T) {
     const int parts = b.split && p.act_dtype != EAT_BF16 ? 3 : 1;
     // dw_router: slices of the tokens until the CUs have an item each (four
     // small ones of the fp32 kernel), none under 4 chunks (64 tokens)
-    const int64_t items = b.split ? groups * ((parts * d + Fold::NA - 1) / Fold::NA) : groups * (d / 64);
+    const int64_t items = b.split ? groups * ((parts * d + Big::NA - 1) / Big::NA) : groups * (d / 64);
     b.splits = 1;
     if (b.split || T > kOneSlice)
         while (items * b.splits * 2 <= (b.split ? 256 : 1024) && T / (b.splits * 2) >= (b.split ? 4 * kBK : 64))

@@ -27,15 +27,16 @@ namespace {
 // One wave per row.  Row t of the call, where it is ignored: its NLL and its
 // dh are zero.  Row i of the list: its hidden row, its target and the target's
 // logit in fp64 (the NLL would depend most on that logit's rounding); rows
-// behind the list up to whole tiles: zeros.  LIST (calls of up to kListedRows
+// behind the list up to whole tiles: zeros (and all again `again` rows on, if it is
+// not 0).  LIST (calls of up to kListedRows
 // rows): every workgroup works the list out for itself, a lane per row, instead of a
 // launch before this one (~5 us).
 constexpr int kGatherWaves = 4, kListedRows = kGatherWaves * kWave;
 template <bool LIST>
 __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
     const uint16_t* __restrict__ h, const uint16_t* __restrict__ w, const int32_t* __restrict__ target, int T, int Tpad,
-    int d, int V, int ignore, int32_t* rows, int32_t* head, uint16_t* hc, int32_t* tc, double* zt, float* nll,
-    uint16_t* dh) {
+    int d, int V, int ignore, int32_t* rows, int32_t* head, uint16_t* hc, int again,
+    int32_t* tc, double* zt, float* nll, uint16_t* dh) {
     __shared__ uint64_t keep[kGatherWaves];
     const int lane = lane_id(), i = blockIdx.x * kGatherWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     int n, t = 0;
@@ -81,7 +82,9 @@ __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
         for (int u = 0; u < kLoads; ++u) {
             const int k = k0 + 8 * kWave * u;
             if (k >= d) break;
-            *reinterpret_cast<uint4*>(hc + static_cast<size_t>(i) * d + k) = i < n ? p[u] : uint4{};
+            const uint4 row = i < n ? p[u] : uint4{};
+            *reinterpret_cast<uint4*>(hc + static_cast<size_t>(i) * d + k) = row;
+            if (again) *reinterpret_cast<uint4*>(hc + static_cast<size_t>(i + again) * d + k) = row;
             const uint32_t pw[4] = {p[u].x, p[u].y, p[u].z, p[u].w}, qw[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -180,9 +183,10 @@ __global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(const float2* __
 // G of the columns whose exponentials the first pass kept, in place: a tile of
 // the first pass x 64 rows per workgroup, 16 bytes per lane.  Twice the piece's
 // bytes against taking its product again (4096 rows of 32000 columns, d 4096:
-// see launch_ce).  Rows behind the list up to a whole reduction chunk: zeros.
+// see launch_ce).  Rows behind the list up to a whole reduction chunk: zeros.  PARTS:
+// in two bf16 parts (the second plane 64 rows on).
 constexpr int kScaleThreads = 256, kScaleRows = 64;
-template <int NA>
+template <int NA, bool PARTS>
 __global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __restrict__ part, int ldpart,
                                                               const float2* __restrict__ stats,
                                                               const int32_t* __restrict__ tc,
@@ -205,25 +209,37 @@ __global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __re
         row[tid] = v;
     }
     uint16_t* const at = g + (r0 + tid / V) * ldg + c0 + 8 * (tid % V);
-    uint4 v[kScaleRows / R];
+    constexpr int K = kScaleRows / R;
+    uint4 v[K], v2[PARTS ? K : 1];
 #pragma unroll
-    for (int k = 0; k < kScaleRows / R; ++k) v[k] = *reinterpret_cast<const uint4*>(at + k * R * ldg);
+    for (int k = 0; k < K; ++k) {
+        v[k] = *reinterpret_cast<const uint4*>(at + k * R * ldg);
+        if constexpr (PARTS) v2[k] = *reinterpret_cast<const uint4*>(at + (64 + k * R) * ldg);
+    }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kScaleRows / R; ++k) {
+    for (int k = 0; k < K; ++k) {
         const int r = tid / V + k * R;
         const float4 p = row[r];
         const int rel = __float_as_int(p.z) - 8 * (tid % V);
         const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-        uint32_t o[4];
+        uint32_t w2[4] = {}, o[4], o2[4];
+        if constexpr (PARTS) { w2[0] = v2[k].x; w2[1] = v2[k].y; w2[2] = v2[k].z; w2[3] = v2[k].w; }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float lo = __uint_as_float(w[e] << 16) * p.x, hi = __uint_as_float(w[e] & 0xffff0000u) * p.x;
-            lo = rel == 2 * e ? p.y : lo;
-            hi = rel == 2 * e + 1 ? p.y : hi;
-            o[e] = r0 + r < n ? pack_bf16x2(lo, hi) : 0u;
+            float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xffff0000u);
+            if constexpr (PARTS) {
+                lo += __uint_as_float(w2[e] << 16);
+                hi += __uint_as_float(w2[e] & 0xffff0000u);
+            }
+            lo = rel == 2 * e ? p.y : lo * p.x;
+            hi = rel == 2 * e + 1 ? p.y : hi * p.x;
+            if (r0 + r >= n) lo = hi = 0.f;
+            o[e] = pack_bf16x2(lo, hi);
+            if constexpr (PARTS) o2[e] = pack_bf16x2(bf16_rest(lo), bf16_rest(hi));
         }
         *reinterpret_cast<uint4*>(at + k * R * ldg) = uint4{o[0], o[1], o[2], o[3]};
+        if constexpr (PARTS) *reinterpret_cast<uint4*>(at + (64 + k * R) * ldg) = uint4{o2[0], o2[1], o2[2], o2[3]};
     }
 }
 
@@ -267,7 +283,8 @@ Size pick_tile(int64_t rows, int64_t cols) {
 constexpr int tile_cols(Size z) { return z == kBig ? Big::NA : Mid::NA; }
 static_assert(Mid::NA == Small::NA, "column tiles of 128 or 256");
 
-// dh, whose reduction is split over what CUs its tiles leave: by the rows alone.
+// dh, whose reduction is split over what CUs its tiles leave: by the rows alone
+// (kSmall: the 128-row tile on G's two planes).
 Size dh_tile(int64_t rows) { return rows <= Small::NB ? kSmall : rows <= 2 * Mid::NB ? kMid : kBig; }
 
 template <bool ACOLS, bool BCOLS, int OUT>
@@ -290,13 +307,13 @@ constexpr int kMinPiece = 4096;
 CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) {
     CePlan p{};
     p.rows_pad = T <= Small::NB ? Small::NB : (T + Big::NB - 1) / Big::NB * Big::NB;
-    const size_t tp = p.rows_pad;
+    const size_t tp = p.rows_pad, planes = T <= Small::NB ? 2 : 1;
     p.tile = tile_cols(pick_tile(T, V));
     p.tiles = (V + p.tile - 1) / p.tile;
     const int vpad = (V + 255) / 256 * 256;
     const int least = std::min(vpad, kMinPiece);
     auto fit = [&](size_t room) {
-        return static_cast<int>(std::max<size_t>(least, std::min<size_t>(vpad, room / (2 * tp) / 256 * 256)));
+        return static_cast<int>(std::max<size_t>(least, std::min<size_t>(vpad, room / (2 * tp * planes) / 256 * 256)));
     };
     // dh: room for its slices, a few of many rows (how many there are is chosen on
     // the device, by the rows that count)
@@ -313,11 +330,11 @@ CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) 
         p.zt = take(tp * 8);
         p.nllc = take(tp * 8);
         p.stats = take(tp * 8);
-        p.hc = take(tp * d * 2);
+        p.hc = take(tp * planes * d * 2);
         p.part = take(tp * p.tiles * 8);
         p.dhp = take(pool * d * 4);
         p.g = off;
-        p.total = off + (dh || dw ? tp * piece * 2 : 0);
+        p.total = off + (dh || dw ? tp * planes * piece * 2 : 0);
     };
     layout(fit(kPieceBytes));
     if (p.total <= bytes || (!dh && !dw)) return p;
@@ -340,15 +357,16 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
     float* const dhp = reinterpret_cast<float*>(ws + p.dhp);
     const int T = c.T, d = c.d, V = c.V;
     const Size zz = pick_tile(T, V), zh = dh_tile(T);
+    const int again = zz == kSmall ? Small::NB : 0;
 
     const int rb = (p.rows_pad + kGatherWaves - 1) / kGatherWaves;
     if (T <= kListedRows) {
         gather_kernel<true><<<rb, kGatherWaves * kWave, 0, s>>>(c.h, c.w, c.target, T, p.rows_pad, d, V, c.ignore, rows,
-                                                                head, hc, tc, zt, c.nll, c.dh);
+                                                                head, hc, again, tc, zt, c.nll, c.dh);
     } else {
         list_kernel<int32_t><<<1, kListThreads, 0, s>>>(c.target, T, c.ignore, rows, head);
         gather_kernel<false><<<rb, kGatherWaves * kWave, 0, s>>>(c.h, c.w, c.target, T, p.rows_pad, d, V, c.ignore, rows,
-                                                                 head, hc, tc, zt, c.nll, c.dh);
+                                                                 head, hc, again, tc, zt, c.nll, c.dh);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -369,8 +387,9 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
         const uint16_t* w = c.w + static_cast<size_t>(v0) * d;
         if (v0 == 0) {
             const dim3 grid((nv + p.tile - 1) / p.tile, p.rows_pad / kScaleRows);
-            if (p.tile == Mid::NA) scale_kernel<Mid::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
-            else scale_kernel<Big::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
+            if (zz == kSmall) scale_kernel<Small::NA, true><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
+            else if (zz == kMid) scale_kernel<Mid::NA, false><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
+            else scale_kernel<Big::NA, false><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
             e = hipGetLastError();
         } else {
             GemmArgs q = z;
@@ -386,13 +405,16 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
             a.pool_rows = p.pool_rows; a.slice_chunks = std::min(p.piece, V + kBK - 1) / kBK; a.slices_out = head + 3;
             a.direct = p.piece < V ? nullptr : c.dh;
             a.out = dhp; a.ldo = d; a.add = v0 > 0; a.rows = rows; a.coef = coef;
-            e = launch_sized<true, false, PART>(zh, a, s);
+            e = zh == kBig   ? launch_gemm<Big, true, false, PART>(a, s)
+                : zh == kMid ? launch_gemm<Mid, true, false, PART>(a, s)
+                             : launch_gemm<Mid, true, false, PART, PLANES>(a, s);
         }
         if (e == hipSuccess && c.dw) {
             GemmArgs a{};
             a.a = hc; a.lda = d; a.na = d; a.a_rows = 1 << 30;
             a.b = gbuf; a.ldb = p.piece; a.nb = nv;
-            a.K = p.rows_pad; a.k_dev = head + 1; a.splits = 1;
+            a.k_times = zz == kSmall ? 2 : 1;              // (both planes of G, over both copies of h)
+            a.K = p.rows_pad * a.k_times; a.k_dev = head + 1; a.splits = 1;
             a.out = c.dw + static_cast<size_t>(v0) * d; a.ldo = d; a.coef = coef;
             e = launch_sized<true, true, ROWS>(pick_tile(nv, d), a, s);
         }

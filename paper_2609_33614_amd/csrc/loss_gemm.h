@@ -59,10 +59,11 @@ struct GemmArgs {
     int lda, ldb;              // elements between stored rows
     int na, nb, K;             // output columns and rows, reduction length (nb, K: upper bounds where *_dev is set)
     const int32_t* nb_dev;     // rows of the output, on the device (or null)
-    const int32_t* k_dev;      // reduction length, on the device (or null)
+    const int32_t* k_dev;      // reduction length, on the device (or null), over k_times
+    int k_times;
     int a_rows;                // stored rows of a "columns" A operand (later ones read the last)
     const int32_t* k_rows;     // GATHER: the stored row of A of each reduction element (whole chunks of them)
-    int segs, map;             // FOLD, B by rows: see loss_gemm
+    int segs, map;             // GROUPS, B by rows: see loss_gemm
     int splits;                // slices of the reduction (PART); 0: chosen on the device (pick_slices)
     int pool_rows, slice_chunks;   // ... by the rows the slices may take and the reduction's chunks
     int32_t* slices_out;       // ... and written there
@@ -225,23 +226,34 @@ __device__ inline int pick_slices(int items, int chunks, int rows, int cols, int
 // where all are -inf, whose sum is 0, or some +inf: then 0).
 __device__ __forceinline__ float tile_ref(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
 
+// What the rounding of v to bf16 leaves.
+__device__ __forceinline__ float bf16_rest(float v) { return v - __uint_as_float(pack_bf16x2(v, 0.f) << 16); }
+
 __device__ __forceinline__ float swap_halves(float v) { return __shfl_xor(v, 32, kWave); }
 
-// FOLD: B holds numbers of more than bf16's digits as sums of bf16 parts, in
-// groups of 64 indices of 4 parts each ([stored row][group][part][64], part 3
-// unused).  B by columns: a tile of 256 is a group, and the products with its
-// first three parts are added into one output row per index.  B by rows: the
-// reduction runs over the groups, `segs` chunks of 64 each: chunk i of a group
-// is its part (map >> 4 i) & 15 (A holds the matching rows, chunk by chunk).
-template <class C, bool ACOLS, bool BCOLS, int OUT, bool FOLD = false, bool GATHER = false>
+// B may hold numbers of more than bf16's digits as sums of bf16 parts.
+//   GROUPS: in groups of 64 indices of 4 parts each ([stored row][group][part]
+//     [64], part 3 unused).  B by columns: a tile of 256 is a group, and the
+//     products with its first three parts are added into one output row per index.
+//     B by rows: the reduction runs over the groups, `segs` chunks of 64 each: chunk
+//     i of a group is its part (map >> 4 i) & 15 (A holds the matching rows, chunk
+//     by chunk).
+//   PLANES: B by rows, 64 of them, and 64 rows on their second parts; the products
+//     with both are added into one output row.
+enum Fold { WHOLE, GROUPS, PLANES };
+
+template <class C, bool ACOLS, bool BCOLS, int OUT, int FOLD = WHOLE, bool GATHER = false>
 __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
-    constexpr bool kFoldRows = FOLD && BCOLS;
-    static_assert(!kFoldRows || (C::NB == 256 && C::WB == 2), "a group per tile, 32 indices per wave");
-    constexpr int FA = C::FA, FB = kFoldRows ? 1 : C::FB, FL = kFoldRows ? 3 : C::FB;   // fragments of B: held, read
-    constexpr int NBO = kFoldRows ? 64 : C::NB;        // output rows per tile
+    constexpr bool kGroupTile = FOLD == GROUPS && BCOLS, kFolds = kGroupTile || FOLD == PLANES;
+    static_assert(!kGroupTile || (C::NB == 256 && C::WB == 2), "a group per tile, 32 indices per wave");
+    static_assert(FOLD != PLANES || (!BCOLS && C::NB == 128 && C::WB == 2), "two planes per tile, 32 rows per wave");
+    constexpr int FA = C::FA, FB = kFolds ? 1 : C::FB;         // fragments of B held, and read
+    constexpr int FL = kGroupTile ? 3 : FOLD == PLANES ? 2 : C::FB;
+    constexpr int NBO = kFolds ? 64 : C::NB;                   // output rows per tile
+    constexpr bool kParts = C::NB == 64;                       // LSE, GRAD: out in two parts, PLANES of 64 rows
     __shared__ __attribute__((aligned(1024))) uint8_t ring[C::SLOTS * C::kSlot];
     const int nb = g.nb_dev ? min(*g.nb_dev, g.nb) : g.nb;
-    const int K = g.k_dev ? min(*g.k_dev, g.K) : g.K;
+    const int K = g.k_dev ? min(*g.k_dev * g.k_times, g.K) : g.K;
     const int nta = (g.na + C::NA - 1) / C::NA, ntb = (nb + NBO - 1) / NBO;
     const int chunks = (K + kBK - 1) / kBK;
     int splits = 1;
@@ -293,7 +305,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
     Operand<C::NA, C::kLA, C::kWaves, ACOLS, GATHER> oa;
     Operand<C::NB, C::kLB, C::kWaves, BCOLS> ob;
     int iwid = wid - per_xcd, left = 1;       // the last A's item, chunks from it on
-    int cb = 0, bfirst = 0;                   // FOLD by rows: B's chunk and first row
+    int cb = 0, bfirst = 0;                   // GROUPS by rows: B's chunk and first row
     Item item{};
     bool fresh = false, ended = false;        // the last A is its item's first; there is none after it
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring)) + 1024 * wave;
@@ -357,7 +369,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
         advance(2);
         srca = uniform(oa.src);
         srcb = uniform(ob.src);
-        if constexpr (FOLD && !BCOLS) {        // the group's part that meets A's chunk (splits is 1: chunks from 0 on)
+        if constexpr (FOLD == GROUPS && !BCOLS) {        // the group's part that meets A's chunk (splits is 1: chunks from 0 on)
             const int c = cb / g.segs * 4 + ((g.map >> (4 * (cb % g.segs))) & 15);
             srcb = uniform(reinterpret_cast<uint64_t>(g.b + static_cast<size_t>(bfirst) * g.ldb) + c * (kBK * 2));
         }
@@ -425,12 +437,12 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
         const uint8_t *sa = ring, *sb = ring;
         auto read = [&](int p, int s) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < FL; ++j) B[p][j] = fragment<C::NB, BCOLS>(sb, brow + (kFoldRows ? 64 : 32) * j, s);
+            for (int j = 0; j < FL; ++j) B[p][j] = fragment<C::NB, BCOLS>(sb, brow + (kFolds ? 64 : 32) * j, s);
 #pragma unroll
             for (int i = 0; i < FA; ++i) A[p][i] = fragment<C::NA, ACOLS>(sa, arow + 32 * i, s);
         };
         auto product = [&](int p, int j, int i) __attribute__((always_inline)) {
-            f32x16& c16 = acc[i][kFoldRows ? 0 : j];
+            f32x16& c16 = acc[i][kFolds ? 0 : j];
             c16 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[p][i], B[p][j], c16, 0, 0, 0);
         };
         auto products = [&](int p) __attribute__((always_inline)) {
@@ -571,10 +583,13 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                 s += swap_halves(s);
                 if (lh == 0) sums(wave)[32 * (FB + j) + l32] = s;
                 const int row0 = cur.b0 + brow + 32 * j;
-                if (kept && row0 < nb)
-                    store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q]; },
-                            [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; },
-                            nb - row0);
+                if (kept && row0 < nb) {
+                    auto to = [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; };
+                    store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q]; }, to, nb - row0);
+                    if constexpr (kParts)
+                        store16(j, [&](int i, int q) __attribute__((always_inline)) { return bf16_rest(acc[i][j][q]); },
+                                [&](int r) { return to(r) + 64 * g.ldo; }, nb - row0);
+                }
             }
             lds_barrier();
             for (int r = threadIdx.x; r < C::NB; r += C::kThreads) {
@@ -601,12 +616,17 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                     const float2 st = stats[j];
                     const int rel = target[j] - (g.col0 + cur.a0 + arow + 4 * lh);
                     const int end = live ? g.na - (cur.a0 + arow + 4 * lh) : 0;     // columns of the piece from here on
-                    store16(j, [&](int i, int q) __attribute__((always_inline)) {
+                    auto grad = [&](int i, int q) __attribute__((always_inline)) {
                         const int v = 32 * i + 8 * (q / 4) + q % 4;
                         float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], kLog2e, -st.x));
                         p = v == rel ? st.y : p;
                         return v < end ? p : 0.f;
-                    }, [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; }, nv);
+                    };
+                    auto to = [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; };
+                    store16(j, grad, to, nv);
+                    if constexpr (kParts)
+                        store16(j, [&](int i, int q) __attribute__((always_inline)) { return bf16_rest(grad(i, q)); },
+                                [&](int r) { return to(r) + 64 * g.ldo; }, nv);
                 } else if (OUT == ROWS || direct) {
                     if (cur.a0 + arow >= g.na) break;      // (columns come in multiples of 64)
                     store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q] * coef; },
@@ -725,9 +745,9 @@ const Geometry& geometry() {
 
 // Persistent: a workgroup per CU (the ring fills its LDS) or per item, a
 // multiple of the XCD count.
-template <class C, bool ACOLS, bool BCOLS, int OUT, bool FOLD = false, bool GATHER = false>
+template <class C, bool ACOLS, bool BCOLS, int OUT, int FOLD = WHOLE, bool GATHER = false>
 hipError_t launch_gemm(GemmArgs g, hipStream_t s) {
-    constexpr int kRows = FOLD && BCOLS ? 64 : C::NB;
+    constexpr int kRows = (FOLD == GROUPS && BCOLS) || FOLD == PLANES ? 64 : C::NB;
     g.xcds = geometry().xcds;
     const int64_t work = static_cast<int64_t>((g.na + C::NA - 1) / C::NA) * ((g.nb + kRows - 1) / kRows) *
                          (g.splits ? g.splits : std::max(1, std::min(kMostSlices, g.slice_chunks / 4)));

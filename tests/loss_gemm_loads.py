@@ -21,6 +21,7 @@ PRELUDE = r"""
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <type_traits>
 #include <vector>
 #define __device__
 #define __forceinline__ inline
@@ -54,7 +55,7 @@ static void note(uint64_t p, uint32_t lds) {
 """
 
 KERNEL = r"""
-template <class C, bool ACOLS, bool BCOLS, int OUT, bool FOLD = false, bool GATHER = false>
+template <class C, bool ACOLS, bool BCOLS, int OUT, int FOLD = WHOLE, bool GATHER = false>
 void stream(GemmArgs g) {
 %(consts)s
     uint8_t* const ring = nullptr;
@@ -74,9 +75,9 @@ void stream(GemmArgs g) {
     }
 }
 
-template <class C, bool ACOLS, bool BCOLS, int OUT, bool FOLD = false, bool GATHER = false>
+template <class C, bool ACOLS, bool BCOLS, int OUT, int FOLD = WHOLE, bool GATHER = false>
 long launch(GemmArgs g, uint64_t a_bytes, uint64_t b_bytes) {
-    constexpr int kRows = FOLD && BCOLS ? 64 : C::NB;
+    constexpr int kRows = (FOLD == GROUPS && BCOLS) || FOLD == PLANES ? 64 : C::NB;
     g.xcds = 8;
     const long work = (long)((g.na + C::NA - 1) / C::NA) * ((g.nb + kRows - 1) / kRows) * (g.splits ? g.splits : kCus);
     if (!work) return 0;
@@ -106,13 +107,17 @@ void ce(int T, int n, int d, int V, int rows_pad, int piece, int pool) {
         GemmArgs a{};
         a.a = A; a.lda = d; a.na = d; a.a_rows = nv; a.b = B; a.ldb = piece; a.nb = T; a.nb_dev = head; a.K = nv;
         a.pool_rows = pool; a.slice_chunks = min(piece, V + 63) / 64; a.slices_out = &slices;
-        total += launch<C, true, false, PART>(a, 2ull * nv * d, 2ull * rows_pad * piece);
-        if constexpr (C::NA == C::NB) {
-            GemmArgs w{};
-            w.a = A; w.lda = d; w.na = d; w.a_rows = 1 << 30; w.b = B; w.ldb = piece; w.nb = nv; w.K = rows_pad;
-            w.k_dev = head + 1; w.splits = 1;
-            total += launch<C, true, true, ROWS>(w, 2ull * rows_pad * d, 2ull * rows_pad * piece);
-        }
+        // (Small: G and h in two planes, the larger tiles)
+        constexpr bool kSmall = C::NB == 64;
+        const int planes = kSmall ? 2 : 1;
+        if constexpr (kSmall) total += launch<Mid, true, false, PART, PLANES>(a, 2ull * nv * d, 4ull * rows_pad * piece);
+        else total += launch<C, true, false, PART>(a, 2ull * nv * d, 2ull * rows_pad * piece);
+        GemmArgs w{};
+        w.a = A; w.lda = d; w.na = d; w.a_rows = 1 << 30; w.b = B; w.ldb = piece; w.nb = nv;
+        w.K = rows_pad * planes; w.k_dev = head + 1; w.k_times = planes; w.splits = 1;
+        using W = std::conditional_t<kSmall, Mid, C>;
+        total += launch<W, true, true, ROWS>(w, 2ull * planes * rows_pad * d, 2ull * planes * rows_pad * piece);
+        if constexpr (kSmall) total += launch<Big, true, true, ROWS>(w, 4ull * rows_pad * d, 4ull * rows_pad * piece);
     }
     printf("ce T %d n %d d %d V %d: %ld loads\n", T, n, d, V, total);
 }
@@ -125,14 +130,15 @@ void balance(int T, int n, int E, int d, int splits, bool gather, int parts, int
     for (int i = 0; i < padn; ++i) rows[i] = n ? (int)((long)min(i, n - 1) * T / n) : 0;
     GemmArgs g{};
     g.a = A; g.lda = g.na = parts * d; g.a_rows = parts == 1 ? T : 1 << 30; g.k_rows = rows.data();
-    g.b = B; g.ldb = 256 * groups; g.nb = E; g.K = (T + 63) / 64 * 64; g.k_dev = head + 1; g.splits = splits;
+    g.b = B; g.ldb = 256 * groups; g.nb = E; g.K = (T + 63) / 64 * 64; g.k_dev = head + 1; g.k_times = 1;
+    g.splits = splits;
     const uint64_t a_bytes = parts == 1 ? 2ull * T * d : 2ull * pad * parts * d, b_bytes = 512ull * pad * groups;
-    long total = gather ? launch<Big, true, true, PART, true, true>(g, a_bytes, b_bytes)
-                        : launch<Big, true, true, PART, true, false>(g, a_bytes, b_bytes);
+    long total = gather ? launch<Big, true, true, PART, GROUPS, true>(g, a_bytes, b_bytes)
+                        : launch<Big, true, true, PART, GROUPS, false>(g, a_bytes, b_bytes);
     GemmArgs x{};
     x.segs = segs; x.map = map; x.K = x.a_rows = groups * segs * 64; x.a = A; x.lda = x.na = d;
     x.b = B; x.ldb = 256 * groups; x.nb = T; x.nb_dev = head; x.splits = 1;
-    total += launch<Big, true, false, ROWS, true>(x, 2ull * x.K * d, b_bytes);
+    total += launch<Big, true, false, ROWS, GROUPS>(x, 2ull * x.K * d, b_bytes);
     printf("balance T %d n %d E %d d %d: %ld loads\n", T, n, E, d, total);
 }
 
@@ -156,7 +162,7 @@ def program(calls: str, header: str = None) -> str:
     operand = re.sub(r'asm volatile\("s_add_u32 m0, %2.*?;', "note(from + o, lds + 1024 * WAVES * j);", operand, flags=re.S)
     assert operand.count("note(") == 2 and "asm volatile" not in operand
     parts = {
-        "consts": cut("    constexpr bool kFoldRows = FOLD && BCOLS;", "    __shared__ __attribute__((aligned(1024))) uint8_t ring"),
+        "consts": cut("    constexpr bool kGroupTile =", "    __shared__ __attribute__((aligned(1024))) uint8_t ring"),
         "items": cut("    const int nb = g.nb_dev ?", "    const int lane = lane_id(), wave = wave_id();"),
         "stream": cut("    auto slice = [&](int sp)", "    // Waits until at most the loads of the parts behind"),
         "prologue": cut("    next_a();\n    if (", "    int slot0 = 0;"),
@@ -168,7 +174,7 @@ def program(calls: str, header: str = None) -> str:
     return (PRELUDE + cut("template <int NA_, int NB_, int WA_, int WB_>\nstruct Tile", "enum Out {")
             + cut("enum Out {", "// (uniform: what depends on it")
             + cut("__device__ __forceinline__ int swz_row", "__device__ __forceinline__ uint64_t uniform")
-            + operand + cut("struct Item {", "// The reference of a row's exponentials") + kernel)
+            + operand + cut("enum Fold {", "template <class C") + cut("struct Item {", "// The reference of a row's exponentials") + kernel)
 
 
 def run(tmp_path, calls: str, header: str = None):

@@ -7,8 +7,8 @@ eps_z = d 2^-24 max_v sum |h w|, and its exponent's argument by a few 2^-24
 (taken in fp64): off by (1 - p_y) times the rest's error, V-term sums in fp32
 trees adding 2^-24 per level (under 100 levels), and one rounding to fp32.  G
 is off by those of two logits (its own and the denominator), relative, and two
-roundings to bf16 (2^-8 each: the exponential as it is kept, then times its
-row's factor); a product of K terms in fp32 by K 2^-24 of the sum of
+roundings (the exponential as it is kept, then times its row's factor): to bf16,
+2^-8 each, or in calls of up to 64 positions to two bf16 parts, 2^-16 each; a product of K terms in fp32 by K 2^-24 of the sum of
 absolute terms; the output by one rounding to bf16."""
 import numpy as np
 import pytest
@@ -92,11 +92,12 @@ def reference(h, w, y, mean, scale, ignore=IGN):
         eps = torch.zeros(0, 1, dtype=torch.float64, device=h.device)
     bn = torch.zeros(T, dtype=torch.float64, device=h.device)
     bn[rows] = (-torch.expm1(-nll) * eps * (1 + eps) + u * nll + 2.0 ** -140)[:, 0]
-    eg = 2 * 2.0 ** -8 + 2.0 ** -16 + 2.02 * eps
+    step = 2.0 ** -16 if T <= 64 else 2.0 ** -8
+    eg = 2 * step + step * step + 2.02 * eps
     bh = torch.zeros_like(dh)
     ga = G.abs()
-    bh[rows] = abs(c) * ((ga * (eg + V * u)) @ wd.abs())
-    bw = abs(c) * ((ga * (eg + n * u)).T @ a.abs())
+    bh[rows] = abs(c) * ((ga * (eg + 2 * V * u)) @ wd.abs())
+    bw = abs(c) * ((ga * (eg + 2 * n * u)).T @ a.abs())
     half = 2.0 ** -8
     tiny = 2.0 ** -126                         # a flushed denormal
     ref["bounds"] = {"loss": abs(c) * bn.sum() + 2 * u * abs(ref["loss"]), "nll": bn,
@@ -208,6 +209,22 @@ def test_several_pieces_of_the_vocabulary(T, V):
         assert torch.equal(got["dh"], again["dh"]) and torch.equal(got["dw"], again["dw"])
         for kw in (dict(dh=False), dict(dw=False)):
             check(f"ce pieces {T} {V} {size} {kw}", call(h, w, y, most=size, **kw), ref)
+
+
+@pytest.mark.parametrize("T", [1, 2, 5])
+@pytest.mark.parametrize("lift", [0.0, 3.0, 9.0])
+def test_few_rows_keep_the_outputs_precision(T, lift):
+    """One entry of G can be a whole gradient row: with few rows nothing averages
+    its rounding.  The gradients' error over their norm stays that of the
+    outputs' own rounding (2^-8 at most, plus the parts' 2^-15)."""
+    for seed in range(6):
+        h, w, y = make(T, 256, 1500, seed=seed, lift=lift)
+        wrong = torch.randint(0, 1500, (T,), device="cuda")
+        h = (h.float() + 12.0 * w[wrong].float()).to(torch.bfloat16)       # confident of something else
+        got, ref = call(h, w, y), reference(h, w, y, True, 1.0)
+        for k in ("dh", "dw"):
+            err = (got[k].double() - ref[k]).norm() / ref[k].norm()
+            assert err <= 2.0 ** -8 + 2.0 ** -14, (seed, k, float(err))
 
 
 @pytest.mark.parametrize("T", [48, 320])
