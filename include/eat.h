@@ -351,13 +351,16 @@ eat_status_t eat_ppl_trend(const void* h, int32_t S, int32_t d, const void* w_vo
  *
  *   nll_t = log(1 + sum_{v != y} exp(z_tv - z_ty)),  y = target_t
  *   loss  = c sum_t nll_t                    (0 when no position counts)
- *   G_tv  = softmax(z_t)_v - [v = y]         (bf16; 0 where t does not count)
+ *   G_tv  = softmax(z_t)_v - [v = y]         (0 where t does not count; in
+ *           bf16, for up to 64 positions as the sum of two bf16 numbers)
  *   dh_t  = c sum_v G_tv W_V[v]     dW_V[v] = c sum_t G_tv h_t
  *
  * A position that does not count has nll 0 and dh 0 and reaches nothing else,
  * whatever its hidden row holds (NaN and infinities too).  A target outside
  * [0, V) that is not `ignore`, or a NaN in the row, gives a NaN nll, a NaN
- * loss and NaN in what the row reaches (its dh, all of dW_V). */
+ * loss and NaN in what the row reaches (its dh, all of dW_V).  A head row that
+ * gives -inf logits takes no probability and its dW_V is 0; its infinities make
+ * dh NaN (0 times infinity). */
 typedef enum { EAT_CE_DH = 1, EAT_CE_DW = 2 } eat_ce_grads_t;
 
 /* Workspace bytes for T positions (0 <= T <= 2^20), width d (a multiple of
@@ -377,7 +380,8 @@ eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grad
  *   scale     finite factor of the loss and its gradients
  *   loss_out  [1] fp32;  nll_out [T] fp32 or NULL;  count_out [1] int32 (n) or NULL
  *   dh        [T][d] bf16 or NULL; it may be h itself
- *   dw        [V][d] bf16 or NULL; must not overlap w_vocab
+ *   dw        [V][d] bf16 or NULL
+ *             (otherwise h, w_vocab, dh and dw must not overlap: INVALID_ARG)
  *   ws        workspace of min_bytes or more (eat_ce_workspace_size), 256-byte aligned
  * T = 0 gives loss 0, n 0 and dw 0 (h and target may then be NULL).  Every sum
  * has a fixed order: results are bit-reproducible (the gradients for one
@@ -418,7 +422,7 @@ eat_status_t eat_balance_workspace_size(eat_handle_t h, int32_t T, size_t* bytes
  *   loss_out  [1] fp32;  count_out [E] int64 (C) and mean_prob_out [E] fp32 (P), or NULL
  *   dlogits   [T][E] fp32 (dz), dx [T][d_model] act_dtype, dw_router [E][d_model]
  *             fp32: each may be NULL; dlogits may be prob itself, dx x itself
- *             where dw_router is NULL
+ *             where dw_router is NULL (other overlaps of these: INVALID_ARG)
  *   ws        workspace of eat_balance_workspace_size(h, T) bytes, 256-byte aligned
  * T = 0 gives loss 0, counts 0, P 0 and dw_router 0.  Every sum has a fixed
  * order.  Enqueues on `stream` only; no synchronisation, no allocation, no

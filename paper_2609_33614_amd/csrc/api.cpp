@@ -52,6 +52,12 @@ eat_status_t check_params(const eat_params_t& p) {
     return EAT_OK;
 }
 
+// Whether two buffers (either may be null) share bytes.
+bool overlap(const void* p, size_t np, const void* q, size_t nq) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return p && q && a < b + nq && b < a + np;
+}
+
 size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
 
 }  // namespace
@@ -538,6 +544,10 @@ eat_status_t eat_ce_loss(const void* h, int32_t T, int32_t d, const void* w_voca
     if (!aligned(h, 16) || !aligned(w_vocab, 16) || !aligned(target, 4) || !aligned(loss_out, 4) ||
         !aligned(nll_out, 4) || !aligned(count_out, 4) || !aligned(dh, 16) || !aligned(dw, 16))
         return EAT_ERR_INVALID_ARG;
+    const size_t hb = static_cast<size_t>(T) * d * 2, wb = static_cast<size_t>(V) * d * 2;
+    if ((dh != h && overlap(dh, hb, h, hb)) || overlap(dh, hb, w_vocab, wb) || overlap(dw, wb, w_vocab, wb) ||
+        overlap(dw, wb, h, hb) || overlap(dh, hb, dw, wb))
+        return EAT_ERR_INVALID_ARG;
     const eat::CePlan p = eat::plan_ce(T, d, V, dh != nullptr, dw != nullptr, ws_bytes);
     if (!ws || ws_bytes < p.total) return EAT_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
@@ -566,6 +576,12 @@ eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const fl
     if (!aligned(x, 16) || !aligned(w_router, 16) || !aligned(prob, 4) || !aligned(mask, 8) || !aligned(loss_out, 4) ||
         !aligned(count_out, 8) || !aligned(mean_prob_out, 4) || !aligned(dlogits, 4) || !aligned(dx, 16) ||
         !aligned(dw_router, 16))
+        return EAT_ERR_INVALID_ARG;
+    const size_t xb = static_cast<size_t>(T) * h->p.d_model * (h->p.act_dtype == EAT_BF16 ? 2 : 4);
+    const size_t rb = static_cast<size_t>(h->p.E) * h->p.d_model * 4, pb = static_cast<size_t>(T) * h->p.E * 4;
+    if ((overlap(dx, xb, x, xb) && (dx != x || dw_router)) || (dlogits != prob && overlap(dlogits, pb, prob, pb)) ||
+        overlap(dx, xb, w_router, rb) || overlap(dw_router, rb, w_router, rb) || overlap(dw_router, rb, x, xb) ||
+        overlap(dx, xb, dw_router, rb))
         return EAT_ERR_INVALID_ARG;
     const eat::BalancePlan b = eat::plan_balance(h->p, T);
     if (!ws || ws_bytes < b.total) return EAT_ERR_WORKSPACE;

@@ -468,9 +468,10 @@ __global__ __launch_bounds__(256) void dw_join_kernel(const float* __restrict__ 
 constexpr int kOneBlock = 4096;           // most probabilities one workgroup sums up
 constexpr int kOneSlice = 64;             // most tokens that dW_r of a small call takes in one slice
 
-// Products on the split operands from here on, on fp32 instructions below.
+// Products on the split operands from here on, on fp32 instructions below.  (A
+// row of x's parts is addressed with 24 bits.)
 bool split_products(const eat_params_t& p, int32_t T) {
-    return static_cast<int64_t>(T) * p.E * p.d_model >= (int64_t{1} << 27);
+    return static_cast<int64_t>(T) * p.E * p.d_model >= (int64_t{1} << 27) && p.d_model <= 1 << 20;
 }
 
 template <int J>
@@ -486,9 +487,12 @@ template <typename XT>
 hipError_t launch_products(const eat_params_t& p, const BalancePlan& b, const BalanceCall& c, const float* dz, float* dwp,
                            hipStream_t s) {
     const int E = p.E, d = p.d_model;
-    const int bw = c.dw ? (E + 63) / 64 * (d / 64) * b.splits : 0, bx = c.dx ? (c.T + 63) / 64 * (d / 64) : 0;
-    const ProductArgs a{dz, c.x, c.w_router, c.valid, c.T, E, d, b.splits, bw, p.inv_temperature, c.dw, dwp, c.dx};
-    if (bw + bx > 0) product_kernel<XT><<<bw + bx, 256, 0, s>>>(a);
+    const int64_t bw = c.dw ? int64_t{(E + 63) / 64} * (d / 64) * b.splits : 0;
+    const int64_t bx = c.dx ? int64_t{(c.T + 63) / 64} * (d / 64) : 0;
+    if (bw + bx > INT32_MAX) return hipErrorInvalidConfiguration;
+    const ProductArgs a{dz, c.x, c.w_router, c.valid, c.T, E, d, b.splits, static_cast<int>(bw), p.inv_temperature, c.dw,
+                        dwp, c.dx};
+    if (bw + bx > 0) product_kernel<XT><<<static_cast<int>(bw + bx), 256, 0, s>>>(a);
     if (c.dw && b.splits > 1)
         dw_join_kernel<<<static_cast<int>((static_cast<int64_t>(E) * d / 4 + 255) / 256), 256, 0, s>>>(
             dwp, b.splits, 1, E, d, p.inv_temperature, c.dw);

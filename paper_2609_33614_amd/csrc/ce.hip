@@ -300,7 +300,7 @@ hipError_t launch_sized(Size z, const GemmArgs& g, hipStream_t s) {
 // from kMinPiece columns on.  The first piece costs a pass over its G, every
 // other one its product again.
 constexpr size_t kPieceBytes = size_t{4} << 30;
-constexpr int kMinPiece = 4096;
+constexpr int kMinPiece = 4096, kMaxPiece = 1 << 22;       // (a row of G is addressed with 24 bits)
 
 }  // namespace
 
@@ -313,7 +313,8 @@ CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) 
     const int vpad = (V + 255) / 256 * 256;
     const int least = std::min(vpad, kMinPiece);
     auto fit = [&](size_t room) {
-        return static_cast<int>(std::max<size_t>(least, std::min<size_t>(vpad, room / (2 * tp * planes) / 256 * 256)));
+        return static_cast<int>(
+            std::max<size_t>(least, std::min<size_t>({size_t(vpad), size_t(kMaxPiece), room / (2 * tp * planes) / 256 * 256})));
     };
     // dh: room for its slices, a few of many rows (how many there are is chosen on
     // the device, by the rows that count)
@@ -338,8 +339,8 @@ CePlan plan_ce(int32_t T, int32_t d, int32_t V, bool dh, bool dw, size_t bytes) 
     };
     layout(fit(kPieceBytes));
     if (p.total <= bytes || (!dh && !dw)) return p;
-    layout(least < vpad ? least : vpad);
-    if (bytes > p.total) layout(std::min(vpad, fit(bytes - p.g)));
+    layout(least);
+    if (bytes > p.total) layout(fit(bytes - p.g));
     return p;
 }
 

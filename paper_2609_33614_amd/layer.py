@@ -6,6 +6,7 @@ entry points of ``_lib``.  All compute runs in libeat.so.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Dict, Optional
 
 import torch
@@ -21,6 +22,37 @@ def _expect(name: str, t: Optional[torch.Tensor], dtype, shape) -> None:
         raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
 
 
+class _Workspace:
+    """A growing device buffer.  One that a graph capture used stays alive as
+    long as its owner does, so that the graph may be replayed after it grew."""
+
+    def __init__(self, device):
+        self.device, self.buf, self.captured = device, None, []
+
+    def get(self, need: int, stream=None) -> torch.Tensor:
+        if self.buf is None or self.buf.numel() < need:
+            self.buf = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+        if torch.cuda.is_current_stream_capturing() and not any(b is self.buf for b in self.captured):
+            self.captured.append(self.buf)
+        _used_on(stream, self.buf)
+        return self.buf[:need]
+
+
+def _used_on(stream, *tensors) -> None:
+    """Tell torch's allocator that ``stream`` uses tensors made on the current one."""
+    if isinstance(stream, torch.cuda.Stream):
+        for t in tensors:
+            t.record_stream(stream)
+
+
+def _on_device(device):
+    """The library launches on the current device: make it the tensors'."""
+    index = device.index
+    if index is None or index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(index)
+
+
 class EatLayer:
     def __init__(self, params: L.eat_params_t, max_tokens: int, weights: Dict[str, torch.Tensor],
                  device: str = "cuda"):
@@ -34,7 +66,7 @@ class EatLayer:
         self.p_total = torch.zeros(E, dtype=torch.float32, device=self.device)
         self.c_s = torch.zeros(E, dtype=torch.float32, device=self.device)
         self._ws: Optional[torch.Tensor] = None
-        self._bws: Optional[torch.Tensor] = None
+        self._bws = _Workspace(self.device)
 
     # account state -------------------------------------------------------
     @property
@@ -111,14 +143,14 @@ class EatLayer:
         _expect("dlogits", dlogits, torch.float32, (T, E))
         _expect("dx", dx, act, (T, d))
         _expect("dw_router", dw_router, torch.float32, (E, d))
-        loss = torch.empty(1, dtype=torch.float32, device=self.device)
-        count = torch.empty(E, dtype=torch.int64, device=self.device)
-        mean = torch.empty(E, dtype=torch.float32, device=self.device)
-        need = L.eat_balance_workspace_size(self.handle, T)
-        if self._bws is None or self._bws.numel() < need:
-            self._bws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        L.eat_balance_loss(self.handle, x, T, self.w["w_router"], prob, mask, valid, coef, entropy_coef, loss, count,
-                           mean, dlogits, dx, dw_router, self._bws, self._bws.numel(), stream)
+        with _on_device(prob.device):
+            loss = torch.empty(1, dtype=torch.float32, device=prob.device)
+            count = torch.empty(E, dtype=torch.int64, device=prob.device)
+            mean = torch.empty(E, dtype=torch.float32, device=prob.device)
+            ws = self._bws.get(L.eat_balance_workspace_size(self.handle, T), stream)
+            _used_on(stream, loss, count, mean)
+            L.eat_balance_loss(self.handle, x, T, self.w["w_router"], prob, mask, valid, coef, entropy_coef, loss, count,
+                               mean, dlogits, dx, dw_router, ws, ws.numel(), stream)
         return loss, count, mean
 
     def close(self) -> None:
@@ -173,15 +205,13 @@ class CrossEntropy:
         _expect("w_vocab", w_vocab, torch.bfloat16, tuple(w_vocab.shape))
         self.w, self.ignore, self.max_workspace = w_vocab, int(ignore), max_workspace
         self.V, self.d = w_vocab.shape
-        self._ws: Optional[torch.Tensor] = None
+        self._ws = _Workspace(w_vocab.device)
 
-    def workspace(self, T: int, grads: int) -> torch.Tensor:
+    def workspace(self, T: int, grads: int, stream=None) -> torch.Tensor:
         need, least = L.eat_ce_workspace_size(T, self.d, self.V, grads)
         if self.max_workspace is not None:
             need = min(need, max(least, int(self.max_workspace)))
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.w.device)
-        return self._ws[:need]        # (its size decides the pieces, so a call's does not depend on earlier ones)
+        return self._ws.get(need, stream)     # (its size decides the pieces: it does not depend on earlier calls)
 
     def loss(self, h: torch.Tensor, target: torch.Tensor, mean: bool = True, scale: float = 1.0,
              nll: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
@@ -193,10 +223,12 @@ class CrossEntropy:
         _expect("count", count, torch.int32, (1,))
         _expect("dh", dh, torch.bfloat16, (T, self.d))
         _expect("dw", dw, torch.bfloat16, (self.V, self.d))
-        out = torch.empty(1, dtype=torch.float32, device=self.w.device)
-        ws = self.workspace(T, (L.EAT_CE_DH if dh is not None else 0) | (L.EAT_CE_DW if dw is not None else 0))
-        L.eat_ce_loss(h, T, self.d, self.w, self.V, target, self.ignore, int(mean), scale, out, nll, count, dh, dw, ws,
-                      ws.numel(), stream)
+        with _on_device(self.w.device):
+            out = torch.empty(1, dtype=torch.float32, device=self.w.device)
+            ws = self.workspace(T, (L.EAT_CE_DH if dh is not None else 0) | (L.EAT_CE_DW if dw is not None else 0), stream)
+            _used_on(stream, out)
+            L.eat_ce_loss(h, T, self.d, self.w, self.V, target, self.ignore, int(mean), scale, out, nll, count, dh, dw, ws,
+                          ws.numel(), stream)
         return out
 
 

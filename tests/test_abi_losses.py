@@ -42,18 +42,29 @@ def test_ce_workspace_is_bounded():
     assert min(L.eat_ce_workspace_size(0, 64, 10, 3)) > 0
 
 
+@pytest.mark.parametrize("T,d,V", [(1, 64, 2 ** 24), (64, 64, 2 ** 24), (256, 65536, 2 ** 24), (2 ** 20, 65536, 2 ** 24),
+                                   (300, 64, 2 ** 23), (1, 64, 1)])
+def test_ce_workspace_at_the_limits(T, d, V):
+    for grads in range(4):
+        most, least = L.eat_ce_workspace_size(T, d, V, grads)
+        assert 0 < least <= most < 2 ** 47
+
+
 def test_ce_validation_happens_on_the_host():
     T, d, V = 100, 128, 1000
     n = L.eat_ce_workspace_size(T, d, V, 3)[1]
 
-    def go(h=F, T=T, d=d, w=F, V=V, y=F, ignore=-100, mean=1, scale=1.0, loss=F, nll=F, count=F, dh=F, dw=F, ws=F, wsn=n):
+    def go(h=F, T=T, d=d, w=4 * F, V=V, y=F, ignore=-100, mean=1, scale=1.0, loss=F, nll=F, count=F, dh=2 * F, dw=3 * F, ws=F, wsn=n):
         L.eat_ce_loss(h, T, d, w, V, y, ignore, mean, scale, loss, nll, count, dh, dw, ws, wsn, stream=0)
 
     bad = L.EAT_ERR_INVALID_ARG
     for kw in (dict(h=None), dict(w=None), dict(y=None), dict(loss=None), dict(mean=2), dict(mean=-1),
                dict(scale=float("nan")), dict(scale=float("inf")), dict(T=-1), dict(d=96), dict(V=0),
                dict(h=F + 8), dict(w=F + 2), dict(y=F + 2), dict(loss=F + 1), dict(nll=F + 2), dict(count=F + 1),
-               dict(dh=F + 8), dict(dw=F + 4), dict(ws=F + 128), dict(T=0, w=None)):
+               dict(dh=F + 8), dict(dw=F + 4), dict(ws=F + 128), dict(T=0, w=None),
+               # overlaps (h: 25600 bytes at F, dh at 2 F, dw: 256000 at 3 F, w at 4 F)
+               dict(dh=F + 16), dict(dh=F - 16), dict(dh=4 * F + 16), dict(dw=4 * F), dict(dw=4 * F - 16), dict(dw=F),
+               dict(dh=3 * F + 255984)):
         refused(bad, go, **kw)
     refused(L.EAT_ERR_WORKSPACE, go, ws=None)
     refused(L.EAT_ERR_WORKSPACE, go, wsn=n - 1)
@@ -72,14 +83,17 @@ def test_balance_validation_happens_on_the_host(handle):
     n = L.eat_balance_workspace_size(handle, T)
     bad = L.EAT_ERR_INVALID_ARG
 
-    def go(h=handle, x=F, T=T, w=F, prob=F, mask=F, valid=F, coef=0.01, ent=0.0, loss=F, count=F, mean=F, dz=F, dx=F,
-           dw=F, ws=F, wsn=n):
+    def go(h=handle, x=F, T=T, w=2 * F, prob=3 * F, mask=F, valid=F, coef=0.01, ent=0.0, loss=F, count=F, mean=F, dz=4 * F,
+           dx=5 * F, dw=6 * F, ws=F, wsn=n):
         L.eat_balance_loss(h, x, T, w, prob, mask, valid, coef, ent, loss, count, mean, dz, dx, dw, ws, wsn, stream=0)
 
     for kw in (dict(h=None), dict(T=-1), dict(T=257), dict(prob=None), dict(mask=None), dict(loss=None),
                dict(coef=float("nan")), dict(ent=float("inf")), dict(x=None), dict(w=None), dict(x=F + 8),
                dict(w=F + 4), dict(prob=F + 2), dict(mask=F + 4), dict(loss=F + 2), dict(count=F + 4), dict(mean=F + 1),
-               dict(dz=F + 2), dict(dx=F + 8), dict(dw=F + 8), dict(ws=F + 64)):
+               dict(dz=F + 2), dict(dx=F + 8), dict(dw=F + 8), dict(ws=F + 64),
+               # overlaps (x and dx: 25600 bytes, w and dw: 30720, prob and dz: 24000)
+               dict(dx=F), dict(dx=F + 16, dw=None), dict(dz=3 * F + 16), dict(dx=2 * F + 30704), dict(dw=2 * F), dict(dw=F),
+               dict(dw=5 * F + 16)):
         refused(bad, go, **kw)
     refused(L.EAT_ERR_WORKSPACE, go, ws=None)
     refused(L.EAT_ERR_WORKSPACE, go, wsn=n - 1)

@@ -60,7 +60,7 @@ def call(layer, x, prob, mask, valid, coef=0.01, ent=0.002, dz=True, dx=True, dw
         bufs["dw_router"] = out(layer.w["w_router"].shape, torch.float32)
     views = {k: v for k, (_, v) in bufs.items()}
     layer.balance_loss(x, prob, mask, valid, coef, ent)
-    layer._bws.fill_(0xFF)
+    layer._bws.buf.fill_(0xFF)
     loss, count, mean = layer.balance_loss(x, prob, mask, valid, coef, ent, **views)
     torch.cuda.synchronize()
     for k, (buf, _) in bufs.items():
@@ -238,7 +238,7 @@ def test_every_choice_of_outputs_and_aliases(T, E, d, bf16):
     layer.balance_loss(xc, pc, mask, valid, 0.01, 0.002, dlogits=pc, dx=xc)
     assert torch.equal(pc, full["dlogits"]) and torch.equal(xc, full["dx"])
     L.eat_balance_loss(layer.handle, None, T, layer.w["w_router"], prob, mask, valid, 0.01, 0.002, full["loss"], None,
-                       None, None, xc, None, layer._bws, layer._bws.numel())
+                       None, None, xc, None, layer._bws.buf, layer._bws.buf.numel())
     assert torch.equal(xc, full["dx"])
 
 

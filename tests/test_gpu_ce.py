@@ -364,6 +364,28 @@ def test_graph_replays(T):
             assert torch.equal(out[k], ref[k]), (seed, k)
 
 
+def test_graph_outlives_its_workspace():
+    """A graph captured with a small workspace is replayed after a larger call
+    gave the object another one (and other tensors took the memory it freed)."""
+    h, w, y = make(900, 192, 1200, ignored=0.2)
+    ce = CrossEntropy(w)
+    hs, ys = h[:100].clone(), y[:100].clone()
+    dh, dw = torch.empty_like(hs), torch.empty_like(w)
+    box = {}
+    g = capture(lambda: box.update(loss=ce.loss(hs, ys, dh=dh, dw=dw)))
+    small = ce._ws.buf.numel()
+    ce.loss(h, y, dh=torch.empty_like(h), dw=torch.empty_like(w))
+    assert ce._ws.buf.numel() > small
+    fill = [torch.full((small,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    ref = call(hs, w, ys)
+    for _ in range(3):
+        dh.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(box["loss"], ref["loss"]) and torch.equal(dh, ref["dh"]) and torch.equal(dw, ref["dw"])
+    assert all((f == 0xFF).all() for f in fill)
+
+
 def test_the_nll_is_the_perplexity_signals():
     """eat_ppl_trend's NLL of the same rows: both are within the NLL's bound."""
     from paper_2609_33614_amd.layer import PplSignal
