@@ -465,13 +465,28 @@ __global__ __launch_bounds__(256) void dw_join_kernel(const float* __restrict__ 
 }
 
 
-constexpr int kOneBlock = 4096;           // most probabilities one workgroup sums up
-constexpr int kOneSlice = 64;             // most tokens that dW_r of a small call takes in one slice
+// Most probabilities that one workgroup sums up, of 1024 tokens at most: two
+// launches less (whole calls, one workgroup | many: 256 x 64: 25 | 31 us;
+// 1024 x 8: 25 | 32; 1024 x 32: 42 | 32; 2048 x 8: 36 | 32).
+constexpr int kOneBlock = 16384;
 
-// Products on the split operands from here on, on fp32 instructions below.  (A
-// row of x's parts is addressed with 24 bits.)
+// Whether the products run on bf16 parts (more launches, faster products) or on
+// fp32 instructions, by measured times of whole calls (fp32 instructions |
+// parts, us).  bf16 tokens, dx on three products and dW_r on two:
+//   T 16384, E 8, d 64: 55 | 47;  E 64, d 512: 73 | 56;  E 256, d 128: 78 | 77
+//   T 8192, E 8, d 512: 39 | 42;  E 256, d 512: 93 | 67
+//   T 4096, E 64, d 512: 36 | 40;  d 2048: 59 | 44;  E 256, d 512: 61 | 60
+//   T 2048, E 64, d 2048: 38 | 40;  T 3000: 49 | 45
+//   T 1024, E 64, d 4096: 35 | 41;  T 512, E 256, d 4096: 50 | 59, d 8192: 89 | 65
+// fp32 tokens are three parts, so six products:
+//   T 2048, E 256, d 2048: 85 | 90;  d 4096: 152 | 120;  T 16384: 1056 | 741
+//   T 16384, E 64, d 4096: 310 | 350;  T 65536, E 8: 850 | 1263
+// (A row of x's parts is addressed with 24 bits.)
 bool split_products(const eat_params_t& p, int32_t T) {
-    return static_cast<int64_t>(T) * p.E * p.d_model >= (int64_t{1} << 27) && p.d_model <= 1 << 20;
+    if (p.d_model > 1 << 20) return false;
+    const int64_t work = static_cast<int64_t>(T) * p.d_model;
+    if (p.act_dtype != EAT_BF16) return p.E > 64 && work * p.E >= int64_t{1} << 31;
+    return T >= 16384 || work * ((p.E + 63) / 64 * 64) >= int64_t{1} << (T >= 2048 ? 29 : 30);
 }
 
 template <int J>
@@ -552,17 +567,20 @@ BalancePlan plan_balance(const eat_params_t& p, int32_t T) {
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += (bytes + 255) & ~size_t(255); return at; };
     // (one workgroup needs no meeting of several, and makes dz of a small call as well)
-    b.blocks = static_cast<int64_t>(T) * p.E <= kOneBlock ? 1 : std::min(kStatBlocks, (T + 63) / 64);
+    b.blocks = T <= 1024 && static_cast<int64_t>(T) * p.E <= kOneBlock ? 1 : std::min(kStatBlocks, (T + 63) / 64);
     b.split = split_products(p, T);
     const size_t groups = (p.E + 63) / 64, d = p.d_model, pad = (static_cast<size_t>(T) + 255) / 256 * 256;
     const int parts = b.split && p.act_dtype != EAT_BF16 ? 3 : 1;
-    // dw_router: slices of the tokens until the CUs have an item each (four
-    // small ones of the fp32 kernel), none under 4 chunks (64 tokens)
+    // dw_router: slices of the tokens, joined by a launch, until the CUs have an
+    // item each (four small ones of the fp32 kernel), none under 512 tokens, or
+    // 128 while CUs would idle.  T 16384, E 8, d 1024, parts: 32 slices of 512
+    // tokens 53 us, 64 of 256 61, 16 of 1024 56; T 65536, E 64, d 512: 64 slices 107
+    // us, 32 112, 128 122; fp32 instructions, T 16384, E 64, d 256: 64 slices of
+    // 256 tokens 59 us, 128 of 128 76, 32 of 512 63.
     const int64_t items = b.split ? groups * ((parts * d + Big::NA - 1) / Big::NA) : groups * (d / 64);
     b.splits = 1;
-    if (b.split || T > kOneSlice)
-        while (items * b.splits * 2 <= (b.split ? 256 : 1024) && T / (b.splits * 2) >= (b.split ? 4 * kBK : 64))
-            b.splits *= 2;
+    for (int n = 2; items * n <= (b.split ? 256 : 1024) && n <= (b.split ? 64 : 256); n *= 2)
+        if (T / n >= (b.split || items * n > 256 ? 512 : 128)) b.splits = n;
     b.head = take(12);
     b.rows = take(b.split ? pad * 4 : 0);
     b.q = take(static_cast<size_t>(p.E) * 4);

@@ -532,7 +532,10 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                 if ((64 / V) * k >= nv) break;
                 const int r = (64 / V) * k + lane / V, v = lane % V;
                 const u32x4 d = *reinterpret_cast<const u32x4*>(tb + at(r, v));
-                if (r < nv) *reinterpret_cast<u32x4*>(dst(r) + 8 * v) = d;
+                // (past the caches, which the operands that are read again need: dW
+                // of 32000 x 4096 from one row took 121 us through them and 70 so,
+                // a router gradient of 16384 x 4096 290 and 246; nothing got slower)
+                if (r < nv) __builtin_nontemporal_store(d, reinterpret_cast<u32x4*>(dst(r) + 8 * v));
                 ++stored;
             }
             wave_lds_sync();

@@ -127,7 +127,8 @@ def routed(E, d, bf16, T, mode="topk", k=2, seed=0, **kw):
                                      (65, 60, 128, 4), (100, 65, 64, 3), (200, 100, 320, 8), (257, 128, 256, 8),
                                      (1000, 200, 128, 8), (777, 256, 512, 8), (2049, 16, 64, 1), (5000, 33, 128, 2),
                                      (2111, 64, 1024, 8), (1030, 256, 576, 8), (4111, 130, 320, 4), (20000, 7, 1024, 2),
-                                     (257, 256, 2112, 2), (64, 250, 8640, 8)])
+                                     (257, 256, 2112, 2), (64, 250, 8640, 8), (16400, 1, 64, 1), (1027, 70, 8192, 4),
+                                     (530, 256, 4096, 8), (250, 64, 67200, 8), (2050, 250, 4224, 8)])
 def test_loss_counts_gradients(T, E, d, k, bf16):
     layer, x, prob, mask = routed(E, d, bf16, T, k=k)
     check(f"bal {T} {E} {d}", call(layer, x, prob, mask, None), reference(layer, x, prob, mask, None, 0.01, 0.002))
@@ -136,7 +137,9 @@ def test_loss_counts_gradients(T, E, d, k, bf16):
 @pytest.mark.parametrize("kind", ["some", "none", "one", "tail"])
 @pytest.mark.parametrize("T,E,d,bf16", [(1, 8, 64, False), (70, 60, 128, True), (600, 130, 192, True), (600, 12, 64, False),
                                         (2300, 60, 1024, True), (2300, 60, 1024, False), (1100, 200, 640, True),
-                                        (1100, 200, 640, False)])
+                                        (1100, 200, 640, False), (2060, 130, 1408, True), (8000, 60, 1152, True),
+                                        (16500, 12, 64, True),
+                                        (2100, 250, 4160, False)])
 def test_tokens_that_do_not_count(T, E, d, bf16, kind):
     layer, x, prob, mask = routed(E, d, bf16, T)
     valid = make_valid(T, kind)
@@ -225,7 +228,8 @@ def test_gradients_against_differences():
         assert (mine - slope).abs() <= bound, (name, float(mine), float(slope))
 
 
-@pytest.mark.parametrize("T,E,d,bf16", [(40, 8, 192, True), (500, 128, 192, True), (2200, 128, 512, True), (2200, 128, 512, False)])
+@pytest.mark.parametrize("T,E,d,bf16", [(40, 8, 192, True), (500, 128, 192, True), (2200, 128, 512, True), (2200, 128, 512, False),
+                                         (4300, 128, 1024, True), (4100, 128, 4160, False)])
 def test_every_choice_of_outputs_and_aliases(T, E, d, bf16):
     layer, x, prob, mask = routed(E, d, bf16, T)
     valid = make_valid(T, "some")
@@ -250,7 +254,7 @@ def test_empty_call():
     assert loss.item() == 0 and (count == 0).all() and (mean == 0).all() and (dw == 0).all()
 
 
-@pytest.mark.parametrize("T,E,d", [(700, 60, 128), (2200, 128, 512)])
+@pytest.mark.parametrize("T,E,d", [(700, 60, 128), (2200, 128, 512), (4300, 128, 1024)])
 def test_other_stream_and_graph_replays(T, E, d):
     layer, x, prob, mask = routed(E, d, True, T)
     valid = make_valid(T, "some")
