@@ -8,14 +8,21 @@
 // row by row, q = dloss / dP.
 //
 // The products of dz with the router weights (dx) and with x (dW_r), small
-// calls: dx_kernel and dw_kernel on fp32 matrix instructions, straight from
-// memory.  Larger ones: the bf16 instructions, which are 16 times as fast, on
+// calls: product_kernel on fp32 matrix instructions, straight from memory, both
+// products in one launch.  Larger ones: the bf16 instructions, which are 16 times
+// as fast, on
 // fp32 numbers written as sums of bf16 parts (each part the rounding of what the
 // ones before leave, so three hold 24 bits or more, two 16): dz in three parts, x
 // as it is (bf16) or in three, the router weights in two (dx in bf16) or three.
 // dW_r takes every product of parts, dx those above its precision (loss_gemm's
 // GROUPS).  Tokens that do not count are left out of the reduction (loss_gemm's
 // GATHER), so nothing of theirs is read.
+//
+// Bounds, measured: small calls by their launches (two to four that wait for each
+// other: 256 tokens, 64 experts, d 2048, dW_r only: 25 us, its bytes are 0.4); large
+// ones by the matrix instructions on the parts (16384 tokens, 256 experts, d 4096:
+// 246 us, of which dx ~95 and dW_r ~105, at 1.1 and 0.98 PFLOP/s of bf16
+// products); in between by both (8000 tokens, 60 experts, d 2048: 58 us, 63 MB).
 #include <math.h>
 
 #include <algorithm>

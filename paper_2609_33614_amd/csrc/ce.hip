@@ -4,17 +4,32 @@
 //   nll_t  = log(1 + sum_{v != y} exp(z_tv - z_ty)),  loss = c sum_t nll_t
 //   G_tv   = exp(z_tv - lse_t) off the target, expm1(-nll_t) on it
 //   dh     = c G W,   dW = c G^T h,   c = scale / (mean ? n : 1)
-// No row of z is kept: a first pass leaves one (maximum, sum of exponentials)
-// pair per row and 256 columns, and the gradients take z again, a piece of the
-// vocabulary at a time, whose G is held in bf16 (kPieceBytes at most) for its
-// two products.
+// The z of all the rows is never there.  A first pass leaves one (maximum, sum of
+// exponentials) pair per row and 128 or 256 columns, and in bf16 the exponentials of
+// the first piece of the vocabulary, over their tile's maximum: G of that piece
+// needs one multiplication per entry.  The gradients take the other pieces' z again,
+// a piece at a time, whose G is held in bf16 (kPieceBytes at most) for its two
+// products.
 //
 // list_kernel lists the rows that count, gather_kernel copies them together
 // (everything after works on n rows, so ignored ones cost nothing and reach
 // nothing) and takes their target's logit in fp64; loss_gemm<LSE> makes the
 // pairs, row_kernel the NLLs, the softmax denominators and the loss;
-// per piece loss_gemm<GRAD> makes G, loss_gemm<PART/ROWS> its products, and
-// join_kernel adds the slices of dh.
+// scale_kernel makes G of the first piece, loss_gemm<GRAD> of the others,
+// loss_gemm<PART/ROWS> the products of a piece, and join_kernel adds the slices of
+// dh.
+//
+// G in bf16 is off by up to 2^-8 of each entry, and that of the first piece by twice
+// that (the exponential's rounding and its own).  Over many rows such errors average
+// out against the rounding of the bf16 results; over few they do not (dW of one row
+// is its G times a number), so up to 64 rows have G in two bf16 parts.
+//
+// Bounds, measured: three products of 2 n d V operations each (1.22 - 1.29 PFLOP/s
+// of 1.25 - 1.4 that a library product reaches: 4096 rows, d 4096, V 32000 take
+// 2.74 ms, 1.17 PFLOP/s over all); with few rows the one pass over W (1 row, 262 MB:
+// 66 us, 4.0 TB/s), then dW's store (131 M entries from one row: 70 us, 3.7
+// TB/s); with small vocabularies the launches, five to seven that wait for each
+// other (32 rows, d 128, V 1024: 33 us).
 #include <math.h>
 
 #include <algorithm>
@@ -271,7 +286,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restr
 // The tile of a product of `rows` x `cols` outputs with one reduction slice:
 // Small up to its 64 rows (the operand of `cols` streams past), else the larger
 // one of Big and Mid whose rounds over the CUs take less time.  (A chunk costs a
-// Big workgroup kBigNs, a Mid one kMidNs.)
+// Big workgroup kBigNs, a Mid one kMidNs.  The loss of 32000 x 4096, Mid | Big:
+// 128 rows 62 | 108 us, 200 92 | 105, 300 124 | 114, 512 161 | 125; of 50000 x 2048:
+// 128 53 | 58, 200 87 | 61; of 8000 x 1024: 768 38 | 42, 2048 59 | 50.)
 enum Size { kSmall, kMid, kBig };
 int64_t tiles_of(int64_t rows, int64_t cols, int nb, int na) { return ((rows + nb - 1) / nb) * ((cols + na - 1) / na); }
 Size pick_tile(int64_t rows, int64_t cols) {
@@ -283,9 +300,15 @@ Size pick_tile(int64_t rows, int64_t cols) {
 constexpr int tile_cols(Size z) { return z == kBig ? Big::NA : Mid::NA; }
 static_assert(Mid::NA == Small::NA, "column tiles of 128 or 256");
 
-// dh, whose reduction is split over what CUs its tiles leave: by the rows alone
-// (kSmall: the 128-row tile on G's two planes).
-Size dh_tile(int64_t rows) { return rows <= Small::NB ? kSmall : rows <= 2 * Mid::NB ? kMid : kBig; }
+// dh, whose reduction of `chunks` is split over what CUs its tiles leave: Mid up
+// to its two tiles of rows, and while Big has few rounds over the CUs.  (kSmall: Mid
+// on G's two planes.  Mid | Big: 50000 x 2048, 128 rows 55 | 92 us, 256 81 | 95, 512
+// 144 | 140; 32000 x 4096, 256 100 | 102, 300 154 | 135; 8000 x 1024 in 8 rounds of
+// 1024 rows 38 | 45, in 16 of 2048 62 | 64.)
+Size dh_tile(int64_t rows, int64_t d, int64_t chunks) {
+    if (rows <= Small::NB) return kSmall;
+    return rows <= 2 * Mid::NB || tiles_of(rows, d, Big::NB, Big::NA) * chunks <= 8 * kCus ? kMid : kBig;
+}
 
 template <bool ACOLS, bool BCOLS, int OUT>
 hipError_t launch_sized(Size z, const GemmArgs& g, hipStream_t s) {
@@ -298,7 +321,9 @@ hipError_t launch_sized(Size z, const GemmArgs& g, hipStream_t s) {
 // G held at a time: a piece of the vocabulary whose G takes kPieceBytes at
 // most (1.4% of the card's memory) and, with a smaller workspace, what fits,
 // from kMinPiece columns on.  The first piece costs a pass over its G, every
-// other one its product again.
+// other one its product again: 8192 rows, d 4096, V 128256 (2.1 GB) take 22.0 ms in
+// one piece, 25.0 in two, 26.6 in four, 29.0 in 32; 512 rows, d 2048, V 50000 take 396
+// us in one, 478 in two, 1108 in 13 (the smallest, too few columns to fill the CUs).
 constexpr size_t kPieceBytes = size_t{4} << 30;
 constexpr int kMinPiece = 4096, kMaxPiece = 1 << 22;       // (a row of G is addressed with 24 bits)
 
@@ -357,7 +382,7 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
     uint16_t* const gbuf = reinterpret_cast<uint16_t*>(ws + p.g);
     float* const dhp = reinterpret_cast<float*>(ws + p.dhp);
     const int T = c.T, d = c.d, V = c.V;
-    const Size zz = pick_tile(T, V), zh = dh_tile(T);
+    const Size zz = pick_tile(T, V), zh = dh_tile(T, d, (std::min(p.piece, V) + kBK - 1) / kBK);
     const int again = zz == kSmall ? Small::NB : 0;
 
     const int rb = (p.rows_pad + kGatherWaves - 1) / kGatherWaves;
