@@ -17,7 +17,7 @@
 // bounds the large tile is the card's power (its clock falls to 1.5 - 1.6 GHz under
 // these products): 1.21 - 1.34 PFLOP/s for LSE, 1.24 - 1.29 for dh, 1.05 - 1.22
 // for dW, where a library product takes 1.29 - 1.53, 1.26 - 1.40 and 1.00 - 1.15
-// (8192 x 4096 x 32000, in turn).
+// (8192 x 4096 x 32768, timed in turn).
 //
 // The header's kernels are instantiated by ce.hip and balance.hip.
 #pragma once
