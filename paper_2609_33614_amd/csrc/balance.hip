@@ -578,16 +578,19 @@ BalancePlan plan_balance(const eat_params_t& p, int32_t T) {
     b.split = split_products(p, T);
     const size_t groups = (p.E + 63) / 64, d = p.d_model, pad = (static_cast<size_t>(T) + 255) / 256 * 256;
     const int parts = b.split && p.act_dtype != EAT_BF16 ? 3 : 1;
-    // dw_router: slices of the tokens, joined by a launch, until the CUs have an
-    // item each (four small ones of the fp32 kernel), none under 512 tokens, or
-    // 128 while CUs would idle.  T 16384, E 8, d 1024, parts: 32 slices of 512
-    // tokens 53 us, 64 of 256 61, 16 of 1024 56; T 65536, E 64, d 512: 64 slices 107
-    // us, 32 112, 128 122; fp32 instructions, T 16384, E 64, d 256: 64 slices of
-    // 256 tokens 59 us, 128 of 128 76, 32 of 512 63.
+    // dw_router: slices of the tokens, joined by a launch.  On parts about 512 tokens
+    // each, 64 at most, while the CUs have no two items (T 16384, E 8, d 1024: 512
+    // tokens 53 us, 384 56, 256 61, 1024 56; T 65536, E 64, d 512: 64 slices 107, 32
+    // 112, 128 122).  On fp32 instructions, of smaller tiles, until there are four
+    // items per CU, none under 512 tokens, or 128 while CUs would idle (T
+    // 16384, E 64, d 256: 64 slices of 256 tokens 59 us, 128 of 128 76, 32 of 512 63).
     const int64_t items = b.split ? groups * ((parts * d + Big::NA - 1) / Big::NA) : groups * (d / 64);
     b.splits = 1;
-    for (int n = 2; items * n <= (b.split ? 256 : 1024) && n <= (b.split ? 64 : 256); n *= 2)
-        if (T / n >= (b.split || items * n > 256 ? 512 : 128)) b.splits = n;
+    if (b.split)
+        b.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({64, 256 / items, (T + 511) / 512})));
+    else
+        for (int n = 2; items * n <= 1024 && n <= 256; n *= 2)
+            if (T / n >= (items * n > 256 ? 512 : 128)) b.splits = n;
     b.head = take(12);
     b.rows = take(b.split ? pad * 4 : 0);
     b.q = take(static_cast<size_t>(p.E) * 4);
