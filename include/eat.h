@@ -381,7 +381,8 @@ eat_status_t eat_ce_workspace_size(int32_t T, int32_t d, int32_t V, int32_t grad
  *   loss_out  [1] fp32;  nll_out [T] fp32 or NULL;  count_out [1] int32 (n) or NULL
  *   dh        [T][d] bf16 or NULL; it may be h itself
  *   dw        [V][d] bf16 or NULL
- *             (otherwise h, w_vocab, dh and dw must not overlap: INVALID_ARG)
+ *             (otherwise nothing that is written, the workspace included, may
+ *             overlap another of the call's arrays: INVALID_ARG)
  *   ws        workspace of min_bytes or more (eat_ce_workspace_size), 256-byte aligned
  * T = 0 gives loss 0, n 0 and dw 0 (h and target may then be NULL).  Every sum
  * has a fixed order: results are bit-reproducible (the gradients for one
@@ -422,7 +423,9 @@ eat_status_t eat_balance_workspace_size(eat_handle_t h, int32_t T, size_t* bytes
  *   loss_out  [1] fp32;  count_out [E] int64 (C) and mean_prob_out [E] fp32 (P), or NULL
  *   dlogits   [T][E] fp32 (dz), dx [T][d_model] act_dtype, dw_router [E][d_model]
  *             fp32: each may be NULL; dlogits may be prob itself, dx x itself
- *             where dw_router is NULL (other overlaps of these: INVALID_ARG)
+ *             where dw_router is NULL (otherwise nothing that is written, the
+ *             workspace included, may overlap another of the call's arrays:
+ *             INVALID_ARG)
  *   ws        workspace of eat_balance_workspace_size(h, T) bytes, 256-byte aligned
  * T = 0 gives loss 0, counts 0, P 0 and dw_router 0.  Every sum has a fixed
  * order.  Enqueues on `stream` only; no synchronisation, no allocation, no

@@ -8,6 +8,7 @@
 #include <cstring>
 #include <cmath>
 #include <functional>
+#include <initializer_list>
 #include <new>
 
 #include "eat_internal.h"
@@ -53,9 +54,25 @@ eat_status_t check_params(const eat_params_t& p) {
 }
 
 // Whether two buffers (either may be null) share bytes.
-bool overlap(const void* p, size_t np, const void* q, size_t nq) {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-    return p && q && a < b + nq && b < a + np;
+struct Span {
+    const void* p;
+    size_t n;
+};
+bool overlap(Span u, Span v) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(u.p), b = reinterpret_cast<uintptr_t>(v.p);
+    return u.p && v.p && a < b + v.n && b < a + u.n;
+}
+// Whether a buffer that a call writes shares bytes with another of its buffers,
+// the pairs apart for which `in_place` holds (same address, written read).
+template <typename F>
+bool clash(std::initializer_list<Span> out, std::initializer_list<Span> in, F in_place) {
+    for (const Span* o = out.begin(); o != out.end(); ++o) {
+        for (const Span* q = o + 1; q != out.end(); ++q)
+            if (overlap(*o, *q)) return true;
+        for (const Span& i : in)
+            if (overlap(*o, i) && !(o->p == i.p && in_place(o->p, i.p))) return true;
+    }
+    return false;
 }
 
 size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
@@ -544,13 +561,13 @@ eat_status_t eat_ce_loss(const void* h, int32_t T, int32_t d, const void* w_voca
     if (!aligned(h, 16) || !aligned(w_vocab, 16) || !aligned(target, 4) || !aligned(loss_out, 4) ||
         !aligned(nll_out, 4) || !aligned(count_out, 4) || !aligned(dh, 16) || !aligned(dw, 16))
         return EAT_ERR_INVALID_ARG;
-    const size_t hb = static_cast<size_t>(T) * d * 2, wb = static_cast<size_t>(V) * d * 2;
-    if ((dh != h && overlap(dh, hb, h, hb)) || overlap(dh, hb, w_vocab, wb) || overlap(dw, wb, w_vocab, wb) ||
-        overlap(dw, wb, h, hb) || overlap(dh, hb, dw, wb))
-        return EAT_ERR_INVALID_ARG;
     const eat::CePlan p = eat::plan_ce(T, d, V, dh != nullptr, dw != nullptr, ws_bytes);
     if (!ws || ws_bytes < p.total) return EAT_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
+    const size_t hb = static_cast<size_t>(T) * d * 2, wb = static_cast<size_t>(V) * d * 2, tb = static_cast<size_t>(T) * 4;
+    if (clash({{loss_out, 4}, {nll_out, tb}, {count_out, 4}, {dh, hb}, {dw, wb}, {ws, p.total}},
+              {{h, hb}, {w_vocab, wb}, {target, tb}}, [&](const void* o, const void* i) { return o == dh && i == h; }))
+        return EAT_ERR_INVALID_ARG;
     const eat::CeCall c{static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(w_vocab), target, T, d, V, ignore,
                         mean, scale, loss_out, nll_out, count_out, static_cast<uint16_t*>(dh),
                         static_cast<uint16_t*>(dw)};
@@ -577,15 +594,15 @@ eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const fl
         !aligned(count_out, 8) || !aligned(mean_prob_out, 4) || !aligned(dlogits, 4) || !aligned(dx, 16) ||
         !aligned(dw_router, 16))
         return EAT_ERR_INVALID_ARG;
-    const size_t xb = static_cast<size_t>(T) * h->p.d_model * (h->p.act_dtype == EAT_BF16 ? 2 : 4);
-    const size_t rb = static_cast<size_t>(h->p.E) * h->p.d_model * 4, pb = static_cast<size_t>(T) * h->p.E * 4;
-    if ((overlap(dx, xb, x, xb) && (dx != x || dw_router)) || (dlogits != prob && overlap(dlogits, pb, prob, pb)) ||
-        overlap(dx, xb, w_router, rb) || overlap(dw_router, rb, w_router, rb) || overlap(dw_router, rb, x, xb) ||
-        overlap(dx, xb, dw_router, rb))
-        return EAT_ERR_INVALID_ARG;
     const eat::BalancePlan b = eat::plan_balance(h->p, T);
     if (!ws || ws_bytes < b.total) return EAT_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
+    const size_t n = static_cast<size_t>(T), E = static_cast<size_t>(h->p.E), d = static_cast<size_t>(h->p.d_model);
+    const size_t xb = n * d * (h->p.act_dtype == EAT_BF16 ? 2 : 4), rb = E * d * 4, pb = n * E * 4;
+    if (clash({{loss_out, 4}, {count_out, E * 8}, {mean_prob_out, E * 4}, {dlogits, pb}, {dx, xb}, {dw_router, rb}, {ws, b.total}},
+              {{x, xb}, {w_router, rb}, {prob, pb}, {mask, n * ((E + 63) / 64) * 8}, {valid, n}},
+              [&](const void* o, const void* i) { return (o == dlogits && i == prob) || (o == dx && i == x && !dw_router); }))
+        return EAT_ERR_INVALID_ARG;
     const eat::BalanceCall c{x, w_router, prob, mask, valid, T, coef, entropy_coef, loss_out, count_out, mean_prob_out,
                              dlogits, dx, dw_router};
     (void)hipGetLastError();

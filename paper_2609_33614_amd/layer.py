@@ -14,35 +14,48 @@ import torch
 from . import _lib as L
 
 
-def _expect(name: str, t: Optional[torch.Tensor], dtype, shape) -> None:
-    """Refuse a tensor (None passes) whose type or shape the library would misread."""
+def _expect(name: str, t: Optional[torch.Tensor], dtype, shape, device=None) -> None:
+    """Refuse a tensor (None passes) whose type, shape or device the library would misread."""
     if t is None:
         return
     if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)) or t.shape != tuple(shape):
         raise ValueError(f"{name}: expected {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, the call's other tensors on {device}")
 
 
 class _Workspace:
     """A growing device buffer.  One that a graph capture used stays alive as
-    long as its owner does, so that the graph may be replayed after it grew."""
+    long as its owner does, so that the graph may be replayed after it grew;
+    one that another stream used than it was made on is not given away before
+    that stream is done."""
 
     def __init__(self, device):
-        self.device, self.buf, self.captured = device, None, []
+        self.device, self.buf, self.home, self.captured = device, None, 0, []
 
     def get(self, need: int, stream=None) -> torch.Tensor:
+        now = torch.cuda.current_stream(self.device)
         if self.buf is None or self.buf.numel() < need:
             self.buf = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
-        if torch.cuda.is_current_stream_capturing() and not any(b is self.buf for b in self.captured):
-            self.captured.append(self.buf)
-        _used_on(stream, self.buf)
+            self.home = now.cuda_stream
+        if torch.cuda.is_current_stream_capturing():
+            if not any(b is self.buf for b in self.captured):
+                self.captured.append(self.buf)
+        else:
+            used = now if stream is None else torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+            if used.cuda_stream != self.home:
+                self.buf.record_stream(used)
         return self.buf[:need]
 
 
 def _used_on(stream, *tensors) -> None:
     """Tell torch's allocator that ``stream`` uses tensors made on the current one."""
-    if isinstance(stream, torch.cuda.Stream):
+    if stream is None:
+        return
+    used = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+    if used.cuda_stream != torch.cuda.current_stream().cuda_stream:
         for t in tensors:
-            t.record_stream(stream)
+            t.record_stream(used)
 
 
 def _on_device(device):
@@ -132,21 +145,24 @@ class EatLayer:
         """The router's balance loss (eat_balance_loss) of the ``prob`` and
         ``mask`` that ``route`` returned for ``x``: (loss [1], selections per
         expert [E] int64, mean probabilities [E]).  The gradients are written
-        to the tensors given.  ``valid`` [T] (bool or uint8): tokens that count."""
+        to the tensors given.  ``valid`` [T] (bool or uint8): tokens that count.
+        Calls of one layer share a workspace: order them on one stream."""
         T, E, d = prob.shape[0], self.params.E, self.params.d_model
         act = torch.bfloat16 if self.params.act_dtype == L.EAT_BF16 else torch.float32
         W = L.mask_words(E)
+        dev = prob.device
         _expect("prob", prob, torch.float32, (T, E))
-        _expect("mask", mask, (torch.int64, torch.uint64), (T,) if mask.dim() == 1 and W == 1 else (T, W))
-        _expect("x", x, act, (T, d))
-        _expect("valid", valid, (torch.bool, torch.uint8), (T,))
-        _expect("dlogits", dlogits, torch.float32, (T, E))
-        _expect("dx", dx, act, (T, d))
-        _expect("dw_router", dw_router, torch.float32, (E, d))
-        with _on_device(prob.device):
-            loss = torch.empty(1, dtype=torch.float32, device=prob.device)
-            count = torch.empty(E, dtype=torch.int64, device=prob.device)
-            mean = torch.empty(E, dtype=torch.float32, device=prob.device)
+        _expect("w_router", self.w["w_router"], torch.float32, (E, d), dev)
+        _expect("mask", mask, (torch.int64, torch.uint64), (T,) if mask.dim() == 1 and W == 1 else (T, W), dev)
+        _expect("x", x, act, (T, d), dev)
+        _expect("valid", valid, (torch.bool, torch.uint8), (T,), dev)
+        _expect("dlogits", dlogits, torch.float32, (T, E), dev)
+        _expect("dx", dx, act, (T, d), dev)
+        _expect("dw_router", dw_router, torch.float32, (E, d), dev)
+        with _on_device(dev):
+            loss = torch.empty(1, dtype=torch.float32, device=dev)
+            count = torch.empty(E, dtype=torch.int64, device=dev)
+            mean = torch.empty(E, dtype=torch.float32, device=dev)
             ws = self._bws.get(L.eat_balance_workspace_size(self.handle, T), stream)
             _used_on(stream, loss, count, mean)
             L.eat_balance_loss(self.handle, x, T, self.w["w_router"], prob, mask, valid, coef, entropy_coef, loss, count,
@@ -217,14 +233,15 @@ class CrossEntropy:
              nll: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
              dh: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         T = h.shape[0]
-        _expect("h", h, torch.bfloat16, (T, self.d))
-        _expect("target", target, torch.int32, (T,))
-        _expect("nll", nll, torch.float32, (T,))
-        _expect("count", count, torch.int32, (1,))
-        _expect("dh", dh, torch.bfloat16, (T, self.d))
-        _expect("dw", dw, torch.bfloat16, (self.V, self.d))
-        with _on_device(self.w.device):
-            out = torch.empty(1, dtype=torch.float32, device=self.w.device)
+        dev = self.w.device
+        _expect("h", h, torch.bfloat16, (T, self.d), dev)
+        _expect("target", target, torch.int32, (T,), dev)
+        _expect("nll", nll, torch.float32, (T,), dev)
+        _expect("count", count, torch.int32, (1,), dev)
+        _expect("dh", dh, torch.bfloat16, (T, self.d), dev)
+        _expect("dw", dw, torch.bfloat16, (self.V, self.d), dev)
+        with _on_device(dev):
+            out = torch.empty(1, dtype=torch.float32, device=dev)
             ws = self.workspace(T, (L.EAT_CE_DH if dh is not None else 0) | (L.EAT_CE_DW if dw is not None else 0), stream)
             _used_on(stream, out)
             L.eat_ce_loss(h, T, self.d, self.w, self.V, target, self.ignore, int(mean), scale, out, nll, count, dh, dw, ws,

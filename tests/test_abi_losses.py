@@ -54,17 +54,22 @@ def test_ce_validation_happens_on_the_host():
     T, d, V = 100, 128, 1000
     n = L.eat_ce_workspace_size(T, d, V, 3)[1]
 
-    def go(h=F, T=T, d=d, w=4 * F, V=V, y=F, ignore=-100, mean=1, scale=1.0, loss=F, nll=F, count=F, dh=2 * F, dw=3 * F, ws=F, wsn=n):
+    W = 64 * F           # (every array at an address of its own)
+
+    def go(h=F, T=T, d=d, w=4 * F, V=V, y=5 * F, ignore=-100, mean=1, scale=1.0, loss=6 * F, nll=7 * F, count=8 * F, dh=2 * F,
+           dw=3 * F, ws=W, wsn=n):
         L.eat_ce_loss(h, T, d, w, V, y, ignore, mean, scale, loss, nll, count, dh, dw, ws, wsn, stream=0)
 
     bad = L.EAT_ERR_INVALID_ARG
     for kw in (dict(h=None), dict(w=None), dict(y=None), dict(loss=None), dict(mean=2), dict(mean=-1),
                dict(scale=float("nan")), dict(scale=float("inf")), dict(T=-1), dict(d=96), dict(V=0),
                dict(h=F + 8), dict(w=F + 2), dict(y=F + 2), dict(loss=F + 1), dict(nll=F + 2), dict(count=F + 1),
-               dict(dh=F + 8), dict(dw=F + 4), dict(ws=F + 128), dict(T=0, w=None),
+               dict(dh=F + 8), dict(dw=F + 4), dict(ws=W + 128), dict(T=0, w=None),
                # overlaps (h: 25600 bytes at F, dh at 2 F, dw: 256000 at 3 F, w at 4 F)
                dict(dh=F + 16), dict(dh=F - 16), dict(dh=4 * F + 16), dict(dw=4 * F), dict(dw=4 * F - 16), dict(dw=F),
-               dict(dh=3 * F + 255984)):
+               dict(dh=3 * F + 255984), dict(loss=F), dict(loss=5 * F + 396), dict(nll=5 * F), dict(nll=4 * F), dict(count=6 * F),
+               dict(nll=8 * F - 396), dict(loss=3 * F), dict(dh=5 * F), dict(dh=W + n - n % 16 - 16), dict(ws=F), dict(ws=3 * F),
+               dict(ws=7 * F - 256), dict(h=W + 1024), dict(y=W)):
         refused(bad, go, **kw)
     refused(L.EAT_ERR_WORKSPACE, go, ws=None)
     refused(L.EAT_ERR_WORKSPACE, go, wsn=n - 1)
@@ -83,17 +88,22 @@ def test_balance_validation_happens_on_the_host(handle):
     n = L.eat_balance_workspace_size(handle, T)
     bad = L.EAT_ERR_INVALID_ARG
 
-    def go(h=handle, x=F, T=T, w=2 * F, prob=3 * F, mask=F, valid=F, coef=0.01, ent=0.0, loss=F, count=F, mean=F, dz=4 * F,
-           dx=5 * F, dw=6 * F, ws=F, wsn=n):
+    W = 64 * F
+
+    def go(h=handle, x=F, T=T, w=2 * F, prob=3 * F, mask=7 * F, valid=8 * F, coef=0.01, ent=0.0, loss=9 * F, count=10 * F,
+           mean=11 * F, dz=4 * F, dx=5 * F, dw=6 * F, ws=W, wsn=n):
         L.eat_balance_loss(h, x, T, w, prob, mask, valid, coef, ent, loss, count, mean, dz, dx, dw, ws, wsn, stream=0)
 
     for kw in (dict(h=None), dict(T=-1), dict(T=257), dict(prob=None), dict(mask=None), dict(loss=None),
                dict(coef=float("nan")), dict(ent=float("inf")), dict(x=None), dict(w=None), dict(x=F + 8),
                dict(w=F + 4), dict(prob=F + 2), dict(mask=F + 4), dict(loss=F + 2), dict(count=F + 4), dict(mean=F + 1),
-               dict(dz=F + 2), dict(dx=F + 8), dict(dw=F + 8), dict(ws=F + 64),
+               dict(dz=F + 2), dict(dx=F + 8), dict(dw=F + 8), dict(ws=W + 64),
                # overlaps (x and dx: 25600 bytes, w and dw: 30720, prob and dz: 24000)
                dict(dx=F), dict(dx=F + 16, dw=None), dict(dz=3 * F + 16), dict(dx=2 * F + 30704), dict(dw=2 * F), dict(dw=F),
-               dict(dw=5 * F + 16)):
+               dict(dw=5 * F + 16), dict(dz=F), dict(dz=5 * F + 25596), dict(dz=2 * F), dict(dz=6 * F), dict(dz=7 * F + 796),
+               dict(dz=8 * F + 96), dict(dx=3 * F), dict(dx=7 * F), dict(dx=8 * F), dict(dw=3 * F + 16), dict(loss=3 * F),
+               dict(loss=10 * F), dict(count=11 * F + 232), dict(mean=8 * F), dict(ws=F), dict(ws=4 * F), dict(ws=11 * F),
+               dict(prob=W), dict(valid=W + 5)):
         refused(bad, go, **kw)
     refused(L.EAT_ERR_WORKSPACE, go, ws=None)
     refused(L.EAT_ERR_WORKSPACE, go, wsn=n - 1)

@@ -285,11 +285,29 @@ def test_other_stream_and_graph_replays(T, E, d):
             assert torch.equal(out[k], ref[k]), (seed, k)
 
 
+def test_workspace_is_not_given_away_while_another_stream_uses_it():
+    layer, x, prob, mask = routed(60, 128, True, 700)
+    ref = call(layer, x, prob, mask, None)
+    side = torch.cuda.Stream()
+    at, size = layer._bws.buf.data_ptr(), layer._bws.buf.numel()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+        loss, count, mean = layer.balance_loss(x, prob, mask, None, 0.01, 0.002)
+    layer.close()
+    del layer
+    fill = [torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    assert all(f.data_ptr() != at for f in fill)
+    torch.cuda.synchronize()
+    assert torch.equal(loss, ref["loss"]) and torch.equal(count, ref["count"]) and torch.equal(mean, ref["mean"])
+
+
 def test_owner_refuses_what_it_would_misread():
     layer, x, prob, mask = routed(60, 128, True, 20)
     for kw in (dict(x=x.float()), dict(prob=prob.double()), dict(mask=mask.to(torch.int32)), dict(mask=mask[:19]),
                dict(valid=torch.ones(20, device="cuda")), dict(dlogits=torch.empty(20, 61, device="cuda")),
                dict(dw_router=torch.empty(60, 128, dtype=torch.bfloat16, device="cuda")),
-               dict(x=x[:, :64])):
+               dict(x=x[:, :64]), dict(x=x.cpu()), dict(mask=mask.cpu()), dict(valid=torch.ones(20, dtype=torch.bool)),
+               dict(dx=torch.empty(20, 128, dtype=torch.bfloat16))):
         with pytest.raises(ValueError):
             layer.balance_loss(**(dict(x=x, prob=prob, mask=mask) | kw))

@@ -386,6 +386,30 @@ def test_graph_outlives_its_workspace():
     assert all((f == 0xFF).all() for f in fill)
 
 
+def test_workspace_is_not_given_away_while_another_stream_uses_it():
+    """Made on one stream, used on another (the current one, or one given) that
+    is still busy when its owner goes: new tensors do not get its memory."""
+    h, w, y = make(500, 128, 3000)
+    ref = call(h, w, y, dw=False)
+    side = torch.cuda.Stream()
+    for given in (False, True, "address"):
+        ce, dh = CrossEntropy(w), torch.empty_like(h)
+        ce.loss(h, y, dh=dh)
+        at, size = ce._ws.buf.data_ptr(), ce._ws.buf.numel()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+            if not given:
+                loss = ce.loss(h, y, dh=dh)
+        if given:
+            loss = ce.loss(h, y, dh=dh, stream=side if given is True else side.cuda_stream)
+        del ce
+        fill = [torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        assert all(f.data_ptr() != at for f in fill)
+        torch.cuda.synchronize()
+        assert torch.equal(loss, ref["loss"]) and torch.equal(dh, ref["dh"])
+
+
 def test_the_nll_is_the_perplexity_signals():
     """eat_ppl_trend's NLL of the same rows: both are within the NLL's bound."""
     from paper_2609_33614_amd.layer import PplSignal
@@ -402,7 +426,8 @@ def test_owner_refuses_what_it_would_misread():
     ce = CrossEntropy(w)
     for kw in (dict(h=h.float()), dict(target=y.long()), dict(h=h[:, :64]), dict(target=y[:7]),
                dict(dh=torch.empty_like(h).float()), dict(dw=torch.empty(300, 64, dtype=torch.bfloat16, device="cuda")),
-               dict(h=h.t().contiguous().t()), dict(nll=torch.empty(7, device="cuda"))):
+               dict(h=h.t().contiguous().t()), dict(nll=torch.empty(7, device="cuda")), dict(target=y.cpu()), dict(h=h.cpu()),
+               dict(dw=torch.empty_like(w, device="cpu"))):
         args = dict(h=h, target=y) | kw
         with pytest.raises(ValueError):
             ce.loss(**args)
