@@ -33,29 +33,31 @@ class _Workspace:
     def __init__(self, device):
         self.device, self.buf, self.home, self.captured = device, None, 0, []
 
-    def get(self, need: int, stream=None) -> torch.Tensor:
-        now = torch.cuda.current_stream(self.device)
+    def get(self, need: int, stream) -> torch.Tensor:
+        """At least `need` bytes for a call on `stream`."""
         if self.buf is None or self.buf.numel() < need:
             self.buf = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
-            self.home = now.cuda_stream
+            self.home = torch.cuda.current_stream(self.device).cuda_stream
         if torch.cuda.is_current_stream_capturing():
             if not any(b is self.buf for b in self.captured):
                 self.captured.append(self.buf)
-        else:
-            used = now if stream is None else torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-            if used.cuda_stream != self.home:
-                self.buf.record_stream(used)
-        return self.buf[:need]
+        elif stream.cuda_stream != self.home:
+            self.buf.record_stream(stream)
+        return self.buf
+
+
+def _on_stream(stream, device):
+    """The stream of a call: the current one, one of torch's or an address."""
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    return torch.cuda.ExternalStream(stream, device) if isinstance(stream, int) else stream
 
 
 def _used_on(stream, *tensors) -> None:
     """Tell torch's allocator that ``stream`` uses tensors made on the current one."""
-    if stream is None:
-        return
-    used = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-    if used.cuda_stream != torch.cuda.current_stream().cuda_stream:
+    if stream.cuda_stream != torch.cuda.current_stream(stream.device).cuda_stream:
         for t in tensors:
-            t.record_stream(used)
+            t.record_stream(stream)
 
 
 def _on_device(device):
@@ -163,10 +165,13 @@ class EatLayer:
             loss = torch.empty(1, dtype=torch.float32, device=dev)
             count = torch.empty(E, dtype=torch.int64, device=dev)
             mean = torch.empty(E, dtype=torch.float32, device=dev)
-            ws = self._bws.get(L.eat_balance_workspace_size(self.handle, T), stream)
-            _used_on(stream, loss, count, mean)
+            on = _on_stream(stream, dev)
+            need = L.eat_balance_workspace_size(self.handle, T)
+            ws = self._bws.get(need, on)
+            if stream is not None:
+                _used_on(on, loss, count, mean)
             L.eat_balance_loss(self.handle, x, T, self.w["w_router"], prob, mask, valid, coef, entropy_coef, loss, count,
-                               mean, dlogits, dx, dw_router, ws, ws.numel(), stream)
+                               mean, dlogits, dx, dw_router, ws, need, on)
         return loss, count, mean
 
     def close(self) -> None:
@@ -223,11 +228,15 @@ class CrossEntropy:
         self.V, self.d = w_vocab.shape
         self._ws = _Workspace(w_vocab.device)
 
-    def workspace(self, T: int, grads: int, stream=None) -> torch.Tensor:
+    def _need(self, T: int, grads: int) -> int:
         need, least = L.eat_ce_workspace_size(T, self.d, self.V, grads)
-        if self.max_workspace is not None:
-            need = min(need, max(least, int(self.max_workspace)))
-        return self._ws.get(need, stream)     # (its size decides the pieces: it does not depend on earlier calls)
+        return need if self.max_workspace is None else min(need, max(least, int(self.max_workspace)))
+
+    def workspace(self, T: int, grads: int, stream=None) -> torch.Tensor:
+        """What a call of T positions gets (its size decides the pieces: it does
+        not depend on earlier calls)."""
+        need = self._need(T, grads)
+        return self._ws.get(need, _on_stream(stream, self.w.device))[:need]
 
     def loss(self, h: torch.Tensor, target: torch.Tensor, mean: bool = True, scale: float = 1.0,
              nll: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
@@ -242,10 +251,13 @@ class CrossEntropy:
         _expect("dw", dw, torch.bfloat16, (self.V, self.d), dev)
         with _on_device(dev):
             out = torch.empty(1, dtype=torch.float32, device=dev)
-            ws = self.workspace(T, (L.EAT_CE_DH if dh is not None else 0) | (L.EAT_CE_DW if dw is not None else 0), stream)
-            _used_on(stream, out)
+            on = _on_stream(stream, dev)
+            need = self._need(T, (L.EAT_CE_DH if dh is not None else 0) | (L.EAT_CE_DW if dw is not None else 0))
+            ws = self._ws.get(need, on)
+            if stream is not None:
+                _used_on(on, out)
             L.eat_ce_loss(h, T, self.d, self.w, self.V, target, self.ignore, int(mean), scale, out, nll, count, dh, dw, ws,
-                          ws.numel(), stream)
+                          need, on)
         return out
 
 
