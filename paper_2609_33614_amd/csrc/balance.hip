@@ -479,13 +479,13 @@ constexpr int kOneBlock = 16384;
 
 // Whether the products run on bf16 parts (more launches, faster products) or on
 // fp32 instructions, by measured times of whole calls (fp32 instructions |
-// parts, us).  bf16 tokens, dx on three products and dW_r on two:
+// parts, us).  bf16 tokens, three products of parts each for dx and dW_r:
 //   T 16384, E 8, d 64: 55 | 47;  E 64, d 512: 73 | 56;  E 256, d 128: 78 | 77
 //   T 8192, E 8, d 512: 39 | 42;  E 256, d 512: 93 | 67
 //   T 4096, E 64, d 512: 36 | 40;  d 2048: 59 | 44;  E 256, d 512: 61 | 60
 //   T 2048, E 64, d 2048: 38 | 40;  T 3000: 49 | 45
 //   T 1024, E 64, d 4096: 35 | 41;  T 512, E 256, d 4096: 50 | 59, d 8192: 89 | 65
-// fp32 tokens are three parts, so six products:
+// fp32 tokens are three parts, so six products for dx and nine for dW_r:
 //   T 2048, E 256, d 2048: 85 | 90;  d 4096: 152 | 120;  T 16384: 1056 | 741
 //   T 16384, E 64, d 4096: 310 | 350;  T 65536, E 8: 850 | 1263
 // (A row of x's parts is addressed with 24 bits.)
