@@ -105,9 +105,14 @@ __device__ __forceinline__ int swz_row(int r) { return (static_cast<unsigned>(r)
 // with 4 (k % 4) puts them on different banks.
 __device__ __forceinline__ int swz_col(int k) { return (k & 3) << 2; }
 
+// v in scalar registers, ready to be a load's address: a vector instruction's
+// write of one wants five wait states before a memory instruction reads it there,
+// which the compiler does not count for loads written in asm.
 __device__ __forceinline__ uint64_t uniform(uint64_t v) {
-    return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32)))) << 32 |
-           static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
+    v = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32)))) << 32 |
+        static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
+    asm volatile("s_nop 4" : "+s"(v));
+    return v;
 }
 
 // Loads of one operand's part of a chunk: where lane l of load j gets the 16
@@ -172,14 +177,15 @@ struct Operand {
     }
     // load j of the chunk (at: src, in scalar registers) into the part at LDS byte `lds` (+ 1024
     // wave); a load is waited for by count: the compiler adds no waits of its own for asm
+    // (nor the wait state between a write of M0 and the load that reads it: s_nop)
     __device__ __forceinline__ void load(uint32_t lds, uint64_t from, int j) const {
         const uint32_t o = off[j];
         if constexpr (GATHER) {
             const uint64_t p = from + static_cast<uint64_t>(at[j]) * ldbytes + o;
-            asm volatile("s_add_u32 m0, %1, %2\n\tglobal_load_lds_dwordx4 %0, off"
+            asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                          :: "v"(p), "s"(lds), "n"(1024 * WAVES * j) : "memory", "m0", "scc");
         } else {
-            asm volatile("s_add_u32 m0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %1"
+            asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                          :: "v"(o), "s"(from), "s"(lds), "n"(1024 * WAVES * j) : "memory", "m0", "scc");
         }
     }
