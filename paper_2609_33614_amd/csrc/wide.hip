@@ -186,7 +186,8 @@ __device__ __forceinline__ ItemLoads<C> item_loads(const WideArgs& a, const Item
 
 // Chunk c of an item into LDS stage st.  asm keeps the compiler from adding
 // waits of its own for these loads; the ring's waits and barriers order
-// them.  Weight blocks load non-temporally (NT) or at device scope (sc1: no
+// them (s_nop: the wait state between a write of M0 and the load that reads
+// it).  Weight blocks load non-temporally (NT) or at device scope (sc1: no
 // allocation in the CU's vector L1 -- a weight line is read once per
 // workgroup); token rows keep the default policy.
 template <class C, bool PACKED>
@@ -201,10 +202,10 @@ __device__ __forceinline__ void issue_weights(const ItemLoads<C>& L, uint8_t* st
         const uint32_t lds = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(
             reinterpret_cast<uintptr_t>(st + C::kRegion + 1024 * (wave + C::kWaves * j))));
         if constexpr (C::NT)
-            asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off nt"
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt"
                          :: "v"(src), "s"(lds) : "memory", "m0");
         else
-            asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off sc1"
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off sc1"
                          :: "v"(src), "s"(lds) : "memory", "m0");
     }
 }
@@ -220,7 +221,7 @@ __device__ __forceinline__ void issue_tokens(const ItemLoads<C>& L, uint8_t* st,
         const uint32_t lds = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(
             reinterpret_cast<uintptr_t>(st + 1024 * (wave + C::kWaves * j))));
         uint64_t save;
-        asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %3\n\ts_mov_b32 m0, %2\n\t"
+        asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 %0, exec\n\ts_mov_b64 exec, %3\n\t"
                      "global_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, %0"
                      : "=&s"(save) : "v"(src), "s"(lds), "s"(L.tmask[j]) : "memory", "m0");
     }

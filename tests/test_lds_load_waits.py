@@ -16,7 +16,7 @@ import pytest
 from paper_2609_33614_amd import build as B
 
 pytestmark = pytest.mark.skipif(not os.path.exists(B.HIPCC) or shutil.which("hipcc") is None, reason="hipcc missing")
-SOURCES = ["ce.hip", "balance.hip"]
+SOURCES = ["ce.hip", "balance.hip", "wide.hip"]
 
 
 def registers(operand):
@@ -86,6 +86,11 @@ def test_loads_to_lds_keep_their_waits(src, tmp_path):
     assert r.returncode == 0, r.stderr[-2000:]
     loads, bad = faults(open(out).read())
     assert loads > 50 and not bad, (loads, bad[:8])
+
+
+def test_every_source_with_such_asm_is_looked_at():
+    has = {f for f in os.listdir(B.CSRC) if "asm volatile" in (s := open(os.path.join(B.CSRC, f)).read()) and "load_lds" in s}
+    assert has == {"wide.hip", "loss_gemm.h"}            # (the header's kernels are in ce.hip and balance.hip)
 
 
 def test_the_check_sees_a_missing_wait():
