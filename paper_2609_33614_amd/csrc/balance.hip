@@ -37,9 +37,11 @@ constexpr int kStatThreads = kStatWaves * kWave;
 constexpr int kStatBlocks = 64;           // most shares of the tokens
 
 // dz of a row whose lanes (EP of them, E rounded up to a power of two up to 64)
-// hold experts e0 + 64 j: p (q - <q, p>), <q, p> in fp64.
+// hold experts e0 + 64 j: p (q - <q, p>), <q, p> in fp64.  Not `live` (or no
+// expert): 0, whatever q holds (a token that counts may have made it NaN).
 template <int J>
-__device__ __forceinline__ void score_grad(const float (&p)[J], const float (&q)[J], int ep, float (&dz)[J]) {
+__device__ __forceinline__ void score_grad(const float (&p)[J], const float (&q)[J], int ep, bool live, int e0, int E,
+                                           float (&dz)[J]) {
     double s = 0.0;
 #pragma unroll
     for (int j = 0; j < J; ++j) s += static_cast<double>(q[j]) * p[j];
@@ -47,7 +49,7 @@ __device__ __forceinline__ void score_grad(const float (&p)[J], const float (&q)
     else
         for (int o = ep / 2; o >= 1; o /= 2) s += __shfl_xor(s, o, kWave);
 #pragma unroll
-    for (int j = 0; j < J; ++j) dz[j] = p[j] * static_cast<float>(q[j] - s);
+    for (int j = 0; j < J; ++j) dz[j] = live && 64 * j + e0 < E ? p[j] * static_cast<float>(q[j] - s) : 0.f;
 }
 
 struct StatArgs {
@@ -192,21 +194,22 @@ __global__ __launch_bounds__(kStatThreads) void stat_kernel(StatArgs a) {
     for (int j = 0; j < J; ++j) q[j] = 64 * j + e0 < E ? qs[64 * j + e0] : 0.f;
     for (int t0 = wave * tpw * kStatRows; t0 < a.T; t0 += kStatWaves * tpw * kStatRows) {
         float p[kStatRows][J];
+        bool live[kStatRows];
 #pragma unroll
         for (int u = 0; u < kStatRows; ++u) {
             const int t = t0 + u * tpw + sub, ts = min(t, a.T - 1);
-            const bool live = t < a.T && (!a.valid || a.valid[ts]);
+            live[u] = t < a.T && (!a.valid || a.valid[ts]);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const float v = a.prob[static_cast<size_t>(ts) * E + min(64 * j + e0, E - 1)];
-                p[u][j] = live && 64 * j + e0 < E ? v : 0.f;
+                p[u][j] = live[u] && 64 * j + e0 < E ? v : 0.f;
             }
         }
 #pragma unroll
         for (int u = 0; u < kStatRows; ++u) {
             const int t = t0 + u * tpw + sub;
             float dz[J];
-            score_grad<J>(p[u], q, ep, dz);
+            score_grad<J>(p[u], q, ep, live[u], e0, E, dz);
 #pragma unroll
             for (int j = 0; j < J; ++j)
                 if (t < a.T && 64 * j + e0 < E) a.dz[static_cast<size_t>(t) * E + 64 * j + e0] = dz[j];
@@ -349,7 +352,7 @@ __global__ __launch_bounds__(kPrepThreads) void prep_kernel(PrepArgs a) {
         const float v = a.stat.prob[static_cast<size_t>(t) * E + min(64 * j + e0, E - 1)];
         p[j] = live && 64 * j + e0 < E ? v : 0.f;
     }
-    score_grad<J>(p, q, ep, dz);
+    score_grad<J>(p, q, ep, live, e0, E, dz);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int e = 64 * j + e0;
