@@ -411,7 +411,10 @@ eat_status_t eat_ce_loss(const void* h, int32_t T, int32_t d, const void* w_voca
  *
  * A uniform load gives coef + entropy_coef log(1/E).  A token that is not
  * valid has dz 0 and dx 0 and reaches nothing else, whatever its rows of x and
- * p hold.  A token that selected no expert counts in n and P alone. */
+ * p, the other tokens and W_r hold.  A token that selected no expert counts in n
+ * and P alone.  An x of a valid token or a W_r that is not finite (or, in fp32, is
+ * 2^128 - 2^119 or more, which bf16 has not) makes the dW_r or dx that it reaches
+ * infinite or NaN, which of the two depends on the call's size. */
 eat_status_t eat_balance_workspace_size(eat_handle_t h, int32_t T, size_t* bytes);
 
 /* One call for layer h (its E, d_model, act_dtype and inv_temperature).

@@ -401,10 +401,12 @@ struct ProductArgs {
     void* dx;
 };
 // out[r][c] = scale sum_k dz[r rs + k ks] v[k][c] over k in [kbeg, kend), those
-// whose valid[k] is 0 left out, for rows r0 .. r0 + 63 and columns c0 .. c0 + 63.
+// whose valid[k] is 0 left out, for rows r0 .. r0 + 63 and columns c0 .. c0 + 63;
+// 0 in rows whose live[r] is 0 (v may hold infinities).  valid, live: null, all.
 template <typename VT, typename OT>
 __device__ __forceinline__ void product_tile(const float* dz, int rs, int ks, const VT* v, const uint8_t* valid, int kbeg,
-                                             int kend, int rows, int r0, int d, int c0, float scale, OT* out) {
+                                             int kend, int rows, int r0, const uint8_t* live, int d, int c0, float scale,
+                                             OT* out) {
     const int lane = lane_id(), wave = threadIdx.x / kWave;
     const int l16 = lane & 15, lk = lane >> 4;
     r0 += 16 * wave;
@@ -436,12 +438,13 @@ __device__ __forceinline__ void product_tile(const float* dz, int rs, int ks, co
         }
     }
 #pragma unroll
-    for (int f = 0; f < 4; ++f)
+    for (int i = 0; i < 4; ++i) {
+        const int r = r0 + 4 * lk + i;
+        const bool on = !live || live[min(r, rows - 1)];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = r0 + 4 * lk + i;
-            if (r < rows) store_f32(out + static_cast<size_t>(r) * d + c0 + 16 * f + l16, acc[f][i] * scale);
-        }
+        for (int f = 0; f < 4; ++f)
+            if (r < rows) store_f32(out + static_cast<size_t>(r) * d + c0 + 16 * f + l16, on ? acc[f][i] * scale : 0.f);
+    }
 }
 
 template <typename XT>
@@ -454,10 +457,10 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
         const int per = ((a.T + a.splits - 1) / a.splits + 3) / 4 * 4;
         const int kbeg = min(a.T, sp * per), kend = min(a.T, kbeg + per);
         float* const out = a.splits == 1 ? a.dw : a.dwp + static_cast<size_t>(sp) * a.E * a.d;
-        product_tile(a.dz, 1, a.E, static_cast<const XT*>(a.x), a.valid, kbeg, kend, a.E, b % tiles * 64, a.d, c0,
+        product_tile(a.dz, 1, a.E, static_cast<const XT*>(a.x), a.valid, kbeg, kend, a.E, b % tiles * 64, nullptr, a.d, c0,
                      a.splits == 1 ? a.scale : 1.f, out);
     } else {
-        product_tile(a.dz, a.E, 1, a.w, nullptr, 0, a.E, a.T, b * 64, a.d, c0, a.scale, static_cast<XT*>(a.dx));
+        product_tile(a.dz, a.E, 1, a.w, nullptr, 0, a.E, a.T, b * 64, a.valid, a.d, c0, a.scale, static_cast<XT*>(a.dx));
     }
 }
 
