@@ -34,10 +34,10 @@ class _Workspace:
         self.device, self.buf, self.home, self.captured = device, None, 0, []
 
     def get(self, need: int, stream) -> torch.Tensor:
-        """At least `need` bytes for a call on `stream`."""
+        """At least `need` bytes for a call on `stream`, the current one."""
         if self.buf is None or self.buf.numel() < need:
             self.buf = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
-            self.home = torch.cuda.current_stream(self.device).cuda_stream
+            self.home = stream.cuda_stream
         if torch.cuda.is_current_stream_capturing():
             if not any(b is self.buf for b in self.captured):
                 self.captured.append(self.buf)
@@ -46,26 +46,26 @@ class _Workspace:
         return self.buf
 
 
-def _on_stream(stream, device):
-    """The stream of a call: the current one, one of torch's or an address."""
+def _calling_on(stream, device):
+    """The context of a call: its tensors' device and its stream (None: the
+    current one; one of torch's, or an address) are the current ones, so that
+    what it allocates is memory which that stream may use at once."""
     if stream is None:
-        return torch.cuda.current_stream(device)
-    return torch.cuda.ExternalStream(stream, device) if isinstance(stream, int) else stream
+        # (the library launches on the current device)
+        index = device.index
+        return contextlib.nullcontext() if index is None or index == torch.cuda.current_device() else torch.cuda.device(index)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device)
+    if stream.device != device:
+        raise ValueError(f"stream: on {stream.device}, the call's tensors on {device}")
+    return torch.cuda.stream(stream)
 
 
-def _used_on(stream, *tensors) -> None:
-    """Tell torch's allocator that ``stream`` uses tensors made on the current one."""
-    if stream.cuda_stream != torch.cuda.current_stream(stream.device).cuda_stream:
+def _hand_out(stream, caller, *tensors) -> None:
+    """Tell torch's allocator that the caller's stream uses what a call on `stream` made."""
+    if stream is not None:
         for t in tensors:
-            t.record_stream(stream)
-
-
-def _on_device(device):
-    """The library launches on the current device: make it the tensors'."""
-    index = device.index
-    if index is None or index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(index)
+            t.record_stream(caller)
 
 
 class EatLayer:
@@ -148,7 +148,9 @@ class EatLayer:
         ``mask`` that ``route`` returned for ``x``: (loss [1], selections per
         expert [E] int64, mean probabilities [E]).  The gradients are written
         to the tensors given.  ``valid`` [T] (bool or uint8): tokens that count.
-        Calls of one layer share a workspace: order them on one stream."""
+        Calls of one layer share a workspace: order them on one stream.
+        ``stream``: what the call is enqueued on (the current one); the tensors
+        given have to be ready there, and what is returned is ready when it is."""
         T, E, d = prob.shape[0], self.params.E, self.params.d_model
         act = torch.bfloat16 if self.params.act_dtype == L.EAT_BF16 else torch.float32
         W = L.mask_words(E)
@@ -161,17 +163,17 @@ class EatLayer:
         _expect("dlogits", dlogits, torch.float32, (T, E), dev)
         _expect("dx", dx, act, (T, d), dev)
         _expect("dw_router", dw_router, torch.float32, (E, d), dev)
-        with _on_device(dev):
+        caller = torch.cuda.current_stream(dev) if stream is not None else None
+        with _calling_on(stream, dev):
             loss = torch.empty(1, dtype=torch.float32, device=dev)
             count = torch.empty(E, dtype=torch.int64, device=dev)
             mean = torch.empty(E, dtype=torch.float32, device=dev)
-            on = _on_stream(stream, dev)
             need = L.eat_balance_workspace_size(self.handle, T)
+            on = torch.cuda.current_stream(dev)
             ws = self._bws.get(need, on)
-            if stream is not None:
-                _used_on(on, loss, count, mean)
             L.eat_balance_loss(self.handle, x, T, self.w["w_router"], prob, mask, valid, coef, entropy_coef, loss, count,
                                mean, dlogits, dx, dw_router, ws, need, on)
+        _hand_out(stream, caller, loss, count, mean)
         return loss, count, mean
 
     def close(self) -> None:
@@ -218,7 +220,8 @@ class CrossEntropy:
     head are written to the tensors given.  ``max_workspace``: bytes of
     workspace to stay under where a call can (the vocabulary is then taken in
     smaller pieces).  Calls of one object share its workspace: order them on
-    one stream."""
+    one stream.  ``stream``: what a call is enqueued on (the current one); the
+    tensors given have to be ready there, and what is returned is ready when it is."""
 
     def __init__(self, w_vocab: torch.Tensor, ignore: int = -100, max_workspace: Optional[int] = None):
         if w_vocab.dim() != 2:
@@ -236,7 +239,8 @@ class CrossEntropy:
         """What a call of T positions gets (its size decides the pieces: it does
         not depend on earlier calls)."""
         need = self._need(T, grads)
-        return self._ws.get(need, _on_stream(stream, self.w.device))[:need]
+        with _calling_on(stream, self.w.device):
+            return self._ws.get(need, torch.cuda.current_stream(self.w.device))[:need]
 
     def loss(self, h: torch.Tensor, target: torch.Tensor, mean: bool = True, scale: float = 1.0,
              nll: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
@@ -249,15 +253,15 @@ class CrossEntropy:
         _expect("count", count, torch.int32, (1,), dev)
         _expect("dh", dh, torch.bfloat16, (T, self.d), dev)
         _expect("dw", dw, torch.bfloat16, (self.V, self.d), dev)
-        with _on_device(dev):
+        caller = torch.cuda.current_stream(dev) if stream is not None else None
+        with _calling_on(stream, dev):
             out = torch.empty(1, dtype=torch.float32, device=dev)
-            on = _on_stream(stream, dev)
             need = self._need(T, (L.EAT_CE_DH if dh is not None else 0) | (L.EAT_CE_DW if dw is not None else 0))
+            on = torch.cuda.current_stream(dev)
             ws = self._ws.get(need, on)
-            if stream is not None:
-                _used_on(on, out)
             L.eat_ce_loss(h, T, self.d, self.w, self.V, target, self.ignore, int(mean), scale, out, nll, count, dh, dw, ws,
                           need, on)
+        _hand_out(stream, caller, out)
         return out
 
 
