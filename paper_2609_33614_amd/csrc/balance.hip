@@ -289,8 +289,11 @@ struct PrepArgs {
     int segs, map;             // part of w in each
     const float* x;            // fp32 x to split
     uint16_t* xs;              // [list row][3][d], or null
-    int blocks_z, blocks_w;    // workgroups of each kind of work
+    int blocks_z, blocks_w, blocks_x;      // workgroups of each kind of work
 };
+// A grid has fewer than 2^32 threads: 256 of them in each of this many
+// workgroups at most, which go on to the next piece of work beyond.
+constexpr int kMostBlocks = 1 << 22;
 
 constexpr int kPrepWaves = 4;
 constexpr int kPrepThreads = kPrepWaves * kWave;
@@ -301,20 +304,20 @@ __global__ __launch_bounds__(kPrepThreads) void prep_kernel(PrepArgs a) {
     const int block = blockIdx.x;
     const int n = a.rows ? a.stat.head[0] : T, padded = (n + kBK - 1) / kBK * kBK;
     if (block >= a.blocks_z + a.blocks_w) {               // x: a list row per workgroup
-        const int i = block - a.blocks_z - a.blocks_w;
-        if (i >= padded) return;
-        const bool live = i < n;
-        const int t = live && a.rows ? a.rows[i] : i;
-        for (int c = 4 * threadIdx.x; c < a.d; c += 4 * kPrepThreads) {
-            f32x4 v{};
-            if (live) v = *reinterpret_cast<const f32x4*>(a.x + static_cast<size_t>(t) * a.d + c);
-            uint16_t p[4][3];
+        for (int i = block - a.blocks_z - a.blocks_w; i < padded; i += a.blocks_x) {
+            const bool live = i < n;
+            const int t = live && a.rows ? a.rows[i] : i;
+            for (int c = 4 * threadIdx.x; c < a.d; c += 4 * kPrepThreads) {
+                f32x4 v{};
+                if (live) v = *reinterpret_cast<const f32x4*>(a.x + static_cast<size_t>(t) * a.d + c);
+                uint16_t p[4][3];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) split3(v[e], p[e]);
+                for (int e = 0; e < 4; ++e) split3(v[e], p[e]);
 #pragma unroll
-            for (int k = 0; k < 3; ++k)
-                *reinterpret_cast<uint2*>(a.xs + (static_cast<size_t>(i) * 3 + k) * a.d + c) =
-                    uint2{p[0][k] | static_cast<uint32_t>(p[1][k]) << 16, p[2][k] | static_cast<uint32_t>(p[3][k]) << 16};
+                for (int k = 0; k < 3; ++k)
+                    *reinterpret_cast<uint2*>(a.xs + (static_cast<size_t>(i) * 3 + k) * a.d + c) =
+                        uint2{p[0][k] | static_cast<uint32_t>(p[1][k]) << 16, p[2][k] | static_cast<uint32_t>(p[3][k]) << 16};
+            }
         }
         return;
     }
@@ -394,7 +397,8 @@ struct ProductArgs {
     const void* x;
     const float* w;
     const uint8_t* valid;
-    int T, E, d, splits, blocks_w;
+    int T, E, d, splits;
+    int64_t blocks_w, blocks_x;
     float scale;
     float* dw;                 // dW_r where splits is 1
     float* dwp;                // else its slices [splits][E][d], unscaled
@@ -449,18 +453,21 @@ __device__ __forceinline__ void product_tile(const float* dz, int rs, int ks, co
 
 template <typename XT>
 __global__ __launch_bounds__(256) void product_kernel(ProductArgs a) {
-    const bool dw = static_cast<int>(blockIdx.x) < a.blocks_w;
-    const int block = dw ? blockIdx.x : blockIdx.x - a.blocks_w, cols = a.d / 64;
-    const int c0 = block % cols * 64, b = block / cols;
-    if (dw) {
-        const int tiles = (a.E + 63) / 64, sp = b / tiles;
-        const int per = ((a.T + a.splits - 1) / a.splits + 3) / 4 * 4;
-        const int kbeg = min(a.T, sp * per), kend = min(a.T, kbeg + per);
-        float* const out = a.splits == 1 ? a.dw : a.dwp + static_cast<size_t>(sp) * a.E * a.d;
-        product_tile(a.dz, 1, a.E, static_cast<const XT*>(a.x), a.valid, kbeg, kend, a.E, b % tiles * 64, nullptr, a.d, c0,
-                     a.splits == 1 ? a.scale : 1.f, out);
-    } else {
-        product_tile(a.dz, a.E, 1, a.w, nullptr, 0, a.E, a.T, b * 64, a.valid, a.d, c0, a.scale, static_cast<XT*>(a.dx));
+    const int cols = a.d / 64;
+    for (int64_t at = blockIdx.x; at < a.blocks_w + a.blocks_x; at += gridDim.x) {
+        const bool dw = at < a.blocks_w;
+        const int block = static_cast<int>(dw ? at : at - a.blocks_w);
+        const int c0 = block % cols * 64, b = block / cols;
+        if (dw) {
+            const int tiles = (a.E + 63) / 64, sp = b / tiles;
+            const int per = ((a.T + a.splits - 1) / a.splits + 3) / 4 * 4;
+            const int kbeg = min(a.T, sp * per), kend = min(a.T, kbeg + per);
+            float* const out = a.splits == 1 ? a.dw : a.dwp + static_cast<size_t>(sp) * a.E * a.d;
+            product_tile(a.dz, 1, a.E, static_cast<const XT*>(a.x), a.valid, kbeg, kend, a.E, b % tiles * 64, nullptr, a.d, c0,
+                         a.splits == 1 ? a.scale : 1.f, out);
+        } else {
+            product_tile(a.dz, a.E, 1, a.w, nullptr, 0, a.E, a.T, b * 64, a.valid, a.d, c0, a.scale, static_cast<XT*>(a.dx));
+        }
     }
 }
 
@@ -517,10 +524,9 @@ hipError_t launch_products(const eat_params_t& p, const BalancePlan& b, const Ba
     const int E = p.E, d = p.d_model;
     const int64_t bw = c.dw ? int64_t{(E + 63) / 64} * (d / 64) * b.splits : 0;
     const int64_t bx = c.dx ? int64_t{(c.T + 63) / 64} * (d / 64) : 0;
-    if (bw + bx > INT32_MAX) return hipErrorInvalidConfiguration;
-    const ProductArgs a{dz, c.x, c.w_router, c.valid, c.T, E, d, b.splits, static_cast<int>(bw), p.inv_temperature, c.dw,
-                        dwp, c.dx};
-    if (bw + bx > 0) product_kernel<XT><<<static_cast<int>(bw + bx), 256, 0, s>>>(a);
+    if (bw > INT32_MAX || bx > INT32_MAX) return hipErrorInvalidConfiguration;
+    const ProductArgs a{dz, c.x, c.w_router, c.valid, c.T, E, d, b.splits, bw, bx, p.inv_temperature, c.dw, dwp, c.dx};
+    if (bw + bx > 0) product_kernel<XT><<<static_cast<int>(std::min<int64_t>(bw + bx, kMostBlocks)), 256, 0, s>>>(a);
     if (c.dw && b.splits > 1)
         dw_join_kernel<<<static_cast<int>((static_cast<int64_t>(E) * d / 4 + 255) / 256), 256, 0, s>>>(
             dwp, b.splits, 1, E, d, p.inv_temperature, c.dw);
@@ -647,7 +653,8 @@ hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const Bal
         if (c.dw && !bf16) {
             r.x = static_cast<const float*>(c.x);
             r.xs = reinterpret_cast<uint16_t*>(ws + b.xs);
-            blocks += places;
+            r.blocks_x = std::min(places, kMostBlocks);
+            blocks += r.blocks_x;
         }
     }
     const PrepArgs* const rp = (dz && !fused) || split ? &r : nullptr;
