@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(const float2* __
             v = lse - z;
         }
         if (y < 0) v = lse = NAN;
-        stats[i] = float2{static_cast<float>(lse * 1.4426950408889634), static_cast<float>(expm1(-v))};
+        stats[i] = float2{static_cast<float>(lse), static_cast<float>(expm1(-v))};
         if (nll) nll[rows[i]] = static_cast<float>(v);
         if (blocks > 1) __hip_atomic_store(nllc + i, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __re
         if (i < n) {
             const float2 st = stats[i];
             const float m = part[static_cast<size_t>(blockIdx.x) * ldpart + i].x;
-            v = float4{m == -INFINITY ? 0.f * st.x : __builtin_amdgcn_exp2f(fmaf(tile_ref(m), kLog2e, -st.x)), st.y,
+            v = float4{m == -INFINITY ? 0.f * st.x : exp_from(tile_ref(m), st.x), st.y,
                        __int_as_float(tc[i] - c0), 0.f};
         }
         row[tid] = v;

@@ -90,7 +90,7 @@ struct GemmArgs {
     float2* part;              // LSE: [column tile][ldpart] (maximum, sum) pairs
     int ldpart;
     const int32_t* target;     // LSE, GRAD: column that is the row's target
-    const float2* stats;       // GRAD: (lse log2 e, G at the target) of a row
+    const float2* stats;       // GRAD: (lse, G at the target) of a row
 };
 
 // (uniform: what depends on it branches on scalars)
@@ -240,6 +240,9 @@ __device__ inline int pick_slices(int items, int chunks, int rows, int cols, int
 // The reference of a row's exponentials over a tile with maximum m (infinite
 // where all are -inf, whose sum is 0, or some +inf: then 0).
 __device__ __forceinline__ float tile_ref(float m) { return fabsf(m) == INFINITY ? 0.f : m; }
+// exp(z - ref).  The difference comes first: either of them times log2 e may be
+// past fp32's range.
+__device__ __forceinline__ float exp_from(float z, float ref) { return __builtin_amdgcn_exp2f((z - ref) * kLog2e); }
 
 // What the rounding of v to bf16 leaves.
 __device__ __forceinline__ float bf16_rest(float v) { return v - __uint_as_float(pack_bf16x2(v, 0.f) << 16); }
@@ -595,7 +598,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                 for (int i = 0; i < FA; ++i)
 #pragma unroll
                     for (int q = 0; q < 16; ++q) {
-                        acc[i][j][q] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], kLog2e, -ref * kLog2e));
+                        acc[i][j][q] = exp_from(acc[i][j][q], ref);
                         s += acc[i][j][q];
                     }
                 s += swap_halves(s);
@@ -636,7 +639,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                     const int end = live ? g.na - (cur.a0 + arow + 4 * lh) : 0;     // columns of the piece from here on
                     auto grad = [&](int i, int q) __attribute__((always_inline)) {
                         const int v = 32 * i + 8 * (q / 4) + q % 4;
-                        float p = __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], kLog2e, -st.x));
+                        float p = exp_from(acc[i][j][q], st.x);
                         p = v == rel ? st.y : p;
                         return v < end ? p : 0.f;
                     };
