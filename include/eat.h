@@ -352,7 +352,7 @@ eat_status_t eat_ppl_trend(const void* h, int32_t S, int32_t d, const void* w_vo
  *   nll_t = log(1 + sum_{v != y} exp(z_tv - z_ty)),  y = target_t
  *   loss  = c sum_t nll_t                    (0 when no position counts)
  *   G_tv  = softmax(z_t)_v - [v = y]         (0 where t does not count; in
- *           bf16, for up to 64 positions as the sum of two bf16 numbers)
+ *           bf16, where n <= 64 as the sum of two bf16 numbers)
  *   dh_t  = c sum_v G_tv W_V[v]     dW_V[v] = c sum_t G_tv h_t
  *
  * A position that does not count has nll 0 and dh 0 and reaches nothing else,

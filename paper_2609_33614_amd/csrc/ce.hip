@@ -22,7 +22,10 @@
 // G in bf16 is off by up to 2^-8 of each entry, and that of the first piece by twice
 // that (the exponential's rounding and its own).  Over many rows such errors average
 // out against the rounding of the bf16 results; over few they do not (dW of one row
-// is its G times a number), so up to 64 rows have G in two bf16 parts.
+// is its G times a number), so up to kFewRows rows that count have G in two bf16
+// parts, and their hidden rows twice: known on the host in calls of so few, else on
+// the device, where the parts are further rows of the products (dh of 200 positions,
+// d 4096, V 32000: 77 of them count, 136 us; 64 in two parts, 147, in one, 136).
 //
 // Bounds, measured: three products of 2 n d V operations each (1.22 - 1.29 PFLOP/s
 // of 1.25 - 1.4 that a library product reaches: 4096 rows, d 4096, V 32000 take
@@ -33,6 +36,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "loss_gemm.h"
 
@@ -42,16 +46,15 @@ namespace {
 // One wave per row.  Row t of the call, where it is ignored: its NLL and its
 // dh are zero.  Row i of the list: its hidden row, its target and the target's
 // logit in fp64 (the NLL would depend most on that logit's rounding); rows
-// behind the list up to whole tiles: zeros (and all again `again` rows on, if it is
-// not 0).  LIST (calls of up to kListedRows
+// behind the list up to whole tiles: zeros.  Of up to kFewRows listed rows all is
+// there again, kFewRows rows on.  LIST (calls of up to kListedRows
 // rows): every workgroup works the list out for itself, a lane per row, instead of a
 // launch before this one (~5 us).
 constexpr int kGatherWaves = 4, kListedRows = kGatherWaves * kWave;
 template <bool LIST>
 __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
     const uint16_t* __restrict__ h, const uint16_t* __restrict__ w, const int32_t* __restrict__ target, int T, int Tpad,
-    int d, int V, int ignore, int32_t* rows, int32_t* head, uint16_t* hc, int again,
-    int32_t* tc, double* zt, float* nll, uint16_t* dh) {
+    int d, int V, int ignore, int32_t* rows, int32_t* head, uint16_t* hc, int32_t* tc, double* zt, float* nll, uint16_t* dh) {
     __shared__ uint64_t keep[kGatherWaves];
     const int lane = lane_id(), i = blockIdx.x * kGatherWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     int n, t = 0;
@@ -80,7 +83,8 @@ __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
             for (int k = 8 * lane; k < d; k += 8 * kWave)
                 *reinterpret_cast<uint4*>(dh + static_cast<size_t>(i) * d + k) = uint4{};
     }
-    if (i >= Tpad || i >= (n + 255) / 256 * 256) return;
+    const bool again = n <= kFewRows;
+    if (i >= Tpad || i >= (n + 255) / 256 * 256 || (again && i >= kFewRows && i < 2 * kFewRows)) return;
     const int y = i < n ? target[t] : 0;
     const bool known = y >= 0 && y < V;
     double z = 0.0;
@@ -99,7 +103,7 @@ __global__ __launch_bounds__(kGatherWaves * kWave) void gather_kernel(
             if (k >= d) break;
             const uint4 row = i < n ? p[u] : uint4{};
             *reinterpret_cast<uint4*>(hc + static_cast<size_t>(i) * d + k) = row;
-            if (again) *reinterpret_cast<uint4*>(hc + static_cast<size_t>(i + again) * d + k) = row;
+            if (again && i < kFewRows) *reinterpret_cast<uint4*>(hc + static_cast<size_t>(i + kFewRows) * d + k) = row;
             const uint32_t pw[4] = {p[u].x, p[u].y, p[u].z, p[u].w}, qw[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -198,10 +202,10 @@ __global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(const float2* __
 // G of the columns whose exponentials the first pass kept, in place: a tile of
 // the first pass x 64 rows per workgroup, 16 bytes per lane.  Twice the piece's
 // bytes against taking its product again (4096 rows of 32000 columns, d 4096:
-// see launch_ce).  Rows behind the list up to a whole reduction chunk: zeros.  PARTS:
-// in two bf16 parts (the second plane 64 rows on).
+// see launch_ce).  Rows behind the list up to a whole reduction chunk: zeros.  Up
+// to kFewRows rows: in two bf16 parts (the second kFewRows rows on).
 constexpr int kScaleThreads = 256, kScaleRows = 64;
-template <int NA, bool PARTS>
+template <int NA>
 __global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __restrict__ part, int ldpart,
                                                               const float2* __restrict__ stats,
                                                               const int32_t* __restrict__ tc,
@@ -225,48 +229,61 @@ __global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __re
     }
     uint16_t* const at = g + (r0 + tid / V) * ldg + c0 + 8 * (tid % V);
     constexpr int K = kScaleRows / R;
-    uint4 v[K], v2[PARTS ? K : 1];
+    auto scale = [&](auto two) __attribute__((always_inline)) {
+        constexpr bool PARTS = decltype(two)::value;
+        constexpr int N = PARTS ? K / 2 : K;               // loads of a plane in flight
+        uint4 v[N], v2[PARTS ? N : 1];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        v[k] = *reinterpret_cast<const uint4*>(at + k * R * ldg);
-        if constexpr (PARTS) v2[k] = *reinterpret_cast<const uint4*>(at + (64 + k * R) * ldg);
-    }
-    __syncthreads();
+        for (int k0 = 0; k0 < K; k0 += N) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int r = tid / V + k * R;
-        const float4 p = row[r];
-        const int rel = __float_as_int(p.z) - 8 * (tid % V);
-        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-        uint32_t w2[4] = {}, o[4], o2[4];
-        if constexpr (PARTS) { w2[0] = v2[k].x; w2[1] = v2[k].y; w2[2] = v2[k].z; w2[3] = v2[k].w; }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xffff0000u);
-            if constexpr (PARTS) {
-                lo += __uint_as_float(w2[e] << 16);
-                hi += __uint_as_float(w2[e] & 0xffff0000u);
+            for (int k = 0; k < N; ++k) {
+                v[k] = *reinterpret_cast<const uint4*>(at + (k0 + k) * R * ldg);
+                if constexpr (PARTS) v2[k] = *reinterpret_cast<const uint4*>(at + (kFewRows + (k0 + k) * R) * ldg);
             }
-            lo = rel == 2 * e ? p.y : lo * p.x;
-            hi = rel == 2 * e + 1 ? p.y : hi * p.x;
-            if (r0 + r >= n) lo = hi = 0.f;
-            o[e] = pack_bf16x2(lo, hi);
-            if constexpr (PARTS) o2[e] = pack_bf16x2(bf16_rest(lo), bf16_rest(hi));
+            if (k0 == 0) __syncthreads();
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int r = tid / V + (k0 + k) * R;
+                const float4 p = row[r];
+                const int rel = __float_as_int(p.z) - 8 * (tid % V);
+                const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+                uint32_t w2[4] = {}, o[4], o2[4];
+                if constexpr (PARTS) { w2[0] = v2[k].x; w2[1] = v2[k].y; w2[2] = v2[k].z; w2[3] = v2[k].w; }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xffff0000u);
+                    if constexpr (PARTS) {
+                        lo += __uint_as_float(w2[e] << 16);
+                        hi += __uint_as_float(w2[e] & 0xffff0000u);
+                    }
+                    lo = rel == 2 * e ? p.y : lo * p.x;
+                    hi = rel == 2 * e + 1 ? p.y : hi * p.x;
+                    if (r0 + r >= n) lo = hi = 0.f;
+                    o[e] = pack_bf16x2(lo, hi);
+                    if constexpr (PARTS) o2[e] = pack_bf16x2(bf16_rest(lo), bf16_rest(hi));
+                }
+                uint16_t* const to = at + (k0 + k) * R * ldg;
+                *reinterpret_cast<uint4*>(to) = uint4{o[0], o[1], o[2], o[3]};
+                if constexpr (PARTS) *reinterpret_cast<uint4*>(to + kFewRows * ldg) = uint4{o2[0], o2[1], o2[2], o2[3]};
+            }
         }
-        *reinterpret_cast<uint4*>(at + k * R * ldg) = uint4{o[0], o[1], o[2], o[3]};
-        if constexpr (PARTS) *reinterpret_cast<uint4*>(at + (64 + k * R) * ldg) = uint4{o2[0], o2[1], o2[2], o2[3]};
-    }
+    };
+    static_assert(kScaleRows == kFewRows, "one workgroup has all rows of both parts");
+    if (n <= kFewRows) scale(std::true_type{});
+    else scale(std::false_type{});
 }
 
 // dh of the listed rows: its slices (head[3] of them) added in order, times c.
+// planes: up to kFewRows rows come in two parts, the second kFewRows rows on.
 constexpr int kJoinThreads = 256;
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int tile_rows, int direct,
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restrict__ part, int tile_rows, int direct, int planes,
                                                             const int32_t* __restrict__ head,
                                                             const int32_t* __restrict__ rows, int d,
                                                             const float* __restrict__ coef, uint16_t* dh) {
     const int n = head[0], splits = head[3];
-    if (splits == 1 && direct) return;                     // (written as it was finished)
-    const int64_t stride = static_cast<int64_t>((n + tile_rows - 1) / tile_rows) * tile_rows * d;
+    const bool two = planes && n <= kFewRows;
+    if (splits == 1 && direct && !two) return;             // (written as it was finished)
+    const int64_t stride = static_cast<int64_t>(((two ? with_parts(n) : n) + tile_rows - 1) / tile_rows) * tile_rows * d;
     const float c = *coef;
     const int64_t total = static_cast<int64_t>(n) * (d / 8);
     for (int64_t at = blockIdx.x * int64_t(kJoinThreads) + threadIdx.x; at < total; at += int64_t(gridDim.x) * kJoinThreads) {
@@ -276,6 +293,13 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const float* __restr
         for (int s = 1; s < splits; ++s) {
             lo += *reinterpret_cast<const f32x4*>(p + s * stride);
             hi += *reinterpret_cast<const f32x4*>(p + s * stride + 4);
+        }
+        if (two) {
+            p += static_cast<size_t>(kFewRows) * d;
+            for (int s = 0; s < splits; ++s) {
+                lo += *reinterpret_cast<const f32x4*>(p + s * stride);
+                hi += *reinterpret_cast<const f32x4*>(p + s * stride + 4);
+            }
         }
         *reinterpret_cast<uint4*>(dh + static_cast<size_t>(rows[i]) * d + k) =
             uint4{pack_bf16x2(lo[0] * c, lo[1] * c), pack_bf16x2(lo[2] * c, lo[3] * c),
@@ -383,16 +407,17 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
     float* const dhp = reinterpret_cast<float*>(ws + p.dhp);
     const int T = c.T, d = c.d, V = c.V;
     const Size zz = pick_tile(T, V), zh = dh_tile(T, d, (std::min(p.piece, V) + kBK - 1) / kBK);
-    const int again = zz == kSmall ? Small::NB : 0;
+    static_assert(Small::NB == kFewRows, "calls of few rows have one tile of them");
+    const int planes = zz == kSmall ? 0 : 1;               // (kSmall: both parts are tiles of their own or folded)
 
     const int rb = (p.rows_pad + kGatherWaves - 1) / kGatherWaves;
     if (T <= kListedRows) {
         gather_kernel<true><<<rb, kGatherWaves * kWave, 0, s>>>(c.h, c.w, c.target, T, p.rows_pad, d, V, c.ignore, rows,
-                                                                head, hc, again, tc, zt, c.nll, c.dh);
+                                                                head, hc, tc, zt, c.nll, c.dh);
     } else {
         list_kernel<int32_t><<<1, kListThreads, 0, s>>>(c.target, T, c.ignore, rows, head);
         gather_kernel<false><<<rb, kGatherWaves * kWave, 0, s>>>(c.h, c.w, c.target, T, p.rows_pad, d, V, c.ignore, rows,
-                                                                 head, hc, again, tc, zt, c.nll, c.dh);
+                                                                 head, hc, tc, zt, c.nll, c.dh);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -413,9 +438,8 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
         const uint16_t* w = c.w + static_cast<size_t>(v0) * d;
         if (v0 == 0) {
             const dim3 grid((nv + p.tile - 1) / p.tile, p.rows_pad / kScaleRows);
-            if (zz == kSmall) scale_kernel<Small::NA, true><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
-            else if (zz == kMid) scale_kernel<Mid::NA, false><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
-            else scale_kernel<Big::NA, false><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
+            if (zz == kBig) scale_kernel<Big::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
+            else scale_kernel<Mid::NA><<<grid, kScaleThreads, 0, s>>>(part, p.rows_pad, stats, tc, head, gbuf, p.piece);
             e = hipGetLastError();
         } else {
             GemmArgs q = z;
@@ -426,8 +450,8 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
         if (e == hipSuccess && c.dh) {
             GemmArgs a{};
             a.a = w; a.lda = d; a.na = d; a.a_rows = nv;
-            a.b = gbuf; a.ldb = p.piece; a.nb = T; a.nb_dev = head;
-            a.K = nv; a.splits = 0;
+            a.b = gbuf; a.ldb = p.piece; a.nb = planes ? std::max(T, 2 * kFewRows) : T; a.nb_dev = head;
+            a.planes = planes; a.K = nv; a.splits = 0;
             a.pool_rows = p.pool_rows; a.slice_chunks = std::min(p.piece, V + kBK - 1) / kBK; a.slices_out = head + 3;
             a.direct = p.piece < V ? nullptr : c.dh;
             a.out = dhp; a.ldo = d; a.add = v0 > 0; a.rows = rows; a.coef = coef;
@@ -440,7 +464,7 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
             a.a = hc; a.lda = d; a.na = d; a.a_rows = 1 << 30;
             a.b = gbuf; a.ldb = p.piece; a.nb = nv;
             a.k_times = zz == kSmall ? 2 : 1;              // (both planes of G, over both copies of h)
-            a.K = p.rows_pad * a.k_times; a.k_dev = head + 1; a.splits = 1;
+            a.K = p.rows_pad * a.k_times; a.k_dev = head + 1; a.splits = 1; a.planes = planes;
             a.out = c.dw + static_cast<size_t>(v0) * d; a.ldo = d; a.coef = coef;
             e = launch_sized<true, true, ROWS>(pick_tile(nv, d), a, s);
         }
@@ -449,7 +473,7 @@ hipError_t launch_ce(const CePlan& p, const CeCall& c, char* ws, hipStream_t s) 
         const int64_t n8 = static_cast<int64_t>(T) * (d / 8);
         if (n8 > 0)
             join_kernel<<<static_cast<int>(std::min<int64_t>((n8 + kJoinThreads - 1) / kJoinThreads, 2048)), kJoinThreads, 0, s>>>(
-                dhp, zh == kSmall ? Small::NB : zh == kMid ? Mid::NB : Big::NB, p.piece < V ? 0 : 1, head, rows, d, coef, c.dh);
+                dhp, zh == kSmall ? Small::NB : zh == kMid ? Mid::NB : Big::NB, p.piece < V ? 0 : 1, planes, head, rows, d, coef, c.dh);
         e = hipGetLastError();
     }
     return e;

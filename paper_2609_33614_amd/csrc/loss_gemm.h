@@ -70,6 +70,7 @@ struct GemmArgs {
     const int32_t* nb_dev;     // rows of the output, on the device (or null)
     const int32_t* k_dev;      // reduction length, on the device (or null), over k_times
     int k_times;
+    int planes;                // 1: up to kFewRows of nb_dev's rows, or of k_dev's, have second parts, kFewRows on, that count too
     int a_rows;                // stored rows of a "columns" A operand (later ones read the last)
     const int32_t* k_rows;     // GATHER: the stored row of A of each reduction element (whole chunks of them)
     int segs, map;             // GROUPS, B by rows: see loss_gemm
@@ -92,6 +93,12 @@ struct GemmArgs {
     const int32_t* target;     // LSE, GRAD: column that is the row's target
     const float2* stats;       // GRAD: (lse, G at the target) of a row
 };
+
+// The cross entropy keeps its G in two bf16 parts up to this many rows that count.
+constexpr int kFewRows = 64;
+// Rows there are when the second parts of so few follow as rows of their own.
+__device__ __forceinline__ int with_parts(int n) { return n > 0 && n <= kFewRows ? kFewRows + n : n; }
+
 
 // (uniform: what depends on it branches on scalars)
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave); }
@@ -268,10 +275,9 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
     constexpr int FA = C::FA, FB = kFolds ? 1 : C::FB;         // fragments of B held, and read
     constexpr int FL = kGroupTile ? 3 : FOLD == PLANES ? 2 : C::FB;
     constexpr int NBO = kFolds ? 64 : C::NB;                   // output rows per tile
-    constexpr bool kParts = C::NB == 64;                       // LSE, GRAD: out in two parts, PLANES of 64 rows
     __shared__ __attribute__((aligned(1024))) uint8_t ring[C::SLOTS * C::kSlot];
-    const int nb = g.nb_dev ? min(*g.nb_dev, g.nb) : g.nb;
-    const int K = g.k_dev ? min(*g.k_dev * g.k_times, g.K) : g.K;
+    const int nb = g.nb_dev ? min(g.planes ? with_parts(*g.nb_dev) : *g.nb_dev, g.nb) : g.nb;
+    const int K = g.k_dev ? min((g.planes ? with_parts(*g.k_dev) : *g.k_dev) * g.k_times, g.K) : g.K;
     const int nta = (g.na + C::NA - 1) / C::NA, ntb = (nb + NBO - 1) / NBO;
     const int chunks = (K + kBK - 1) / kBK;
     int splits = 1;
@@ -283,7 +289,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
             if (blockIdx.x == 0 && threadIdx.x == 0) *g.slices_out = splits;
         }
     }
-    const bool direct = OUT == PART && splits == 1 && g.direct;
+    const bool direct = OUT == PART && splits == 1 && g.direct && !(g.planes && *g.nb_dev <= kFewRows);
     const int64_t split_stride = g.split_stride ? g.split_stride : static_cast<int64_t>(ntb) * NBO * g.ldo;
     const int work = nta * ntb * splits;
     // contiguous parts of the work list per XCD (workgroups are dealt to XCDs
@@ -310,6 +316,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
     const int lane = lane_id(), wave = wave_id();
     const int l32 = lane & 31, lh = lane >> 5;
     const int arow = 32 * FA * (wave % C::WA), brow = 32 * FB * (wave / C::WA);
+    const bool parts = C::NB == kFewRows || nb <= kFewRows;     // LSE, GRAD: out in two parts, the second kFewRows rows on
     const float coef = (OUT == ROWS || OUT == ROWS32 || OUT == PART) ? (g.coef ? *g.coef : g.factor) : 1.f;
 
     auto slice = [&](int sp) { return chunks * sp / splits; };     // first chunk of a slice
@@ -607,9 +614,9 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                 if (kept && row0 < nb) {
                     auto to = [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; };
                     store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q]; }, to, nb - row0);
-                    if constexpr (kParts)
+                    if (parts)
                         store16(j, [&](int i, int q) __attribute__((always_inline)) { return bf16_rest(acc[i][j][q]); },
-                                [&](int r) { return to(r) + 64 * g.ldo; }, nb - row0);
+                                [&](int r) { return to(r) + kFewRows * g.ldo; }, nb - row0);
                 }
             }
             lds_barrier();
@@ -645,9 +652,9 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                     };
                     auto to = [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; };
                     store16(j, grad, to, nv);
-                    if constexpr (kParts)
+                    if (parts)
                         store16(j, [&](int i, int q) __attribute__((always_inline)) { return bf16_rest(grad(i, q)); },
-                                [&](int r) { return to(r) + 64 * g.ldo; }, nv);
+                                [&](int r) { return to(r) + kFewRows * g.ldo; }, nv);
                 } else if (OUT == ROWS || direct) {
                     if (cur.a0 + arow >= g.na) break;      // (columns come in multiples of 64)
                     store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q] * coef; },
