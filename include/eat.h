@@ -360,7 +360,8 @@ eat_status_t eat_ppl_trend(const void* h, int32_t S, int32_t d, const void* w_vo
  * [0, V) that is not `ignore`, or a NaN in the row, gives a NaN nll, a NaN
  * loss and NaN in what the row reaches (its dh, all of dW_V).  A head row that
  * gives -inf logits takes no probability and its dW_V is 0; its infinities make
- * dh NaN (0 times infinity). */
+ * dh NaN (0 times infinity).  A logit of +inf gives an infinite or NaN nll and
+ * loss, and NaN in the row's dh and in dW_V (of its entry and of others). */
 typedef enum { EAT_CE_DH = 1, EAT_CE_DW = 2 } eat_ce_grads_t;
 
 /* Workspace bytes for T positions (0 <= T <= 2^20), width d (a multiple of

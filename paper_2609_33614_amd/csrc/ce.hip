@@ -5,7 +5,7 @@
 //   G_tv   = exp(z_tv - lse_t) off the target, expm1(-nll_t) on it
 //   dh     = c G W,   dW = c G^T h,   c = scale / (mean ? n : 1)
 // The z of all the rows is never there.  A first pass leaves one (maximum, sum of
-// exponentials) pair per row and 128 or 256 columns, and in bf16 the exponentials of
+// exponentials) pair per row and 128 or 256 columns, and in 16 bits the exponentials of
 // the first piece of the vocabulary, over their tile's maximum: G of that piece
 // needs one multiplication per entry.  The gradients take the other pieces' z again,
 // a piece at a time, whose G is held in bf16 (kPieceBytes at most) for its two
@@ -19,8 +19,8 @@
 // loss_gemm<PART/ROWS> the products of a piece, and join_kernel adds the slices of
 // dh.
 //
-// G in bf16 is off by up to 2^-8 of each entry, and that of the first piece by twice
-// that (the exponential's rounding and its own).  Over many rows such errors average
+// G in bf16 is off by up to 2^-8 of each entry, that of the first piece by 2^-10 more
+// (the exponential's rounding: pack_kept).  Over many rows such errors average
 // out against the rounding of the bf16 results; over few they do not (dW of one row
 // is its G times a number), so up to kFewRows rows that count have G in two bf16
 // parts, and their hidden rows twice: known on the host in calls of so few, else on
@@ -199,7 +199,8 @@ __global__ __launch_bounds__(kRowWaves * kWave) void row_kernel(const float2* __
     }
 }
 
-// G of the columns whose exponentials the first pass kept, in place: a tile of
+// G of the columns whose exponentials the first pass kept, in place (NaN in a row
+// and tile with a logit of +inf, whose exponentials are not below 1): a tile of
 // the first pass x 64 rows per workgroup, 16 bytes per lane.  Twice the piece's
 // bytes against taking its product again (4096 rows of 32000 columns, d 4096:
 // see launch_ce).  Rows behind the list up to a whole reduction chunk: zeros.  Up
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __re
         if (i < n) {
             const float2 st = stats[i];
             const float m = part[static_cast<size_t>(blockIdx.x) * ldpart + i].x;
-            v = float4{m == -INFINITY ? 0.f * st.x : exp_from(tile_ref(m), st.x), st.y,
+            v = float4{m == INFINITY ? NAN : m == -INFINITY ? 0.f * st.x : exp_from(tile_ref(m), st.x), st.y,
                        __int_as_float(tc[i] - c0), 0.f};
         }
         row[tid] = v;
@@ -251,10 +252,13 @@ __global__ __launch_bounds__(kScaleThreads) void scale_kernel(const float2* __re
                 if constexpr (PARTS) { w2[0] = v2[k].x; w2[1] = v2[k].y; w2[2] = v2[k].z; w2[3] = v2[k].w; }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xffff0000u);
+                    float lo, hi;
                     if constexpr (PARTS) {
-                        lo += __uint_as_float(w2[e] << 16);
-                        hi += __uint_as_float(w2[e] & 0xffff0000u);
+                        lo = __uint_as_float(w[e] << 16) + __uint_as_float(w2[e] << 16);
+                        hi = __uint_as_float(w[e] & 0xffff0000u) + __uint_as_float(w2[e] & 0xffff0000u);
+                    } else {
+                        lo = kept_lo(w[e]);
+                        hi = kept_hi(w[e]);
                     }
                     lo = rel == 2 * e ? p.y : lo * p.x;
                     hi = rel == 2 * e + 1 ? p.y : hi * p.x;

@@ -83,7 +83,7 @@ struct GemmArgs {
     void* out;                 // GRAD, ROWS, LSE: bf16; ROWS32: fp32; PART: fp32 slices
     int64_t ldo;
     int64_t split_stride;      // PART: between slices (0: the output's whole tiles of rows)
-    int kept;                  // LSE: columns below it leave exp(z - the tile's maximum) in out
+    int kept;                  // LSE: columns below it leave exp(z - the tile's maximum) in out, by pack_kept or in two parts
     const int32_t* rows;       // ROWS, ROWS32: destination of each output row (or null: itself)
     const float* coef;         // ROWS: factor c on the device, or null: factor
     float factor;
@@ -250,6 +250,16 @@ __device__ __forceinline__ float tile_ref(float m) { return fabsf(m) == INFINITY
 // exp(z - ref).  The difference comes first: either of them times log2 e may be
 // past fp32's range.
 __device__ __forceinline__ float exp_from(float z, float ref) { return __builtin_amdgcn_exp2f((z - ref) * kLog2e); }
+
+// Exponentials of 0 to 1 in 16 bits each: fp32's 7 lower exponent bits (the sign and
+// the upper one are 0 below 2) and 9 of its digits, two more than bf16 has, so
+// that the rounding of what is made of them counts and theirs hardly does.
+__device__ __forceinline__ uint32_t pack_kept(float a, float b) {
+    const uint32_t x = (__float_as_uint(a) << 2) + 0x8000u, y = (__float_as_uint(b) << 2) + 0x8000u;
+    return __builtin_amdgcn_perm(y, x, 0x07060302);        // (the upper halves)
+}
+__device__ __forceinline__ float kept_lo(uint32_t w) { return __uint_as_float((w & 0xffffu) << 14); }
+__device__ __forceinline__ float kept_hi(uint32_t w) { return __uint_as_float((w >> 2) & 0x3fffc000u); }
 
 // What the rounding of v to bf16 leaves.
 __device__ __forceinline__ float bf16_rest(float v) { return v - __uint_as_float(pack_bf16x2(v, 0.f) << 16); }
@@ -541,7 +551,8 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
         uint8_t* const tb = share(wave);
         // FA fragments' 32 rows of 64 FA bytes, turned around through the
         // wave's share of LDS so that adjacent lanes store adjacent pieces
-        auto store16 = [&](int j, auto val, auto dst, int nv) __attribute__((always_inline)) {
+        auto as_bf16 = [](float a, float b) __attribute__((always_inline)) { return pack_bf16x2(a, b); };
+        auto store16 = [&](int j, auto val, auto dst, int nv, auto pack) __attribute__((always_inline)) {
             constexpr int V = 4 * FA;         // 16-byte pieces per row
             auto at = [&](int r, int v) { return r * (64 * FA) + ((v ^ (FA == 1 ? (r >> 1) & 3 : r & (4 * FA - 1))) << 4); };
 #pragma unroll
@@ -549,8 +560,7 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
 #pragma unroll
                 for (int qb = 0; qb < 4; ++qb)
                     *reinterpret_cast<uint2*>(tb + at(l32, 4 * i + qb) + 8 * lh) =
-                        uint2{pack_bf16x2(val(i, 4 * qb), val(i, 4 * qb + 1)),
-                              pack_bf16x2(val(i, 4 * qb + 2), val(i, 4 * qb + 3))};
+                        uint2{pack(val(i, 4 * qb), val(i, 4 * qb + 1)), pack(val(i, 4 * qb + 2), val(i, 4 * qb + 3))};
             wave_lds_sync();
 #pragma unroll
             for (int k = 0; k < 32 * V / 64; ++k) {
@@ -613,10 +623,14 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                 const int row0 = cur.b0 + brow + 32 * j;
                 if (kept && row0 < nb) {
                     auto to = [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; };
-                    store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q]; }, to, nb - row0);
-                    if (parts)
+                    auto value = [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q]; };
+                    if (parts) {
+                        store16(j, value, to, nb - row0, as_bf16);
                         store16(j, [&](int i, int q) __attribute__((always_inline)) { return bf16_rest(acc[i][j][q]); },
-                                [&](int r) { return to(r) + kFewRows * g.ldo; }, nb - row0);
+                                [&](int r) { return to(r) + kFewRows * g.ldo; }, nb - row0, as_bf16);
+                    } else {
+                        store16(j, value, to, nb - row0, [](float a, float b) __attribute__((always_inline)) { return pack_kept(a, b); });
+                    }
                 }
             }
             lds_barrier();
@@ -651,17 +665,17 @@ __global__ __launch_bounds__(C::kThreads) void loss_gemm(GemmArgs g) {
                         return v < end ? p : 0.f;
                     };
                     auto to = [&](int r) { return static_cast<uint16_t*>(g.out) + (row0 + r) * g.ldo + cur.a0 + arow; };
-                    store16(j, grad, to, nv);
+                    store16(j, grad, to, nv, as_bf16);
                     if (parts)
                         store16(j, [&](int i, int q) __attribute__((always_inline)) { return bf16_rest(grad(i, q)); },
-                                [&](int r) { return to(r) + kFewRows * g.ldo; }, nv);
+                                [&](int r) { return to(r) + kFewRows * g.ldo; }, nv, as_bf16);
                 } else if (OUT == ROWS || direct) {
                     if (cur.a0 + arow >= g.na) break;      // (columns come in multiples of 64)
                     store16(j, [&](int i, int q) __attribute__((always_inline)) { return acc[i][j][q] * coef; },
                             [&](int r) {
                                 const int64_t to = g.rows && r < nv ? g.rows[row0 + r] : row0 + r;
                                 return static_cast<uint16_t*>(direct ? g.direct : g.out) + to * g.ldo + cur.a0 + arow;
-                            }, nv);
+                            }, nv, as_bf16);
                 } else {
                     auto at = [&](int r, int v) { return r * 128 + ((v ^ (r & 7)) << 4); };
 #pragma unroll
