@@ -367,8 +367,9 @@ typedef enum { EAT_CE_DH = 1, EAT_CE_DW = 2 } eat_ce_grads_t;
 /* Workspace bytes for T positions (0 <= T <= 2^20), width d (a multiple of
  * 64, at most 65536: EAT_ERR_UNSUPPORTED beyond) and vocabulary V (1..2^24)
  * with the gradients `grads` (eat_ce_grads_t bits).  *bytes: the largest a
- * call has a use for (pieces of up to 4 GiB); *min_bytes (or NULL): the
- * smallest it takes (pieces of 4096 entries).  Any size between them is taken
+ * call has a use for (pieces of up to 4 GiB, or of 4096 entries, which are up
+ * to 8 GiB beyond 2^19 positions); *min_bytes (or NULL): the smallest it takes
+ * (pieces of 4096 entries).  Any size between them is taken
  * as it is, with pieces that fit: the first piece costs a pass over its
  * gradient, every other one the product z of its entries again.
  * EAT_ERR_INVALID_ARG otherwise. */

@@ -21,8 +21,8 @@
 // Bounds, measured: small calls by their launches (two to four that wait for each
 // other: 256 tokens, 64 experts, d 2048, dW_r only: 25 us, its bytes are 0.4); large
 // ones by the matrix instructions on the parts (16384 tokens, 256 experts, d 4096:
-// 244 us, of which dx 105 and dW_r 97, at 0.98 and 1.06 PFLOP/s of bf16
-// products); in between by both (8000 tokens, 60 experts, d 2048: 55 us, 63 MB).
+// 242 - 254 us, of which dx 105 and dW_r 97, at 0.98 and 1.06 PFLOP/s of bf16
+// products); in between by both (8000 tokens, 60 experts, d 2048: 56 us, 63 MB).
 #include <math.h>
 
 #include <algorithm>

@@ -25,14 +25,14 @@
 // is its G times a number), so up to kFewRows rows that count have G in two bf16
 // parts, and their hidden rows twice: known on the host in calls of so few, else on
 // the device, where the parts are further rows of the products (dh of 200 positions,
-// d 4096, V 32000: 77 of them count, 136 us; 64 in two parts, 147, in one, 136).
+// d 4096, V 32000, of which 64 count: 129 us of kernels, 119 in one part).
 //
-// Bounds, measured: three products of 2 n d V operations each (1.22 - 1.29 PFLOP/s
-// of 1.25 - 1.4 that a library product reaches: 4096 rows, d 4096, V 32000 take
-// 2.74 ms, 1.17 PFLOP/s over all); with few rows the one pass over W (1 row, 262 MB:
+// Bounds, measured: three products of 2 n d V operations each (1.06 - 1.18 PFLOP/s
+// at 4096 rows, d 4096, V 32000, where a call takes 2.74 ms, 1.16 - 1.26 at 8192 rows,
+// V 128256; a library product reaches 1.1 - 1.4); with few rows the one pass over W (1 row, 262 MB:
 // 66 us, 4.0 TB/s), then dW's store (131 M entries from one row: 70 us, 3.7
 // TB/s); with small vocabularies the launches, five to seven that wait for each
-// other (32 rows, d 128, V 1024: 33 us).
+// other (32 rows, d 128, V 1024: 34.5 us).
 #include <math.h>
 
 #include <algorithm>
@@ -348,7 +348,8 @@ hipError_t launch_sized(Size z, const GemmArgs& g, hipStream_t s) {
 
 // G held at a time: a piece of the vocabulary whose G takes kPieceBytes at
 // most (1.4% of the card's memory) and, with a smaller workspace, what fits,
-// from kMinPiece columns on.  The first piece costs a pass over its G, every
+// from kMinPiece columns on (which take more than kPieceBytes beyond 2^19 rows, 8
+// GiB at the most).  The first piece costs a pass over its G, every
 // other one its product again: 8192 rows, d 4096, V 128256 (2.1 GB) take 22.0 ms in
 // one piece, 25.0 in two, 26.6 in four, 29.0 in 32; 512 rows, d 2048, V 50000 take 396
 // us in one, 478 in two, 1108 in 13 (the smallest, too few columns to fill the CUs).
