@@ -440,6 +440,62 @@ eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const fl
                               float* loss_out, int64_t* count_out, float* mean_prob_out, float* dlogits, void* dx,
                               float* dw_router, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---- tokens sorted by expert, and back ---------------------------------------
+ *
+ * What stands between a layer's routing and experts that are run on their own,
+ * with the gradients.  The R selected pairs (t, e) of the masks that eat_route
+ * wrote are laid out expert by expert, an expert's tokens in increasing order:
+ * expert e owns rows offsets[e] .. offsets[e+1], token[r] is row r's token and
+ * place[t][e] the pair's row (-1 for pairs that are not selected).
+ *
+ *   sort      rows[place(t, e)] = x_t            dx_t = sum_{e in S_t} drows[place(t, e)]
+ *   combine   y_t = sum_{e in S_t} g_te rows[place(t, e)]
+ *             drows[place(t, e)] = g_te dy_t     dg_te = <dy_t, rows[place(t, e)]>
+ *             dz_te = [e in S_t] g_te (dg_te - G_t) - p_te G_t eps / (P_t + eps),
+ *             G_t = sum_{S_t} g dg, P_t = sum_{S_t} p: the gradient of the scaled scores
+ *             z (p = softmax(z), with expert_scale too) through g = p / (P + eps),
+ *             the selections held, as eat_balance_loss gives its own
+ *
+ * A token that selected no expert gets y 0, dx 0, dg 0 and dz 0.  Sums are in
+ * fp32, in the experts' order, rounded once.  `cap` is the number of rows that the
+ * caller's arrays hold: pairs past it are left out (place -1, offsets and all
+ * sums end at cap).  Rows from offsets[E] on are not written.  Places outside
+ * [0, cap) count as -1. */
+eat_status_t eat_sort_workspace_size(eat_handle_t h, int32_t T, size_t* bytes);
+
+/* For layer h (its E, d_model, act_dtype; top_k and the mode play no part).
+ *   x, rows_out  [T][d_model], [cap][d_model] act_dtype; both NULL: the indices alone
+ *   mask         [T][W] uint64
+ *   offsets_out  [E+1] int32, token_out [cap] int32 (NULL where cap = 0), place_out [T][E] int32
+ *   ws           eat_sort_workspace_size(h, T) bytes, 256-byte aligned (NULL where that is 0)
+ * T = 0 gives offsets 0.  Nothing that is written may overlap another of the
+ * call's arrays (INVALID_ARG).  These calls enqueue on `stream` only; no
+ * synchronisation, no allocation, no memset.  Errors: EAT_ERR_INVALID_ARG,
+ * EAT_ERR_WORKSPACE, EAT_ERR_HIP. */
+eat_status_t eat_sort_tokens(eat_handle_t h, const void* x, int32_t T, const uint64_t* mask, int32_t cap, void* rows_out,
+                             int32_t* offsets_out, int32_t* token_out, int32_t* place_out, void* ws, size_t ws_bytes,
+                             hipStream_t stream);
+
+/* dx [T][d_model] of drows [cap][d_model], both act_dtype (formulas above). */
+eat_status_t eat_sort_backward(eat_handle_t h, const void* drows, int32_t cap, int32_t T, const uint64_t* mask,
+                               const int32_t* place, void* dx, hipStream_t stream);
+
+/* y [T][d_model] of rows [cap][d_model], both act_dtype; gate [T][E] fp32, read
+ * where selected. */
+eat_status_t eat_combine(eat_handle_t h, const void* rows, int32_t cap, int32_t T, const uint64_t* mask, const float* gate,
+                         const int32_t* place, void* y, hipStream_t stream);
+
+/* The gradients of eat_combine for dy [T][d_model].
+ *   rows     [cap][d_model] (only dgate and dlogits read it; else may be NULL)
+ *   prob     [T][E] fp32 (only dlogits reads it; else may be NULL)
+ *   drows    [cap][d_model] act_dtype, dgate [T][E] fp32, dlogits [T][E] fp32: each
+ *            may be NULL; drows may be rows itself, dlogits prob itself, dgate gate
+ *            itself (otherwise no overlaps, as above)
+ * eps is the handle's. */
+eat_status_t eat_combine_backward(eat_handle_t h, const void* dy, const void* rows, int32_t cap, int32_t T,
+                                  const uint64_t* mask, const float* gate, const int32_t* place, const float* prob,
+                                  void* drows, float* dgate, float* dlogits, hipStream_t stream);
+
 /* ---- packed expert weights -------------------------------------------------
  *
  * Write the PACKED form (eat_layout_t) of `groups` row-major bf16 matrices

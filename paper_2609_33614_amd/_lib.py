@@ -99,13 +99,20 @@ def load() -> C.CDLL:
         lib.eat_balance_workspace_size.argtypes = [P, C.c_int32, C.POINTER(C.c_size_t)]
         lib.eat_balance_loss.argtypes = [P, P, C.c_int32, P, P, P, P, C.c_float, C.c_float, P, P, P, P, P, P, P,
                                          C.c_size_t, P]
+    if hasattr(lib, "eat_sort_tokens"):
+        lib.eat_sort_workspace_size.argtypes = [P, C.c_int32, C.POINTER(C.c_size_t)]
+        lib.eat_sort_tokens.argtypes = [P, P, C.c_int32, P, C.c_int32, P, P, P, P, P, C.c_size_t, P]
+        lib.eat_sort_backward.argtypes = [P, P, C.c_int32, C.c_int32, P, P, P, P]
+        lib.eat_combine.argtypes = [P, P, C.c_int32, C.c_int32, P, P, P, P, P]
+        lib.eat_combine_backward.argtypes = [P, P, P, C.c_int32, C.c_int32, P, P, P, P, P, P, P, P]
     lib.eat_status_string.argtypes = [C.c_int]
     lib.eat_status_string.restype = C.c_char_p
     for name in ("eat_params_default", "eat_create", "eat_destroy", "eat_workspace_size", "eat_route_workspace_size",
                  "eat_reset_accounts", "eat_route", "eat_moe_forward", "eat_moe_forward_profiled",
                  "eat_stack_workspace_size", "eat_stack_forward", "eat_ppl_workspace_size", "eat_ppl_reset",
                  "eat_ppl_trend", "eat_pack_weights", "eat_moe_forward_noalloc", "eat_ce_workspace_size", "eat_ce_loss",
-                 "eat_balance_workspace_size", "eat_balance_loss"):
+                 "eat_balance_workspace_size", "eat_balance_loss", "eat_sort_workspace_size", "eat_sort_tokens",
+                 "eat_sort_backward", "eat_combine", "eat_combine_backward"):
         if hasattr(lib, name):
             getattr(lib, name).restype = st
     _lib = lib
@@ -301,3 +308,33 @@ def eat_balance_loss(handle: int, x, T: int, w_router, prob, mask, valid, coef: 
                                    float(coef), float(entropy_coef), _ptr(loss_out), _ptr(count_out),
                                    _ptr(mean_prob_out), _ptr(dlogits), _ptr(dx), _ptr(dw_router), _ptr(ws),
                                    int(ws_bytes), _stream(stream)), "eat_balance_loss")
+
+
+def eat_sort_workspace_size(handle: int, T: int) -> int:
+    b = C.c_size_t()
+    _check(load().eat_sort_workspace_size(handle, int(T), C.byref(b)), "eat_sort_workspace_size")
+    return b.value
+
+
+def eat_sort_tokens(handle: int, x, T: int, mask, cap: int, rows_out, offsets_out, token_out, place_out, ws=None,
+                    ws_bytes: int = 0, stream=None) -> None:
+    _check(load().eat_sort_tokens(handle, _ptr(x), int(T), _ptr(mask), int(cap), _ptr(rows_out), _ptr(offsets_out),
+                                  _ptr(token_out), _ptr(place_out), _ptr(ws), int(ws_bytes), _stream(stream)),
+           "eat_sort_tokens")
+
+
+def eat_sort_backward(handle: int, drows, cap: int, T: int, mask, place, dx, stream=None) -> None:
+    _check(load().eat_sort_backward(handle, _ptr(drows), int(cap), int(T), _ptr(mask), _ptr(place), _ptr(dx),
+                                    _stream(stream)), "eat_sort_backward")
+
+
+def eat_combine(handle: int, rows, cap: int, T: int, mask, gate, place, y, stream=None) -> None:
+    _check(load().eat_combine(handle, _ptr(rows), int(cap), int(T), _ptr(mask), _ptr(gate), _ptr(place), _ptr(y),
+                              _stream(stream)), "eat_combine")
+
+
+def eat_combine_backward(handle: int, dy, rows, cap: int, T: int, mask, gate, place, prob, drows, dgate, dlogits,
+                         stream=None) -> None:
+    _check(load().eat_combine_backward(handle, _ptr(dy), _ptr(rows), int(cap), int(T), _ptr(mask), _ptr(gate), _ptr(place),
+                                       _ptr(prob), _ptr(drows), _ptr(dgate), _ptr(dlogits), _stream(stream)),
+           "eat_combine_backward")

@@ -610,6 +610,108 @@ eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const fl
     return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
 }
 
+eat_status_t eat_sort_workspace_size(eat_handle_t h, int32_t T, size_t* bytes) {
+    if (!h || !bytes || T < 0 || T > h->max_tokens) return EAT_ERR_INVALID_ARG;
+    *bytes = align256(eat::sort_workspace(T, h->p.E));
+    return EAT_OK;
+}
+
+// What the calls between tokens and sorted rows have in common: their sizes.
+static eat_status_t check_sorted(const eat_ctx* h, int32_t T, int32_t cap, const uint64_t* mask, const int32_t* place) {
+    if (!h || T < 0 || T > h->max_tokens || cap < 0) return EAT_ERR_INVALID_ARG;
+    if (T > 0 && (!mask || !place)) return EAT_ERR_INVALID_ARG;
+    return aligned(mask, 8) && aligned(place, 4) ? EAT_OK : EAT_ERR_INVALID_ARG;
+}
+
+namespace {
+
+struct SortBytes {
+    size_t x, rows, mask, pairs;
+    SortBytes(const eat_ctx& h, int32_t T, int32_t cap) {
+        const size_t n = static_cast<size_t>(T), row = static_cast<size_t>(h.p.d_model) * (h.p.act_dtype == EAT_BF16 ? 2 : 4);
+        x = n * row;
+        rows = static_cast<size_t>(cap) * row;
+        mask = n * eat::mask_words(h.p.E) * 8;
+        pairs = n * h.p.E * 4;
+    }
+};
+eat::SortCall sort_call(const eat_ctx& h, const uint64_t* mask, const int32_t* place, const float* gate, int32_t T, int32_t cap) {
+    return eat::SortCall{mask, place, gate, T, h.p.E, h.p.d_model, cap, h.p.act_dtype == EAT_BF16};
+}
+bool in_place_none(const void*, const void*) { return false; }
+
+}  // namespace
+
+eat_status_t eat_sort_tokens(eat_handle_t h, const void* x, int32_t T, const uint64_t* mask, int32_t cap, void* rows_out,
+                             int32_t* offsets_out, int32_t* token_out, int32_t* place_out, void* ws, size_t ws_bytes,
+                             hipStream_t stream) {
+    const eat_status_t st = check_sorted(h, T, cap, mask, place_out);
+    if (st != EAT_OK) return st;
+    if (!offsets_out || (cap > 0 && !token_out) || (rows_out && T > 0 && !x) || (x && cap > 0 && !rows_out)) return EAT_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(rows_out, 16) || !aligned(offsets_out, 4) || !aligned(token_out, 4)) return EAT_ERR_INVALID_ARG;
+    const size_t need = align256(eat::sort_workspace(T, h->p.E));
+    if (need > 0 && (!ws || ws_bytes < need)) return EAT_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
+    const SortBytes b(*h, T, cap);
+    if (clash({{rows_out, b.rows}, {offsets_out, (static_cast<size_t>(h->p.E) + 1) * 4}, {token_out, static_cast<size_t>(cap) * 4},
+               {place_out, b.pairs}, {ws, need}}, {{x, b.x}, {mask, b.mask}}, in_place_none))
+        return EAT_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    const hipError_t e = eat::launch_sort(sort_call(*h, mask, nullptr, nullptr, T, cap), x, cap > 0 ? rows_out : nullptr,
+                                          offsets_out, token_out, place_out, ws, stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+eat_status_t eat_sort_backward(eat_handle_t h, const void* drows, int32_t cap, int32_t T, const uint64_t* mask,
+                               const int32_t* place, void* dx, hipStream_t stream) {
+    const eat_status_t st = check_sorted(h, T, cap, mask, place);
+    if (st != EAT_OK) return st;
+    if (T > 0 && (!dx || (cap > 0 && !drows))) return EAT_ERR_INVALID_ARG;
+    if (!aligned(drows, 16) || !aligned(dx, 16)) return EAT_ERR_INVALID_ARG;
+    const SortBytes b(*h, T, cap);
+    if (clash({{dx, b.x}}, {{drows, b.rows}, {mask, b.mask}, {place, b.pairs}}, in_place_none)) return EAT_ERR_INVALID_ARG;
+    if (T == 0) return EAT_OK;
+    (void)hipGetLastError();
+    return eat::launch_gather(sort_call(*h, mask, place, nullptr, T, cap), drows, dx, stream) == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+eat_status_t eat_combine(eat_handle_t h, const void* rows, int32_t cap, int32_t T, const uint64_t* mask, const float* gate,
+                         const int32_t* place, void* y, hipStream_t stream) {
+    const eat_status_t st = check_sorted(h, T, cap, mask, place);
+    if (st != EAT_OK) return st;
+    if (T > 0 && (!y || !gate || (cap > 0 && !rows))) return EAT_ERR_INVALID_ARG;
+    if (!aligned(rows, 16) || !aligned(y, 16) || !aligned(gate, 4)) return EAT_ERR_INVALID_ARG;
+    const SortBytes b(*h, T, cap);
+    if (clash({{y, b.x}}, {{rows, b.rows}, {mask, b.mask}, {place, b.pairs}, {gate, b.pairs}}, in_place_none))
+        return EAT_ERR_INVALID_ARG;
+    if (T == 0) return EAT_OK;
+    (void)hipGetLastError();
+    return eat::launch_gather(sort_call(*h, mask, place, gate, T, cap), rows, y, stream) == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+eat_status_t eat_combine_backward(eat_handle_t h, const void* dy, const void* rows, int32_t cap, int32_t T,
+                                  const uint64_t* mask, const float* gate, const int32_t* place, const float* prob,
+                                  void* drows, float* dgate, float* dlogits, hipStream_t stream) {
+    const eat_status_t st = check_sorted(h, T, cap, mask, place);
+    if (st != EAT_OK) return st;
+    if (T > 0 && (!dy || !gate || (dlogits && !prob) || ((dgate || dlogits) && cap > 0 && !rows))) return EAT_ERR_INVALID_ARG;
+    if (!aligned(dy, 16) || !aligned(rows, 16) || !aligned(drows, 16) || !aligned(gate, 4) || !aligned(prob, 4) ||
+        !aligned(dgate, 4) || !aligned(dlogits, 4))
+        return EAT_ERR_INVALID_ARG;
+    const SortBytes b(*h, T, cap);
+    if (clash({{drows, b.rows}, {dgate, b.pairs}, {dlogits, b.pairs}},
+              {{dy, b.x}, {rows, b.rows}, {mask, b.mask}, {place, b.pairs}, {gate, b.pairs}, {prob, b.pairs}},
+              [&](const void* o, const void* i) {
+                  return (o == drows && i == rows) || (o == dlogits && i == prob) || (o == dgate && i == gate);
+              }))
+        return EAT_ERR_INVALID_ARG;
+    if (T == 0 || (!drows && !dgate && !dlogits)) return EAT_OK;
+    (void)hipGetLastError();
+    const hipError_t e = eat::launch_combine_grad(sort_call(*h, mask, place, gate, T, cap), dy, rows, prob, h->p.eps, drows,
+                                                  dgate, dlogits, stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
 const char* eat_status_string(eat_status_t s) {
     // a C caller may pass any int: read the argument's bits, not the enum
     // (a C++ enum value outside its enumerators' range is undefined)

@@ -291,6 +291,24 @@ struct BalanceCall {
 BalancePlan plan_balance(const eat_params_t& p, int32_t T);
 hipError_t launch_balance(const eat_params_t& p, const BalancePlan& b, const BalanceCall& c, char* ws, hipStream_t s);
 
+// Tokens sorted by expert, their rows back (sort.hip).
+struct SortCall {
+    const uint64_t* mask;    // [T][mask_words(E)]
+    const int32_t* place;    // [T][E]: a selected pair's row, or -1
+    const float* gate;       // [T][E] or null: 1
+    int32_t T, E, d, cap;    // cap: rows there are
+    bool bf16;
+};
+// Up to so many mask words every workgroup of the index launch counts all
+// tokens itself; beyond, two launches count them first.
+constexpr int kDirectTokens = 16384;
+size_t sort_workspace(int32_t T, int E);
+hipError_t launch_sort(const SortCall& c, const void* x, void* rows, int32_t* offsets, int32_t* token, int32_t* place,
+                       void* ws, hipStream_t s);
+hipError_t launch_gather(const SortCall& c, const void* rows, void* y, hipStream_t s);
+hipError_t launch_combine_grad(const SortCall& c, const void* dy, const void* rows, const float* prob, float eps, void* drows,
+                               float* dgate, float* dlogits, hipStream_t s);
+
 // Forward entry points (api.cpp): host-side argument checks, and the
 // enqueue of one layer forward into a workspace of plan_workspace(h, T).total
 // bytes at `ws` (arguments checked, T > 0).  `residual` (bf16 [T][d] or

@@ -1,0 +1,495 @@
+// Tokens sorted by expert and back, with their gradients (gfx950).
+//
+//   sort             rows[place(t, e)] = x[t] for every selected (t, e), expert-major, tokens in
+//                    order inside an expert's segment; its backward dx[t] = sum_e drows[place(t, e)]
+//   combine          y[t] = sum_e gate[t][e] rows[place(t, e)]
+//   combine backward drows[place(t, e)] = gate[t][e] dy[t],  dg_te = <dy[t], rows[place(t, e)]>,
+//                    dz_te = [e in S_t] g_te (dg_te - G) - p_te G eps / (P + eps)
+//                    with G = sum_S g dg, P = sum_S p: what g = p / (P + eps) and the softmax give
+//
+// Everything moves rows of d elements once: bound by memory.  The places come
+// from the selection masks alone: a bit transpose turns 64 tokens' masks into
+// each expert's tokens as bits (eat_device.h), whose popcounts are ranks.
+#include <algorithm>
+
+#include "eat_device.h"
+#include "eat_internal.h"
+
+namespace eat {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kChunk = 256;               // tokens per workgroup of the index kernels
+constexpr int kBatch = 8;                 // rows of a token in flight together
+
+// 16 bytes of a row as fp32 numbers and back.
+template <typename T>
+struct Vec;
+template <>
+struct Vec<uint16_t> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void get(const uint4& q, float (&v)[8]) {
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ uint4 put(const float (&v)[8]) {
+        return uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    }
+};
+template <>
+struct Vec<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void get(const uint4& q, float (&v)[4]) {
+        v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+    }
+    static __device__ __forceinline__ uint4 put(const float (&v)[4]) {
+        return uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    }
+};
+
+// ---- index -----------------------------------------------------------------
+
+// Selections per expert of each chunk of tokens: cnt[chunk][E].
+__global__ __launch_bounds__(kThreads) void count_kernel(const uint64_t* __restrict__ mask, int T, int E, int W,
+                                                         int32_t* __restrict__ cnt) {
+    __shared__ int part[kWaves][kMaxExperts];
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int t = blockIdx.x * kChunk + wave * kWave + lane;
+    for (int w = 0; w < W; ++w)
+        part[wave][kWave * w + lane] = __popcll(bit_transpose(t < T ? mask[static_cast<size_t>(t) * W + w] : 0ull));
+    __syncthreads();
+    const int e = threadIdx.x;
+    if (e >= E) return;
+    int n = 0;
+#pragma unroll
+    for (int q = 0; q < kWaves; ++q) n += part[q][e];
+    cnt[static_cast<size_t>(blockIdx.x) * E + e] = n;
+}
+
+// Per expert (a workgroup each): cnt becomes the selections in earlier chunks,
+// total[e] those of all.
+__global__ __launch_bounds__(kThreads) void scan_kernel(int32_t* __restrict__ cnt, int chunks, int E, int32_t* __restrict__ total) {
+    __shared__ int part[kWaves];
+    const int e = blockIdx.x, lane = lane_id(), wave = threadIdx.x / kWave;
+    int carry = 0;
+    for (int c0 = 0; c0 < chunks; c0 += kThreads) {
+        const int c = c0 + static_cast<int>(threadIdx.x);
+        const int n = c < chunks ? cnt[static_cast<size_t>(c) * E + e] : 0;
+        const int s = wave_scan(n);
+        if (lane == kWave - 1) part[wave] = s;
+        __syncthreads();
+        int before = carry, all = 0;
+#pragma unroll
+        for (int q = 0; q < kWaves; ++q) {
+            before += q < wave ? part[q] : 0;
+            all += part[q];
+        }
+        if (c < chunks) cnt[static_cast<size_t>(c) * E + e] = before + s - n;
+        carry += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) total[e] = carry;
+}
+
+struct IndexArgs {
+    const uint64_t* mask;      // [T][W]
+    int T, E, W, cap;
+    const int32_t* cnt;        // [chunks][E] selections in earlier chunks (null: counted here)
+    const int32_t* total;      // [E]
+    int32_t* offsets;          // [E+1]
+    int32_t* token;            // [cap]
+    int32_t* place;            // [T][E]
+};
+
+// offsets, token and place of one chunk of tokens per workgroup of NW waves.
+// Without counts every workgroup counts all tokens itself, 64 per wave at a
+// time: no launches to wait for, and the masks (8 W bytes a token) come from L2.
+template <int NW>
+__global__ __launch_bounds__(NW* kWave) void index_kernel(IndexArgs a) {
+    __shared__ int tot[kMaxExperts], before[kMaxExperts], base[kMaxExperts];
+    __shared__ int own[kChunk / kWave][kMaxExperts];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int t0 = blockIdx.x * kChunk;
+    for (int e = threadIdx.x; e < kMaxExperts; e += NW * kWave) {
+        const bool given = a.cnt && e < a.E;
+        tot[e] = given ? a.total[e] : 0;
+        before[e] = given ? a.cnt[static_cast<size_t>(blockIdx.x) * a.E + e] : 0;
+    }
+    __syncthreads();
+    if (!a.cnt) {
+        for (int w = 0; w < a.W; ++w) {
+            int all = 0, pre = 0;
+            for (int g = wave; g * kWave < a.T; g += NW) {
+                const int t = g * kWave + lane;
+                const int n = __popcll(bit_transpose(t < a.T ? a.mask[static_cast<size_t>(t) * a.W + w] : 0ull));
+                all += n;
+                pre += g * kWave < t0 ? n : 0;
+            }
+            atomicAdd(&tot[kWave * w + lane], all);      // (whole numbers: any order gives the same sum)
+            atomicAdd(&before[kWave * w + lane], pre);
+        }
+    }
+    // (waves past the chunk's groups take part in the barriers alone)
+    constexpr int kGroups = kChunk / kWave;
+    uint64_t col[kMaxExperts / kWave];
+    const int t = t0 + wave * kWave + lane;
+#pragma unroll
+    for (int w = 0; w < kMaxExperts / kWave; ++w) {
+        col[w] = 0;
+        if (w < a.W && wave < kGroups) {
+            col[w] = bit_transpose(t < a.T ? a.mask[static_cast<size_t>(t) * a.W + w] : 0ull);
+            own[wave][kWave * w + lane] = __popcll(col[w]);
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {
+        int carry = 0;
+        for (int e0 = 0; e0 < a.E; e0 += kWave) {
+            const int e = e0 + lane;
+            const int n = e < a.E ? tot[e] : 0;
+            const int s = wave_scan(n);
+            if (e < a.E) {
+                base[e] = carry + s - n;
+                if (blockIdx.x == 0) {
+                    a.offsets[e] = min(base[e], a.cap);
+                    if (e == a.E - 1) a.offsets[a.E] = min(carry + s, a.cap);
+                }
+            }
+            carry += __builtin_amdgcn_readlane(s, kWave - 1);
+        }
+    }
+    __syncthreads();
+    if (wave >= kGroups) return;
+#pragma unroll
+    for (int w = 0; w < kMaxExperts / kWave; ++w) {
+        const int e = kWave * w + lane;
+        if (w >= a.W || e >= a.E) continue;
+        int row = base[e] + before[e];
+        for (int q = 0; q < wave; ++q) row += own[q][e];
+        uint64_t m = col[w];
+        for (int i = 0; i < kWave; ++i) {
+            const int ti = t0 + wave * kWave + i;
+            if (ti >= a.T) break;                         // uniform
+            int at = -1;
+            if ((m >> i) & 1ull) {
+                if (row < a.cap) {
+                    at = row;
+                    a.token[row] = ti;
+                }
+                ++row;
+            }
+            a.place[static_cast<size_t>(ti) * a.E + e] = at;
+        }
+    }
+}
+
+// ---- rows ------------------------------------------------------------------
+
+struct RowArgs {
+    const uint64_t* mask;      // [T][W]
+    const int32_t* place;      // [T][E]
+    const float* gate;         // [T][E] or null: 1
+    int T, E, W, cap;
+    int vecs;                  // 16-byte vectors of a row
+    int tpb;                   // tokens per workgroup at a time
+    const uint4* src;
+    uint4* dst;
+};
+
+// A token's next up to kBatch selected experts, from word w with bits `rest`
+// left: their places (-1: none, or outside the rows) and gates; returns how many
+// bits were taken.
+struct Cursor {
+    int w;
+    uint64_t rest;
+};
+template <bool GATES>
+__device__ __forceinline__ int next_rows(const RowArgs& a, int t, Cursor& c, int (&rows)[kBatch], float (&gates)[kBatch],
+                                         int (&es)[kBatch]) {
+    const uint64_t* const m = a.mask + static_cast<size_t>(t) * a.W;
+    int n = 0;
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+        while (c.rest == 0 && c.w + 1 < a.W) {
+            c.rest = m[++c.w];
+            if (c.w + 1 == a.W && a.E % kWave) c.rest &= ~0ull >> (kWave - a.E % kWave);
+        }
+        rows[b] = -1;
+        gates[b] = 1.f;
+        es[b] = 0;
+        if (c.rest != 0) {
+            const int e = kWave * c.w + __builtin_ctzll(c.rest);
+            c.rest &= c.rest - 1;
+            es[b] = e;
+            const int r = a.place[static_cast<size_t>(t) * a.E + e];
+            rows[b] = static_cast<unsigned>(r) < static_cast<unsigned>(a.cap) ? r : -1;
+            if constexpr (GATES) gates[b] = a.gate[static_cast<size_t>(t) * a.E + e];
+            n = b + 1;
+        }
+    }
+    return n;
+}
+__device__ __forceinline__ Cursor first_rows(const RowArgs& a, int t) {
+    uint64_t m = a.mask[static_cast<size_t>(t) * a.W];
+    if (a.W == 1 && a.E % kWave) m &= ~0ull >> (kWave - a.E % kWave);
+    return Cursor{0, m};
+}
+
+// rows[place] = x[t]: each token's row is read once.
+__global__ __launch_bounds__(kThreads) void spread_kernel(RowArgs a) {
+    const int v0 = a.tpb > 1 ? threadIdx.x % a.vecs : threadIdx.x, sub = a.tpb > 1 ? threadIdx.x / a.vecs : 0;
+    if (sub >= a.tpb) return;
+    for (int64_t t = static_cast<int64_t>(blockIdx.x) * a.tpb + sub; t < a.T; t += static_cast<int64_t>(gridDim.x) * a.tpb) {
+        Cursor c = first_rows(a, t);
+        for (;;) {
+            int rows[kBatch], es[kBatch];
+            float gates[kBatch];
+            const int n = next_rows<false>(a, t, c, rows, gates, es);
+            if (n == 0) break;
+            for (int v = v0; v < a.vecs; v += kThreads) {
+                const uint4 q = a.src[t * a.vecs + v];
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b)
+                    if (rows[b] >= 0) a.dst[static_cast<int64_t>(rows[b]) * a.vecs + v] = q;
+            }
+            if (n < kBatch) break;
+        }
+    }
+}
+
+// y[t] = sum gate rows[place] (gate null: 1), in fp32 in the experts' order.
+template <typename T, bool GATES>
+__global__ __launch_bounds__(kThreads) void gather_kernel(RowArgs a) {
+    using V = Vec<T>;
+    const int v0 = a.tpb > 1 ? threadIdx.x % a.vecs : threadIdx.x, sub = a.tpb > 1 ? threadIdx.x / a.vecs : 0;
+    if (sub >= a.tpb) return;
+    for (int64_t t = static_cast<int64_t>(blockIdx.x) * a.tpb + sub; t < a.T; t += static_cast<int64_t>(gridDim.x) * a.tpb) {
+        for (int v = v0; v < a.vecs; v += kThreads) {
+            float acc[V::N];
+#pragma unroll
+            for (int i = 0; i < V::N; ++i) acc[i] = 0.f;
+            Cursor c = first_rows(a, t);
+            for (;;) {
+                int rows[kBatch], es[kBatch];
+                float gates[kBatch];
+                const int n = next_rows<GATES>(a, t, c, rows, gates, es);
+                if (n == 0) break;
+                uint4 q[kBatch];
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b)
+                    if (rows[b] >= 0) q[b] = a.src[static_cast<int64_t>(rows[b]) * a.vecs + v];
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) {
+                    if (rows[b] < 0) continue;
+                    float f[V::N];
+                    V::get(q[b], f);
+#pragma unroll
+                    for (int i = 0; i < V::N; ++i) acc[i] = GATES ? fmaf(gates[b], f[i], acc[i]) : acc[i] + f[i];
+                }
+                if (n < kBatch) break;
+            }
+            a.dst[t * a.vecs + v] = V::put(acc);
+        }
+    }
+}
+
+struct GradArgs {
+    RowArgs r;                 // src: dy [T][d], dst: drows (or null)
+    const uint4* rows;         // [cap][d] (read where dots)
+    bool dots;                 // dg is asked for
+    const float* prob;         // [T][E] (dlogits only)
+    float eps;
+    float* dgate;              // [T][E] or null
+    float* dlogits;            // [T][E] or null
+};
+
+// One token per NT threads (a wave or the workgroup): its rows in batches, dy
+// read again per batch (from L1), the batch's dot products reduced together.
+template <typename T, int NT>
+__global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
+    using V = Vec<T>;
+    constexpr int kSub = kThreads / NT;
+    __shared__ float dgs[kSub][kMaxExperts];
+    __shared__ float gs[kSub][kMaxExperts];
+    __shared__ float red[kBatch][kWaves];
+    const RowArgs& a = g.r;
+    const int sub = threadIdx.x / NT, id = threadIdx.x % NT, lane = lane_id(), wave = threadIdx.x / kWave;
+    auto sync = [&]() __attribute__((always_inline)) {
+        if constexpr (NT == kWave) wave_lds_sync();
+        else __syncthreads();
+    };
+    for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kSub; t0 < a.T; t0 += static_cast<int64_t>(gridDim.x) * kSub) {
+        const int64_t t = t0 + sub;
+        if (NT == kWave && t >= a.T) break;               // (the wave's own tokens are over)
+        for (int e = id; e < a.E; e += NT) { dgs[sub][e] = 0.f; gs[sub][e] = 0.f; }
+        sync();
+        Cursor c = first_rows(a, t);
+        float P = 0.f;
+        for (;;) {
+            int rows[kBatch], es[kBatch];
+            float gates[kBatch], dot[kBatch];
+            const int n = next_rows<true>(a, t, c, rows, gates, es);
+            if (n == 0) break;
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) dot[b] = 0.f;
+            for (int v = id; v < a.vecs; v += NT) {
+                float dy[V::N];
+                V::get(a.src[t * a.vecs + v], dy);
+                uint4 q[kBatch];
+                if (g.dots) {
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b)
+                        if (rows[b] >= 0) q[b] = g.rows[static_cast<int64_t>(rows[b]) * a.vecs + v];
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b) {
+                        if (rows[b] < 0) continue;
+                        float f[V::N];
+                        V::get(q[b], f);
+#pragma unroll
+                        for (int i = 0; i < V::N; ++i) dot[b] = fmaf(dy[i], f[i], dot[b]);
+                    }
+                }
+                if (a.dst) {
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b) {
+                        if (rows[b] < 0) continue;
+                        float o[V::N];
+#pragma unroll
+                        for (int i = 0; i < V::N; ++i) o[i] = gates[b] * dy[i];
+                        a.dst[static_cast<int64_t>(rows[b]) * a.vecs + v] = V::put(o);
+                    }
+                }
+            }
+            if (g.dots) {
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) {
+                    dot[b] = wave_sum(dot[b]);
+                    if (NT > kWave && lane == 0) red[b][wave] = dot[b];
+                }
+                if constexpr (NT > kWave) __syncthreads();
+                if (id == 0) {
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b) {
+                        if (b >= n) continue;
+                        float s = dot[b];
+                        if constexpr (NT > kWave) {
+                            s = 0.f;
+#pragma unroll
+                            for (int q = 0; q < kWaves; ++q) s += red[b][q];
+                        }
+                        dgs[sub][es[b]] = s;
+                        gs[sub][es[b]] = gates[b];
+                    }
+                }
+                if (g.dlogits) {
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b)
+                        if (b < n) P += g.prob[static_cast<size_t>(t) * a.E + es[b]];
+                }
+                sync();
+            }
+            if (n < kBatch) break;
+        }
+        if (!g.dots) continue;
+        sync();
+        float G = 0.f;
+        if (g.dlogits) {
+            // (every wave of the token adds the same numbers in the same order)
+            for (int e = lane; e < a.E; e += kWave) G = fmaf(gs[sub][e], dgs[sub][e], G);
+            G = wave_sum(G);
+        }
+        const float rest = P + g.eps > 0.f ? g.eps / (P + g.eps) : 0.f;
+        for (int e = id; e < a.E; e += NT) {
+            const size_t at = static_cast<size_t>(t) * a.E + e;
+            const float dg = dgs[sub][e];
+            if (g.dgate) g.dgate[at] = dg;
+            if (g.dlogits) {
+                const bool on = (a.mask[static_cast<size_t>(t) * a.W + e / kWave] >> (e % kWave)) & 1ull;
+                const float out = g.prob[at] * G * rest;
+                g.dlogits[at] = on ? fmaf(gs[sub][e], dg - G, -out) : -out;
+            }
+        }
+        sync();
+    }
+}
+
+int64_t row_blocks(int64_t units) { return std::max<int64_t>(1, std::min<int64_t>(units, int64_t{1} << 20)); }
+
+template <typename T>
+RowArgs row_args(const SortCall& c, const void* src, void* dst) {
+    const int vecs = c.d * static_cast<int>(sizeof(T)) / 16;
+    return RowArgs{c.mask, c.place, c.gate, c.T, c.E, mask_words(c.E), c.cap, vecs, std::max(1, kThreads / vecs),
+                   static_cast<const uint4*>(src), static_cast<uint4*>(dst)};
+}
+
+}  // namespace
+
+size_t sort_workspace(int32_t T, int E) {
+    if (static_cast<int64_t>(T) * mask_words(E) <= kDirectTokens) return 0;
+    const size_t chunks = (static_cast<size_t>(T) + kChunk - 1) / kChunk;
+    return (chunks + 1) * E * 4;
+}
+
+hipError_t launch_sort(const SortCall& c, const void* x, void* rows, int32_t* offsets, int32_t* token, int32_t* place,
+                       void* ws, hipStream_t s) {
+    const int W = mask_words(c.E), chunks = std::max(1, (c.T + kChunk - 1) / kChunk);
+    const bool direct = static_cast<int64_t>(c.T) * W <= kDirectTokens;
+    int32_t* const cnt = direct ? nullptr : static_cast<int32_t*>(ws);
+    int32_t* const total = direct ? nullptr : cnt + static_cast<size_t>(chunks) * c.E;
+    hipError_t e = hipSuccess;
+    if (!direct) {
+        count_kernel<<<chunks, kThreads, 0, s>>>(c.mask, c.T, c.E, W, cnt);
+        e = hipGetLastError();
+        if (e == hipSuccess) {
+            scan_kernel<<<c.E, kThreads, 0, s>>>(cnt, chunks, c.E, total);
+            e = hipGetLastError();
+        }
+    }
+    if (e != hipSuccess) return e;
+    const IndexArgs ia{c.mask, c.T, c.E, W, c.cap, cnt, total, offsets, token, place};
+    if (direct) index_kernel<16><<<chunks, 16 * kWave, 0, s>>>(ia);
+    else index_kernel<kWaves><<<chunks, kThreads, 0, s>>>(ia);
+    e = hipGetLastError();
+    if (e != hipSuccess || !rows || c.T == 0) return e;
+    SortCall p = c;
+    p.place = place;
+    const RowArgs a = c.bf16 ? row_args<uint16_t>(p, x, rows) : row_args<float>(p, x, rows);
+    spread_kernel<<<row_blocks((c.T + a.tpb - 1) / a.tpb), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_gather(const SortCall& c, const void* rows, void* y, hipStream_t s) {
+    const RowArgs a = c.bf16 ? row_args<uint16_t>(c, rows, y) : row_args<float>(c, rows, y);
+    const int64_t blocks = row_blocks((c.T + a.tpb - 1) / a.tpb);
+    if (c.bf16) {
+        if (c.gate) gather_kernel<uint16_t, true><<<blocks, kThreads, 0, s>>>(a);
+        else gather_kernel<uint16_t, false><<<blocks, kThreads, 0, s>>>(a);
+    } else {
+        if (c.gate) gather_kernel<float, true><<<blocks, kThreads, 0, s>>>(a);
+        else gather_kernel<float, false><<<blocks, kThreads, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_combine_grad(const SortCall& c, const void* dy, const void* rows, const float* prob, float eps, void* drows,
+                               float* dgate, float* dlogits, hipStream_t s) {
+    const RowArgs a = c.bf16 ? row_args<uint16_t>(c, dy, drows) : row_args<float>(c, dy, drows);
+    const GradArgs g{a, static_cast<const uint4*>(rows), dgate || dlogits, prob, eps, dgate, dlogits};
+    const bool one = a.vecs <= kWave;
+    const int64_t blocks = row_blocks(one ? (c.T + kWaves - 1) / kWaves : c.T);
+    if (c.bf16) {
+        if (one) combine_grad_kernel<uint16_t, kWave><<<blocks, kThreads, 0, s>>>(g);
+        else combine_grad_kernel<uint16_t, kThreads><<<blocks, kThreads, 0, s>>>(g);
+    } else {
+        if (one) combine_grad_kernel<float, kWave><<<blocks, kThreads, 0, s>>>(g);
+        else combine_grad_kernel<float, kThreads><<<blocks, kThreads, 0, s>>>(g);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace eat

@@ -176,6 +176,105 @@ class EatLayer:
         _hand_out(stream, caller, loss, count, mean)
         return loss, count, mean
 
+    # tokens sorted by expert, and back ------------------------------------
+    def _act(self):
+        return torch.bfloat16 if self.params.act_dtype == L.EAT_BF16 else torch.float32
+
+    def _expect_mask(self, mask: torch.Tensor, T: int, dev) -> None:
+        W = L.mask_words(self.params.E)
+        _expect("mask", mask, (torch.int64, torch.uint64), (T,) if mask.dim() == 1 and W == 1 else (T, W), dev)
+
+    def sort(self, x: Optional[torch.Tensor], mask: torch.Tensor, cap: Optional[int] = None,
+             rows: Optional[torch.Tensor] = None, stream=None):
+        """The tokens ``x`` sorted by the experts that ``mask`` (from ``route``)
+        selects (eat_sort_tokens): (rows [cap][d], offsets [E+1] int32, token
+        [cap] int32, place [T][E] int32); rows is None where ``x`` is.  ``cap``:
+        the rows to make room for; pairs past it are left out.  Without it, every
+        pair that the layer's mode can select has a row (EAT and Top-P: T E of
+        them).  Entries behind the last selected pair are not written.  Calls of one layer
+        share a workspace: order them on one stream.  ``stream`` as in ``balance_loss``."""
+        T, E, d, dev = mask.shape[0], self.params.E, self.params.d_model, mask.device
+        self._expect_mask(mask, T, dev)
+        _expect("x", x, self._act(), (T, d), dev)
+        if cap is None:
+            p = self.params
+            cap = T * (p.top_k if p.mode == L.EAT_MODE_TOPK else p.top_p_cap if p.mode == L.EAT_MODE_TOPP and p.top_p_cap else E)
+        if rows is not None and x is None:
+            raise ValueError("rows: nothing to write without x")
+        _expect("rows", rows, self._act(), (cap, d), dev)
+        caller = torch.cuda.current_stream(dev) if stream is not None else None
+        with _calling_on(stream, dev):
+            given = rows is not None
+            if x is not None and not given:
+                rows = torch.empty(cap, d, dtype=x.dtype, device=dev)
+            offsets = torch.empty(E + 1, dtype=torch.int32, device=dev)
+            token = torch.empty(cap, dtype=torch.int32, device=dev)
+            place = torch.empty(T, E, dtype=torch.int32, device=dev)
+            need = L.eat_sort_workspace_size(self.handle, T)
+            on = torch.cuda.current_stream(dev)
+            ws = self._bws.get(need, on) if need else None
+            L.eat_sort_tokens(self.handle, x, T, mask, cap, rows, offsets, token, place, ws, need, on)
+        _hand_out(stream, caller, offsets, token, place, *(() if given or rows is None else (rows,)))
+        return rows, offsets, token, place
+
+    def sort_backward(self, drows: torch.Tensor, mask: torch.Tensor, place: torch.Tensor,
+                      dx: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The gradient of ``sort``'s tokens [T][d] from its rows' (eat_sort_backward)."""
+        return self._from_rows(drows, mask, None, place, dx, "drows", "dx", stream)
+
+    def combine(self, rows: torch.Tensor, mask: torch.Tensor, gate: torch.Tensor, place: torch.Tensor,
+                y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The experts' ``rows`` [cap][d] back to their tokens, weighted by
+        ``gate`` (from ``route``; eat_combine): y [T][d]."""
+        _expect("gate", gate, torch.float32, (mask.shape[0], self.params.E), rows.device)
+        return self._from_rows(rows, mask, gate, place, y, "rows", "y", stream)
+
+    def _from_rows(self, rows, mask, gate, place, out, src_name, out_name, stream):
+        T, E, d, dev = mask.shape[0], self.params.E, self.params.d_model, rows.device
+        cap = rows.shape[0]
+        _expect(src_name, rows, self._act(), (cap, d), dev)
+        self._expect_mask(mask, T, dev)
+        _expect("place", place, torch.int32, (T, E), dev)
+        _expect(out_name, out, self._act(), (T, d), dev)
+        caller = torch.cuda.current_stream(dev) if stream is not None else None
+        with _calling_on(stream, dev):
+            given = out is not None
+            if not given:
+                out = torch.empty(T, d, dtype=rows.dtype, device=dev)
+            on = torch.cuda.current_stream(dev)
+            if gate is None:
+                L.eat_sort_backward(self.handle, rows, cap, T, mask, place, out, on)
+            else:
+                L.eat_combine(self.handle, rows, cap, T, mask, gate, place, out, on)
+        if not given:
+            _hand_out(stream, caller, out)
+        return out
+
+    def combine_backward(self, dy: torch.Tensor, rows: Optional[torch.Tensor], mask: torch.Tensor, gate: torch.Tensor,
+                         place: torch.Tensor, prob: Optional[torch.Tensor] = None, drows: Optional[torch.Tensor] = None,
+                         dgate: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, stream=None) -> None:
+        """The gradients of ``combine`` (eat_combine_backward), written to the
+        tensors given: of its rows, of the gates, and through the gates'
+        renormalisation and the softmax (``prob`` from ``route``) of the router's
+        scaled scores, as ``balance_loss`` gives its own."""
+        T, E, d, dev = mask.shape[0], self.params.E, self.params.d_model, dy.device
+        some = rows if rows is not None else drows
+        cap = 0 if some is None else some.shape[0]
+        _expect("dy", dy, self._act(), (T, d), dev)
+        _expect("rows", rows, self._act(), (cap, d), dev)
+        self._expect_mask(mask, T, dev)
+        _expect("gate", gate, torch.float32, (T, E), dev)
+        _expect("place", place, torch.int32, (T, E), dev)
+        _expect("prob", prob, torch.float32, (T, E), dev)
+        _expect("drows", drows, self._act(), (cap, d), dev)
+        _expect("dgate", dgate, torch.float32, (T, E), dev)
+        _expect("dlogits", dlogits, torch.float32, (T, E), dev)
+        if rows is None and (dgate is not None or dlogits is not None):
+            raise ValueError("rows: the gates' gradients need them")
+        with _calling_on(stream, dev):
+            L.eat_combine_backward(self.handle, dy, rows, cap, T, mask, gate, place, prob, drows, dgate, dlogits,
+                                   torch.cuda.current_stream(dev))
+
     def close(self) -> None:
         if self.handle:
             L.eat_destroy(self.handle)
