@@ -496,6 +496,83 @@ eat_status_t eat_combine_backward(eat_handle_t h, const void* dy, const void* ro
                                   const uint64_t* mask, const float* gate, const int32_t* place, const float* prob,
                                   void* drows, float* dgate, float* dlogits, hipStream_t stream);
 
+/* ---- matrices in 8 bits --------------------------------------------------------
+ *
+ * A matrix's numbers are held as OCP e4m3 (4 significant bits) with one power of
+ * two per 128 x 128 block, a row's with one per 128 elements: the smallest 2^k,
+ * -126 <= k, with largest finite magnitude / 2^k <= 448, held as the byte k + 127
+ * (e8m0; a block of zeros: 127).  Q(v) = round(v / 2^k) 2^k, ties to even; numbers
+ * that are not finite are held as NaN and leave k alone.  With the rows r of group g at
+ * offsets[g] .. offsets[g+1] (as eat_sort_tokens lays experts' rows out):
+ *
+ *   out_r = Q(x_row(r)) . Q(w_g)^T         row(r) = token[r], or r
+ *
+ * in fp32, rounded once.  A row that holds NaN or an infinity gives NaN in its
+ * own results alone, a weight row in its own feature's of its group.
+ *
+ * Storage of [groups][M][K]: q [groups][M][Kp] bytes, rows padded with zeros to Kp
+ * = K rounded up to 128; scales [groups][ceil(M / 128)][S] bytes, S = 4 ceil(K /
+ * 512).  Limits: M and K multiples of 8 up to 2^20, M Kp < 2^31, 1 <= groups <=
+ * 256, at most 2^24 rows (EAT_ERR_UNSUPPORTED beyond). */
+
+/* Bytes of q and of the scales of a matrix [groups][M][K]. */
+eat_status_t eat_fp8_size(int32_t groups, int32_t M, int32_t K, size_t* q_bytes, size_t* scale_bytes);
+
+/* w [groups][M][K] (dtype: eat_dtype_t) to q and scale, 256-byte aligned as every
+ * array of these calls that holds 8 bits; transposed = 1: the same numbers as a
+ * matrix [groups][K][M] (for the gradient of the rows).  Enqueues on `stream` only.
+ * Nothing may overlap (INVALID_ARG). */
+eat_status_t eat_fp8_quantize(const void* w, int32_t dtype, int32_t groups, int32_t M, int32_t K, int32_t transposed, void* q,
+                              void* scale, hipStream_t stream);
+
+/* Workspace of a product of `rows` rows of K elements out of src_rows. */
+eat_status_t eat_fp8_product_workspace_size(int32_t src_rows, int32_t rows, int32_t groups, int32_t M, int32_t K, size_t* bytes);
+
+/* The product above.
+ *   x        [src_rows][K] bf16
+ *   token    [rows] int32, kept inside [0, src_rows) by the call; NULL: row r is x's r (src_rows = rows)
+ *   offsets  [groups+1] int32, not decreasing, kept inside [0, rows]; NULL: all rows (groups = 1)
+ *   q, scale of the matrix [groups][M][K]
+ *   out      [rows][M] out_dtype; rows outside the groups are not written
+ *   ws       eat_fp8_product_workspace_size bytes, 256-byte aligned
+ * Nothing that is written may overlap another array of the call (INVALID_ARG).
+ * Enqueues on `stream` only; no synchronisation, no allocation, no memset.  Sums
+ * have a fixed order for given sizes.  Errors: EAT_ERR_INVALID_ARG,
+ * EAT_ERR_UNSUPPORTED, EAT_ERR_WORKSPACE, EAT_ERR_HIP. */
+eat_status_t eat_fp8_product(const void* x, int32_t src_rows, const int32_t* token, const int32_t* offsets, int32_t rows,
+                             const void* q, const void* scale, int32_t groups, int32_t M, int32_t K, void* out,
+                             int32_t out_dtype, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The SwiGLU experts of layer h (E, d_model, d_ffn; bf16 activations,
+ * EAT_ERR_UNSUPPORTED otherwise) on such products, over rows sorted by expert:
+ *
+ *   g_r = Q(x_token(r)) . Q(W1_e)^T    u_r = Q(x_token(r)) . Q(W3_e)^T    h = silu(g) u
+ *   y_r = Q(h_r) . Q(W2_e)^T
+ *
+ * and, the weights held constant, of the sorted tokens x_token(r) from dy, with g
+ * and u as `saved` keeps them (bf16), s = 1 / (1 + e^-g):
+ *
+ *   dh = Q(dy) . Q(W2)    dg = dh u s (1 + g (1 - s))    du = dh g s
+ *   dx_r = Q(dg_r) . Q(W1) + Q(du_r) . Q(W3)
+ *
+ * eat_fp8_experts_quantize writes the weights (bf16, eat_moe_forward's row-major
+ * layout) to `buf` once: 3 E F d bytes and their scales, with grads = 1 (for
+ * eat_fp8_experts_backward) their transposes too. */
+eat_status_t eat_fp8_experts_size(eat_handle_t h, int32_t grads, size_t* bytes);
+eat_status_t eat_fp8_experts_quantize(eat_handle_t h, const void* w1, const void* w3, const void* w2, int32_t grads, void* buf,
+                                      hipStream_t stream);
+/* Workspace of a call of `rows` rows: grads 0 the forward of T tokens, 1 the backward. */
+eat_status_t eat_fp8_experts_workspace_size(eat_handle_t h, int32_t T, int32_t rows, int32_t grads, size_t* bytes);
+/*   x [T][d_model] bf16;  token [rows], offsets [E+1] int32 (eat_sort_tokens), as in eat_fp8_product
+ *   y [rows][d_model] bf16;  saved [rows][2 d_ffn] bf16 (g, then u) or NULL;  dy, dx [rows][d_model] bf16
+ * Rows outside the segments are neither read (of dy and saved) nor written.  Other rules
+ * as eat_fp8_product's. */
+eat_status_t eat_fp8_experts_forward(eat_handle_t h, const void* x, int32_t T, const int32_t* token, const int32_t* offsets,
+                                     int32_t rows, const void* buf, void* y, void* saved, void* ws, size_t ws_bytes,
+                                     hipStream_t stream);
+eat_status_t eat_fp8_experts_backward(eat_handle_t h, const void* dy, const int32_t* offsets, int32_t rows, const void* buf,
+                                      const void* saved, void* dx, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ---- packed expert weights -------------------------------------------------
  *
  * Write the PACKED form (eat_layout_t) of `groups` row-major bf16 matrices

@@ -11,5 +11,7 @@ from ._lib import (  # noqa: F401
     eat_ppl_reset, eat_ppl_trend, EAT_LAYOUT_PACKED, EAT_LAYOUT_ROWS, eat_pack_weights, mask_words,
     eat_moe_forward_noalloc, EAT_NOALLOC_SCRATCH_BYTES, EAT_CE_DH, EAT_CE_DW, eat_ce_workspace_size, eat_ce_loss,
     eat_balance_workspace_size, eat_balance_loss, eat_sort_workspace_size, eat_sort_tokens, eat_sort_backward,
-    eat_combine, eat_combine_backward,
+    eat_combine, eat_combine_backward, eat_fp8_size, eat_fp8_quantize, eat_fp8_product_workspace_size, eat_fp8_product,
+    eat_fp8_experts_size, eat_fp8_experts_quantize, eat_fp8_experts_workspace_size, eat_fp8_experts_forward,
+    eat_fp8_experts_backward,
 )

@@ -105,6 +105,17 @@ def load() -> C.CDLL:
         lib.eat_sort_backward.argtypes = [P, P, C.c_int32, C.c_int32, P, P, P, P]
         lib.eat_combine.argtypes = [P, P, C.c_int32, C.c_int32, P, P, P, P, P]
         lib.eat_combine_backward.argtypes = [P, P, P, C.c_int32, C.c_int32, P, P, P, P, P, P, P, P]
+    if hasattr(lib, "eat_fp8_product"):
+        I, S = C.c_int32, C.POINTER(C.c_size_t)
+        lib.eat_fp8_size.argtypes = [I, I, I, S, S]
+        lib.eat_fp8_quantize.argtypes = [P, I, I, I, I, I, P, P, P]
+        lib.eat_fp8_product_workspace_size.argtypes = [I, I, I, I, I, S]
+        lib.eat_fp8_product.argtypes = [P, I, P, P, I, P, P, I, I, I, P, I, P, C.c_size_t, P]
+        lib.eat_fp8_experts_size.argtypes = [P, I, S]
+        lib.eat_fp8_experts_quantize.argtypes = [P, P, P, P, I, P, P]
+        lib.eat_fp8_experts_workspace_size.argtypes = [P, I, I, I, S]
+        lib.eat_fp8_experts_forward.argtypes = [P, P, I, P, P, I, P, P, P, P, C.c_size_t, P]
+        lib.eat_fp8_experts_backward.argtypes = [P, P, P, I, P, P, P, P, C.c_size_t, P]
     lib.eat_status_string.argtypes = [C.c_int]
     lib.eat_status_string.restype = C.c_char_p
     for name in ("eat_params_default", "eat_create", "eat_destroy", "eat_workspace_size", "eat_route_workspace_size",
@@ -112,7 +123,9 @@ def load() -> C.CDLL:
                  "eat_stack_workspace_size", "eat_stack_forward", "eat_ppl_workspace_size", "eat_ppl_reset",
                  "eat_ppl_trend", "eat_pack_weights", "eat_moe_forward_noalloc", "eat_ce_workspace_size", "eat_ce_loss",
                  "eat_balance_workspace_size", "eat_balance_loss", "eat_sort_workspace_size", "eat_sort_tokens",
-                 "eat_sort_backward", "eat_combine", "eat_combine_backward"):
+                 "eat_sort_backward", "eat_combine", "eat_combine_backward", "eat_fp8_size", "eat_fp8_quantize",
+                 "eat_fp8_product_workspace_size", "eat_fp8_product", "eat_fp8_experts_size", "eat_fp8_experts_quantize",
+                 "eat_fp8_experts_workspace_size", "eat_fp8_experts_forward", "eat_fp8_experts_backward"):
         if hasattr(lib, name):
             getattr(lib, name).restype = st
     _lib = lib
@@ -338,3 +351,58 @@ def eat_combine_backward(handle: int, dy, rows, cap: int, T: int, mask, gate, pl
     _check(load().eat_combine_backward(handle, _ptr(dy), _ptr(rows), int(cap), int(T), _ptr(mask), _ptr(gate), _ptr(place),
                                        _ptr(prob), _ptr(drows), _ptr(dgate), _ptr(dlogits), _stream(stream)),
            "eat_combine_backward")
+
+
+def eat_fp8_size(groups: int, M: int, K: int) -> "tuple[int, int]":
+    """(bytes of the e4m3 numbers, bytes of the scales) of a matrix [groups][M][K]."""
+    q, s = C.c_size_t(), C.c_size_t()
+    _check(load().eat_fp8_size(int(groups), int(M), int(K), C.byref(q), C.byref(s)), "eat_fp8_size")
+    return q.value, s.value
+
+
+def eat_fp8_quantize(w, dtype: int, groups: int, M: int, K: int, transposed: int, q, scale, stream=None) -> None:
+    _check(load().eat_fp8_quantize(_ptr(w), int(dtype), int(groups), int(M), int(K), int(transposed), _ptr(q), _ptr(scale),
+                                   _stream(stream)), "eat_fp8_quantize")
+
+
+def eat_fp8_product_workspace_size(src_rows: int, rows: int, groups: int, M: int, K: int) -> int:
+    b = C.c_size_t()
+    _check(load().eat_fp8_product_workspace_size(int(src_rows), int(rows), int(groups), int(M), int(K), C.byref(b)),
+           "eat_fp8_product_workspace_size")
+    return b.value
+
+
+def eat_fp8_product(x, src_rows: int, token, offsets, rows: int, q, scale, groups: int, M: int, K: int, out, out_dtype: int, ws,
+                    ws_bytes: int, stream=None) -> None:
+    _check(load().eat_fp8_product(_ptr(x), int(src_rows), _ptr(token), _ptr(offsets), int(rows), _ptr(q), _ptr(scale), int(groups),
+                                  int(M), int(K), _ptr(out), int(out_dtype), _ptr(ws), int(ws_bytes), _stream(stream)),
+           "eat_fp8_product")
+
+
+def eat_fp8_experts_size(handle: int, grads: int = 0) -> int:
+    b = C.c_size_t()
+    _check(load().eat_fp8_experts_size(handle, int(grads), C.byref(b)), "eat_fp8_experts_size")
+    return b.value
+
+
+def eat_fp8_experts_quantize(handle: int, w1, w3, w2, grads: int, buf, stream=None) -> None:
+    _check(load().eat_fp8_experts_quantize(handle, _ptr(w1), _ptr(w3), _ptr(w2), int(grads), _ptr(buf), _stream(stream)),
+           "eat_fp8_experts_quantize")
+
+
+def eat_fp8_experts_workspace_size(handle: int, T: int, rows: int, grads: int = 0) -> int:
+    b = C.c_size_t()
+    _check(load().eat_fp8_experts_workspace_size(handle, int(T), int(rows), int(grads), C.byref(b)),
+           "eat_fp8_experts_workspace_size")
+    return b.value
+
+
+def eat_fp8_experts_forward(handle: int, x, T: int, token, offsets, rows: int, buf, y, saved, ws, ws_bytes: int,
+                            stream=None) -> None:
+    _check(load().eat_fp8_experts_forward(handle, _ptr(x), int(T), _ptr(token), _ptr(offsets), int(rows), _ptr(buf), _ptr(y),
+                                          _ptr(saved), _ptr(ws), int(ws_bytes), _stream(stream)), "eat_fp8_experts_forward")
+
+
+def eat_fp8_experts_backward(handle: int, dy, offsets, rows: int, buf, saved, dx, ws, ws_bytes: int, stream=None) -> None:
+    _check(load().eat_fp8_experts_backward(handle, _ptr(dy), _ptr(offsets), int(rows), _ptr(buf), _ptr(saved), _ptr(dx), _ptr(ws),
+                                           int(ws_bytes), _stream(stream)), "eat_fp8_experts_backward")

@@ -712,6 +712,283 @@ eat_status_t eat_combine_backward(eat_handle_t h, const void* dy, const void* ro
     return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
 }
 
+// ---- matrices in 8 bits
+
+namespace {
+
+constexpr int32_t kMaxFp8Width = 1 << 20, kMaxFp8Rows = 1 << 24;
+
+eat_status_t check_fp8(int32_t groups, int32_t M, int32_t K) {
+    if (groups < 1 || M < 1 || K < 1) return EAT_ERR_INVALID_ARG;
+    if (groups > eat::kMaxExperts || M % 8 || K % 8 || M > kMaxFp8Width || K > kMaxFp8Width) return EAT_ERR_UNSUPPORTED;
+    return static_cast<int64_t>(M) * eat::fp8::pad(K) < (int64_t{1} << 31) ? EAT_OK : EAT_ERR_UNSUPPORTED;
+}
+
+struct Carver {
+    size_t off = 0;
+    size_t take(size_t bytes) {
+        const size_t at = off;
+        off += align256(bytes);
+        return at;
+    }
+};
+size_t q_bytes(int32_t groups, int32_t M, int32_t Kp) { return static_cast<size_t>(groups) * M * Kp; }
+size_t s_bytes(int32_t groups, int32_t M, int32_t lds) { return static_cast<size_t>(groups) * ((M + 127) / 128) * lds; }
+eat::fp8::Matrix matrix_at(const void* q, const void* s, int32_t M, int32_t K) {
+    return eat::fp8::Matrix{static_cast<uint8_t*>(const_cast<void*>(q)), static_cast<uint8_t*>(const_cast<void*>(s)), M,
+                            eat::fp8::pad(K), eat::fp8::scale_bytes(K)};
+}
+
+// A product's workspace: the rows in 8 bits and, where the reduction is split, its slices.
+struct ProductPlan {
+    size_t q, s, part, total;
+    int splits;
+    ProductPlan(const eat::fp8::Rows& r, int32_t M, int32_t K) {
+        Carver c;
+        splits = eat::fp8::product_slices(r, M, eat::fp8::pad(K));
+        q = c.take(static_cast<size_t>(r.src_rows) * eat::fp8::pad(K));
+        s = c.take(static_cast<size_t>(r.src_rows) * eat::fp8::scale_bytes(K));
+        part = c.take(splits > 1 ? static_cast<size_t>(splits) * r.cap * M * 4 : 0);
+        total = c.off;
+    }
+};
+
+// The experts' weights in their buffer.
+struct ExpertsPlan {
+    size_t w1, s1, w3, s3, w2, s2, w2t, s2t, w13t, s13t, total;
+    ExpertsPlan(const eat_params_t& p, bool grads) {
+        Carver c;
+        const int E = p.E, d = p.d_model, F = p.d_ffn, dp = eat::fp8::pad(d), Fp = eat::fp8::pad(F);
+        const int ld = eat::fp8::scale_bytes(d), lf = eat::fp8::scale_bytes(F), l2 = eat::fp8::scale_bytes(2 * Fp);
+        w1 = c.take(q_bytes(E, F, dp));
+        s1 = c.take(s_bytes(E, F, ld));
+        w3 = c.take(q_bytes(E, F, dp));
+        s3 = c.take(s_bytes(E, F, ld));
+        w2 = c.take(q_bytes(E, d, Fp));
+        s2 = c.take(s_bytes(E, d, lf));
+        w2t = c.take(grads ? q_bytes(E, F, dp) : 0);
+        s2t = c.take(grads ? s_bytes(E, F, ld) : 0);
+        w13t = c.take(grads ? q_bytes(E, d, 2 * Fp) : 0);
+        s13t = c.take(grads ? s_bytes(E, d, l2) : 0);
+        total = c.off;
+    }
+};
+
+// The workspace of one call over the experts.
+struct ExpertsCall {
+    size_t q, s, h, hs, part, total;
+    int up, down;                // slices of the first and of the second product
+    ExpertsCall(const eat_params_t& p, const eat::fp8::Rows& r, bool back) {
+        Carver c;
+        const int d = p.d_model, F = p.d_ffn, dp = eat::fp8::pad(d), Fp = eat::fp8::pad(F);
+        const int K2 = back ? 2 * Fp : Fp;
+        const size_t src = static_cast<size_t>(r.src_rows), n = static_cast<size_t>(r.cap);
+        up = back ? eat::fp8::product_slices(r, F, dp) : eat::fp8::gated_slices(r, F, dp);
+        down = eat::fp8::product_slices(r, d, K2);
+        q = c.take(src * dp);
+        s = c.take(src * eat::fp8::scale_bytes(d));
+        h = c.take(n * K2);
+        hs = c.take(n * eat::fp8::scale_bytes(K2));
+        // (the first product's slices are used up before the second's are written)
+        const size_t first = back ? up * n * F * 4 : up > 1 ? 2 * up * n * F * 4 : 0;
+        part = c.take(std::max<size_t>(first, down > 1 ? down * n * d * 4 : 0));
+        total = c.off;
+    }
+};
+
+eat_status_t check_experts(const eat_ctx* h, int32_t T, int32_t rows) {
+    if (!h || T < 0 || T > h->max_tokens || rows < 0 || (rows > 0 && T == 0)) return EAT_ERR_INVALID_ARG;
+    if (h->p.act_dtype != EAT_BF16 || rows > kMaxFp8Rows || T > kMaxFp8Rows) return EAT_ERR_UNSUPPORTED;
+    const eat_status_t st = check_fp8(h->p.E, h->p.d_model, 2 * eat::fp8::pad(h->p.d_ffn));
+    return st != EAT_OK ? st : check_fp8(h->p.E, h->p.d_ffn, h->p.d_model);
+}
+
+}  // namespace
+
+eat_status_t eat_fp8_size(int32_t groups, int32_t M, int32_t K, size_t* q_out, size_t* scale_out) {
+    if (!q_out || !scale_out) return EAT_ERR_INVALID_ARG;
+    const eat_status_t st = check_fp8(groups, M, K);
+    if (st != EAT_OK) return st;
+    *q_out = q_bytes(groups, M, eat::fp8::pad(K));
+    *scale_out = s_bytes(groups, M, eat::fp8::scale_bytes(K));
+    return EAT_OK;
+}
+
+eat_status_t eat_fp8_quantize(const void* w, int32_t dtype, int32_t groups, int32_t M, int32_t K, int32_t transposed, void* q,
+                              void* scale, hipStream_t stream) {
+    if ((dtype != EAT_F32 && dtype != EAT_BF16) || (transposed != 0 && transposed != 1)) return EAT_ERR_INVALID_ARG;
+    eat_status_t st = check_fp8(groups, M, K);
+    if (st == EAT_OK) st = check_fp8(groups, K, M);
+    if (st != EAT_OK) return st;
+    if (!w || !q || !scale || !aligned(w, 16) || !aligned(q, 256) || !aligned(scale, 256)) return EAT_ERR_INVALID_ARG;
+    const int32_t rows = transposed ? K : M, cols = transposed ? M : K;
+    const eat::fp8::Matrix m = matrix_at(q, scale, rows, cols);
+    if (clash({{q, q_bytes(groups, rows, m.Kp)}, {scale, s_bytes(groups, rows, m.lds)}},
+              {{w, static_cast<size_t>(groups) * M * K * (dtype == EAT_BF16 ? 2 : 4)}}, in_place_none))
+        return EAT_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    const hipError_t e = eat::fp8::launch_quantize_weights(w, dtype == EAT_BF16, groups, M, K, transposed ? nullptr : &m,
+                                                           transposed ? &m : nullptr, 0, stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+static eat_status_t check_product(int32_t src_rows, int32_t rows, int32_t groups, int32_t M, int32_t K) {
+    if (src_rows < 0 || rows < 0 || (rows > 0 && src_rows == 0)) return EAT_ERR_INVALID_ARG;
+    const eat_status_t st = check_fp8(groups, M, K);
+    if (st != EAT_OK) return st;
+    return src_rows > kMaxFp8Rows || rows > kMaxFp8Rows ? EAT_ERR_UNSUPPORTED : EAT_OK;
+}
+
+eat_status_t eat_fp8_product_workspace_size(int32_t src_rows, int32_t rows, int32_t groups, int32_t M, int32_t K, size_t* bytes) {
+    if (!bytes) return EAT_ERR_INVALID_ARG;
+    const eat_status_t st = check_product(src_rows, rows, groups, M, K);
+    if (st != EAT_OK) return st;
+    // (with offsets there are more tiles, so fewer slices: the larger of the two)
+    const int32_t dummy = 0;
+    const ProductPlan all(eat::fp8::Rows{nullptr, nullptr, src_rows, rows, groups}, M, K);
+    const ProductPlan cut(eat::fp8::Rows{nullptr, &dummy, src_rows, rows, groups}, M, K);
+    *bytes = std::max(all.total, cut.total);
+    return EAT_OK;
+}
+
+eat_status_t eat_fp8_product(const void* x, int32_t src_rows, const int32_t* token, const int32_t* offsets, int32_t rows,
+                             const void* q, const void* scale, int32_t groups, int32_t M, int32_t K, void* out,
+                             int32_t out_dtype, void* ws, size_t ws_bytes, hipStream_t stream) {
+    const eat_status_t st = check_product(src_rows, rows, groups, M, K);
+    if (st != EAT_OK) return st;
+    if ((out_dtype != EAT_F32 && out_dtype != EAT_BF16) || (!offsets && groups != 1) || (!token && src_rows != rows)) return EAT_ERR_INVALID_ARG;
+    if (!q || !scale || (rows > 0 && (!x || !out))) return EAT_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(token, 4) || !aligned(offsets, 4) || !aligned(q, 256) || !aligned(scale, 256) || !aligned(out, 16))
+        return EAT_ERR_INVALID_ARG;
+    const eat::fp8::Rows r{token, offsets, src_rows, rows, groups};
+    const ProductPlan p(r, M, K);
+    if (p.total > 0 && (!ws || ws_bytes < p.total)) return EAT_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
+    const eat::fp8::Matrix w = matrix_at(q, scale, M, K);
+    const size_t n = static_cast<size_t>(rows), xb = static_cast<size_t>(src_rows) * K * 2;
+    if (clash({{out, n * M * (out_dtype == EAT_BF16 ? 2 : 4)}, {ws, p.total}},
+              {{x, xb}, {token, n * 4}, {offsets, (static_cast<size_t>(groups) + 1) * 4}, {q, q_bytes(groups, M, w.Kp)},
+               {scale, s_bytes(groups, M, w.lds)}}, in_place_none))
+        return EAT_ERR_INVALID_ARG;
+    if (rows == 0) return EAT_OK;
+    uint8_t* const base = static_cast<uint8_t*>(ws);
+    (void)hipGetLastError();
+    hipError_t e = eat::fp8::launch_quantize_rows(static_cast<const uint16_t*>(x), r, K, base + p.q, base + p.s, stream);
+    if (e == hipSuccess)
+        e = eat::fp8::launch_product(r, base + p.q, base + p.s, w.lds, w, out_dtype == EAT_BF16, out, p.splits,
+                                     reinterpret_cast<float*>(base + p.part), stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+eat_status_t eat_fp8_experts_size(eat_handle_t h, int32_t grads, size_t* bytes) {
+    const eat_status_t st = check_experts(h, 0, 0);
+    if (st != EAT_OK) return st;
+    if (!bytes || (grads != 0 && grads != 1)) return EAT_ERR_INVALID_ARG;
+    *bytes = ExpertsPlan(h->p, grads == 1).total;
+    return EAT_OK;
+}
+
+eat_status_t eat_fp8_experts_quantize(eat_handle_t h, const void* w1, const void* w3, const void* w2, int32_t grads, void* buf,
+                                      hipStream_t stream) {
+    const eat_status_t st = check_experts(h, 0, 0);
+    if (st != EAT_OK) return st;
+    if (!w1 || !w3 || !w2 || !buf || (grads != 0 && grads != 1)) return EAT_ERR_INVALID_ARG;
+    if (!aligned(w1, 16) || !aligned(w3, 16) || !aligned(w2, 16) || !aligned(buf, 256)) return EAT_ERR_INVALID_ARG;
+    const eat_params_t& p = h->p;
+    const ExpertsPlan x(p, grads == 1);
+    const size_t wb = static_cast<size_t>(p.E) * p.d_model * p.d_ffn * 2;
+    if (clash({{buf, x.total}}, {{w1, wb}, {w3, wb}, {w2, wb}}, in_place_none)) return EAT_ERR_INVALID_ARG;
+    uint8_t* const b = static_cast<uint8_t*>(buf);
+    const int E = p.E, d = p.d_model, F = p.d_ffn, Fp = eat::fp8::pad(F);
+    const eat::fp8::Matrix m1 = matrix_at(b + x.w1, b + x.s1, F, d), m3 = matrix_at(b + x.w3, b + x.s3, F, d),
+                           m2 = matrix_at(b + x.w2, b + x.s2, d, F), t2 = matrix_at(b + x.w2t, b + x.s2t, F, d),
+                           t13 = matrix_at(b + x.w13t, b + x.s13t, d, 2 * Fp);
+    (void)hipGetLastError();
+    hipError_t e = eat::fp8::launch_quantize_weights(w1, true, E, F, d, &m1, grads ? &t13 : nullptr, 0, stream);
+    if (e == hipSuccess) e = eat::fp8::launch_quantize_weights(w3, true, E, F, d, &m3, grads ? &t13 : nullptr, Fp, stream);
+    if (e == hipSuccess) e = eat::fp8::launch_quantize_weights(w2, true, E, d, F, &m2, grads ? &t2 : nullptr, 0, stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+eat_status_t eat_fp8_experts_workspace_size(eat_handle_t h, int32_t T, int32_t rows, int32_t grads, size_t* bytes) {
+    const eat_status_t st = check_experts(h, grads == 1 && rows > 0 ? 1 : T, rows);
+    if (st != EAT_OK) return st;
+    if (!bytes || (grads != 0 && grads != 1)) return EAT_ERR_INVALID_ARG;
+    const int32_t dummy = 0;
+    *bytes = ExpertsCall(h->p, eat::fp8::Rows{nullptr, &dummy, grads ? rows : T, rows, h->p.E}, grads == 1).total;
+    return EAT_OK;
+}
+
+eat_status_t eat_fp8_experts_forward(eat_handle_t h, const void* x, int32_t T, const int32_t* token, const int32_t* offsets,
+                                     int32_t rows, const void* buf, void* y, void* saved, void* ws, size_t ws_bytes,
+                                     hipStream_t stream) {
+    const eat_status_t st = check_experts(h, T, rows);
+    if (st != EAT_OK) return st;
+    if (!buf || !offsets || (rows > 0 && (!x || !token || !y))) return EAT_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(token, 4) || !aligned(offsets, 4) || !aligned(buf, 256) || !aligned(y, 16) || !aligned(saved, 16))
+        return EAT_ERR_INVALID_ARG;
+    const eat_params_t& p = h->p;
+    const eat::fp8::Rows r{token, offsets, T, rows, p.E};
+    const ExpertsCall c(p, r, false);
+    if (c.total > 0 && (!ws || ws_bytes < c.total)) return EAT_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
+    const ExpertsPlan w(p, false);            // (the transposes lie behind)
+    const size_t n = static_cast<size_t>(rows), d = static_cast<size_t>(p.d_model);
+    if (clash({{y, n * d * 2}, {saved, n * p.d_ffn * 4}, {ws, c.total}},
+              {{x, T * d * 2}, {token, n * 4}, {offsets, (static_cast<size_t>(p.E) + 1) * 4}, {buf, w.total}}, in_place_none))
+        return EAT_ERR_INVALID_ARG;
+    if (rows == 0) return EAT_OK;
+    const uint8_t* const b = static_cast<const uint8_t*>(buf);
+    uint8_t* const base = static_cast<uint8_t*>(ws);
+    const int F = p.d_ffn, ld = eat::fp8::scale_bytes(p.d_model);
+    float* const part = reinterpret_cast<float*>(base + c.part);
+    (void)hipGetLastError();
+    hipError_t e = eat::fp8::launch_quantize_rows(static_cast<const uint16_t*>(x), r, p.d_model, base + c.q, base + c.s, stream);
+    if (e == hipSuccess)
+        e = eat::fp8::launch_gated(r, base + c.q, base + c.s, ld, matrix_at(b + w.w1, b + w.s1, F, p.d_model),
+                                   matrix_at(b + w.w3, b + w.s3, F, p.d_model), base + c.h, base + c.hs,
+                                   static_cast<uint16_t*>(saved), c.up, part, stream);
+    if (e == hipSuccess)
+        e = eat::fp8::launch_product(eat::fp8::Rows{nullptr, offsets, rows, rows, p.E}, base + c.h, base + c.hs, eat::fp8::scale_bytes(F),
+                                     matrix_at(b + w.w2, b + w.s2, p.d_model, F), true, y, c.down, part, stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
+eat_status_t eat_fp8_experts_backward(eat_handle_t h, const void* dy, const int32_t* offsets, int32_t rows, const void* buf,
+                                      const void* saved, void* dx, void* ws, size_t ws_bytes, hipStream_t stream) {
+    const eat_status_t st = check_experts(h, rows > 0 ? 1 : 0, rows);
+    if (st != EAT_OK) return st;
+    if (!buf || !offsets || (rows > 0 && (!dy || !saved || !dx))) return EAT_ERR_INVALID_ARG;
+    if (!aligned(dy, 16) || !aligned(offsets, 4) || !aligned(buf, 256) || !aligned(saved, 16) || !aligned(dx, 16)) return EAT_ERR_INVALID_ARG;
+    const eat_params_t& p = h->p;
+    const eat::fp8::Rows r{nullptr, offsets, rows, rows, p.E};
+    const ExpertsCall c(p, r, true);
+    if (c.total > 0 && (!ws || ws_bytes < c.total)) return EAT_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return EAT_ERR_INVALID_ARG;
+    const ExpertsPlan w(p, true);
+    const size_t n = static_cast<size_t>(rows), db = n * p.d_model * 2;
+    if (clash({{dx, db}, {ws, c.total}},
+              {{dy, db}, {offsets, (static_cast<size_t>(p.E) + 1) * 4}, {buf, w.total}, {saved, n * p.d_ffn * 4}},
+              [&](const void* o, const void* i) { return o == dx && i == dy; }))
+        return EAT_ERR_INVALID_ARG;
+    if (rows == 0) return EAT_OK;
+    const uint8_t* const b = static_cast<const uint8_t*>(buf);
+    uint8_t* const base = static_cast<uint8_t*>(ws);
+    const int F = p.d_ffn, Fp = eat::fp8::pad(F), ld = eat::fp8::scale_bytes(p.d_model), l2 = eat::fp8::scale_bytes(2 * Fp);
+    float* const part = reinterpret_cast<float*>(base + c.part);
+    (void)hipGetLastError();
+    hipError_t e = eat::fp8::launch_quantize_rows(static_cast<const uint16_t*>(dy), r, p.d_model, base + c.q, base + c.s, stream);
+    if (e == hipSuccess)
+        e = eat::fp8::launch_product(r, base + c.q, base + c.s, ld, matrix_at(b + w.w2t, b + w.s2t, F, p.d_model), false,
+                                     nullptr, c.up, part, stream);
+    if (e == hipSuccess)
+        e = eat::fp8::launch_gate_backward(r, part, c.up, F, static_cast<const uint16_t*>(saved), base + c.h, base + c.hs, l2, stream);
+    if (e == hipSuccess)
+        e = eat::fp8::launch_product(r, base + c.h, base + c.hs, l2, matrix_at(b + w.w13t, b + w.s13t, p.d_model, 2 * Fp), true, dx,
+                                     c.down, part, stream);
+    return e == hipSuccess ? EAT_OK : EAT_ERR_HIP;
+}
+
 const char* eat_status_string(eat_status_t s) {
     // a C caller may pass any int: read the argument's bits, not the enum
     // (a C++ enum value outside its enumerators' range is undefined)

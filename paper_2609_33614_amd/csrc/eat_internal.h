@@ -309,6 +309,42 @@ hipError_t launch_gather(const SortCall& c, const void* rows, void* y, hipStream
 hipError_t launch_combine_grad(const SortCall& c, const void* dy, const void* rows, const float* prob, float eps, void* drows,
                                float* dgate, float* dlogits, hipStream_t s);
 
+// Products in 8 bits (fp8.hip).  A matrix [groups][M][K]: e4m3 rows of Kp = K padded
+// to whole blocks of 128, and a byte per 128 x 128 block in rows of `lds`.
+namespace fp8 {
+struct Matrix {
+    uint8_t* q;
+    uint8_t* s;
+    int M, Kp, lds;
+};
+inline int pad(int K) { return (K + 127) / 128 * 128; }
+inline int scale_bytes(int K) { return (K + 511) / 512 * 4; }
+// The rows of a call: row r of `cap` is row token[r] (null: r) of src_rows, group by
+// group as offsets [groups + 1] says (null: one group of all).
+struct Rows {
+    const int32_t* token;
+    const int32_t* offsets;
+    int src_rows, cap, groups;
+};
+// The rows x of a call in 8 bits: all of src_rows where they are gathered, those of the groups otherwise.
+hipError_t launch_quantize_rows(const uint16_t* x, const Rows& r, int K, uint8_t* q, uint8_t* scale, hipStream_t s);
+// w [groups][M][K] into m and, transposed ([groups][K][M], from column `column` of its rows), t (either may be null).
+hipError_t launch_quantize_weights(const void* w, bool bf16, int groups, int M, int K, const Matrix* m, const Matrix* t, int column,
+                                   hipStream_t s);
+// Slices of the reduction that the launches below take (1: `part` is not used).
+int product_slices(const Rows& r, int M, int Kp);
+int gated_slices(const Rows& r, int M, int Kp);
+// out [cap][M] (null: the slices [splits][cap][M] stay in part)
+hipError_t launch_product(const Rows& r, const uint8_t* q, const uint8_t* sq, int lds, const Matrix& w, bool bf16, void* out,
+                              int splits, float* part, hipStream_t s);
+// h [cap][pad(M)], sh [cap][scale_bytes(M)]: silu(w1 x) (w3 x) in 8 bits; saved [cap][2 M] bf16 or null; part: 2 x the slices
+hipError_t launch_gated(const Rows& r, const uint8_t* q, const uint8_t* sq, int lds, const Matrix& w1, const Matrix& w3,
+                            uint8_t* h, uint8_t* sh, uint16_t* saved, int splits, float* part, hipStream_t s);
+// dh's slices [splits][cap][F] and saved -> [dg | du] in 8 bits, [cap][2 pad(F)]
+hipError_t launch_gate_backward(const Rows& r, const float* dh, int splits, int F, const uint16_t* saved, uint8_t* q, uint8_t* scale,
+                                    int lds, hipStream_t s);
+}  // namespace fp8
+
 // Forward entry points (api.cpp): host-side argument checks, and the
 // enqueue of one layer forward into a workspace of plan_workspace(h, T).total
 // bytes at `ws` (arguments checked, T > 0).  `residual` (bf16 [T][d] or

@@ -1,0 +1,864 @@
+// Products of rows and matrices held in 8 bits with a power of two per block of
+// 128 (gfx950): the grouped product over expert segments, the SwiGLU up
+// projection with its result quantised again, and the slices of a split reduction.
+//
+//   y[r][m] = sum_b 2^(kx(r, b) + kw(m / 128, b)) sum_{k in b} qx[r][k] qw[m][k]
+//
+// v_mfma_scale_f32_32x32x64_f8f6f4 takes both scales with its operands (a byte per
+// lane), so the sums stay in its fp32 accumulators from the first block to the
+// last; weights are A and rows B, so that a lane ends with 4 consecutive features
+// of one row.
+//
+// A workgroup owns a tile of TM rows x NW weight rows (the gated projection: NW / 2
+// rows of W1 and the matching ones of W3) and walks the reduction in chunks of one
+// block through a ring of LDS stages filled by direct global->LDS loads several
+// chunks ahead.  The grid is persistent, its work list cut into one contiguous
+// part per XCD, and the loads run on over the ends of the items, whatever their
+// length.
+#include <algorithm>
+#include <type_traits>
+
+#include "fp8_device.h"
+#include "loss_gemm.h"
+
+namespace eat {
+namespace fp8 {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+template <int TM_, int NW_, int WT_, int WW_, int STAGES_, bool NT_>
+struct Tile {
+    static constexpr int TM = TM_, NW = NW_, WT = WT_, WW = WW_, STAGES = STAGES_;
+    static constexpr bool NT = NT_;                       // weights stream past the caches
+    static constexpr int kWaves = WT * WW, kThreads = kWaves * kWave;
+    static constexpr int TF = TM / (32 * WT), WF = NW / (32 * WW);
+    static constexpr int kTokens = TM * kBlk;             // bytes of a stage's rows
+    static constexpr int kScales = kTokens + NW * kBlk;   // where a stage's scales begin: 256 bytes per wave
+    static constexpr int kStage = kScales + 256 * kWaves;
+    static constexpr int kBT = TM / 8 / kWaves, kBW = NW / 8 / kWaves;   // 1 KB loads per wave
+    static constexpr int kLoads = kBT + kBW + 1;          // ... and the scales
+    static constexpr int kAhead = STAGES - 1;             // chunks on their way beside the one computed
+    static_assert(kBT * 8 * kWaves == TM && kBW * 8 * kWaves == NW && 8 * kBT <= 32, "loads split evenly over the waves");
+    static_assert(TF * 32 * WT == TM && WF * 32 * WW == NW && WF == 2 && NW == 256, "fragments cover the tile; a gated tile is one block wide");
+    static_assert(kAhead >= 1 && kAhead <= 3, "waits count up to three chunks");
+};
+using Big = Tile<256, 256, 2, 4, 2, false>;
+using Mid = Tile<128, 256, 2, 4, 3, false>;
+using Few = Tile<32, 256, 1, 4, 4, true>;
+
+// SLICES is fp32 slices of the reduction, EXACT the same on exact sums, as ROWS32.
+enum Out { ROWS16, ROWS32, SLICES, EXACT, GATED };
+
+struct Args {
+    const uint8_t* wa;         // [groups][M][Kp]
+    const uint8_t* wb;         // GATED: W3
+    const uint8_t* sa;         // [groups][ceil(M / 128)][ldw] scales
+    const uint8_t* sb;
+    int ldw;
+    const uint8_t* x;          // [src_rows][Kp]
+    const uint8_t* sx;         // [src_rows][ldx]
+    int ldx, src_rows;
+    const int32_t* token;      // row -> row of x, or null
+    const int32_t* offsets;    // [groups + 1], or null: one group of all rows
+    int groups, cap, M, Kp;
+    int splits;                // SLICES: of the reduction
+    int xcds;
+    void* out;                 // ROWS16, ROWS32: [cap][M]; SLICES: [splits][cap][M] fp32; GATED: [cap][Mp] 8 bits
+    uint8_t* sout;             // GATED: [cap][ldo] scales
+    int ldo;
+    uint16_t* saved;           // GATED: [cap][2 M] bf16 or null
+};
+
+// 16-byte vector v of 128-byte row r in LDS: two rows to a line of the 64 banks,
+// the vector index XORed with the line so that 16 rows' vectors v lie on
+// distinct banks.
+__device__ __forceinline__ int swz(int r) { return (static_cast<unsigned>(r) >> 1) & 7; }
+__device__ __forceinline__ int at_row(int r, int v) { return r * kBlk + ((v ^ swz(r)) << 4); }
+
+// A work item: rows [r0, r0 + n) of group e against weight rows from m0, chunks
+// [c0, c0 + nc) of the reduction (slice sp).
+struct Item {
+    int e, r0, n, m0, c0, nc, sp;
+};
+
+// Where this lane's loads of an item's next chunk come from.  Row block j of the
+// wave holds rows 8 (wave + kWaves j) + lane / 8 of the tile, a 16-byte vector per
+// lane; lane l < 8 kBT also fetches the word of scales of row 8 (wave + kWaves (l /
+// 8)) + l % 8, lanes 32 and 33 those of the two blocks of weight rows.
+template <class C>
+struct Loads {
+    const uint8_t* rows[C::kBT];
+    uint64_t live[C::kBT];                 // lanes whose row is in the item
+    const uint8_t* wmat[C::kBW];
+    uint32_t woff[C::kBW];
+    const uint8_t* scale;
+};
+
+// silu(a) b for a result that is rounded to 4 bits: the hardware reciprocal will
+// do.  Both factors a quarter: the reciprocal gives no denormals.
+__device__ __forceinline__ float swiglu(float a, float b) {
+    return 0.25f * a * __builtin_amdgcn_rcpf(fmaf(0.25f, __expf(-a), 0.25f)) * b;
+}
+
+// Eight e4m3 numbers times a power of two as bf16, which holds them exactly.
+__device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
+                 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+template <Out OUT, class C>
+__global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
+    constexpr int TM = C::TM, NW = C::NW, TF = C::TF, WF = C::WF, kOut = OUT == GATED ? NW / 2 : NW;
+    constexpr bool kSlices = OUT == SLICES || OUT == EXACT, kExact = OUT == ROWS32 || OUT == EXACT;
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[C::STAGES * C::kStage];
+    __shared__ int tstart[kMaxExperts + 1];
+    __shared__ int soff[kMaxExperts + 1];
+    __shared__ __attribute__((aligned(256))) int32_t index[2][C::kWaves][kWave];   // the rows of x of the next items
+
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
+    const int nch = a.Kp / kBlk, nxm = (a.M + kOut - 1) / kOut;
+    const int splits = kSlices ? a.splits : 1;
+
+    // segments, kept inside the rows there are whatever the offsets hold
+    int ntiles;
+    if (a.offsets) {
+        for (int g = threadIdx.x; g <= a.groups; g += C::kThreads) soff[g] = min(max(a.offsets[g], 0), a.cap);
+        __syncthreads();
+        if (wave == 0) {
+            int carry = 0;
+            for (int g0 = 0; g0 < a.groups; g0 += kWave) {
+                const int g = g0 + lane;
+                int c = g < a.groups ? (max(soff[g + 1] - soff[g], 0) + TM - 1) / TM : 0;
+                c = wave_scan(c);
+                if (g < a.groups) tstart[g + 1] = carry + c;
+                carry += __builtin_amdgcn_readlane(c, kWave - 1);
+            }
+            if (lane == 0) tstart[0] = 0;
+        }
+        __syncthreads();
+        ntiles = __builtin_amdgcn_readfirstlane(tstart[a.groups]);
+    } else {
+        ntiles = (a.cap + TM - 1) / TM;
+    }
+    const int nx = nxm * splits;
+    const int work = ntiles * nx;             // (below 2^31: the entry points' limits)
+    const int xcd = blockIdx.x % a.xcds, slot = blockIdx.x / a.xcds, per = gridDim.x / a.xcds;
+    const int part = (work + a.xcds - 1) / a.xcds, wbeg = xcd * part, wend = min(work, wbeg + part);
+
+    // item wid of the list: a group's items weight tile by weight tile (slices
+    // outermost), its row tiles adjacent.  `es`: the group found last (items only
+    // increase).
+    auto item_at = [&](int wid, int& es) __attribute__((always_inline)) {
+        Item it;
+        int tile, xt;
+        if (a.offsets) {
+            while (tstart[es + 1] * nx <= wid) ++es;
+            const int nt = tstart[es + 1] - tstart[es];
+            const int local = wid - tstart[es] * nx;
+            xt = local / nt;
+            tile = local % nt;
+            it.e = es;
+            it.r0 = soff[es] + tile * TM;
+            it.n = min(TM, soff[es + 1] - it.r0);
+        } else {
+            xt = wid / ntiles;
+            tile = wid % ntiles;
+            it.e = 0;
+            it.r0 = tile * TM;
+            it.n = min(TM, a.cap - it.r0);
+        }
+        it.sp = xt / nxm;
+        it.m0 = (xt - it.sp * nxm) * kOut;
+        it.c0 = static_cast<int>(static_cast<int64_t>(nch) * it.sp / splits);
+        it.nc = static_cast<int>(static_cast<int64_t>(nch) * (it.sp + 1) / splits) - it.c0;
+        it.e = __builtin_amdgcn_readfirstlane(it.e);
+        it.r0 = __builtin_amdgcn_readfirstlane(it.r0);
+        it.n = __builtin_amdgcn_readfirstlane(it.n);
+        it.m0 = __builtin_amdgcn_readfirstlane(it.m0);
+        it.c0 = __builtin_amdgcn_readfirstlane(it.c0);
+        it.nc = __builtin_amdgcn_readfirstlane(it.nc);
+        it.sp = __builtin_amdgcn_readfirstlane(it.sp);
+        return it;
+    };
+
+    if (wbeg + slot >= wend) return;          // uniform over the workgroup
+
+    // Lane l < 8 kBT stands for row 8 (wave + kWaves (l / 8)) + l % 8 of the tile
+    // (rows past the item's: its last).
+    auto tile_row = [&](const Item& it) __attribute__((always_inline)) {
+        const int l = lane & (8 * C::kBT - 1);
+        return it.r0 + min(8 * (wave + C::kWaves * (l / 8)) + l % 8, it.n - 1);
+    };
+    auto fetch_index = [&](const Item& it, int p) __attribute__((always_inline)) {
+        lds_load4(a.token + tile_row(it), lds_address(&index[p][wave][0]));
+    };
+    auto item_loads = [&](const Item& it, int srow) __attribute__((always_inline)) {
+        Loads<C> L;
+        const int slot16 = lane % 8;
+        srow = static_cast<int>(min(static_cast<unsigned>(srow), static_cast<unsigned>(a.src_rows - 1)));
+#pragma unroll
+        for (int j = 0; j < C::kBT; ++j) {
+            const int r = 8 * (wave + C::kWaves * j) + lane / 8;
+            L.live[j] = ballot(r < it.n);
+            L.rows[j] = a.x + static_cast<size_t>(__shfl(srow, 8 * j + lane / 8, kWave)) * a.Kp + it.c0 * kBlk + ((slot16 ^ swz(r)) << 4);
+        }
+        const size_t emat = static_cast<size_t>(it.e) * a.M * a.Kp;
+#pragma unroll
+        for (int j = 0; j < C::kBW; ++j) {
+            const int r0 = 8 * (wave + C::kWaves * j), r = r0 + lane / 8;
+            // (a last tile past M loads its last row again; those results are not used)
+            const int row = min(it.m0 + (OUT == GATED ? r & (NW / 2 - 1) : r), a.M - 1);
+            L.woff[j] = static_cast<uint32_t>(row) * static_cast<uint32_t>(a.Kp) + it.c0 * kBlk + ((slot16 ^ swz(r)) << 4);
+            L.wmat[j] = (OUT == GATED && r0 >= NW / 2 ? a.wb : a.wa) + emat;
+        }
+        const int mb = (a.M + kBlk - 1) / kBlk, b = lane & 1;
+        const int blk = min(it.m0 / kBlk + (OUT == GATED ? 0 : b), mb - 1);
+        const uint8_t* const w = (OUT == GATED && b ? a.sb : a.sa) + (static_cast<size_t>(it.e) * mb + blk) * a.ldw;
+        L.scale = lane < 32 ? a.sx + static_cast<size_t>(srow) * a.ldx : w;
+        return L;
+    };
+    // chunk c of the item (from its c0) into stage st
+    auto issue = [&](const Loads<C>& L, const Item& it, uint8_t* st, int c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < C::kBT; ++j)
+            lds_load16_masked(L.rows[j] + c * kBlk, lds_address(st + 1024 * (wave + C::kWaves * j)), L.live[j]);
+#pragma unroll
+        for (int j = 0; j < C::kBW; ++j) {
+            const uint8_t* const src = L.wmat[j] + (L.woff[j] + static_cast<uint32_t>(c) * kBlk);
+            const uint32_t dst = lds_address(st + C::kTokens + 1024 * (wave + C::kWaves * j));
+            if constexpr (C::NT) lds_load16_nt(src, dst);
+            else lds_load16(src, dst);
+        }
+        lds_load4(L.scale + ((it.c0 + c) & ~3), lds_address(st + C::kScales + 256 * wave));
+    };
+
+    // The load side runs ahead of the products by up to kAhead chunks, over the
+    // ends of items.  The rows of x that an item gathers are fetched to LDS while
+    // the item before is loaded: kAhead or more chunks' loads later (else after a
+    // wait for all) they have arrived, since loads complete in order.
+    int lwid = wbeg + slot;
+    int les = 0, lc = 0, lpar = 0, ls = 0, ahead = 0;
+    Item lit = item_at(lwid, les), lnext = lit;
+    bool more = lwid + per < wend, live = true;
+    Loads<C> L = item_loads(lit, a.token ? a.token[tile_row(lit)] : tile_row(lit));
+    auto look_ahead = [&]() __attribute__((always_inline)) {
+        if (!more) return;
+        lnext = item_at(lwid + per, les);
+        if (a.token) fetch_index(lnext, lpar);
+    };
+    look_ahead();
+    auto issue_next = [&]() __attribute__((always_inline)) {
+        if (!live) return;
+        issue(L, lit, ring + ls * C::kStage, lc);
+        ls = ls + 1 == C::STAGES ? 0 : ls + 1;
+        ++ahead;
+        if (++lc < lit.nc) return;
+        lc = 0;
+        if (!more) {
+            live = false;
+            return;
+        }
+        int srow = tile_row(lnext);
+        if (a.token) {
+            if (lit.nc < C::kAhead + 1) wait_vm<0>();
+            asm volatile("" ::: "memory");
+            srow = *static_cast<volatile int32_t*>(&index[lpar][wave][lane]);
+        }
+        lpar ^= 1;
+        lit = lnext;
+        lwid += per;
+        more = lwid + per < wend;
+        L = item_loads(lit, srow);
+        look_ahead();
+    };
+    for (int c = 0; c < C::kAhead; ++c) issue_next();
+
+    const int l32 = lane & 31, lh = lane >> 5;
+    const int wm = wave / C::WW, wn = wave % C::WW;       // row group, weight group
+    const int brow = 32 * TF * wm;
+    auto arow = [&](int i) __attribute__((always_inline)) {
+        return OUT == GATED ? NW / 2 * i + 32 * wn : 64 * wn + 32 * i;
+    };
+    // where the word of scales of row r lies among the stage's scales
+    auto scale_at = [&](int r) __attribute__((always_inline)) {
+        const int b = r / 8;
+        return 256 * (b % C::kWaves) + 4 * (8 * (b / C::kWaves) + r % 8);
+    };
+
+    int cs = 0, es = 0, stored = 0;
+    for (int wid = wbeg + slot; wid < wend; wid += per) {
+        const Item cur = item_at(wid, es);
+        const bool active = brow < cur.n;                 // this wave's rows hold some of the item's
+        f32x16 acc[WF][TF];
+#pragma unroll
+        for (int i = 0; i < WF; ++i)
+#pragma unroll
+            for (int j = 0; j < TF; ++j) acc[i][j] = f32x16{};
+
+        for (int c = 0; c < cur.nc; ++c) {
+            // This wave's loads of the chunk have arrived; later chunks' (and the
+            // stores of the item before, issued after the chunks that were then on
+            // their way) may be under way.  Then everyone's have, and everyone is
+            // done with the stage that is filled next.
+            {
+                const int later = ahead - 1;
+                const int st = c < C::kAhead ? stored : 0;
+                auto wait = [&](auto n) __attribute__((always_inline)) {
+                    constexpr int N = decltype(n)::value;
+                    if (st == 0) wait_vm<N>();
+                    else if (st < 8) wait_vm<N + 1>();
+                    else wait_vm<N + 8>();
+                };
+                if (C::kAhead >= 3 && later >= 2) wait(std::integral_constant<int, (C::kAhead >= 3 ? 2 : 0) * C::kLoads>{});
+                else if (C::kAhead >= 2 && later >= 1) wait(std::integral_constant<int, (C::kAhead >= 2 ? 1 : 0) * C::kLoads>{});
+                else wait(std::integral_constant<int, 0>{});
+            }
+            lds_barrier();
+            --ahead;
+            const uint8_t* const st = ring + cs * C::kStage;
+            cs = cs + 1 == C::STAGES ? 0 : cs + 1;
+            issue_next();
+            if (!active) continue;
+            const int sh = 8 * ((cur.c0 + c) & 3);
+            int ws[WF], xs[TF];
+#pragma unroll
+            for (int i = 0; i < WF; ++i)
+                ws[i] = *reinterpret_cast<const uint32_t*>(st + C::kScales + 256 * wave + 128 + 4 * (arow(i) / kBlk)) >> sh;
+#pragma unroll
+            for (int j = 0; j < TF; ++j)
+                xs[j] = *reinterpret_cast<const uint32_t*>(st + C::kScales + scale_at(brow + 32 * j + l32)) >> sh;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                i32x8 A[WF], B[TF];
+                // (which of a block's numbers meet does not matter as long as both sides agree)
+                auto frag = [&](const uint8_t* base, int r) __attribute__((always_inline)) {
+                    const i32x4 lo = *reinterpret_cast<const i32x4*>(base + at_row(r, 4 * k + lh));
+                    const i32x4 hi = *reinterpret_cast<const i32x4*>(base + at_row(r, 4 * k + 2 + lh));
+                    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                };
+#pragma unroll
+                for (int i = 0; i < WF; ++i) A[i] = frag(st + C::kTokens, arow(i) + l32);
+#pragma unroll
+                for (int j = 0; j < TF; ++j) B[j] = frag(st, brow + 32 * j + l32);
+                if constexpr (kExact) {
+                    // a wave's weight rows lie in one block, so that both scales go to the rows
+                    static_assert(OUT != GATED, "one scale for both weight fragments");
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        bf16x8 Ab[WF];
+#pragma unroll
+                        for (int i = 0; i < WF; ++i) Ab[i] = widen(A[i][2 * p], A[i][2 * p + 1], 1.0f);
+#pragma unroll
+                        for (int j = 0; j < TF; ++j) {
+                            const int e = (xs[j] & 255) + (ws[0] & 255) - 127;
+                            const bf16x8 Bb = widen(B[j][2 * p], B[j][2 * p + 1], __uint_as_float(static_cast<uint32_t>(min(max(e, 1), 254)) << 23));
+#pragma unroll
+                            for (int i = 0; i < WF; ++i)
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Ab[i], Bb, acc[i][j], 0, 0, 0);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < TF; ++j)
+#pragma unroll
+                        for (int i = 0; i < WF; ++i)
+                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A[i], B[j], acc[i][j], 0, 0, 0, ws[i], 0, xs[j]);
+                }
+            }
+        }
+
+        // A lane holds features 8 (q / 4) + 4 lh + q % 4 of each 32-row weight
+        // fragment for row brow + 32 j + l32.  Rows are turned around through the
+        // stage computed last (free after a barrier; refilled after the next).
+        lds_barrier();
+        uint8_t* const free_stage = ring + (cs == 0 ? C::STAGES - 1 : cs - 1) * C::kStage;
+        stored = 0;
+        if constexpr (OUT == GATED) {
+            // h = silu(g) u; the largest of a row's 128 features over its 2 lanes and
+            // the WW waves; 8 bits each, whole 128-byte rows stored.
+            float* const most = reinterpret_cast<float*>(free_stage + TM * kBlk);      // [WW][TM]
+            if (a.saved) {
+#pragma unroll
+                for (int j = 0; j < TF; ++j) {
+                    const int r = brow + 32 * j + l32;
+                    if (r >= cur.n) continue;
+                    uint16_t* const g = a.saved + static_cast<size_t>(cur.r0 + r) * 2 * a.M + cur.m0 + 32 * wn + 4 * lh;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int qb = 0; qb < 4; ++qb)
+                            if (cur.m0 + 32 * wn + 8 * qb < a.M)
+                                *reinterpret_cast<uint2*>(g + i * a.M + 8 * qb) =
+                                    uint2{pack_bf16x2(acc[i][j][4 * qb], acc[i][j][4 * qb + 1]), pack_bf16x2(acc[i][j][4 * qb + 2], acc[i][j][4 * qb + 3])};
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < TF; ++j) {
+                float m = 0.f;
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    // (M is a multiple of 8: whole groups of a lane pair lie past it)
+                    const float h = cur.m0 + 32 * wn + 8 * (q / 4) < a.M ? swiglu(acc[0][j][q], acc[1][j][q]) : 0.f;
+                    acc[0][j][q] = h;
+                    m = fmaxf(m, finite_abs(h));
+                }
+                m = fmaxf(m, __shfl_xor(m, 32, kWave));
+                if (lh == 0) most[wn * TM + brow + 32 * j + l32] = m;
+            }
+            lds_barrier();
+#pragma unroll
+            for (int j = 0; j < TF; ++j) {
+                const int r = brow + 32 * j + l32;
+                float m = most[r];
+#pragma unroll
+                for (int w = 1; w < C::WW; ++w) m = fmaxf(m, most[w * TM + r]);
+                const uint32_t b = scale_byte(m);
+                const float s = scale_inverse(b);
+                if (wn == 0 && lh == 0 && r < cur.n) a.sout[static_cast<size_t>(cur.r0 + r) * a.ldo + cur.m0 / kBlk] = static_cast<uint8_t>(b);
+#pragma unroll
+                for (int qb = 0; qb < 4; ++qb) {
+                    float o[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) o[q] = or_nan(acc[0][j][4 * qb + q]) * s;
+                    // features 32 wn + 8 qb + 4 lh ..: 4 bytes of vector 2 wn + qb / 2
+                    *reinterpret_cast<uint32_t*>(free_stage + at_row(r, 2 * wn + qb / 2) + 8 * (qb & 1) + 4 * lh) = pack_e4m3(o[0], o[1], o[2], o[3]);
+                }
+            }
+            lds_barrier();
+            const size_t Mp = static_cast<size_t>((a.M + kBlk - 1) / kBlk) * kBlk;
+#pragma unroll
+            for (int k = 0; k < TM / 8 / C::kWaves; ++k) {
+                const int r = 8 * (wave + C::kWaves * k) + lane / 8, v = lane % 8;
+                if (r < cur.n) {
+                    const u32x4 d = *reinterpret_cast<const u32x4*>(free_stage + at_row(r, v));
+                    *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.out) + (cur.r0 + r) * Mp + cur.m0 + 16 * v) = d;
+                }
+            }
+            // (what the waves read of `free_stage` is refilled after the next chunk's barrier)
+        } else {
+            uint8_t* const tb = free_stage + wave * (C::kScales / C::kWaves);
+            static_assert(C::kScales / C::kWaves >= 4096, "32 rows of 128 bytes per wave");
+#pragma unroll
+            for (int j = 0; j < TF; ++j) {
+                const int nv = min(32, cur.n - brow - 32 * j);    // uniform
+                if (nv <= 0) break;
+                const size_t row0 = static_cast<size_t>(cur.r0 + brow + 32 * j);
+                auto rows_out = [&](uint8_t* op, size_t pitch, int room) __attribute__((always_inline)) {
+                    wave_lds_sync();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (8 * k >= nv) break;
+                        const int r = 8 * k + lane / 8, v = lane % 8;
+                        const u32x4 d = *reinterpret_cast<const u32x4*>(tb + r * kBlk + ((v ^ (r & 7)) << 4));
+                        if (r < nv && 16 * v < room) *reinterpret_cast<u32x4*>(op + (row0 + r) * pitch + 16 * v) = d;
+                        if (room > 0) ++stored;
+                    }
+                    wave_lds_sync();
+                };
+                if constexpr (OUT == ROWS16) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int qb = 0; qb < 4; ++qb)
+                            *reinterpret_cast<uint2*>(tb + l32 * kBlk + (((4 * i + qb) ^ (l32 & 7)) << 4) + 8 * lh) =
+                                uint2{pack_bf16x2(acc[i][j][4 * qb + 0], acc[i][j][4 * qb + 1]),
+                                      pack_bf16x2(acc[i][j][4 * qb + 2], acc[i][j][4 * qb + 3])};
+                    const int f = cur.m0 + 64 * wn;
+                    rows_out(reinterpret_cast<uint8_t*>(static_cast<uint16_t*>(a.out) + f), static_cast<size_t>(a.M) * 2, 2 * (a.M - f));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int f = cur.m0 + 64 * wn + 32 * i;
+#pragma unroll
+                        for (int qb = 0; qb < 4; ++qb)
+                            *reinterpret_cast<f32x4*>(tb + l32 * kBlk + (((2 * qb + lh) ^ (l32 & 7)) << 4)) =
+                                f32x4{acc[i][j][4 * qb + 0], acc[i][j][4 * qb + 1], acc[i][j][4 * qb + 2], acc[i][j][4 * qb + 3]};
+                        float* const op = static_cast<float*>(a.out) + static_cast<size_t>(cur.sp) * a.cap * a.M + f;
+                        rows_out(reinterpret_cast<uint8_t*>(op), static_cast<size_t>(a.M) * 4, 4 * (a.M - f));
+                    }
+                }
+            }
+        }
+    }
+}
+
+// ---- rows and weights to 8 bits ----------------------------------------------
+
+// The rows that belong to a group: [first, end) of `cap`.
+struct Range {
+    const int32_t* offsets;    // or null: all
+    int groups, cap;
+    __device__ __forceinline__ int first() const { return offsets ? min(max(offsets[0], 0), cap) : 0; }
+    __device__ __forceinline__ int end() const { return offsets ? min(max(offsets[groups], 0), cap) : cap; }
+};
+
+// x [rows][K] bf16 -> q [rows][Kp], scale [rows][lds]; 4 blocks of a row per wave.
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const uint16_t* __restrict__ x, Range rows, int K, int Kp, uint8_t* __restrict__ q, uint8_t* __restrict__ scale, int lds) {
+    const int lane = lane_id();
+    const int pieces = lds / 4;
+    const int r0 = rows.first();
+    const int64_t items = static_cast<int64_t>(max(rows.end() - r0, 0)) * pieces;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; i < items; i += static_cast<int64_t>(gridDim.x) * 4) {
+        const int64_t r = r0 + i / pieces;
+        const int piece = static_cast<int>(i % pieces), col = 512 * piece + 8 * lane;
+        uint4 w{0, 0, 0, 0};
+        if (col < K) w = *reinterpret_cast<const uint4*>(x + r * K + col);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = __uint_as_float(u[j] << 16);
+            v[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
+        }
+        uint2 o;
+        const uint32_t b = quantize_lane(v, o);
+        if (col < Kp) *reinterpret_cast<uint2*>(q + r * Kp + col) = o;
+        if (lane % 16 == 0) scale[r * lds + 4 * piece + lane / 16] = static_cast<uint8_t>(b);
+    }
+}
+
+// One 128 x 128 block of w [groups][M][K] per workgroup: 8 bits as they lie (q:
+// rows of ldq bytes, `gq` per group) and, where asked for, transposed (qt).
+struct WeightArgs {
+    const void* w;
+    int M, K;
+    uint8_t* q;                // or null
+    size_t gq;
+    int ldq;
+    uint8_t* s;                // scales: [ceil(M / 128)][lds] per group
+    size_t gs;
+    int lds;
+    uint8_t* qt;               // or null: [K] rows of ldt bytes, M side by side
+    size_t gt;
+    int ldt;
+    uint8_t* st;               // [ceil(K / 128)][ldst] per group
+    size_t gst;
+    int ldst;
+    int st_end;                // where such a row ends
+};
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_weights_kernel(WeightArgs a) {
+    __shared__ float red[4];
+    __shared__ uint8_t turned[kBlk][kBlk + 4];
+    const int kb = blockIdx.x, mb = blockIdx.y, g = blockIdx.z, lane = lane_id(), wave = threadIdx.x / kWave;
+    const int nkb = (a.K + kBlk - 1) / kBlk, nmb = (a.M + kBlk - 1) / kBlk;
+    const T* const w = static_cast<const T*>(a.w) + static_cast<size_t>(g) * a.M * a.K;
+    const int c8 = 8 * (threadIdx.x % 16), r0 = threadIdx.x / 16, col = kb * kBlk + c8;
+    float v[8][8];
+    float m = 0.f;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        const int row = mb * kBlk + 16 * p + r0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[p][i] = 0.f;
+        if (row < a.M && col < a.K) {          // (K is a multiple of 8)
+            const T* const src = w + static_cast<size_t>(row) * a.K + col;
+            if constexpr (sizeof(T) == 2) {
+                const uint4 u = *reinterpret_cast<const uint4*>(src);
+                const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[p][2 * i] = __uint_as_float(x[i] << 16);
+                    v[p][2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[p][i] = src[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(v[p][i]));
+    }
+    m = wave_max(m);
+    if (lane == 0) red[wave] = m;
+    __syncthreads();
+    const uint32_t b = scale_byte(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+    const float s = scale_inverse(b);
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        const int r = 16 * p + r0, row = mb * kBlk + r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[p][i] = or_nan(v[p][i]) * s;
+        const uint2 o{pack_e4m3(v[p][0], v[p][1], v[p][2], v[p][3]), pack_e4m3(v[p][4], v[p][5], v[p][6], v[p][7])};
+        if (a.q && row < a.M) *reinterpret_cast<uint2*>(a.q + g * a.gq + static_cast<size_t>(row) * a.ldq + col) = o;
+        if (a.qt) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) turned[c8 + i][r] = static_cast<uint8_t>((i < 4 ? o.x : o.y) >> (8 * (i & 3)));
+        }
+    }
+    // the block's byte, and the bytes that fill the last word of a row of them
+    if (threadIdx.x < 4) {
+        const int i = threadIdx.x;
+        if (a.s && (i == 0 || (kb == nkb - 1 && kb + i < a.lds)))
+            a.s[g * a.gs + static_cast<size_t>(mb) * a.lds + kb + i] = static_cast<uint8_t>(i == 0 ? b : 127);
+        // (transposed scales may share their rows with another matrix's, whose bytes follow)
+        if (a.st && (i == 0 || (mb == nmb - 1 && mb + i < a.st_end)))
+            a.st[g * a.gst + static_cast<size_t>(kb) * a.ldst + mb + i] = static_cast<uint8_t>(i == 0 ? b : 127);
+    }
+    if (!a.qt) return;
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int r = 32 * p + threadIdx.x / 8, row = kb * kBlk + r, c = 16 * (threadIdx.x % 8);
+        if (row >= a.K) continue;
+        const uint32_t* const src = reinterpret_cast<const uint32_t*>(&turned[r][c]);      // (rows of 132 bytes)
+        *reinterpret_cast<u32x4*>(a.qt + g * a.gt + static_cast<size_t>(row) * a.ldt + mb * kBlk + c) = u32x4{src[0], src[1], src[2], src[3]};
+    }
+}
+
+// ---- slices of a split reduction ----------------------------------------------
+
+// out = the sum of `splits` fp32 slices [cap][M], in their order; 4 numbers per thread.
+template <bool BF16>
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, int splits, Range rows, int M,
+                                                   void* __restrict__ out) {
+    const int64_t stride = static_cast<int64_t>(rows.cap) * M, n = static_cast<int64_t>(rows.end()) * M;
+    for (int64_t i = static_cast<int64_t>(rows.first()) * M + 4 * (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x); i < n; i += static_cast<int64_t>(gridDim.x) * 1024) {
+        f32x4 v = *reinterpret_cast<const f32x4*>(part + i);
+        for (int s = 1; s < splits; ++s) {
+            const f32x4 u = *reinterpret_cast<const f32x4*>(part + s * stride + i);
+            v[0] += u[0]; v[1] += u[1]; v[2] += u[2]; v[3] += u[3];
+        }
+        if constexpr (BF16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + i) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        else *reinterpret_cast<f32x4*>(static_cast<float*>(out) + i) = v;
+    }
+}
+
+// Between the experts' products, 16 lanes per row and 128 features:
+//   forward:  g, u (the sums of their slices) -> h = silu(g) u in 8 bits (and g, u in bf16)
+//   backward: dh (the sum of its slices), g, u (bf16) -> dg = dh u s (1 + g (1 - s)), du = dh g s
+//             in 8 bits, s = 1 / (1 + e^-g)
+struct GateArgs {
+    const float* a;            // [splits][cap][F] g or dh
+    const float* b;            // forward: [splits][cap][F] u
+    int splits, F, Fp;
+    Range rows;
+    uint16_t* saved;           // [cap][2 F] bf16 (forward: or null)
+    uint8_t* q;                // [cap][Fp], backward [cap][2 Fp]
+    uint8_t* scale;            // [cap][lds]
+    int lds;
+};
+template <bool BACK>
+__global__ __launch_bounds__(256) void gate_kernel(GateArgs a) {
+    const int lane = lane_id(), blocks = a.Fp / kBlk;
+    const int r0 = a.rows.first();
+    const int64_t n = static_cast<int64_t>(max(a.rows.end() - r0, 0)) * blocks, stride = static_cast<int64_t>(a.rows.cap) * a.F;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 16 + threadIdx.x / 16; i < n; i += static_cast<int64_t>(gridDim.x) * 16) {
+        const int64_t r = r0 + i / blocks;
+        const int blk = static_cast<int>(i % blocks), f = blk * kBlk + 8 * (lane % 16);
+        const bool in = f < a.F;               // (F is a multiple of 8)
+        float x[8], y[8], o[8], p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = y[j] = 0.f;
+        if (in) {
+            auto sum = [&](const float* src, float (&v)[8]) __attribute__((always_inline)) {
+                for (int s = 0; s < a.splits; ++s) {
+                    const f32x4* const at = reinterpret_cast<const f32x4*>(src + s * stride + r * a.F + f);
+                    const f32x4 lo = at[0], hi = at[1];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        v[j] += lo[j];
+                        v[4 + j] += hi[j];
+                    }
+                }
+            };
+            sum(a.a, x);
+            if constexpr (!BACK) sum(a.b, y);
+        }
+        uint16_t* const sv = a.saved ? a.saved + r * 2 * a.F + f : nullptr;
+        if constexpr (BACK) {
+            uint4 gw{0, 0, 0, 0}, uw{0, 0, 0, 0};
+            if (in) {
+                gw = *reinterpret_cast<const uint4*>(sv);
+                uw = *reinterpret_cast<const uint4*>(sv + a.F);
+            }
+            const uint32_t gp[4] = {gw.x, gw.y, gw.z, gw.w}, up[4] = {uw.x, uw.y, uw.z, uw.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float g = __uint_as_float(j & 1 ? gp[j / 2] & 0xffff0000u : gp[j / 2] << 16);
+                const float u = __uint_as_float(j & 1 ? up[j / 2] & 0xffff0000u : up[j / 2] << 16);
+                const float s = 1.f / (1.f + __expf(-g));
+                o[j] = x[j] * u * s * (1.f + g * (1.f - s));
+                p[j] = x[j] * g * s;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = swiglu(x[j], y[j]);
+            if (sv && in) {
+                *reinterpret_cast<uint4*>(sv) = uint4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+                *reinterpret_cast<uint4*>(sv + a.F) = uint4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
+            }
+        }
+        const int width = BACK ? 2 * a.Fp : a.Fp;
+        uint2 w;
+        uint32_t b = quantize_lane(o, w);
+        *reinterpret_cast<uint2*>(a.q + r * width + f) = w;
+        if (lane % 16 == 0) a.scale[r * a.lds + blk] = static_cast<uint8_t>(b);
+        if constexpr (BACK) {
+            b = quantize_lane(p, w);
+            *reinterpret_cast<uint2*>(a.q + r * width + a.Fp + f) = w;
+            if (lane % 16 == 0) a.scale[r * a.lds + blocks + blk] = static_cast<uint8_t>(b);
+        }
+    }
+}
+
+// Most row tiles: every group may end in a partial one.
+int64_t most_tiles(const Rows& r, int tm) {
+    const int64_t whole = (static_cast<int64_t>(r.cap) + tm - 1) / tm;
+    return r.offsets ? std::min<int64_t>(r.cap, whole + r.groups) : whole;
+}
+
+template <Out OUT, class C>
+hipError_t launch_tile(Args& a, const Rows& r, hipStream_t s) {
+    a.xcds = geometry().xcds;
+    const int out = OUT == GATED ? C::NW / 2 : C::NW;
+    const int64_t work = most_tiles(r, C::TM) * ((a.M + out - 1) / out) * a.splits;
+    int64_t blocks = std::min<int64_t>(work, geometry().cus);             // (a workgroup fills a CU's LDS)
+    blocks = std::max<int64_t>(a.xcds, (blocks + a.xcds - 1) / a.xcds * a.xcds);
+    product_kernel<OUT, C><<<static_cast<int>(blocks), C::kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <Out OUT>
+hipError_t launch_out(int tm, Args& a, const Rows& r, hipStream_t s) {
+    if (tm == Big::TM) return launch_tile<OUT, Big>(a, r, s);
+    if (tm == Mid::TM) return launch_tile<OUT, Mid>(a, r, s);
+    return launch_tile<OUT, Few>(a, r, s);
+}
+
+int64_t some_blocks(int64_t n) { return std::max<int64_t>(1, std::min<int64_t>(n, 65536)); }
+
+// Rows of a tile, by the rows that a group has on average.
+int tile_rows(const Rows& r) {
+    const int64_t each = (static_cast<int64_t>(r.cap) + r.groups - 1) / r.groups;
+    return each > 160 ? Big::TM : each > 32 ? Mid::TM : Few::TM;
+}
+// Slices of the reduction where the items leave CUs without work; a slice keeps 4 chunks.
+int slices(const Rows& r, int tm, int64_t columns, int Kp) {
+    const int64_t items = most_tiles(r, tm) * columns;
+    int s = 1;
+    while (items * s * 2 <= 256 && Kp / kBlk / (2 * s) >= 4) s *= 2;
+    return s;
+}
+
+Args base_args(const Rows& r, const Matrix& w, const uint8_t* q, const uint8_t* sq, int lds) {
+    Args a{};
+    a.wa = w.q;
+    a.sa = w.s;
+    a.ldw = w.lds;
+    a.x = q;
+    a.sx = sq;
+    a.ldx = lds;
+    a.src_rows = r.src_rows;
+    a.token = r.token;
+    a.offsets = r.offsets;
+    a.groups = r.groups;
+    a.cap = r.cap;
+    a.M = w.M;
+    a.Kp = w.Kp;
+    a.splits = 1;
+    return a;
+}
+Range range_of(const Rows& r) { return Range{r.offsets, r.groups, r.cap}; }
+
+}  // namespace
+
+int product_slices(const Rows& r, int M, int Kp) { return slices(r, tile_rows(r), (M + Big::NW - 1) / Big::NW, Kp); }
+int gated_slices(const Rows& r, int M, int Kp) {
+    const int tm = tile_rows(r);
+    // (unsplit, the gated tile's items are 128 features wide; split, W1 and W3 are products of their own)
+    const int s = slices(r, tm, (M + kBlk - 1) / kBlk, Kp);
+    return s > 1 ? slices(r, tm, (M + Big::NW - 1) / Big::NW * 2, Kp) : 1;
+}
+
+hipError_t launch_quantize_rows(const uint16_t* x, const Rows& r, int K, uint8_t* q, uint8_t* scale, hipStream_t s) {
+    const Range rows = r.token ? Range{nullptr, 0, r.src_rows} : range_of(r);
+    if (rows.cap == 0) return hipSuccess;
+    const int Kp = pad(K), lds = scale_bytes(K);
+    quantize_rows_kernel<<<some_blocks((static_cast<int64_t>(rows.cap) * (lds / 4) + 3) / 4), 256, 0, s>>>(x, rows, K, Kp, q, scale, lds);
+    return hipGetLastError();
+}
+
+hipError_t launch_quantize_weights(const void* w, bool bf16, int groups, int M, int K, const Matrix* m, const Matrix* t, int column,
+                                   hipStream_t s) {
+    WeightArgs a{};
+    a.w = w;
+    a.M = M;
+    a.K = K;
+    if (m) {
+        a.q = m->q;
+        a.gq = static_cast<size_t>(M) * m->Kp;
+        a.ldq = m->Kp;
+        a.s = m->s;
+        a.gs = static_cast<size_t>((M + kBlk - 1) / kBlk) * m->lds;
+        a.lds = m->lds;
+    }
+    if (t) {
+        a.qt = t->q + column;
+        a.gt = static_cast<size_t>(K) * t->Kp;
+        a.ldt = t->Kp;
+        a.st = t->s + column / kBlk;
+        a.gst = static_cast<size_t>((K + kBlk - 1) / kBlk) * t->lds;
+        a.ldst = t->lds;
+        a.st_end = t->lds - column / kBlk;
+    }
+    const dim3 grid((K + kBlk - 1) / kBlk, (M + kBlk - 1) / kBlk, groups);
+    if (bf16) quantize_weights_kernel<uint16_t><<<grid, 256, 0, s>>>(a);
+    else quantize_weights_kernel<float><<<grid, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_product(const Rows& r, const uint8_t* q, const uint8_t* sq, int lds, const Matrix& w, bool bf16, void* out,
+                              int splits, float* part, hipStream_t s) {
+    if (r.cap == 0) return hipSuccess;
+    Args a = base_args(r, w, q, sq, lds);
+    const int tm = tile_rows(r);
+    if (splits == 1 && out) {
+        a.out = out;
+        return bf16 ? launch_out<ROWS16>(tm, a, r, s) : launch_out<ROWS32>(tm, a, r, s);
+    }
+    a.out = part;
+    a.splits = splits;
+    const hipError_t e = out && !bf16 ? launch_out<EXACT>(tm, a, r, s) : launch_out<SLICES>(tm, a, r, s);
+    if (e != hipSuccess || !out) return e;
+    const int64_t blocks = some_blocks((static_cast<int64_t>(r.cap) * w.M / 4 + 255) / 256);
+    if (bf16) join_kernel<true><<<blocks, 256, 0, s>>>(part, splits, range_of(r), w.M, out);
+    else join_kernel<false><<<blocks, 256, 0, s>>>(part, splits, range_of(r), w.M, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_gated(const Rows& r, const uint8_t* q, const uint8_t* sq, int lds, const Matrix& w1, const Matrix& w3,
+                            uint8_t* h, uint8_t* sh, uint16_t* saved, int splits, float* part, hipStream_t s) {
+    if (r.cap == 0) return hipSuccess;
+    const int ldh = scale_bytes(w1.M);
+    if (splits == 1) {
+        Args a = base_args(r, w1, q, sq, lds);
+        a.wb = w3.q;
+        a.sb = w3.s;
+        a.out = h;
+        a.sout = sh;
+        a.ldo = ldh;
+        a.saved = saved;
+        return launch_out<GATED>(tile_rows(r), a, r, s);
+    }
+    const size_t one = static_cast<size_t>(splits) * r.cap * w1.M;
+    hipError_t e = launch_product(r, q, sq, lds, w1, false, nullptr, splits, part, s);
+    if (e == hipSuccess) e = launch_product(r, q, sq, lds, w3, false, nullptr, splits, part + one, s);
+    if (e != hipSuccess) return e;
+    const GateArgs g{part, part + one, splits, w1.M, pad(w1.M), range_of(r), saved, h, sh, ldh};
+    gate_kernel<false><<<some_blocks((static_cast<int64_t>(r.cap) * (g.Fp / kBlk) + 15) / 16), 256, 0, s>>>(g);
+    return hipGetLastError();
+}
+
+hipError_t launch_gate_backward(const Rows& r, const float* dh, int splits, int F, const uint16_t* saved, uint8_t* q, uint8_t* scale,
+                                    int lds, hipStream_t s) {
+    if (r.cap == 0) return hipSuccess;
+    const GateArgs g{dh, nullptr, splits, F, pad(F), range_of(r), const_cast<uint16_t*>(saved), q, scale, lds};
+    gate_kernel<true><<<some_blocks((static_cast<int64_t>(r.cap) * (g.Fp / kBlk) + 15) / 16), 256, 0, s>>>(g);
+    return hipGetLastError();
+}
+
+}  // namespace fp8
+}  // namespace eat

@@ -364,6 +364,160 @@ class CrossEntropy:
         return out
 
 
+class Fp8Matrix:
+    """A matrix ``w`` [M][K] or matrices [groups][M][K] (bf16 or fp32) held in 8
+    bits with a power of two per 128 x 128 block (eat_fp8_quantize): ``q`` e4m3
+    [groups][M][K padded to 128], ``scale`` e8m0 bytes.  ``product(x)`` is x . w^T
+    with the rows rounded the same way, a power of two per 128 elements; with
+    ``gradients`` the transposed numbers are kept too, for ``product_backward``.
+    Calls of one object share its workspace: order them on one stream.
+    ``stream``: what a call is enqueued on (the current one); the tensors given
+    have to be ready there, and what is returned is ready when it is."""
+
+    def __init__(self, w: torch.Tensor, gradients: bool = False, stream=None):
+        if w.dim() not in (2, 3):
+            raise ValueError("w: expected [M][K] or [groups][M][K]")
+        self.groups, self.M, self.K = (1, *w.shape) if w.dim() == 2 else tuple(w.shape)
+        _expect("w", w, (torch.bfloat16, torch.float32), tuple(w.shape))
+        self.device = w.device
+        dtype = L.EAT_BF16 if w.dtype == torch.bfloat16 else L.EAT_F32
+        caller = torch.cuda.current_stream(w.device) if stream is not None else None
+        with _calling_on(stream, w.device):
+            on = torch.cuda.current_stream(w.device)
+            made = []
+            for rows, cols in ((self.M, self.K), (self.K, self.M))[:1 + bool(gradients)]:
+                L.eat_fp8_size(self.groups, rows, cols)
+                q = torch.empty(self.groups, rows, -(-cols // 128) * 128, dtype=torch.float8_e4m3fn, device=w.device)
+                s = torch.empty(self.groups, -(-rows // 128), -(-cols // 512) * 4, dtype=torch.uint8, device=w.device)
+                L.eat_fp8_quantize(w, dtype, self.groups, self.M, self.K, len(made) // 2, q, s, on)
+                made += [q, s]
+        _hand_out(stream, caller, *made)
+        self.q, self.scale = made[:2]
+        self.qt, self.scale_t = made[2:] if gradients else (None, None)
+        self._ws = _Workspace(w.device)
+
+    def _run(self, x, offsets, token, out, q, scale, M, K, names, stream):
+        dev, src = self.device, x.shape[0]
+        rows = src if token is None else token.shape[0]
+        _expect(names[0], x, torch.bfloat16, (src, K), dev)
+        _expect("offsets", offsets, torch.int32, (self.groups + 1,), dev)
+        _expect("token", token, torch.int32, (rows,), dev)
+        _expect(names[1], out, (torch.bfloat16, torch.float32), (rows, M), dev)
+        if offsets is None and self.groups != 1:
+            raise ValueError("offsets: several matrices need them")
+        caller = torch.cuda.current_stream(dev) if stream is not None else None
+        with _calling_on(stream, dev):
+            given = out is not None
+            if not given:
+                out = torch.empty(rows, M, dtype=torch.bfloat16, device=dev)
+            need = L.eat_fp8_product_workspace_size(src, rows, self.groups, M, K)
+            on = torch.cuda.current_stream(dev)
+            ws = self._ws.get(need, on)
+            L.eat_fp8_product(x, src, token, offsets, rows, q, scale, self.groups, M, K, out,
+                              L.EAT_BF16 if out.dtype == torch.bfloat16 else L.EAT_F32, ws, need, on)
+        if not given:
+            _hand_out(stream, caller, out)
+        return out
+
+    def product(self, x: torch.Tensor, offsets: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """out [rows][M] (bf16, or the type of ``out``) of the rows x [rows][K] bf16,
+        or of x[token]; ``offsets`` [groups+1] int32: where each matrix's rows begin
+        (``EatLayer.sort``).  Rows outside the groups are not written."""
+        return self._run(x, offsets, token, out, self.q, self.scale, self.M, self.K, ("x", "out"), stream)
+
+    def product_backward(self, dy: torch.Tensor, offsets: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+        """dx [rows][K] of dy [rows][M] bf16, the weights held constant: dy . w, dy rounded as rows are."""
+        if self.qt is None:
+            raise ValueError("made without gradients")
+        return self._run(dy, offsets, None, dx, self.qt, self.scale_t, self.K, self.M, ("dy", "dx"), stream)
+
+
+class Fp8Experts:
+    """A layer's SwiGLU experts in 8 bits (eat_fp8_experts_*): ``weights`` as
+    EatLayer's (w1, w3 [E][F][d], w2 [E][d][F], bf16, row-major), of which the
+    object keeps e4m3 numbers with a power of two per 128 x 128 block, with
+    ``gradients`` their transposes too.  They are constants: ``backward`` gives
+    the rows' gradient.  Streams and workspace as Fp8Matrix's."""
+
+    def __init__(self, weights: Dict[str, torch.Tensor], gradients: bool = False, stream=None):
+        w1, w3, w2 = weights["w1"], weights["w3"], weights["w2"]
+        if w1.dim() != 3:
+            raise ValueError("w1: expected [E][F][d]")
+        self.E, self.F, self.d = w1.shape
+        dev = self.device = w1.device
+        _expect("w1", w1, torch.bfloat16, (self.E, self.F, self.d))
+        _expect("w3", w3, torch.bfloat16, (self.E, self.F, self.d), dev)
+        _expect("w2", w2, torch.bfloat16, (self.E, self.d, self.F), dev)
+        self.gradients, self.handle = bool(gradients), 0
+        self.handle = L.eat_create(L.eat_params_default(mode="topk", E=self.E, d_model=self.d, d_ffn=self.F, top_k=1), 1 << 24)
+        caller = torch.cuda.current_stream(dev) if stream is not None else None
+        with _calling_on(stream, dev):
+            self.buf = torch.empty(L.eat_fp8_experts_size(self.handle, int(gradients)), dtype=torch.uint8, device=dev)
+            L.eat_fp8_experts_quantize(self.handle, w1, w3, w2, int(gradients), self.buf, torch.cuda.current_stream(dev))
+        _hand_out(stream, caller, self.buf)
+        self._ws = _Workspace(dev)
+
+    def forward(self, x: torch.Tensor, offsets: torch.Tensor, token: torch.Tensor, y: Optional[torch.Tensor] = None,
+                saved: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The experts' rows y [rows][d] of the tokens x [T][d], with ``offsets`` and
+        ``token`` from ``EatLayer.sort``; what ``backward`` needs is written to
+        ``saved`` [rows][2 F] bf16.  Rows behind the last segment are not written."""
+        T, rows, dev = x.shape[0], token.shape[0], self.device
+        _expect("x", x, torch.bfloat16, (T, self.d), dev)
+        _expect("offsets", offsets, torch.int32, (self.E + 1,), dev)
+        _expect("token", token, torch.int32, (rows,), dev)
+        _expect("y", y, torch.bfloat16, (rows, self.d), dev)
+        _expect("saved", saved, torch.bfloat16, (rows, 2 * self.F), dev)
+        caller = torch.cuda.current_stream(dev) if stream is not None else None
+        with _calling_on(stream, dev):
+            given = y is not None
+            if not given:
+                y = torch.empty(rows, self.d, dtype=torch.bfloat16, device=dev)
+            need = L.eat_fp8_experts_workspace_size(self.handle, T, rows, 0)
+            on = torch.cuda.current_stream(dev)
+            ws = self._ws.get(need, on)
+            L.eat_fp8_experts_forward(self.handle, x, T, token, offsets, rows, self.buf, y, saved, ws, need, on)
+        if not given:
+            _hand_out(stream, caller, y)
+        return y
+
+    def backward(self, dy: torch.Tensor, saved: torch.Tensor, offsets: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                 stream=None) -> torch.Tensor:
+        """dx [rows][d] of the sorted tokens from dy [rows][d] (dx may be dy)."""
+        if not self.gradients:
+            raise ValueError("made without gradients")
+        rows, dev = dy.shape[0], self.device
+        _expect("dy", dy, torch.bfloat16, (rows, self.d), dev)
+        _expect("saved", saved, torch.bfloat16, (rows, 2 * self.F), dev)
+        _expect("offsets", offsets, torch.int32, (self.E + 1,), dev)
+        _expect("dx", dx, torch.bfloat16, (rows, self.d), dev)
+        caller = torch.cuda.current_stream(dev) if stream is not None else None
+        with _calling_on(stream, dev):
+            given = dx is not None
+            if not given:
+                dx = torch.empty(rows, self.d, dtype=torch.bfloat16, device=dev)
+            need = L.eat_fp8_experts_workspace_size(self.handle, 0, rows, 1)
+            on = torch.cuda.current_stream(dev)
+            ws = self._ws.get(need, on)
+            L.eat_fp8_experts_backward(self.handle, dy, offsets, rows, self.buf, saved, dx, ws, need, on)
+        if not given:
+            _hand_out(stream, caller, dx)
+        return dx
+
+    def close(self) -> None:
+        if self.handle:
+            L.eat_destroy(self.handle)
+            self.handle = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
 def layerwise_caps(n_layers: int, lower: int, k_lower: int, k_upper: int):
     """Per-layer caps K for layer-wise sparsity: the paper's layer analysis
     (Sec. 4) finds lower layers' experts less critical than higher layers',
