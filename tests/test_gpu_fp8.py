@@ -166,7 +166,7 @@ def experts_reference(x, w, off, token):
     F = w["w1"].shape[1]
     w1, w3, w2 = (R.quantize(w[k], 128)[0] for k in ("w1", "w3", "w2"))
     xq = R.quantize(x)[0][token]
-    (g, eg, vg), (u, eu, vu) = R.grouped(xq, w1, off), R.grouped(xq, w3, off)
+    (g, eg, _), (u, eu, _) = R.grouped(xq, w1, off, exact=True), R.grouped(xq, w3, off, exact=True)
     g, u = g.nan_to_num(0.0), u.nan_to_num(0.0)
     sg = g * torch.sigmoid(g)
     h = sg * u
@@ -174,16 +174,14 @@ def experts_reference(x, w, off, token):
     own = (g.abs() + 8) * 2 * U * h.abs() + 2.0 ** -100
     hq, he = R.quantize_between(h, 1.1 * eg * (u.abs() + eu) + sg.abs() * eu + own)
     y, ey, vy = R.grouped(hq, w2, off, he)
-    # (an error of 4 times the cuts' root mean square is rare)
-    hr = R.quantize_between(h, 4 * (1.1 * vg.sqrt() * u.abs() + sg.abs() * vu.sqrt() + own))[1]
-    vy = vy + R.grouped(hr.square(), w2.square(), off)[0] + (2.0 ** -8 * y).square()
+    vy = vy + R.grouped(he.square(), w2.square(), off)[0] + (2.0 ** -8 * y).square()
     return (y, (1 + 2.0 ** -8) * ey + 2.0 ** -8 * y.abs() + TINY, vy), (torch.cat([g, u], 1), torch.cat([eg, eu], 1))
 
 
 def backward_reference(dy, saved, w, off):
     F = w["w1"].shape[1]
     w1, w3, w2 = (R.quantize(w[k], 128)[0] for k in ("w1", "w3", "w2"))
-    dh, eh, vh = R.grouped(R.quantize(dy)[0], w2.transpose(1, 2), off)
+    dh, eh, _ = R.grouped(R.quantize(dy)[0], w2.transpose(1, 2), off, exact=True)
     dh = dh.nan_to_num(0.0)
     g, u = saved.double().split(F, 1)
     s = torch.sigmoid(g)
@@ -195,8 +193,7 @@ def backward_reference(dy, saved, w, off):
     (gq, ge), (uq, ue) = R.quantize_between(dg, eh * ag + og), R.quantize_between(du, eh * au + ou)
     a, b = R.grouped(gq, w1.transpose(1, 2), off, ge), R.grouped(uq, w3.transpose(1, 2), off, ue)
     dx = a[0] + b[0]
-    gr, ur = R.quantize_between(dg, 4 * (vh.sqrt() * ag + og))[1], R.quantize_between(du, 4 * (vh.sqrt() * au + ou))[1]
-    var = a[2] + b[2] + R.grouped(gr.square(), w1.transpose(1, 2).square(), off)[0] + R.grouped(ur.square(), w3.transpose(1, 2).square(), off)[0]
+    var = a[2] + b[2] + R.grouped(ge.square(), w1.transpose(1, 2).square(), off)[0] + R.grouped(ue.square(), w3.transpose(1, 2).square(), off)[0]
     # (one sum over both products)
     return dx, (1 + 2.0 ** -8) * 2 * (a[1] + b[1]) + 2.0 ** -8 * dx.abs() + TINY, var + (2.0 ** -8 * dx).square()
 
