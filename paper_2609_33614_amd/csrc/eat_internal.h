@@ -299,9 +299,6 @@ struct SortCall {
     int32_t T, E, d, cap;    // cap: rows there are
     bool bf16;
 };
-// Up to so many mask words every workgroup of the index launch counts all
-// tokens itself; beyond, two launches count them first.
-constexpr int kDirectTokens = 16384;
 size_t sort_workspace(int32_t T, int E);
 hipError_t launch_sort(const SortCall& c, const void* x, void* rows, int32_t* offsets, int32_t* token, int32_t* place,
                        void* ws, hipStream_t s);

@@ -21,6 +21,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kChunk = 256;               // tokens per workgroup of the index kernels
+constexpr int kSumChunks = 64;            // more chunks' counts are added up in a launch of their own
 constexpr int kBatch = 8;                 // rows of a token in flight together
 
 // 16 bytes of a row as fp32 numbers and back.
@@ -51,6 +52,15 @@ struct Vec<float> {
         return uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
     }
 };
+
+// (rows are read or written once, in bulk: past the caches)
+__device__ __forceinline__ uint4 load_row(const uint4* p) {
+    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    return uint4{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store_row(uint4* p, const uint4& q) {
+    __builtin_nontemporal_store(u32x4{q.x, q.y, q.z, q.w}, reinterpret_cast<u32x4*>(p));
+}
 
 // ---- index -----------------------------------------------------------------
 
@@ -99,63 +109,67 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(int32_t* __restrict__ cn
 struct IndexArgs {
     const uint64_t* mask;      // [T][W]
     int T, E, W, cap;
-    const int32_t* cnt;        // [chunks][E] selections in earlier chunks (null: counted here)
-    const int32_t* total;      // [E]
+    const int32_t* cnt;        // [chunks][E] selections of each chunk, or in earlier chunks where total is set
+    int chunks;
+    const int32_t* total;      // [E] or null
     int32_t* offsets;          // [E+1]
     int32_t* token;            // [cap]
     int32_t* place;            // [T][E]
 };
 
-// offsets, token and place of one chunk of tokens per workgroup of NW waves.
-// Without counts every workgroup counts all tokens itself, 64 per wave at a
-// time: no launches to wait for, and the masks (8 W bytes a token) come from L2.
-template <int NW>
-__global__ __launch_bounds__(NW* kWave) void index_kernel(IndexArgs a) {
+// offsets, token and place of one chunk of tokens per workgroup.  A bit transpose
+// costs 100 instructions per 64 tokens: where every workgroup counted all tokens
+// itself, 16384 tokens of 64 experts took 15 us, and the two launches take 10.
+constexpr int kIndexWaves = 16;
+__global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) {
+    constexpr int NW = kIndexWaves, kGroups = kChunk / kWave;
     __shared__ int tot[kMaxExperts], before[kMaxExperts], base[kMaxExperts];
-    __shared__ int own[kChunk / kWave][kMaxExperts];
+    __shared__ int own[kGroups][kMaxExperts];
+    __shared__ uint64_t cols[kGroups][kMaxExperts];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
-    const int t0 = blockIdx.x * kChunk;
-    for (int e = threadIdx.x; e < kMaxExperts; e += NW * kWave) {
-        const bool given = a.cnt && e < a.E;
-        tot[e] = given ? a.total[e] : 0;
-        before[e] = given ? a.cnt[static_cast<size_t>(blockIdx.x) * a.E + e] : 0;
+    const int t0 = blockIdx.x * kChunk, blk = blockIdx.x;
+    // the chunk's own masks: (group, word) pairs, one per wave
+    static_assert(kGroups * kMaxExperts / kWave <= NW, "a pair per wave");
+    const int og = wave % kGroups, ow = wave / kGroups, ot = t0 + og * kWave + lane;
+    const uint64_t mine = ow < a.W && ot < a.T ? a.mask[static_cast<size_t>(ot) * a.W + ow] : 0ull;
+    const int e0 = threadIdx.x % kMaxExperts, part = threadIdx.x / kMaxExperts;
+    if (part == 0) {
+        const bool given = a.total && e0 < a.E;
+        tot[e0] = given ? a.total[e0] : 0;
+        before[e0] = given ? a.cnt[static_cast<size_t>(blk) * a.E + e0] : 0;
     }
     __syncthreads();
-    if (!a.cnt) {
-        for (int w = 0; w < a.W; ++w) {
-            int all = 0, pre = 0;
-            for (int g = wave; g * kWave < a.T; g += NW) {
-                const int t = g * kWave + lane;
-                const int n = __popcll(bit_transpose(t < a.T ? a.mask[static_cast<size_t>(t) * a.W + w] : 0ull));
-                all += n;
-                pre += g * kWave < t0 ? n : 0;
-            }
-            atomicAdd(&tot[kWave * w + lane], all);      // (whole numbers: any order gives the same sum)
-            atomicAdd(&before[kWave * w + lane], pre);
-        }
-    }
-    // (waves past the chunk's groups take part in the barriers alone)
-    constexpr int kGroups = kChunk / kWave;
-    uint64_t col[kMaxExperts / kWave];
-    const int t = t0 + wave * kWave + lane;
+    if (!a.total && e0 < a.E) {
+        constexpr int kStep = NW * kWave / kMaxExperts, kPre = 8;
+        int all = 0, pre = 0;
+        for (int c0 = part; c0 < a.chunks; c0 += kStep * kPre) {
+            int n[kPre];
 #pragma unroll
-    for (int w = 0; w < kMaxExperts / kWave; ++w) {
-        col[w] = 0;
-        if (w < a.W && wave < kGroups) {
-            col[w] = bit_transpose(t < a.T ? a.mask[static_cast<size_t>(t) * a.W + w] : 0ull);
-            own[wave][kWave * w + lane] = __popcll(col[w]);
+            for (int i = 0; i < kPre; ++i) n[i] = c0 + kStep * i < a.chunks ? a.cnt[static_cast<size_t>(c0 + kStep * i) * a.E + e0] : 0;
+#pragma unroll
+            for (int i = 0; i < kPre; ++i) {
+                all += n[i];
+                pre += c0 + kStep * i < blk ? n[i] : 0;
+            }
         }
+        atomicAdd(&tot[e0], all);                          // (whole numbers: any order gives the same sum)
+        atomicAdd(&before[e0], pre);
+    }
+    if (ow < a.W) {
+        const uint64_t m = bit_transpose(mine);
+        cols[og][kWave * ow + lane] = m;
+        own[og][kWave * ow + lane] = __popcll(m);
     }
     __syncthreads();
     if (wave == 0) {
         int carry = 0;
-        for (int e0 = 0; e0 < a.E; e0 += kWave) {
-            const int e = e0 + lane;
+        for (int e1 = 0; e1 < a.E; e1 += kWave) {
+            const int e = e1 + lane;
             const int n = e < a.E ? tot[e] : 0;
             const int s = wave_scan(n);
             if (e < a.E) {
                 base[e] = carry + s - n;
-                if (blockIdx.x == 0) {
+                if (blk == 0) {
                     a.offsets[e] = min(base[e], a.cap);
                     if (e == a.E - 1) a.offsets[a.E] = min(carry + s, a.cap);
                 }
@@ -164,27 +178,67 @@ __global__ __launch_bounds__(NW* kWave) void index_kernel(IndexArgs a) {
         }
     }
     __syncthreads();
-    if (wave >= kGroups) return;
-#pragma unroll
-    for (int w = 0; w < kMaxExperts / kWave; ++w) {
-        const int e = kWave * w + lane;
-        if (w >= a.W || e >= a.E) continue;
-        int row = base[e] + before[e];
-        for (int q = 0; q < wave; ++q) row += own[q][e];
-        uint64_t m = col[w];
-        for (int i = 0; i < kWave; ++i) {
-            const int ti = t0 + wave * kWave + i;
-            if (ti >= a.T) break;                         // uniform
-            int at = -1;
-            if ((m >> i) & 1ull) {
-                if (row < a.cap) {
-                    at = row;
-                    a.token[row] = ti;
-                }
+    // places: the chunk's (group, word) pairs again, in parts of 64 / parts tokens so
+    // that every wave has some
+    const int parts = max(1, NW / (kGroups * a.W)), len = kWave / parts;
+    for (int p = wave; p < kGroups * a.W * parts; p += NW) {
+        const int g = p % kGroups, w = p / kGroups % a.W, k0 = p / (kGroups * a.W) * len, e = kWave * w + lane;
+        if (e >= a.E) continue;
+        uint64_t m = cols[g][e];
+        int row = base[e] + before[e] + __popcll(m & ((1ull << k0) - 1));
+        for (int q = 0; q < g; ++q) row += own[q][e];
+        m >>= k0;
+        const int first = t0 + g * kWave + k0, n = min(len, a.T - first);
+        int32_t* to = a.place + static_cast<size_t>(first) * a.E + e;
+        for (int k = 0; k < n; ++k, m >>= 1, to += a.E) {
+            const bool on = m & 1ull;
+            *to = on && row < a.cap ? row : -1;
+            if (on) {
+                if (row < a.cap) a.token[row] = first + k;
                 ++row;
             }
-            a.place[static_cast<size_t>(ti) * a.E + e] = at;
         }
+    }
+}
+
+// Calls of up to kFusedTokens tokens, indices and rows in one launch: a workgroup
+// per token works out all segments (build_segments), then its token's places and
+// copies (two launches: 18 us for 64 tokens of 4096 elements).
+__global__ __launch_bounds__(kThreads) void small_sort_kernel(IndexArgs a, const uint4* __restrict__ x, uint4* __restrict__ rows, int vecs) {
+    constexpr int NC = kFusedTokens / kWave;
+    __shared__ uint64_t cols[kMaxExperts * NC];
+    __shared__ int soff[kMaxExperts + 1];
+    __shared__ int list[kMaxExperts], found;
+    const int t = blockIdx.x, e = threadIdx.x;
+    // (the token's first vectors arrive meanwhile)
+    uint4 q{0, 0, 0, 0};
+    if (rows && t < a.T && e < vecs) q = x[static_cast<size_t>(t) * vecs + e];
+    if (e == 0) found = 0;
+    build_segments<kWaves, NC>(a.mask, a.T, a.E, a.W, cols, soff);
+    if (t == 0)
+        for (int i = e; i <= a.E; i += kThreads) a.offsets[i] = min(soff[i], a.cap);
+    if (t >= a.T) return;                                 // (no tokens: one workgroup for the offsets)
+    if (e < a.E) {
+        const uint64_t* const c = cols + e * NC;
+        int row = -1;
+        if ((c[t / kWave] >> (t % kWave)) & 1ull) {
+            row = soff[e] + __popcll(c[t / kWave] & ((1ull << (t % kWave)) - 1));
+            for (int i = 0; i < t / kWave; ++i) row += __popcll(c[i]);
+            if (row < a.cap) {
+                a.token[row] = t;
+                list[atomicAdd(&found, 1)] = row;          // (the order of copies does not matter)
+            } else {
+                row = -1;
+            }
+        }
+        a.place[static_cast<size_t>(t) * a.E + e] = row;
+    }
+    if (!rows) return;
+    __syncthreads();
+    const int n = found;
+    for (int v = e; v < vecs; v += kThreads) {
+        if (v != e) q = x[static_cast<size_t>(t) * vecs + v];
+        for (int i = 0; i < n; ++i) rows[static_cast<size_t>(list[i]) * vecs + v] = q;
     }
 }
 
@@ -255,7 +309,7 @@ __global__ __launch_bounds__(kThreads) void spread_kernel(RowArgs a) {
                 const uint4 q = a.src[t * a.vecs + v];
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b)
-                    if (rows[b] >= 0) a.dst[static_cast<int64_t>(rows[b]) * a.vecs + v] = q;
+                    if (rows[b] >= 0) store_row(a.dst + static_cast<int64_t>(rows[b]) * a.vecs + v, q);
             }
             if (n < kBatch) break;
         }
@@ -282,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(RowArgs a) {
                 uint4 q[kBatch];
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b)
-                    if (rows[b] >= 0) q[b] = a.src[static_cast<int64_t>(rows[b]) * a.vecs + v];
+                    if (rows[b] >= 0) q[b] = load_row(a.src + static_cast<int64_t>(rows[b]) * a.vecs + v);
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b) {
                     if (rows[b] < 0) continue;
@@ -344,7 +398,7 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
                 if (g.dots) {
 #pragma unroll
                     for (int b = 0; b < kBatch; ++b)
-                        if (rows[b] >= 0) q[b] = g.rows[static_cast<int64_t>(rows[b]) * a.vecs + v];
+                        if (rows[b] >= 0) q[b] = load_row(g.rows + static_cast<int64_t>(rows[b]) * a.vecs + v);
 #pragma unroll
                     for (int b = 0; b < kBatch; ++b) {
                         if (rows[b] < 0) continue;
@@ -361,7 +415,7 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
                         float o[V::N];
 #pragma unroll
                         for (int i = 0; i < V::N; ++i) o[i] = gates[b] * dy[i];
-                        a.dst[static_cast<int64_t>(rows[b]) * a.vecs + v] = V::put(o);
+                        store_row(a.dst + static_cast<int64_t>(rows[b]) * a.vecs + v, V::put(o));
                     }
                 }
             }
@@ -430,32 +484,34 @@ RowArgs row_args(const SortCall& c, const void* src, void* dst) {
 }  // namespace
 
 size_t sort_workspace(int32_t T, int E) {
-    if (static_cast<int64_t>(T) * mask_words(E) <= kDirectTokens) return 0;
+    if (T <= kFusedTokens) return 0;
     const size_t chunks = (static_cast<size_t>(T) + kChunk - 1) / kChunk;
     return (chunks + 1) * E * 4;
 }
 
 hipError_t launch_sort(const SortCall& c, const void* x, void* rows, int32_t* offsets, int32_t* token, int32_t* place,
                        void* ws, hipStream_t s) {
-    const int W = mask_words(c.E), chunks = std::max(1, (c.T + kChunk - 1) / kChunk);
-    const bool direct = static_cast<int64_t>(c.T) * W <= kDirectTokens;
-    int32_t* const cnt = direct ? nullptr : static_cast<int32_t*>(ws);
-    int32_t* const total = direct ? nullptr : cnt + static_cast<size_t>(chunks) * c.E;
-    hipError_t e = hipSuccess;
-    if (!direct) {
-        count_kernel<<<chunks, kThreads, 0, s>>>(c.mask, c.T, c.E, W, cnt);
+    const int W = mask_words(c.E), chunks = (c.T + kChunk - 1) / kChunk;
+    IndexArgs ia{c.mask, c.T, c.E, W, c.cap, nullptr, chunks, nullptr, offsets, token, place};
+    if (c.T <= kFusedTokens) {
+        small_sort_kernel<<<std::max(1, c.T), kThreads, 0, s>>>(ia, static_cast<const uint4*>(x), static_cast<uint4*>(rows),
+                                                                c.d * (c.bf16 ? 2 : 4) / 16);
+        return hipGetLastError();
+    }
+    int32_t* const cnt = static_cast<int32_t*>(ws);
+    ia.cnt = cnt;
+    count_kernel<<<chunks, kThreads, 0, s>>>(c.mask, c.T, c.E, W, cnt);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && chunks > kSumChunks) {
+        int32_t* const total = cnt + static_cast<size_t>(chunks) * c.E;
+        ia.total = total;
+        scan_kernel<<<c.E, kThreads, 0, s>>>(cnt, chunks, c.E, total);
         e = hipGetLastError();
-        if (e == hipSuccess) {
-            scan_kernel<<<c.E, kThreads, 0, s>>>(cnt, chunks, c.E, total);
-            e = hipGetLastError();
-        }
     }
     if (e != hipSuccess) return e;
-    const IndexArgs ia{c.mask, c.T, c.E, W, c.cap, cnt, total, offsets, token, place};
-    if (direct) index_kernel<16><<<chunks, 16 * kWave, 0, s>>>(ia);
-    else index_kernel<kWaves><<<chunks, kThreads, 0, s>>>(ia);
+    index_kernel<<<chunks, kIndexWaves * kWave, 0, s>>>(ia);
     e = hipGetLastError();
-    if (e != hipSuccess || !rows || c.T == 0) return e;
+    if (e != hipSuccess || !rows) return e;
     SortCall p = c;
     p.place = place;
     const RowArgs a = c.bf16 ? row_args<uint16_t>(p, x, rows) : row_args<float>(p, x, rows);

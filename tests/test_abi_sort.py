@@ -28,7 +28,7 @@ def handle():
 
 
 def test_workspace_sizes(handle):
-    assert L.eat_sort_workspace_size(handle, 0) == 0 and L.eat_sort_workspace_size(handle, 16384) == 0
+    assert L.eat_sort_workspace_size(handle, 0) == 0 and L.eat_sort_workspace_size(handle, 256) == 0
     n = L.eat_sort_workspace_size(handle, 40000)
     assert n >= (157 + 1) * E * 4 and n < 2 ** 20
     for t in (-1, 40001):
