@@ -37,27 +37,35 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-template <int TM_, int NW_, int WT_, int WW_, int STAGES_, bool NT_>
+template <int TM_, int NW_, int WT_, int WW_, int STAGES_, bool NT_, bool DEEP_>
 struct Tile {
     static constexpr int TM = TM_, NW = NW_, WT = WT_, WW = WW_, STAGES = STAGES_;
     static constexpr bool NT = NT_;                       // weights stream past the caches
+    static constexpr bool DEEP = DEEP_;                   // operands are read ahead of the products before
     static constexpr int kWaves = WT * WW, kThreads = kWaves * kWave;
     static constexpr int TF = TM / (32 * WT), WF = NW / (32 * WW);
     static constexpr int kTokens = TM * kBlk;             // bytes of a stage's rows
-    static constexpr int kScales = kTokens + NW * kBlk;   // where a stage's scales begin: 256 bytes per wave
-    static constexpr int kStage = kScales + 256 * kWaves;
     static constexpr int kBT = TM / 8 / kWaves, kBW = NW / 8 / kWaves;   // 1 KB loads per wave
-    static constexpr int kLoads = kBT + kBW + 1;          // ... and the scales
+    static constexpr int kRows = 8 * kBT;                 // rows whose scales a wave fetches, a word per lane
+    static constexpr int kWords = kRows > 32 ? 2 : 1;     // ... with the weights' in the upper lanes, or in a second load
+    static constexpr int kScales = kTokens + NW * kBlk;   // where a stage's scales begin
+    static constexpr int kArea = 256 * kWords + 32;       // a wave's scales (32: eight rows' words of each wave on banks of their own)
+    static constexpr int kStage = kScales + kArea * kWaves;
+    static constexpr int kWeightWord = 256 * kWords - 128;               // where the weights' words begin in a wave's
+    static constexpr int kLoads = kBT + kBW + kWords;
+    static constexpr int kFrag = WF / 2;                  // gated: 32-feature fragments per wave
     static constexpr int kAhead = STAGES - 1;             // chunks on their way beside the one computed
-    static_assert(kBT * 8 * kWaves == TM && kBW * 8 * kWaves == NW && 8 * kBT <= 32, "loads split evenly over the waves");
-    static_assert(TF * 32 * WT == TM && WF * 32 * WW == NW && WF == 2 && NW == 256, "fragments cover the tile; a gated tile is one block wide");
+    static_assert(kBT * 8 * kWaves == TM && kBW * 8 * kWaves == NW && kRows <= 64, "loads split evenly over the waves");
+    static_assert(TF * 32 * WT == TM && WF * 32 * WW == NW && (WF == 2 || WF == 4) && NW == 256, "fragments cover the tile; a gated tile is one block wide");
     static_assert(kAhead >= 1 && kAhead <= 3, "waits count up to three chunks");
 };
-using Big = Tile<256, 256, 2, 4, 2, false>;
-using Mid = Tile<128, 256, 2, 4, 3, false>;
-using Few = Tile<32, 256, 1, 4, 4, true>;
+using Big = Tile<256, 256, 2, 2, 2, false, true>;
+using BigExact = Tile<256, 256, 2, 4, 2, false, false>;   // (two waves a SIMD: one widens numbers while the other multiplies)
+using Mid = Tile<128, 256, 2, 4, 3, false, true>;
+using Few = Tile<32, 256, 1, 4, 4, true, true>;
 
 // SLICES is fp32 slices of the reduction, EXACT the same on exact sums, as are ROWS32 and GATED.
+constexpr int kBand = 4;                  // weight tiles side by side in the work list
 enum Out { ROWS16, ROWS32, SLICES, EXACT, GATED };
 
 struct Args {
@@ -94,15 +102,18 @@ struct Item {
 
 // Where this lane's loads of an item's next chunk come from.  Row block j of the
 // wave holds rows 8 (wave + kWaves j) + lane / 8 of the tile, a 16-byte vector per
-// lane; lane l < 8 kBT also fetches the word of scales of row 8 (wave + kWaves (l /
-// 8)) + l % 8, lanes 32 and 33 those of the two blocks of weight rows.
+// lane; lane l < kRows also fetches the word of scales of row 8 (wave + kWaves (l /
+// 8)) + l % 8, lanes 32 and 33 (of a second load where rows take all lanes) those
+// of the two blocks of weight rows.
 template <class C>
 struct Loads {
     const uint8_t* rows[C::kBT];
     uint64_t live[C::kBT];                 // lanes whose row is in the item
+    uint64_t some;                         // all lanes, or none once the list is over
     const uint8_t* wmat[C::kBW];
     uint32_t woff[C::kBW];
     const uint8_t* scale;
+    const uint8_t* wscale;                 // kWords == 2
 };
 
 // silu(a) b for a result that is rounded to 4 bits: the hardware reciprocal will
@@ -122,7 +133,7 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
 }
 
 template <Out OUT, class C>
-__global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
+__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kWaves / 4, C::kWaves / 4))) void product_kernel(Args a) {
     constexpr int TM = C::TM, NW = C::NW, TF = C::TF, WF = C::WF, kOut = OUT == GATED ? NW / 2 : NW;
     constexpr bool kSlices = OUT == SLICES || OUT == EXACT, kExact = OUT != ROWS16 && OUT != SLICES;
     __shared__ __attribute__((aligned(1024))) uint8_t ring[C::STAGES * C::kStage];
@@ -160,28 +171,26 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
     const int xcd = blockIdx.x % a.xcds, slot = blockIdx.x / a.xcds, per = gridDim.x / a.xcds;
     const int part = (work + a.xcds - 1) / a.xcds, wbeg = xcd * part, wend = min(work, wbeg + part);
 
-    // item wid of the list: a group's items weight tile by weight tile (slices
-    // outermost), its row tiles adjacent.  `es`: the group found last (items only
-    // increase).
+    // item wid of the list: a group's items in bands of kBand weight tiles (slices
+    // outermost), a band row tile by row tile: the 32 workgroups of an XCD then share
+    // about 4 weight tiles and 8 row tiles instead of one and 32.  `es`: the group
+    // found last (items only increase).
     auto item_at = [&](int wid, int& es) __attribute__((always_inline)) {
         Item it;
-        int tile, xt;
+        int nt, local;
         if (a.offsets) {
             while (tstart[es + 1] * nx <= wid) ++es;
-            const int nt = tstart[es + 1] - tstart[es];
-            const int local = wid - tstart[es] * nx;
-            xt = local / nt;
-            tile = local % nt;
-            it.e = es;
-            it.r0 = soff[es] + tile * TM;
-            it.n = min(TM, soff[es + 1] - it.r0);
+            nt = tstart[es + 1] - tstart[es];
+            local = wid - tstart[es] * nx;
         } else {
-            xt = wid / ntiles;
-            tile = wid % ntiles;
-            it.e = 0;
-            it.r0 = tile * TM;
-            it.n = min(TM, a.cap - it.r0);
+            nt = ntiles;
+            local = wid;
         }
+        const int band = local / (nt * kBand), in = local - band * nt * kBand, width = min(kBand, nx - band * kBand);
+        const int tile = in / width, xt = band * kBand + in - tile * width;
+        it.e = a.offsets ? es : 0;
+        it.r0 = (a.offsets ? soff[es] : 0) + tile * TM;
+        it.n = min(TM, (a.offsets ? soff[es + 1] : a.cap) - it.r0);
         it.sp = xt / nxm;
         it.m0 = (xt - it.sp * nxm) * kOut;
         it.c0 = static_cast<int>(static_cast<int64_t>(nch) * it.sp / splits);
@@ -198,17 +207,19 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
 
     if (wbeg + slot >= wend) return;          // uniform over the workgroup
 
-    // Lane l < 8 kBT stands for row 8 (wave + kWaves (l / 8)) + l % 8 of the tile
+    // Lane l < kRows stands for row 8 (wave + kWaves (l / 8)) + l % 8 of the tile
     // (rows past the item's: its last).
     auto tile_row = [&](const Item& it) __attribute__((always_inline)) {
-        const int l = lane & (8 * C::kBT - 1);
+        const int l = lane & (C::kRows - 1);
         return it.r0 + min(8 * (wave + C::kWaves * (l / 8)) + l % 8, it.n - 1);
     };
     auto fetch_index = [&](const Item& it, int p) __attribute__((always_inline)) {
-        lds_load4(a.token + tile_row(it), lds_address(&index[p][wave][0]));
+        lds_load4_masked(a.token + tile_row(it), lds_address(&index[p][wave][0]), ~0ull);
     };
     auto item_loads = [&](const Item& it, int srow) __attribute__((always_inline)) {
         Loads<C> L;
+        int lane = lane_id();
+        asm volatile("" : "+v"(lane));                    // (worked out per item, not kept through the products)
         const int slot16 = lane % 8;
         srow = static_cast<int>(min(static_cast<unsigned>(srow), static_cast<unsigned>(a.src_rows - 1)));
 #pragma unroll
@@ -229,22 +240,31 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
         const int mb = (a.M + kBlk - 1) / kBlk, b = lane & 1;
         const int blk = min(it.m0 / kBlk + (OUT == GATED ? 0 : b), mb - 1);
         const uint8_t* const w = (OUT == GATED && b ? a.sb : a.sa) + (static_cast<size_t>(it.e) * mb + blk) * a.ldw;
-        L.scale = lane < 32 ? a.sx + static_cast<size_t>(srow) * a.ldx : w;
+        const uint8_t* const x = a.sx + static_cast<size_t>(srow) * a.ldx;
+        L.scale = C::kWords == 2 || lane < 32 ? x : w;
+        L.wscale = w;
+        L.some = ~0ull;
         return L;
     };
-    // chunk c of the item (from its c0) into stage st
-    auto issue = [&](const Loads<C>& L, const Item& it, uint8_t* st, int c) __attribute__((always_inline)) {
+    // loads [first, end) of chunk c of the item (from its c0) into stage st
+    auto issue = [&](const Loads<C>& L, const Item& it, uint8_t* st, int c, int first, int end, uint64_t lanes) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < C::kBT; ++j)
-            lds_load16_masked(L.rows[j] + c * kBlk, lds_address(st + 1024 * (wave + C::kWaves * j)), L.live[j]);
-#pragma unroll
-        for (int j = 0; j < C::kBW; ++j) {
-            const uint8_t* const src = L.wmat[j] + (L.woff[j] + static_cast<uint32_t>(c) * kBlk);
-            const uint32_t dst = lds_address(st + C::kTokens + 1024 * (wave + C::kWaves * j));
-            if constexpr (C::NT) lds_load16_nt(src, dst);
-            else lds_load16(src, dst);
+        for (int n = 0; n < C::kLoads; ++n) {
+            if (n < first || n >= end) continue;
+            if (n < C::kBT) {
+                lds_load16_masked(L.rows[n] + c * kBlk, lds_address(st + 1024 * (wave + C::kWaves * n)), L.live[n] & lanes);
+            } else if (n < C::kBT + C::kBW) {
+                const int j = n - C::kBT;
+                const uint8_t* const src = L.wmat[j] + (L.woff[j] + static_cast<uint32_t>(c) * kBlk);
+                const uint32_t dst = lds_address(st + C::kTokens + 1024 * (wave + C::kWaves * j));
+                if constexpr (C::NT) lds_load16_masked_nt(src, dst, L.some & lanes);
+                else lds_load16_masked(src, dst, L.some & lanes);
+            } else if (n == C::kBT + C::kBW) {
+                lds_load4_masked(L.scale + ((it.c0 + c) & ~3), lds_address(st + C::kScales + C::kArea * wave), L.some & lanes);
+            } else {
+                lds_load4_masked(L.wscale + ((it.c0 + c) & ~3), lds_address(st + C::kScales + C::kArea * wave + 256), L.some & lanes);
+            }
         }
-        lds_load4(L.scale + ((it.c0 + c) & ~3), lds_address(st + C::kScales + 256 * wave));
     };
 
     // The load side runs ahead of the products by up to kAhead chunks, over the
@@ -252,9 +272,9 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
     // the item before is loaded: kAhead or more chunks' loads later (else after a
     // wait for all) they have arrived, since loads complete in order.
     int lwid = wbeg + slot;
-    int les = 0, lc = 0, lpar = 0, ls = 0, ahead = 0;
+    int les = 0, lc = 0, lpar = 0, ls = 0;
     Item lit = item_at(lwid, les), lnext = lit;
-    bool more = lwid + per < wend, live = true;
+    bool more = lwid + per < wend;
     Loads<C> L = item_loads(lit, a.token ? a.token[tile_row(lit)] : tile_row(lit));
     auto look_ahead = [&]() __attribute__((always_inline)) {
         if (!more) return;
@@ -262,15 +282,20 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
         if (a.token) fetch_index(lnext, lpar);
     };
     look_ahead();
-    auto issue_next = [&]() __attribute__((always_inline)) {
-        if (!live) return;
-        issue(L, lit, ring + ls * C::kStage, lc);
+    // The next chunk's loads, a part at a time between products (all at once they hold
+    // up a wave's own reads and products for half a chunk); then on to the one after.
+    // Past the list's end they are instructions without lanes, which count like the others.
+    auto issue_part = [&](int first, int end, uint64_t lanes = ~0ull) __attribute__((always_inline)) {
+        issue(L, lit, ring + ls * C::kStage, lc, first, end, lanes);
+    };
+    auto issued = [&]() __attribute__((always_inline)) {
         ls = ls + 1 == C::STAGES ? 0 : ls + 1;
-        ++ahead;
         if (++lc < lit.nc) return;
         lc = 0;
         if (!more) {
-            live = false;
+            L.some = 0;
+#pragma unroll
+            for (int j = 0; j < C::kBT; ++j) L.live[j] = 0;
             return;
         }
         int srow = tile_row(lnext);
@@ -286,18 +311,25 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
         L = item_loads(lit, srow);
         look_ahead();
     };
-    for (int c = 0; c < C::kAhead; ++c) issue_next();
+#pragma unroll 1
+    for (int c = 0; c < C::kAhead; ++c) {
+        issue_part(0, C::kLoads);
+        issued();
+    }
 
     const int l32 = lane & 31, lh = lane >> 5;
     const int wm = wave / C::WW, wn = wave % C::WW;       // row group, weight group
     const int brow = 32 * TF * wm;
+    constexpr int FG = C::kFrag;
+    // the first weight row of fragment i: the gated tile's second half of fragments
+    // are the W3 rows of the first half's features
     auto arow = [&](int i) __attribute__((always_inline)) {
-        return OUT == GATED ? NW / 2 * i + 32 * wn : 64 * wn + 32 * i;
+        return OUT == GATED ? (i < FG ? 0 : NW / 2) + 32 * (FG * wn + i % FG) : 32 * (WF * wn + i);
     };
     // where the word of scales of row r lies among the stage's scales
     auto scale_at = [&](int r) __attribute__((always_inline)) {
         const int b = r / 8;
-        return 256 * (b % C::kWaves) + 4 * (8 * (b / C::kWaves) + r % 8);
+        return C::kArea * (b % C::kWaves) + 4 * (8 * (b / C::kWaves) + r % 8);
     };
 
     int cs = 0, es = 0, stored = 0;
@@ -310,76 +342,232 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
 #pragma unroll
             for (int j = 0; j < TF; ++j) acc[i][j] = f32x16{};
 
-        for (int c = 0; c < cur.nc; ++c) {
-            // This wave's loads of the chunk have arrived; later chunks' (and the
-            // stores of the item before, issued after the chunks that were then on
-            // their way) may be under way.  Then everyone's have, and everyone is
-            // done with the stage that is filled next.
-            {
-                const int later = ahead - 1;
-                const int st = c < C::kAhead ? stored : 0;
-                auto wait = [&](auto n) __attribute__((always_inline)) {
-                    constexpr int N = decltype(n)::value;
-                    if (st == 0) wait_vm<N>();
-                    else if (st < 8) wait_vm<N + 1>();
-                    else wait_vm<N + 8>();
-                };
-                if (C::kAhead >= 3 && later >= 2) wait(std::integral_constant<int, (C::kAhead >= 3 ? 2 : 0) * C::kLoads>{});
-                else if (C::kAhead >= 2 && later >= 1) wait(std::integral_constant<int, (C::kAhead >= 2 ? 1 : 0) * C::kLoads>{});
-                else wait(std::integral_constant<int, 0>{});
-            }
+        // Chunk c: this wave's loads of it have arrived; later chunks' (and the stores
+        // of the item before, issued after the chunks that were then on their way) may
+        // be under way.  Then everyone's have, and everyone is done with the stage that
+        // is filled next.
+        auto arrive = [&](int c) __attribute__((always_inline)) {
+            constexpr int N = (C::kAhead - 1) * C::kLoads;
+            if (c >= C::kAhead || stored == 0) wait_vm<N>();
+            else if (stored < 8) wait_vm<N + 1>();
+            else wait_vm<N + 8>();
             lds_barrier();
-            --ahead;
-            const uint8_t* const st = ring + cs * C::kStage;
+            const uint8_t* const at = ring + cs * C::kStage;
             cs = cs + 1 == C::STAGES ? 0 : cs + 1;
-            issue_next();
-            if (!active) continue;
+            return at;
+        };
+        // half k of a chunk's operands (which of a block's numbers meet does not
+        // matter as long as both sides agree)
+        auto frag = [&](const uint8_t* base, int r, int k) __attribute__((always_inline)) {
+            const i32x4 lo = *reinterpret_cast<const i32x4*>(base + at_row(r, 4 * k + lh));
+            const i32x4 hi = *reinterpret_cast<const i32x4*>(base + at_row(r, 4 * k + 2 + lh));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        auto read_a = [&](i32x8 (&A)[WF], const uint8_t* st, int k) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < WF; ++i) A[i] = frag(st + C::kTokens, arow(i) + l32, k);
+        };
+        auto read_b = [&](const uint8_t* st, int j, int k) __attribute__((always_inline)) { return frag(st, brow + 32 * j + l32, k); };
+        struct Scales {
+            int w[2], x[TF];
+        };
+        // (the words of four chunks' scales; `pick` leaves chunk c's in the lowest byte)
+        auto read_scales = [&](Scales& s, const uint8_t* st) __attribute__((always_inline)) {
+            const uint8_t* const at = st + C::kScales;
+            s.w[0] = *reinterpret_cast<const uint32_t*>(at + C::kArea * wave + C::kWeightWord + 4 * (arow(0) / kBlk));
+            s.w[1] = OUT == GATED ? *reinterpret_cast<const uint32_t*>(at + C::kArea * wave + C::kWeightWord + 4) : s.w[0];
+#pragma unroll
+            for (int j = 0; j < TF; ++j) s.x[j] = *reinterpret_cast<const uint32_t*>(at + scale_at(brow + 32 * j + l32));
+        };
+        auto pick = [&](Scales& s, int c) __attribute__((always_inline)) {
             const int sh = 8 * ((cur.c0 + c) & 3);
-            int ws[WF], xs[TF];
+            s.w[0] = static_cast<uint32_t>(s.w[0]) >> sh;
+            s.w[1] = static_cast<uint32_t>(s.w[1]) >> sh;
 #pragma unroll
-            for (int i = 0; i < WF; ++i)
-                ws[i] = *reinterpret_cast<const uint32_t*>(st + C::kScales + 256 * wave + 128 + 4 * (arow(i) / kBlk)) >> sh;
+            for (int j = 0; j < TF; ++j) s.x[j] = static_cast<uint32_t>(s.x[j]) >> sh;
+        };
+        // the products of A with row fragment j
+        auto multiply = [&](const i32x8 (&A)[WF], const i32x8& B, int j, const Scales& s) __attribute__((always_inline)) {
+            // (products have no side effects: unless their sums are asked for here, the
+            // compiler moves them behind the loads, to where the sums are used)
+            auto done = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < TF; ++j)
-                xs[j] = *reinterpret_cast<const uint32_t*>(st + C::kScales + scale_at(brow + 32 * j + l32)) >> sh;
+                for (int i = 0; i < WF; ++i) {
+                    if constexpr (WF * TF == 16) asm volatile("" : "+a"(acc[i][j]));
+                    else asm volatile("" : "+v"(acc[i][j]));
+                }
+            };
+            if constexpr (kExact) {
+                // both scales go to the rows, so that no factor leaves bf16's range unless
+                // the result does; W3 (another block) gets its scale's ratio to W1's
+                const float ratio = OUT == GATED ? power((s.w[1] & 255) - (s.w[0] & 255) + 127) : 1.0f;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                i32x8 A[WF], B[TF];
-                // (which of a block's numbers meet does not matter as long as both sides agree)
-                auto frag = [&](const uint8_t* base, int r) __attribute__((always_inline)) {
-                    const i32x4 lo = *reinterpret_cast<const i32x4*>(base + at_row(r, 4 * k + lh));
-                    const i32x4 hi = *reinterpret_cast<const i32x4*>(base + at_row(r, 4 * k + 2 + lh));
-                    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                };
+                for (int p = 0; p < 4; ++p) {
+                    const bf16x8 b = widen(B[2 * p], B[2 * p + 1], power((s.x[j] & 255) + (s.w[0] & 255) - 127));
 #pragma unroll
-                for (int i = 0; i < WF; ++i) A[i] = frag(st + C::kTokens, arow(i) + l32);
+                    for (int i = 0; i < WF; ++i)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            widen(A[i][2 * p], A[i][2 * p + 1], OUT == GATED && i >= FG ? ratio : 1.0f), b, acc[i][j], 0, 0, 0);
+                }
+            } else {
 #pragma unroll
-                for (int j = 0; j < TF; ++j) B[j] = frag(st, brow + 32 * j + l32);
-                if constexpr (kExact) {
-                    // both scales go to the rows, so that no factor leaves bf16's range unless
-                    // the result does; W3 (another block) gets its scale's ratio to W1's
-                    const float ratio = OUT == GATED ? power((ws[1] & 255) - (ws[0] & 255) + 127) : 1.0f;
+                for (int i = 0; i < WF; ++i)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A[i], B, acc[i][j], 0, 0, 0, s.w[0], 0, s.x[j]);
+            }
+            done();
+        };
+
+        // group g of the 2 TF groups of products between two arrivals, and its part of the loads
+        constexpr int kGroups = 2 * TF;
+        auto part = [&](int g) __attribute__((always_inline)) {
+            issue_part(C::kLoads * g / kGroups, C::kLoads * (g + 1) / kGroups);
+        };
+        // Half by half: the next half's weights are read ahead of a half's products,
+        // its rows fragment by fragment as the products are done with them; the next
+        // chunk's barrier lies before the second half's products.  (Not DEEP: two
+        // waves a SIMD fill in for each other.)
+        if constexpr (!C::DEEP) {
+#pragma unroll 1
+            for (int c = 0; c < cur.nc; ++c) {
+                const uint8_t* const st = arrive(c);
+                if (!active) {
+                    issue_part(0, C::kLoads);
+                    issued();
+                    continue;
+                }
+                Scales sc;
+                read_scales(sc, st);
+                pick(sc, c);
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        bf16x8 Ab[WF];
+                for (int k = 0; k < 2; ++k) {
+                    i32x8 A[WF], B[TF];
+                    read_a(A, st, k);
 #pragma unroll
-                        for (int i = 0; i < WF; ++i) Ab[i] = widen(A[i][2 * p], A[i][2 * p + 1], i == 0 ? 1.0f : ratio);
+                    for (int j = 0; j < TF; ++j) B[j] = read_b(st, j, k);
+                    if constexpr (OUT != GATED) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int j = 0; j < TF; ++j) {
-                            const bf16x8 Bb = widen(B[j][2 * p], B[j][2 * p + 1], power((xs[j] & 255) + (ws[0] & 255) - 127));
+                    for (int j = 0; j < TF; ++j) {
+                        multiply(A, B[j], j, sc);
+                        if (k == 0) issue_part(C::kLoads * j / TF, C::kLoads * (j + 1) / TF);
+                    }
+                }
+                issued();
+            }
+        } else if constexpr (!kExact && WF == 4 && TF == 4) {
+            // One wave a SIMD, so a product's 64 cycles are the time for everything else:
+            // after each of a half's 16 a slot with a read for the next half (weights
+            // into registers of their own, rows where the products are done with the old)
+            // and, in a chunk's second half, loads of the chunk after the next.
+            const uint8_t* st = arrive(0);
+            i32x8 A0[WF], A1[WF], B[TF - 1], L0, L1;      // L: the last row fragment
+            Scales sc, sn;
+            auto half = [&](const i32x8 (&A)[WF], const i32x8& last, auto slot) __attribute__((always_inline)) {
 #pragma unroll
-                            for (int i = 0; i < WF; ++i)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Ab[i], Bb, acc[i][j], 0, 0, 0);
-                        }
+                for (int q = 0; q < WF * TF; ++q) {
+                    const int j = q / WF, i = q % WF;
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A[i], j == TF - 1 ? last : B[j < TF - 1 ? j : 0], acc[i][j], 0, 0, 0, sc.w[0], 0, sc.x[j]);
+                    slot(q);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                // (products have no side effects: unless their sums are asked for here, the
+                // compiler moves them to where they are used)
+#pragma unroll
+                for (int j = 0; j < TF; ++j)
+#pragma unroll
+                    for (int i = 0; i < WF; ++i) asm volatile("" : "+a"(acc[i][j]));
+            };
+            auto read_next = [&](i32x8 (&A)[WF], i32x8& last, int k, int q) __attribute__((always_inline)) {
+                if (q < WF) A[q] = frag(st + C::kTokens, arow(q) + l32, k);
+                else if (q % WF == 0) B[q / WF - 1] = read_b(st, q / WF - 1, k);
+                else if (q == WF * TF - 2) last = read_b(st, TF - 1, k);
+            };
+            // (waves whose rows lie past the item's multiply what they find: branches around
+            // the products would cost registers)
+            read_scales(sc, st);
+            read_a(A0, st, 0);
+            pick(sc, 0);
+#pragma unroll
+            for (int j = 0; j < TF - 1; ++j) B[j] = read_b(st, j, 0);
+            L0 = read_b(st, TF - 1, 0);
+            issue_part(0, C::kLoads);
+            issued();
+            // (the last chunk's second half goes through the same code: what it reads is
+            // not used, its loads have no lanes)
+#pragma unroll 1
+            for (int c = 0; c < cur.nc; ++c) {
+                half(A0, L0, [&](int q) __attribute__((always_inline)) { read_next(A1, L1, 1, q); });
+                const bool next = c + 1 < cur.nc;
+                if (next) {
+                    st = arrive(c + 1);
+                    read_scales(sn, st);
+                }
+                const uint64_t lanes = next ? ~0ull : 0ull;
+                half(A1, L1, [&](int q) __attribute__((always_inline)) {
+                    read_next(A0, L0, 0, q);
+                    issue_part(C::kLoads * q / 16, C::kLoads * (q + 1) / 16, lanes);
+                });
+                sc = sn;
+                pick(sc, c + 1);
+                if (next) issued();
+            }
+        } else {
+            const uint8_t* st = arrive(0);
+            i32x8 A0[WF], A1[WF], B[TF];
+            Scales sc, sn;
+            if (active) {
+                read_scales(sc, st);
+                pick(sc, 0);
+                read_a(A0, st, 0);
+#pragma unroll
+                for (int j = 0; j < TF; ++j) B[j] = read_b(st, j, 0);
+            }
+            issue_part(0, C::kLoads * TF / kGroups);
+            auto chunk = [&](int c, auto more_chunks) __attribute__((always_inline)) {
+                constexpr bool kNext = decltype(more_chunks)::value;
+                if (active) {
+                    read_a(A1, st, 1);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int j = 0; j < TF; ++j) {
+                        multiply(A0, B[j], j, sc);
+                        B[j] = read_b(st, j, 1);
+                        part(TF + j);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                 } else {
-#pragma unroll
-                    for (int j = 0; j < TF; ++j)
-#pragma unroll
-                        for (int i = 0; i < WF; ++i)
-                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A[i], B[j], acc[i][j], 0, 0, 0, ws[i], 0, xs[j]);
+                    issue_part(C::kLoads * TF / kGroups, C::kLoads);
                 }
-            }
+                issued();
+                if constexpr (kNext) {
+                    st = arrive(c + 1);
+                    if (active) {
+                        read_scales(sn, st);
+                        read_a(A0, st, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (active) {
+#pragma unroll
+                    for (int j = 0; j < TF; ++j) {
+                        multiply(A1, B[j], j, sc);
+                        if constexpr (kNext) {
+                            B[j] = read_b(st, j, 0);
+                            part(j);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                } else if (kNext) {
+                    issue_part(0, C::kLoads * TF / kGroups);
+                }
+                if constexpr (kNext) {
+                    sc = sn;
+                    pick(sc, c + 1);
+                }
+            };
+            int c = 0;
+#pragma unroll 1
+            for (; c + 1 < cur.nc; ++c) chunk(c, std::true_type{});
+            chunk(c, std::false_type{});
         }
 
         // A lane holds features 8 (q / 4) + 4 lh + q % 4 of each 32-row weight
@@ -388,34 +576,80 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
         lds_barrier();
         uint8_t* const free_stage = ring + (cs == 0 ? C::STAGES - 1 : cs - 1) * C::kStage;
         stored = 0;
+        // (the epilogue's addresses are worked out here, not kept in registers through the products)
+        int lane_now = lane_id();
+        asm volatile("" : "+v"(lane_now));
+        const int lane = lane_now, l32 = lane & 31, lh = lane >> 5;
+        uint8_t* const tb = free_stage + wave * (C::kScales / C::kWaves);
+        static_assert(C::kScales / C::kWaves >= 4096, "32 rows of 128 bytes per wave");
+        // 128-byte rows of the wave, 32 of them: `put` writes this lane's row (row
+        // l32, 16-byte slots XORed with it), then adjacent lanes store adjacent 16
+        // bytes, slots 0..3 from `lo` on and 4..7 from `hi` on, where they are inside
+        // the output (room bytes left from each).
+        auto rows_out = [&](int nv, uint8_t* lo, int room_lo, uint8_t* hi, int room_hi, size_t pitch) __attribute__((always_inline)) {
+            wave_lds_sync();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (8 * k >= nv) break;
+                const int r = 8 * k + lane / 8, v = lane % 8;
+                const u32x4 d = *reinterpret_cast<const u32x4*>(tb + r * kBlk + ((v ^ (r & 7)) << 4));
+                const bool first = v < 4;
+                if (r < nv && 16 * (v & 3) < (first ? room_lo : room_hi))
+                    *reinterpret_cast<u32x4*>((first ? lo : hi) + r * pitch + 16 * (v & 3)) = d;
+                if (room_lo > 0) ++stored;
+            }
+            wave_lds_sync();
+        };
+        // (the 256 accumulators stay where they are until a fragment's turn comes)
+        auto take = [&](f32x16& v) __attribute__((always_inline)) {
+            if constexpr (WF * TF == 16) asm volatile("" : "+a"(v));
+        };
+        auto slot_at = [&](int v) __attribute__((always_inline)) { return tb + l32 * kBlk + ((v ^ (l32 & 7)) << 4); };
+        // two fragments as bf16: 32 features each
+        auto put16 = [&](const f32x16& p, const f32x16& q) __attribute__((always_inline)) {
+#pragma unroll
+            for (int qb = 0; qb < 4; ++qb) {
+                *reinterpret_cast<uint2*>(slot_at(qb) + 8 * lh) = uint2{pack_bf16x2(p[4 * qb], p[4 * qb + 1]), pack_bf16x2(p[4 * qb + 2], p[4 * qb + 3])};
+                __builtin_amdgcn_sched_barrier(0);
+                *reinterpret_cast<uint2*>(slot_at(4 + qb) + 8 * lh) = uint2{pack_bf16x2(q[4 * qb], q[4 * qb + 1]), pack_bf16x2(q[4 * qb + 2], q[4 * qb + 3])};
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
         if constexpr (OUT == GATED) {
-            // h = silu(g) u; the largest of a row's 128 features over its 2 lanes and
-            // the WW waves; 8 bits each, whole 128-byte rows stored.
-            float* const most = reinterpret_cast<float*>(free_stage + TM * kBlk);      // [WW][TM]
-            if (a.saved) {
+            if (a.saved) {                                // g and u of the same 32 features side by side
 #pragma unroll
                 for (int j = 0; j < TF; ++j) {
-                    const int r = brow + 32 * j + l32;
-                    if (r >= cur.n) continue;
-                    uint16_t* const g = a.saved + static_cast<size_t>(cur.r0 + r) * 2 * a.M + cur.m0 + 32 * wn + 4 * lh;
+                    const int nv = min(32, cur.n - brow - 32 * j);
+                    if (nv <= 0) break;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int qb = 0; qb < 4; ++qb)
-                            if (cur.m0 + 32 * wn + 8 * qb < a.M)
-                                *reinterpret_cast<uint2*>(g + i * a.M + 8 * qb) =
-                                    uint2{pack_bf16x2(acc[i][j][4 * qb], acc[i][j][4 * qb + 1]), pack_bf16x2(acc[i][j][4 * qb + 2], acc[i][j][4 * qb + 3])};
+                    for (int i = 0; i < FG; ++i) {
+                        const int f = cur.m0 + 32 * (FG * wn + i), room = 2 * (a.M - f);
+                        __builtin_amdgcn_sched_barrier(0);
+                        put16(acc[i][j], acc[FG + i][j]);
+                        uint8_t* const to = reinterpret_cast<uint8_t*>(a.saved + static_cast<size_t>(cur.r0 + brow + 32 * j) * 2 * a.M + f);
+                        rows_out(nv, to, room, to + 2 * static_cast<size_t>(a.M), room, 4 * static_cast<size_t>(a.M));
+                    }
                 }
+                lds_barrier();                            // (the waves' rows give way to what follows)
             }
+            // h = silu(g) u; the largest of a row's 128 features over its 2 lanes and
+            // the WW waves; 8 bits each, whole 128-byte rows stored.  (h is worked out
+            // twice: 128 more numbers per lane would not stay in registers.)
+            float* const most = reinterpret_cast<float*>(free_stage + TM * kBlk);      // [WW][TM]
+            // (M is a multiple of 8: whole groups of a lane pair lie past it, as zeros)
+            auto hidden = [&](int i, int j, int q) __attribute__((always_inline)) {
+                const uint32_t keep = cur.m0 + 32 * (FG * wn + i) + 8 * (q / 4) < a.M ? ~0u : 0u;
+                return __uint_as_float(__float_as_uint(swiglu(acc[i][j][q], acc[FG + i][j][q])) & keep);
+            };
 #pragma unroll
             for (int j = 0; j < TF; ++j) {
                 float m = 0.f;
 #pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    // (M is a multiple of 8: whole groups of a lane pair lie past it)
-                    const float h = cur.m0 + 32 * wn + 8 * (q / 4) < a.M ? swiglu(acc[0][j][q], acc[1][j][q]) : 0.f;
-                    acc[0][j][q] = h;
-                    m = fmaxf(m, finite_abs(h));
+                for (int i = 0; i < FG; ++i) {
+                    take(acc[i][j]);
+                    take(acc[FG + i][j]);
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) m = fmaxf(m, finite_abs(hidden(i, j, q)));
                 }
                 m = fmaxf(m, __shfl_xor(m, 32, kWave));
                 if (lh == 0) most[wn * TM + brow + 32 * j + l32] = m;
@@ -431,65 +665,59 @@ __global__ __launch_bounds__(C::kThreads) void product_kernel(Args a) {
                 const float s = scale_inverse(b);
                 if (wn == 0 && lh == 0 && r < cur.n) a.sout[static_cast<size_t>(cur.r0 + r) * a.ldo + cur.m0 / kBlk] = static_cast<uint8_t>(b);
 #pragma unroll
-                for (int qb = 0; qb < 4; ++qb) {
-                    float o[4];
+                for (int i = 0; i < FG; ++i) {
+                    take(acc[i][j]);
+                    take(acc[FG + i][j]);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) o[q] = or_nan(acc[0][j][4 * qb + q]) * s;
-                    // features 32 wn + 8 qb + 4 lh ..: 4 bytes of vector 2 wn + qb / 2
-                    *reinterpret_cast<uint32_t*>(free_stage + at_row(r, 2 * wn + qb / 2) + 8 * (qb & 1) + 4 * lh) = pack_e4m3(o[0], o[1], o[2], o[3]);
+                    for (int qb = 0; qb < 4; ++qb) {
+                        float o[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) o[q] = or_nan(hidden(i, j, 4 * qb + q)) * s;
+                        // features 32 (FG wn + i) + 8 qb + 4 lh ..: 4 bytes of vector 2 (FG wn + i) + qb / 2
+                        *reinterpret_cast<uint32_t*>(free_stage + at_row(r, 2 * (FG * wn + i) + qb / 2) + 8 * (qb & 1) + 4 * lh) = pack_e4m3(o[0], o[1], o[2], o[3]);
+                    }
                 }
             }
             lds_barrier();
             const size_t Mp = static_cast<size_t>((a.M + kBlk - 1) / kBlk) * kBlk;
+            stored = 0;
 #pragma unroll
             for (int k = 0; k < TM / 8 / C::kWaves; ++k) {
-                const int r = 8 * (wave + C::kWaves * k) + lane / 8, v = lane % 8;
+                const int r0 = 8 * (wave + C::kWaves * k), r = r0 + lane / 8, v = lane % 8;
                 if (r < cur.n) {
                     const u32x4 d = *reinterpret_cast<const u32x4*>(free_stage + at_row(r, v));
                     *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.out) + (cur.r0 + r) * Mp + cur.m0 + 16 * v) = d;
                 }
+                if (r0 < cur.n) ++stored;
             }
             // (what the waves read of `free_stage` is refilled after the next chunk's barrier)
         } else {
-            uint8_t* const tb = free_stage + wave * (C::kScales / C::kWaves);
-            static_assert(C::kScales / C::kWaves >= 4096, "32 rows of 128 bytes per wave");
 #pragma unroll
             for (int j = 0; j < TF; ++j) {
                 const int nv = min(32, cur.n - brow - 32 * j);    // uniform
                 if (nv <= 0) break;
                 const size_t row0 = static_cast<size_t>(cur.r0 + brow + 32 * j);
-                auto rows_out = [&](uint8_t* op, size_t pitch, int room) __attribute__((always_inline)) {
-                    wave_lds_sync();
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (8 * k >= nv) break;
-                        const int r = 8 * k + lane / 8, v = lane % 8;
-                        const u32x4 d = *reinterpret_cast<const u32x4*>(tb + r * kBlk + ((v ^ (r & 7)) << 4));
-                        if (r < nv && 16 * v < room) *reinterpret_cast<u32x4*>(op + (row0 + r) * pitch + 16 * v) = d;
-                        if (room > 0) ++stored;
-                    }
-                    wave_lds_sync();
-                };
                 if constexpr (OUT == ROWS16) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int qb = 0; qb < 4; ++qb)
-                            *reinterpret_cast<uint2*>(tb + l32 * kBlk + (((4 * i + qb) ^ (l32 & 7)) << 4) + 8 * lh) =
-                                uint2{pack_bf16x2(acc[i][j][4 * qb + 0], acc[i][j][4 * qb + 1]),
-                                      pack_bf16x2(acc[i][j][4 * qb + 2], acc[i][j][4 * qb + 3])};
-                    const int f = cur.m0 + 64 * wn;
-                    rows_out(reinterpret_cast<uint8_t*>(static_cast<uint16_t*>(a.out) + f), static_cast<size_t>(a.M) * 2, 2 * (a.M - f));
+                    for (int i = 0; i < WF; i += 2) {
+                        const int f = cur.m0 + 32 * (WF * wn + i), room = 2 * (a.M - f);
+                        take(acc[i][j]);
+                        take(acc[i + 1][j]);
+                        put16(acc[i][j], acc[i + 1][j]);
+                        uint8_t* const to = reinterpret_cast<uint8_t*>(static_cast<uint16_t*>(a.out) + row0 * a.M + f);
+                        rows_out(nv, to, room, to + 64, room - 64, 2 * static_cast<size_t>(a.M));
+                    }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int f = cur.m0 + 64 * wn + 32 * i;
+                    for (int i = 0; i < WF; ++i) {
+                        const int f = cur.m0 + 32 * (WF * wn + i), room = 4 * (a.M - f);
+                        take(acc[i][j]);
 #pragma unroll
                         for (int qb = 0; qb < 4; ++qb)
-                            *reinterpret_cast<f32x4*>(tb + l32 * kBlk + (((2 * qb + lh) ^ (l32 & 7)) << 4)) =
+                            *reinterpret_cast<f32x4*>(slot_at(2 * qb + lh)) =
                                 f32x4{acc[i][j][4 * qb + 0], acc[i][j][4 * qb + 1], acc[i][j][4 * qb + 2], acc[i][j][4 * qb + 3]};
-                        float* const op = static_cast<float*>(a.out) + static_cast<size_t>(cur.sp) * a.cap * a.M + f;
-                        rows_out(reinterpret_cast<uint8_t*>(op), static_cast<size_t>(a.M) * 4, 4 * (a.M - f));
+                        float* const op = static_cast<float*>(a.out) + static_cast<size_t>(cur.sp) * a.cap * a.M + row0 * a.M + f;
+                        rows_out(nv, reinterpret_cast<uint8_t*>(op), room, reinterpret_cast<uint8_t*>(op) + 64, room - 64, 4 * static_cast<size_t>(a.M));
                     }
                 }
             }
@@ -735,7 +963,7 @@ hipError_t launch_tile(Args& a, const Rows& r, hipStream_t s) {
 }
 template <Out OUT>
 hipError_t launch_out(int tm, Args& a, const Rows& r, hipStream_t s) {
-    if (tm == Big::TM) return launch_tile<OUT, Big>(a, r, s);
+    if (tm == Big::TM) return launch_tile<OUT, std::conditional_t<OUT == ROWS16 || OUT == SLICES, Big, BigExact>>(a, r, s);
     if (tm == Mid::TM) return launch_tile<OUT, Mid>(a, r, s);
     return launch_tile<OUT, Few>(a, r, s);
 }

@@ -122,24 +122,27 @@ __device__ __forceinline__ uint64_t uniform(uint64_t v) {
     return v;
 }
 
-// Loads to LDS from an address per lane: 16 bytes a lane to lds + 16 lane (nt: past
-// the caches; masked: of the lanes given), 4 bytes to lds + 4 lane.  In asm, so
-// that the compiler adds no waits for them to every LDS read (fp8.hip counts them); the
-// s_nop as in Operand::load, in the masked form the moves of exec.
-__device__ __forceinline__ void lds_load16(const void* src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(src), "s"(lds) : "memory", "m0");
-}
-__device__ __forceinline__ void lds_load16_nt(const void* src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" :: "v"(src), "s"(lds) : "memory", "m0");
-}
+// Loads to LDS of the lanes given, from an address per lane: 16 bytes a lane to lds
+// + 16 lane (nt: past the caches), 4 bytes to lds + 4 lane.  In asm, so that the
+// compiler adds no waits for them to every LDS read (fp8.hip counts them); the moves of
+// exec are the wait state after the write of M0.
 __device__ __forceinline__ void lds_load16_masked(const void* src, uint32_t lds, uint64_t lanes) {
     uint64_t save;
     asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 %0, exec\n\ts_mov_b64 exec, %3\n\t"
                  "global_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, %0"
                  : "=&s"(save) : "v"(src), "s"(lds), "s"(lanes) : "memory", "m0");
 }
-__device__ __forceinline__ void lds_load4(const void* src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(src), "s"(lds) : "memory", "m0");
+__device__ __forceinline__ void lds_load16_masked_nt(const void* src, uint32_t lds, uint64_t lanes) {
+    uint64_t save;
+    asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 %0, exec\n\ts_mov_b64 exec, %3\n\t"
+                 "global_load_lds_dwordx4 %1, off nt\n\ts_mov_b64 exec, %0"
+                 : "=&s"(save) : "v"(src), "s"(lds), "s"(lanes) : "memory", "m0");
+}
+__device__ __forceinline__ void lds_load4_masked(const void* src, uint32_t lds, uint64_t lanes) {
+    uint64_t save;
+    asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 %0, exec\n\ts_mov_b64 exec, %3\n\t"
+                 "global_load_lds_dword %1, off\n\ts_mov_b64 exec, %0"
+                 : "=&s"(save) : "v"(src), "s"(lds), "s"(lanes) : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)));
