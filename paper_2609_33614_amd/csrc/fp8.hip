@@ -37,11 +37,10 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-template <int TM_, int NW_, int WT_, int WW_, int STAGES_, bool NT_, bool DEEP_>
+template <int TM_, int NW_, int WT_, int WW_, int STAGES_, bool NT_>
 struct Tile {
     static constexpr int TM = TM_, NW = NW_, WT = WT_, WW = WW_, STAGES = STAGES_;
     static constexpr bool NT = NT_;                       // weights stream past the caches
-    static constexpr bool DEEP = DEEP_;                   // operands are read ahead of the products before
     static constexpr int kWaves = WT * WW, kThreads = kWaves * kWave;
     static constexpr int TF = TM / (32 * WT), WF = NW / (32 * WW);
     static constexpr int kTokens = TM * kBlk;             // bytes of a stage's rows
@@ -59,14 +58,14 @@ struct Tile {
     static_assert(TF * 32 * WT == TM && WF * 32 * WW == NW && (WF == 2 || WF == 4) && NW == 256, "fragments cover the tile; a gated tile is one block wide");
     static_assert(kAhead >= 1 && kAhead <= 3, "waits count up to three chunks");
 };
-using Big = Tile<256, 256, 2, 2, 2, false, true>;
-using BigExact = Tile<256, 256, 2, 4, 2, false, false>;   // (two waves a SIMD: one widens numbers while the other multiplies)
-using Mid = Tile<128, 256, 2, 4, 3, false, true>;
-using Few = Tile<32, 256, 1, 4, 4, true, true>;
+using Big = Tile<256, 256, 2, 2, 2, false>;
+using Mid = Tile<128, 256, 2, 4, 3, false>;
+using Few = Tile<32, 256, 1, 4, 4, true>;
 
-// SLICES is fp32 slices of the reduction, EXACT the same on exact sums, as are ROWS32 and GATED.
+// SLICES is fp32 slices of the reduction, EXACT the same on exact sums, as are ROWS32,
+// GATED and SAVED (GATED that also leaves g and u in bf16).
 constexpr int kBand = 4;                  // weight tiles side by side in the work list
-enum Out { ROWS16, ROWS32, SLICES, EXACT, GATED };
+enum Out { ROWS16, ROWS32, SLICES, EXACT, GATED, SAVED };
 
 struct Args {
     const uint8_t* wa;         // [groups][M][Kp]
@@ -85,7 +84,7 @@ struct Args {
     void* out;                 // ROWS16, ROWS32: [cap][M]; SLICES: [splits][cap][M] fp32; GATED: [cap][Mp] 8 bits
     uint8_t* sout;             // GATED: [cap][ldo] scales
     int ldo;
-    uint16_t* saved;           // GATED: [cap][2 M] bf16 or null
+    uint16_t* saved;           // SAVED: [cap][2 M] bf16
 };
 
 // 16-byte vector v of 128-byte row r in LDS: two rows to a line of the 64 banks,
@@ -134,7 +133,8 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
 
 template <Out OUT, class C>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::kWaves / 4, C::kWaves / 4))) void product_kernel(Args a) {
-    constexpr int TM = C::TM, NW = C::NW, TF = C::TF, WF = C::WF, kOut = OUT == GATED ? NW / 2 : NW;
+    constexpr bool kGated = OUT == GATED || OUT == SAVED;
+    constexpr int TM = C::TM, NW = C::NW, TF = C::TF, WF = C::WF, kOut = kGated ? NW / 2 : NW;
     constexpr bool kSlices = OUT == SLICES || OUT == EXACT, kExact = OUT != ROWS16 && OUT != SLICES;
     __shared__ __attribute__((aligned(1024))) uint8_t ring[C::STAGES * C::kStage];
     __shared__ int tstart[kMaxExperts + 1];
@@ -233,13 +233,13 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
         for (int j = 0; j < C::kBW; ++j) {
             const int r0 = 8 * (wave + C::kWaves * j), r = r0 + lane / 8;
             // (a last tile past M loads its last row again; those results are not used)
-            const int row = min(it.m0 + (OUT == GATED ? r & (NW / 2 - 1) : r), a.M - 1);
+            const int row = min(it.m0 + (kGated ? r & (NW / 2 - 1) : r), a.M - 1);
             L.woff[j] = static_cast<uint32_t>(row) * static_cast<uint32_t>(a.Kp) + it.c0 * kBlk + ((slot16 ^ swz(r)) << 4);
-            L.wmat[j] = (OUT == GATED && r0 >= NW / 2 ? a.wb : a.wa) + emat;
+            L.wmat[j] = (kGated && r0 >= NW / 2 ? a.wb : a.wa) + emat;
         }
         const int mb = (a.M + kBlk - 1) / kBlk, b = lane & 1;
-        const int blk = min(it.m0 / kBlk + (OUT == GATED ? 0 : b), mb - 1);
-        const uint8_t* const w = (OUT == GATED && b ? a.sb : a.sa) + (static_cast<size_t>(it.e) * mb + blk) * a.ldw;
+        const int blk = min(it.m0 / kBlk + (kGated ? 0 : b), mb - 1);
+        const uint8_t* const w = (kGated && b ? a.sb : a.sa) + (static_cast<size_t>(it.e) * mb + blk) * a.ldw;
         const uint8_t* const x = a.sx + static_cast<size_t>(srow) * a.ldx;
         L.scale = C::kWords == 2 || lane < 32 ? x : w;
         L.wscale = w;
@@ -324,7 +324,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
     // the first weight row of fragment i: the gated tile's second half of fragments
     // are the W3 rows of the first half's features
     auto arow = [&](int i) __attribute__((always_inline)) {
-        return OUT == GATED ? (i < FG ? 0 : NW / 2) + 32 * (FG * wn + i % FG) : 32 * (WF * wn + i);
+        return kGated ? (i < FG ? 0 : NW / 2) + 32 * (FG * wn + i % FG) : 32 * (WF * wn + i);
     };
     // where the word of scales of row r lies among the stage's scales
     auto scale_at = [&](int r) __attribute__((always_inline)) {
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
         auto read_scales = [&](Scales& s, const uint8_t* st) __attribute__((always_inline)) {
             const uint8_t* const at = st + C::kScales;
             s.w[0] = *reinterpret_cast<const uint32_t*>(at + C::kArea * wave + C::kWeightWord + 4 * (arow(0) / kBlk));
-            s.w[1] = OUT == GATED ? *reinterpret_cast<const uint32_t*>(at + C::kArea * wave + C::kWeightWord + 4) : s.w[0];
+            s.w[1] = kGated ? *reinterpret_cast<const uint32_t*>(at + C::kArea * wave + C::kWeightWord + 4) : s.w[0];
 #pragma unroll
             for (int j = 0; j < TF; ++j) s.x[j] = *reinterpret_cast<const uint32_t*>(at + scale_at(brow + 32 * j + l32));
         };
@@ -388,33 +388,27 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
         };
         // the products of A with row fragment j
         auto multiply = [&](const i32x8 (&A)[WF], const i32x8& B, int j, const Scales& s) __attribute__((always_inline)) {
-            // (products have no side effects: unless their sums are asked for here, the
-            // compiler moves them behind the loads, to where the sums are used)
-            auto done = [&]() __attribute__((always_inline)) {
-#pragma unroll
-                for (int i = 0; i < WF; ++i) {
-                    if constexpr (WF * TF == 16) asm volatile("" : "+a"(acc[i][j]));
-                    else asm volatile("" : "+v"(acc[i][j]));
-                }
-            };
             if constexpr (kExact) {
                 // both scales go to the rows, so that no factor leaves bf16's range unless
                 // the result does; W3 (another block) gets its scale's ratio to W1's
-                const float ratio = OUT == GATED ? power((s.w[1] & 255) - (s.w[0] & 255) + 127) : 1.0f;
+                const float ratio = kGated ? power((s.w[1] & 255) - (s.w[0] & 255) + 127) : 1.0f;
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
                     const bf16x8 b = widen(B[2 * p], B[2 * p + 1], power((s.x[j] & 255) + (s.w[0] & 255) - 127));
 #pragma unroll
                     for (int i = 0; i < WF; ++i)
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            widen(A[i][2 * p], A[i][2 * p + 1], OUT == GATED && i >= FG ? ratio : 1.0f), b, acc[i][j], 0, 0, 0);
+                            widen(A[i][2 * p], A[i][2 * p + 1], kGated && i >= FG ? ratio : 1.0f), b, acc[i][j], 0, 0, 0);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < WF; ++i)
                     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A[i], B, acc[i][j], 0, 0, 0, s.w[0], 0, s.x[j]);
             }
-            done();
+            // (products have no side effects: unless their sums are asked for here, the
+            // compiler moves them behind the loads, to where the sums are used)
+#pragma unroll
+            for (int i = 0; i < WF; ++i) asm volatile("" : "+v"(acc[i][j]));
         };
 
         // group g of the 2 TF groups of products between two arrivals, and its part of the loads
@@ -422,38 +416,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
         auto part = [&](int g) __attribute__((always_inline)) {
             issue_part(C::kLoads * g / kGroups, C::kLoads * (g + 1) / kGroups);
         };
-        // Half by half: the next half's weights are read ahead of a half's products,
-        // its rows fragment by fragment as the products are done with them; the next
-        // chunk's barrier lies before the second half's products.  (Not DEEP: two
-        // waves a SIMD fill in for each other.)
-        if constexpr (!C::DEEP) {
-#pragma unroll 1
-            for (int c = 0; c < cur.nc; ++c) {
-                const uint8_t* const st = arrive(c);
-                if (!active) {
-                    issue_part(0, C::kLoads);
-                    issued();
-                    continue;
-                }
-                Scales sc;
-                read_scales(sc, st);
-                pick(sc, c);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    i32x8 A[WF], B[TF];
-                    read_a(A, st, k);
-#pragma unroll
-                    for (int j = 0; j < TF; ++j) B[j] = read_b(st, j, k);
-                    if constexpr (OUT != GATED) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int j = 0; j < TF; ++j) {
-                        multiply(A, B[j], j, sc);
-                        if (k == 0) issue_part(C::kLoads * j / TF, C::kLoads * (j + 1) / TF);
-                    }
-                }
-                issued();
-            }
-        } else if constexpr (!kExact && WF == 4 && TF == 4) {
+        if constexpr (!kExact && WF == 4 && TF == 4) {
             // One wave a SIMD, so a product's 64 cycles are the time for everything else:
             // after each of a half's 16 a slot with a read for the next half (weights
             // into registers of their own, rows where the products are done with the old)
@@ -510,7 +473,92 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 pick(sc, c + 1);
                 if (next) issued();
             }
+        } else if constexpr (kExact && WF == 4 && TF == 4) {
+            // The same on exact products: a chunk is four parts of 16 bytes a lane and row,
+            // a part two groups of 16 products.  Under a group's products the next
+            // group's numbers are widened (two registers' worth a product) and, in a part's
+            // second group, the part after the next is read.
+            const uint8_t* st = arrive(0);
+            i32x4 R[2][WF + TF];                          // numbers of a part: weights, then rows
+            u32x4 W[2][WF + TF];                          // a group's, widened
+            float px[TF], ratio = 1.f;
+            Scales sn;
+            auto factors = [&](Scales& s, int c) __attribute__((always_inline)) {
+                pick(s, c);
+                // both scales go to the rows, so that no factor leaves bf16's range unless the
+                // result does; W3 (another block) gets its scale's ratio to W1's
+                if constexpr (kGated) ratio = power((s.w[1] & 255) - (s.w[0] & 255) + 127);
+#pragma unroll
+                for (int j = 0; j < TF; ++j) px[j] = power((s.x[j] & 255) + (s.w[0] & 255) - 127);
+            };
+            auto read_part = [&](int f, int t) __attribute__((always_inline)) {
+                const int r = f < WF ? arow(f) + l32 : brow + 32 * (f - WF) + l32;
+                R[t & 1][f] = *reinterpret_cast<const i32x4*>((f < WF ? st + C::kTokens : st) + at_row(r, 2 * t + lh));
+            };
+            // piece q (two of a fragment's four registers) of group g of part t
+            auto widen_piece = [&](int t, int g, int q) __attribute__((always_inline)) {
+                constexpr int kOrder[8] = {0, WF, 1, 2, 3, WF + 1, WF + 2, WF + 3};
+                const int f = kOrder[q / 2], d = 2 * g + q % 2;
+                const float s = f >= WF ? px[f - WF] : kGated && f >= FG ? ratio : 1.f;
+                W[g][f][2 * (q % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(R[t & 1][f][d], s, false));
+                W[g][f][2 * (q % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(R[t & 1][f][d], s, true));
+            };
+            auto group = [&](int g, auto slot) __attribute__((always_inline)) {
+#pragma unroll
+                for (int q = 0; q < WF * TF; ++q) {
+                    const int j = q / WF, i = q % WF;
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, W[g][i]), __builtin_bit_cast(bf16x8, W[g][WF + j]),
+                                                                       acc[i][j], 0, 0, 0);
+                    slot(q);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            read_scales(sn, st);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int f = 0; f < WF + TF; ++f) read_part(f, t);
+            factors(sn, 0);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) widen_piece(0, 0, q);
+            issue_part(0, C::kLoads);
+            issued();
+#pragma unroll 1
+            for (int c = 0; c < cur.nc; ++c) {
+                const bool next = c + 1 < cur.nc;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const uint64_t lanes = next ? ~0ull : 0ull;
+                    group(0, [&](int q) __attribute__((always_inline)) {
+                        widen_piece(t, 1, q);
+                        if (t == 3) issue_part(C::kLoads * q / 32, C::kLoads * (q + 1) / 32, lanes);
+                    });
+                    // (chunk c's last reads lie behind: its stage may be filled)
+                    if (t == 2) {
+#pragma unroll
+                        for (int f = 0; f < WF + TF; ++f) asm volatile("" : "+v"(W[1][f]));
+#pragma unroll
+                        for (int j = 0; j < TF; ++j)
+#pragma unroll
+                            for (int i = 0; i < WF; ++i) asm volatile("" : "+a"(acc[i][j]));
+                        if (next) {
+                            st = arrive(c + 1);
+                            read_scales(sn, st);
+                        }
+                    }
+                    if (t == 3) factors(sn, c + 1);
+                    group(1, [&](int q) __attribute__((always_inline)) {
+                        widen_piece(t + 1, 0, q);
+                        if (q % 2 == 0) read_part(q / 2, (t + 2) & 3);
+                        if (t == 3) issue_part(C::kLoads * (q + 16) / 32, C::kLoads * (q + 17) / 32, lanes);
+                    });
+                }
+                if (next) issued();
+            }
         } else {
+            // Half by half: the next half's weights are read ahead of a half's products,
+            // its rows fragment by fragment as the products are done with them; the next
+            // chunk's barrier lies before the second half's products.
             const uint8_t* st = arrive(0);
             i32x8 A0[WF], A1[WF], B[TF];
             Scales sc, sn;
@@ -615,16 +663,16 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        if constexpr (OUT == GATED) {
-            if (a.saved) {                                // g and u of the same 32 features side by side
+        if constexpr (kGated) {
+            if constexpr (OUT == SAVED) {                 // g and u of the same 32 features side by side
 #pragma unroll
                 for (int j = 0; j < TF; ++j) {
                     const int nv = min(32, cur.n - brow - 32 * j);
-                    if (nv <= 0) break;
 #pragma unroll
                     for (int i = 0; i < FG; ++i) {
                         const int f = cur.m0 + 32 * (FG * wn + i), room = 2 * (a.M - f);
-                        __builtin_amdgcn_sched_barrier(0);
+                        take(acc[i][j]);
+                        take(acc[FG + i][j]);
                         put16(acc[i][j], acc[FG + i][j]);
                         uint8_t* const to = reinterpret_cast<uint8_t*>(a.saved + static_cast<size_t>(cur.r0 + brow + 32 * j) * 2 * a.M + f);
                         rows_out(nv, to, room, to + 2 * static_cast<size_t>(a.M), room, 4 * static_cast<size_t>(a.M));
@@ -633,23 +681,31 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 lds_barrier();                            // (the waves' rows give way to what follows)
             }
             // h = silu(g) u; the largest of a row's 128 features over its 2 lanes and
-            // the WW waves; 8 bits each, whole 128-byte rows stored.  (h is worked out
-            // twice: 128 more numbers per lane would not stay in registers.)
+            // the WW waves; 8 bits each, whole 128-byte rows stored.
             float* const most = reinterpret_cast<float*>(free_stage + TM * kBlk);      // [WW][TM]
-            // (M is a multiple of 8: whole groups of a lane pair lie past it, as zeros)
-            auto hidden = [&](int i, int j, int q) __attribute__((always_inline)) {
-                const uint32_t keep = cur.m0 + 32 * (FG * wn + i) + 8 * (q / 4) < a.M ? ~0u : 0u;
-                return __uint_as_float(__float_as_uint(swiglu(acc[i][j][q], acc[FG + i][j][q])) & keep);
-            };
 #pragma unroll
             for (int j = 0; j < TF; ++j) {
-                float m = 0.f;
+                float m = 0.f;                            // (the maximum passes NaN over)
 #pragma unroll
                 for (int i = 0; i < FG; ++i) {
                     take(acc[i][j]);
                     take(acc[FG + i][j]);
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) m = fmaxf(m, finite_abs(hidden(i, j, q)));
+                    for (int q = 0; q < 16; ++q) {
+                        // (M is a multiple of 8: whole groups of a lane pair lie past it, as zeros)
+                        const uint32_t keep = cur.m0 + 32 * (FG * wn + i) + 8 * (q / 4) < a.M ? ~0u : 0u;
+                        const float h = __uint_as_float(__float_as_uint(swiglu(acc[i][j][q], acc[FG + i][j][q])) & keep);
+                        m = fmaxf(m, fabsf(h));
+                        acc[i][j][q] = h;
+                    }
+                    take(acc[i][j]);
+                }
+                if (__any(!is_finite(m))) {               // infinities leave the scale alone
+                    m = 0.f;
+#pragma unroll
+                    for (int i = 0; i < FG; ++i)
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) m = fmaxf(m, finite_abs(acc[i][j][q]));
                 }
                 m = fmaxf(m, __shfl_xor(m, 32, kWave));
                 if (lh == 0) most[wn * TM + brow + 32 * j + l32] = m;
@@ -667,15 +723,11 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
 #pragma unroll
                 for (int i = 0; i < FG; ++i) {
                     take(acc[i][j]);
-                    take(acc[FG + i][j]);
 #pragma unroll
-                    for (int qb = 0; qb < 4; ++qb) {
-                        float o[4];
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) o[q] = or_nan(hidden(i, j, 4 * qb + q)) * s;
+                    for (int qb = 0; qb < 4; ++qb)
                         // features 32 (FG wn + i) + 8 qb + 4 lh ..: 4 bytes of vector 2 (FG wn + i) + qb / 2
-                        *reinterpret_cast<uint32_t*>(free_stage + at_row(r, 2 * (FG * wn + i) + qb / 2) + 8 * (qb & 1) + 4 * lh) = pack_e4m3(o[0], o[1], o[2], o[3]);
-                    }
+                        *reinterpret_cast<uint32_t*>(free_stage + at_row(r, 2 * (FG * wn + i) + qb / 2) + 8 * (qb & 1) + 4 * lh) =
+                            pack_e4m3(acc[i][j][4 * qb] * s, acc[i][j][4 * qb + 1] * s, acc[i][j][4 * qb + 2] * s, acc[i][j][4 * qb + 3] * s);
                 }
             }
             lds_barrier();
@@ -821,7 +873,7 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(WeightArgs a) {
     for (int p = 0; p < 8; ++p) {
         const int r = 16 * p + r0, row = mb * kBlk + r;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[p][i] = or_nan(v[p][i]) * s;
+        for (int i = 0; i < 8; ++i) v[p][i] *= s;
         const uint2 o{pack_e4m3(v[p][0], v[p][1], v[p][2], v[p][3]), pack_e4m3(v[p][4], v[p][5], v[p][6], v[p][7])};
         if (a.q && row < a.M) *reinterpret_cast<uint2*>(a.q + g * a.gq + static_cast<size_t>(row) * a.ldq + col) = o;
         if (a.qt) {
@@ -954,7 +1006,7 @@ int64_t most_tiles(const Rows& r, int tm) {
 template <Out OUT, class C>
 hipError_t launch_tile(Args& a, const Rows& r, hipStream_t s) {
     a.xcds = geometry().xcds;
-    const int out = OUT == GATED ? C::NW / 2 : C::NW;
+    const int out = OUT == GATED || OUT == SAVED ? C::NW / 2 : C::NW;
     const int64_t work = most_tiles(r, C::TM) * ((a.M + out - 1) / out) * a.splits;
     int64_t blocks = std::min<int64_t>(work, geometry().cus);             // (a workgroup fills a CU's LDS)
     blocks = std::max<int64_t>(a.xcds, (blocks + a.xcds - 1) / a.xcds * a.xcds);
@@ -963,23 +1015,33 @@ hipError_t launch_tile(Args& a, const Rows& r, hipStream_t s) {
 }
 template <Out OUT>
 hipError_t launch_out(int tm, Args& a, const Rows& r, hipStream_t s) {
-    if (tm == Big::TM) return launch_tile<OUT, std::conditional_t<OUT == ROWS16 || OUT == SLICES, Big, BigExact>>(a, r, s);
+    if (tm == Big::TM) return launch_tile<OUT, Big>(a, r, s);
     if (tm == Mid::TM) return launch_tile<OUT, Mid>(a, r, s);
     return launch_tile<OUT, Few>(a, r, s);
 }
 
 int64_t some_blocks(int64_t n) { return std::max<int64_t>(1, std::min<int64_t>(n, 65536)); }
 
-// Rows of a tile, by the rows that a group has on average.
-int tile_rows(const Rows& r) {
-    const int64_t each = (static_cast<int64_t>(r.cap) + r.groups - 1) / r.groups;
-    return each > 160 ? Big::TM : each > 32 ? Mid::TM : Few::TM;
+// Rows of a tile.  Up to 32 rows a group on average one Few tile holds most groups;
+// beyond, the tile whose rounds over the CUs take less time, the groups' last tiles
+// half filled: a Mid tile takes 0.55 of a Big one (60 groups of 267 rows, 1408 x 2048:
+// Mid 101 us, Big 121; 8 groups of 250, 4096 x 4096: 66 and 61; 64 experts of 512 rows,
+// 2048 x 1024: equal).
+int tile_rows(const Rows& r, int64_t columns) {
+    if (r.cap <= 32 * r.groups) return Few::TM;
+    auto rounds = [&](int tm) {
+        const int64_t tiles = r.offsets ? r.cap / tm + (r.groups + 1) / 2 : (r.cap + tm - 1) / tm;
+        return (tiles * columns + kRoundItems - 1) / kRoundItems;
+    };
+    return 100 * rounds(Big::TM) <= 55 * rounds(Mid::TM) ? Big::TM : Mid::TM;
 }
+int64_t product_columns(int M) { return (M + Big::NW - 1) / Big::NW; }
+int64_t gated_columns(int M) { return (M + kBlk - 1) / kBlk; }
 // Slices of the reduction where the items leave CUs without work; a slice keeps 4 chunks.
 int slices(const Rows& r, int tm, int64_t columns, int Kp) {
     const int64_t items = most_tiles(r, tm) * columns;
     int s = 1;
-    while (items * s * 2 <= 256 && Kp / kBlk / (2 * s) >= 4) s *= 2;
+    while (items * s * 2 <= kRoundItems && Kp / kBlk / (2 * s) >= 4) s *= 2;
     return s;
 }
 
@@ -1005,12 +1067,14 @@ Range range_of(const Rows& r) { return Range{r.offsets, r.groups, r.cap}; }
 
 }  // namespace
 
-int product_slices(const Rows& r, int M, int Kp) { return slices(r, tile_rows(r), (M + Big::NW - 1) / Big::NW, Kp); }
+int product_slices(const Rows& r, int M, int Kp) {
+    const int64_t columns = product_columns(M);
+    return slices(r, tile_rows(r, columns), columns, Kp);
+}
 int gated_slices(const Rows& r, int M, int Kp) {
-    const int tm = tile_rows(r);
-    // (unsplit, the gated tile's items are 128 features wide; split, W1 and W3 are products of their own)
-    const int s = slices(r, tm, (M + kBlk - 1) / kBlk, Kp);
-    return s > 1 ? slices(r, tm, (M + Big::NW - 1) / Big::NW * 2, Kp) : 1;
+    const int64_t columns = gated_columns(M);
+    // (split, W1 and W3 are products of their own)
+    return slices(r, tile_rows(r, columns), columns, Kp) > 1 ? std::max(2, product_slices(r, M, Kp)) : 1;
 }
 
 hipError_t launch_quantize_rows(const uint16_t* x, const Rows& r, int K, uint8_t* q, uint8_t* scale, hipStream_t s) {
@@ -1054,7 +1118,7 @@ hipError_t launch_product(const Rows& r, const uint8_t* q, const uint8_t* sq, in
                               int splits, float* part, hipStream_t s) {
     if (r.cap == 0) return hipSuccess;
     Args a = base_args(r, w, q, sq, lds);
-    const int tm = tile_rows(r);
+    const int tm = tile_rows(r, product_columns(w.M));
     if (splits == 1 && out) {
         a.out = out;
         return bf16 ? launch_out<ROWS16>(tm, a, r, s) : launch_out<ROWS32>(tm, a, r, s);
@@ -1081,7 +1145,8 @@ hipError_t launch_gated(const Rows& r, const uint8_t* q, const uint8_t* sq, int 
         a.sout = sh;
         a.ldo = ldh;
         a.saved = saved;
-        return launch_out<GATED>(tile_rows(r), a, r, s);
+        const int tm = tile_rows(r, gated_columns(w1.M));
+        return saved ? launch_out<SAVED>(tm, a, r, s) : launch_out<GATED>(tm, a, r, s);
     }
     const size_t one = static_cast<size_t>(splits) * r.cap * w1.M;
     hipError_t e = launch_product(r, q, sq, lds, w1, false, nullptr, splits, part, s);

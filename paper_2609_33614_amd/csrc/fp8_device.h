@@ -32,12 +32,12 @@ __device__ __forceinline__ uint32_t scale_byte(float amax) {
 // 2^-(b - 127), 1 <= b <= 253.
 __device__ __forceinline__ float scale_inverse(uint32_t b) { return __uint_as_float((254u - b) << 23); }
 
-// Four numbers, already divided, to e4m3 (round to nearest even; NaN for what is not finite).
+// Four numbers, already divided, to e4m3 (round to nearest even; NaN for NaN and, as
+// the format has no infinities, for them).
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
 }
-__device__ __forceinline__ float or_nan(float v) { return is_finite(v) ? v : __uint_as_float(0x7fc00000u); }
 
 // The largest over the 16 lanes of a row of lanes.
 __device__ __forceinline__ float row_max(float v) {
@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t quantize_lane(const float (&v)[8], uint2& q)
     const float s = scale_inverse(b);
     float o[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = or_nan(v[i]) * s;
+    for (int i = 0; i < 8; ++i) o[i] = v[i] * s;
     q = uint2{pack_e4m3(o[0], o[1], o[2], o[3]), pack_e4m3(o[4], o[5], o[6], o[7])};
     return b;
 }
