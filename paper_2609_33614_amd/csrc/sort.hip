@@ -399,16 +399,8 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
 #pragma unroll
                     for (int b = 0; b < kBatch; ++b)
                         if (rows[b] >= 0) q[b] = load_row(g.rows + static_cast<int64_t>(rows[b]) * a.vecs + v);
-#pragma unroll
-                    for (int b = 0; b < kBatch; ++b) {
-                        if (rows[b] < 0) continue;
-                        float f[V::N];
-                        V::get(q[b], f);
-#pragma unroll
-                        for (int i = 0; i < V::N; ++i) dot[b] = fmaf(dy[i], f[i], dot[b]);
-                    }
                 }
-                if (a.dst) {
+                if (a.dst) {                              // (while the rows are on their way)
 #pragma unroll
                     for (int b = 0; b < kBatch; ++b) {
                         if (rows[b] < 0) continue;
@@ -416,6 +408,16 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
 #pragma unroll
                         for (int i = 0; i < V::N; ++i) o[i] = gates[b] * dy[i];
                         store_row(a.dst + static_cast<int64_t>(rows[b]) * a.vecs + v, V::put(o));
+                    }
+                }
+                if (g.dots) {
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b) {
+                        if (rows[b] < 0) continue;
+                        float f[V::N];
+                        V::get(q[b], f);
+#pragma unroll
+                        for (int i = 0; i < V::N; ++i) dot[b] = fmaf(dy[i], f[i], dot[b]);
                     }
                 }
             }
