@@ -305,6 +305,29 @@ def test_a_bad_row_stays_with_itself_through_the_experts():
     assert torch.equal(a[keep], b[keep]) and b[9].isnan().all()
 
 
+def test_an_overflowing_h_is_not_a_number():
+    """g and u finite, their product past fp32 (as an infinite h has no 8-bit number): NaN in the
+    rows where it happens, in every kind of call; the others keep their bits."""
+    d, F, E = 128, 256, 2
+    for T in (1, 40, 300, 3000):
+        w, x, off, token = make_experts(T, d, F, E, 1, "even")
+        token = torch.arange(T).int().cuda()
+        x = x.float().clamp(-4, 4)
+        off = off.int().cuda()
+        ex = Fp8Experts({"w1": w["w1"] * 2.0 ** 20, "w3": w["w3"] * 2.0 ** 60, "w2": w["w2"]})
+        quiet = (x * 2.0 ** -30).to(torch.bfloat16)
+        want = ex.forward(quiet, off, token)
+        assert want.isfinite().all()
+        loud = quiet.clone()
+        loud[::3] *= 2.0 ** 80                        # g about 2^70, u about 2^110: h past 2^128
+        got = ex.forward(loud, off, token)
+        bad = torch.zeros(T, dtype=torch.bool, device="cuda")
+        bad[::3] = True
+        assert got[bad].isnan().all() and torch.equal(got[~bad], want[~bad])
+        saved = torch.empty(T, 2 * F, dtype=torch.bfloat16, device="cuda")
+        assert torch.equal(ex.forward(loud, off, token, saved=saved)[~bad], want[~bad]) and saved.isfinite().all()
+
+
 def test_streams_and_graphs():
     """Eager, on a named stream behind pending work, and captured and replayed over new inputs."""
     T, d, F, E, k = 60, 256, 320, 8, 2
