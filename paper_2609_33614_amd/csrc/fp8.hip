@@ -121,8 +121,8 @@ __device__ __forceinline__ float swiglu(float a, float b) {
     return 0.25f * a * __builtin_amdgcn_rcpf(fmaf(0.25f, __expf(-a), 0.25f)) * b;
 }
 
-// 2^(b - 127), kept inside fp32's normal numbers.
-__device__ __forceinline__ float power(int b) { return __uint_as_float(static_cast<uint32_t>(min(max(b, 1), 254)) << 23); }
+// 2^(b - 127) of the lowest byte b (1 to 254).
+__device__ __forceinline__ float power(int b) { return __uint_as_float((static_cast<uint32_t>(b) & 255u) << 23); }
 
 // Eight e4m3 numbers times a power of two as bf16, which holds them exactly.
 __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
@@ -389,16 +389,15 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
         // the products of A with row fragment j
         auto multiply = [&](const i32x8 (&A)[WF], const i32x8& B, int j, const Scales& s) __attribute__((always_inline)) {
             if constexpr (kExact) {
-                // both scales go to the rows, so that no factor leaves bf16's range unless
-                // the result does; W3 (another block) gets its scale's ratio to W1's
-                const float ratio = kGated ? power((s.w[1] & 255) - (s.w[0] & 255) + 127) : 1.0f;
+                // (each side with its own scale: the numbers themselves, which bf16 holds)
+                const float pw[2] = {power(s.w[0]), power(s.w[1])};
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    const bf16x8 b = widen(B[2 * p], B[2 * p + 1], power((s.x[j] & 255) + (s.w[0] & 255) - 127));
+                    const bf16x8 b = widen(B[2 * p], B[2 * p + 1], power(s.x[j]));
 #pragma unroll
                     for (int i = 0; i < WF; ++i)
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            widen(A[i][2 * p], A[i][2 * p + 1], kGated && i >= FG ? ratio : 1.0f), b, acc[i][j], 0, 0, 0);
+                            widen(A[i][2 * p], A[i][2 * p + 1], pw[kGated && i >= FG]), b, acc[i][j], 0, 0, 0);
                 }
             } else {
 #pragma unroll
@@ -481,15 +480,15 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
             const uint8_t* st = arrive(0);
             i32x4 R[2][WF + TF];                          // numbers of a part: weights, then rows
             u32x4 W[2][WF + TF];                          // a group's, widened
-            float px[TF], ratio = 1.f;
+            float px[TF], pw[2];
             Scales sn;
             auto factors = [&](Scales& s, int c) __attribute__((always_inline)) {
                 pick(s, c);
-                // both scales go to the rows, so that no factor leaves bf16's range unless the
-                // result does; W3 (another block) gets its scale's ratio to W1's
-                if constexpr (kGated) ratio = power((s.w[1] & 255) - (s.w[0] & 255) + 127);
+                // (each side with its own scale: the numbers themselves, which bf16 holds)
+                pw[0] = power(s.w[0]);
+                pw[1] = power(s.w[1]);
 #pragma unroll
-                for (int j = 0; j < TF; ++j) px[j] = power((s.x[j] & 255) + (s.w[0] & 255) - 127);
+                for (int j = 0; j < TF; ++j) px[j] = power(s.x[j]);
             };
             auto read_part = [&](int f, int t) __attribute__((always_inline)) {
                 const int r = f < WF ? arow(f) + l32 : brow + 32 * (f - WF) + l32;
@@ -499,7 +498,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
             auto widen_piece = [&](int t, int g, int q) __attribute__((always_inline)) {
                 constexpr int kOrder[8] = {0, WF, 1, 2, 3, WF + 1, WF + 2, WF + 3};
                 const int f = kOrder[q / 2], d = 2 * g + q % 2;
-                const float s = f >= WF ? px[f - WF] : kGated && f >= FG ? ratio : 1.f;
+                const float s = f >= WF ? px[f - WF] : pw[kGated && f >= FG];
                 W[g][f][2 * (q % 2)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(R[t & 1][f][d], s, false));
                 W[g][f][2 * (q % 2) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(R[t & 1][f][d], s, true));
             };

@@ -305,6 +305,35 @@ def test_a_bad_row_stays_with_itself_through_the_experts():
     assert torch.equal(a[keep], b[keep]) and b[9].isnan().all()
 
 
+@pytest.mark.parametrize("n", [20, 300, 2600])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ex,ew", [(-80, -60), (116, 18), (60, 60), (-120, 100), (100, -110), (10, -118)])
+def test_scales_far_apart(n, dtype, ex, ew):
+    """Powers of two whose sum no fp32 holds while the results are ordinary, and the other way round: weights
+    2^-8 or 2^-14 of their block's largest, and zeros, where the largest would give infinity."""
+    K, M = 640, 1032
+    x, w = normal(n, K, std=1.0).float().clamp(-3, 3), normal(1, M, K, dtype=torch.float32).clamp(-3, 3)
+    w[:, 1::2] *= 2.0 ** (-14 if ew == 18 else -8)
+    w[:, 2::4] = 0.0
+    if ew == 18:
+        w[:, ::4] *= (torch.arange(K, device="cuda") == 5)            # (the largest alone in its rows)
+        x[:, 5] = 0.0
+        w[0, ::4, 5] = 3.0
+    x, w = (x * 2.0 ** ex).to(torch.bfloat16), w * 2.0 ** ew
+    m = Fp8Matrix(w)
+    out = torch.full((n, M), 7.0, dtype=dtype, device="cuda")
+    m.product(x, out=out)
+    off = torch.tensor([0, n])
+    xq, wq = R.quantize(x)[0], R.quantize(w, 128)[0]
+    ref, bound, _ = R.grouped(xq, wq, off, exact=dtype == torch.float32)
+    # numbers below 2^-126 may count as zeros, on either side and in the sums
+    bound = bound + 2.0 ** -126 * (K + xq.abs().sum(1)[:, None] + wq[0].abs().sum(1)[None])
+    if dtype == torch.bfloat16:
+        bound = (1 + 2.0 ** -8) * bound + 2.0 ** -8 * ref.abs() + 2.0 ** -126
+    assert ref.isfinite().all() and float(ref.abs().max()) < 2.0 ** 128 * (1 - 2.0 ** -7)   # (bf16 ends at 2^128 (1 - 2^-8))
+    within(f"scales {n} {ex} {ew}", out, ref, bound)
+
+
 def test_an_overflowing_h_is_not_a_number():
     """g and u finite, their product past fp32 (as an infinite h has no 8-bit number): NaN in the
     rows where it happens, in every kind of call; the others keep their bits."""
