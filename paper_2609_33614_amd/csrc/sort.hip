@@ -123,7 +123,10 @@ struct IndexArgs {
 constexpr int kIndexWaves = 16;
 __global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) {
     constexpr int NW = kIndexWaves, kGroups = kChunk / kWave;
-    __shared__ int tot[kMaxExperts], before[kMaxExperts], base[kMaxExperts];
+    // (pairs are counted in unsigned numbers: 2^24 tokens of 256 experts have up to 2^32)
+    __shared__ int tot[kMaxExperts], before[kMaxExperts];
+    __shared__ uint32_t base[kMaxExperts];
+    const uint32_t cap = a.cap;
     __shared__ int own[kGroups][kMaxExperts];
     __shared__ uint64_t cols[kGroups][kMaxExperts];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
@@ -162,19 +165,19 @@ __global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) 
     }
     __syncthreads();
     if (wave == 0) {
-        int carry = 0;
+        uint32_t carry = 0;
         for (int e1 = 0; e1 < a.E; e1 += kWave) {
             const int e = e1 + lane;
             const int n = e < a.E ? tot[e] : 0;
-            const int s = wave_scan(n);
+            const int s = wave_scan(n);                    // (at most 2^30)
             if (e < a.E) {
-                base[e] = carry + s - n;
+                base[e] = carry + static_cast<uint32_t>(s - n);
                 if (blk == 0) {
-                    a.offsets[e] = min(base[e], a.cap);
-                    if (e == a.E - 1) a.offsets[a.E] = min(carry + s, a.cap);
+                    a.offsets[e] = static_cast<int32_t>(min(base[e], cap));
+                    if (e == a.E - 1) a.offsets[a.E] = static_cast<int32_t>(base[e] >= cap ? cap : min(base[e] + static_cast<uint32_t>(n), cap));
                 }
             }
-            carry += __builtin_amdgcn_readlane(s, kWave - 1);
+            carry += static_cast<uint32_t>(__builtin_amdgcn_readlane(s, kWave - 1));
         }
     }
     __syncthreads();
@@ -185,16 +188,16 @@ __global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) 
         const int g = p % kGroups, w = p / kGroups % a.W, k0 = p / (kGroups * a.W) * len, e = kWave * w + lane;
         if (e >= a.E) continue;
         uint64_t m = cols[g][e];
-        int row = base[e] + before[e] + __popcll(m & ((1ull << k0) - 1));
+        uint32_t row = base[e] + before[e] + __popcll(m & ((1ull << k0) - 1));
         for (int q = 0; q < g; ++q) row += own[q][e];
         m >>= k0;
         const int first = t0 + g * kWave + k0, n = min(len, a.T - first);
         int32_t* to = a.place + static_cast<size_t>(first) * a.E + e;
         for (int k = 0; k < n; ++k, m >>= 1, to += a.E) {
             const bool on = m & 1ull;
-            *to = on && row < a.cap ? row : -1;
+            *to = on && row < cap ? static_cast<int32_t>(row) : -1;
             if (on) {
-                if (row < a.cap) a.token[row] = first + k;
+                if (row < cap) a.token[row] = first + k;
                 ++row;
             }
         }

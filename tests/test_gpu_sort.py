@@ -172,6 +172,25 @@ def test_pairs_past_the_rows_are_left_out(T, cap):
         within(f"cap {name}", out[name], ref, bound)
 
 
+@pytest.mark.parametrize("cap", [1000, 2 ** 31 - 1])
+def test_more_pairs_than_31_bits_count(cap):
+    """2^23 + 5 tokens that select all of 256 experts: the pairs past the rows are left out, those
+    before them have theirs (17 GB of places and tokens)."""
+    T, E = 2 ** 23 + 5, 256
+    lay = make_layer(E, 64, True, T)
+    mask = torch.full((T, 4), -1, dtype=torch.int64, device="cuda")
+    _, off, token, place = lay.sort(None, mask, cap=cap)
+    want = (torch.arange(E + 1) * T).clamp(max=cap)
+    assert torch.equal(off.cpu().long(), want)
+    for r in range(0, cap, 1 << 27):
+        at = torch.arange(r, min(cap, r + (1 << 27)), device="cuda")
+        assert torch.equal(token[r: r + at.numel()].long(), at % T)
+    e = torch.arange(E, device="cuda") * T
+    for t in range(0, T, 1 << 19):
+        ref = torch.arange(t, min(T, t + (1 << 19)), device="cuda")[:, None] + e
+        assert torch.equal(place[t: t + ref.shape[0]].long(), torch.where(ref < cap, ref, -1))
+
+
 def test_places_outside_the_rows_are_not_followed():
     """Whole numbers from elsewhere in `place`: they count as not placed."""
     T, E, d = 70, 60, 128
