@@ -145,7 +145,9 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
     const int nch = a.Kp / kBlk, nxm = (a.M + kOut - 1) / kOut;
     const int splits = kSlices ? a.splits : 1;
 
-    // segments, kept inside the rows there are whatever the offsets hold
+    // segments, kept inside the rows there are whatever the offsets hold (ones that
+    // overlap could hold more items than are counted: those are left out)
+    const int nx = nxm * splits, most = (1 << 30) / nx;
     int ntiles;
     if (a.offsets) {
         for (int g = threadIdx.x; g <= a.groups; g += C::kThreads) soff[g] = min(max(a.offsets[g], 0), a.cap);
@@ -156,7 +158,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 const int g = g0 + lane;
                 int c = g < a.groups ? (max(soff[g + 1] - soff[g], 0) + TM - 1) / TM : 0;
                 c = wave_scan(c);
-                if (g < a.groups) tstart[g + 1] = carry + c;
+                if (g < a.groups) tstart[g + 1] = min(carry + c, most);
                 carry += __builtin_amdgcn_readlane(c, kWave - 1);
             }
             if (lane == 0) tstart[0] = 0;
@@ -164,10 +166,9 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
         __syncthreads();
         ntiles = __builtin_amdgcn_readfirstlane(tstart[a.groups]);
     } else {
-        ntiles = (a.cap + TM - 1) / TM;
+        ntiles = min((a.cap + TM - 1) / TM, most);
     }
-    const int nx = nxm * splits;
-    const int work = ntiles * nx;             // (below 2^31: the entry points' limits)
+    const int work = ntiles * nx;
     const int xcd = blockIdx.x % a.xcds, slot = blockIdx.x / a.xcds, per = gridDim.x / a.xcds;
     const int part = (work + a.xcds - 1) / a.xcds, wbeg = xcd * part, wend = min(work, wbeg + part);
 
