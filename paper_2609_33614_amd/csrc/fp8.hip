@@ -642,8 +642,13 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 const int r = 8 * k + lane / 8, v = lane % 8;
                 const u32x4 d = *reinterpret_cast<const u32x4*>(tb + r * kBlk + ((v ^ (r & 7)) << 4));
                 const bool first = v < 4;
-                if (r < nv && 16 * (v & 3) < (first ? room_lo : room_hi))
-                    *reinterpret_cast<u32x4*>((first ? lo : hi) + r * pitch + 16 * (v & 3)) = d;
+                if (r < nv && 16 * (v & 3) < (first ? room_lo : room_hi)) {
+                    u32x4* const to = reinterpret_cast<u32x4*>((first ? lo : hi) + r * pitch + 16 * (v & 3));
+                    // (results go past the caches that the operands are read through: 32768 x 1024 x
+                    // 2048 in 64 groups 128 -> 113 us; slices and what `backward` reads do not)
+                    if constexpr (OUT == ROWS16 || OUT == ROWS32) __builtin_nontemporal_store(d, to);
+                    else *to = d;
+                }
                 if (room_lo > 0) ++stored;
             }
             wave_lds_sync();
