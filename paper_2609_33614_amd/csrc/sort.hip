@@ -265,7 +265,7 @@ struct Cursor {
     int w;
     uint64_t rest;
 };
-template <bool GATES>
+template <bool GATES, bool WHOLE>
 __device__ __forceinline__ int next_rows(const RowArgs& a, int t, Cursor& c, int (&rows)[kBatch], float (&gates)[kBatch],
                                          int (&es)[kBatch]) {
     const uint64_t* const m = a.mask + static_cast<size_t>(t) * a.W;
@@ -276,17 +276,32 @@ __device__ __forceinline__ int next_rows(const RowArgs& a, int t, Cursor& c, int
             c.rest = m[++c.w];
             if (c.w + 1 == a.W && a.E % kWave) c.rest &= ~0ull >> (kWave - a.E % kWave);
         }
-        rows[b] = -1;
-        gates[b] = 1.f;
         es[b] = 0;
         if (c.rest != 0) {
-            const int e = kWave * c.w + __builtin_ctzll(c.rest);
+            es[b] = kWave * c.w + __builtin_ctzll(c.rest);
             c.rest &= c.rest - 1;
-            es[b] = e;
-            const int r = a.place[static_cast<size_t>(t) * a.E + e];
-            rows[b] = static_cast<unsigned>(r) < static_cast<unsigned>(a.cap) ? r : -1;
-            if constexpr (GATES) gates[b] = a.gate[static_cast<size_t>(t) * a.E + e];
             n = b + 1;
+        }
+    }
+    // (without branches, so that these loads are under way together: 16384 tokens x 2048, 8 rows
+    // each, sort and its gradient 252 -> 220 us, combine and its gradients 358 -> 336)
+    const size_t at = static_cast<size_t>(t) * a.E;
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+        rows[b] = a.place[at + es[b]];
+        gates[b] = GATES ? a.gate[at + es[b]] : 1.f;
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b)
+        if (b >= n || static_cast<unsigned>(rows[b]) >= static_cast<unsigned>(a.cap)) rows[b] = -1;
+    if constexpr (WHOLE) {                    // the wave has one token, so its rows are scalars (registers
+                                              // of combine_grad_kernel 148 -> 100, 336 -> 330 us; 8192 x 1024, 4 rows: 88 -> 79)
+        n = __builtin_amdgcn_readfirstlane(n);
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            rows[b] = __builtin_amdgcn_readfirstlane(rows[b]);
+            es[b] = __builtin_amdgcn_readfirstlane(es[b]);
+            gates[b] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(gates[b])));
         }
     }
     return n;
@@ -306,7 +321,7 @@ __global__ __launch_bounds__(kThreads) void spread_kernel(RowArgs a) {
         for (;;) {
             int rows[kBatch], es[kBatch];
             float gates[kBatch];
-            const int n = next_rows<false>(a, t, c, rows, gates, es);
+            const int n = next_rows<false, false>(a, t, c, rows, gates, es);
             if (n == 0) break;
             for (int v = v0; v < a.vecs; v += kThreads) {
                 const uint4 q = a.src[t * a.vecs + v];
@@ -334,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(RowArgs a) {
             for (;;) {
                 int rows[kBatch], es[kBatch];
                 float gates[kBatch];
-                const int n = next_rows<GATES>(a, t, c, rows, gates, es);
+                const int n = next_rows<GATES, false>(a, t, c, rows, gates, es);
                 if (n == 0) break;
                 uint4 q[kBatch];
 #pragma unroll
@@ -390,8 +405,12 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
         for (;;) {
             int rows[kBatch], es[kBatch];
             float gates[kBatch], dot[kBatch];
-            const int n = next_rows<true>(a, t, c, rows, gates, es);
+            const int n = next_rows<true, true>(a, t, c, rows, gates, es);
             if (n == 0) break;
+            if (g.dlogits) {
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) P += b < n ? g.prob[static_cast<size_t>(t) * a.E + es[b]] : 0.f;
+            }
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) dot[b] = 0.f;
             for (int v = id; v < a.vecs; v += NT) {
@@ -444,11 +463,6 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
                         dgs[sub][es[b]] = s;
                         gs[sub][es[b]] = gates[b];
                     }
-                }
-                if (g.dlogits) {
-#pragma unroll
-                    for (int b = 0; b < kBatch; ++b)
-                        if (b < n) P += g.prob[static_cast<size_t>(t) * a.E + es[b]];
                 }
                 sync();
             }
