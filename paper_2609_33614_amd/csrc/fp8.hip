@@ -11,8 +11,8 @@
 // kept below the largest of them (and cut towards zero; eights are added in fp32):
 // 1.5e-5 of a result of Gaussian numbers, 3.8e-5 where some are 16 times the
 // others, at any K from 128 to 14336 and without a bias, a hundredth of what a bf16
-// result rounds, at 1.6 times the rate of exact products (8192 x 4096 x 4096: 170 and
-// 273 us).  Exact sums go to results in fp32 (ROWS32, EXACT) and to what is rounded to
+// result rounds, at 1.5 times the rate of exact products (8192 x 4096 x 4096 with the
+// rows' rounding: 152 and 219 us).  Exact sums go to results in fp32 (ROWS32, EXACT) and to what is rounded to
 // 8 bits again (GATED, dh), where a sum off by 2e-5 picks another 4-bit number once
 // in a few thousand: 0.0025 to 0.009 of the result's norm where the rest of the
 // arithmetic has 0.0017.  They take the numbers, which 8 bits of a bf16 hold, as
@@ -58,6 +58,12 @@ struct Tile {
     static_assert(TF * 32 * WT == TM && WF * 32 * WW == NW && (WF == 2 || WF == 4) && NW == 256, "fragments cover the tile; a gated tile is one block wide");
     static_assert(kAhead >= 1 && kAhead <= 3, "waits count up to three chunks");
 };
+// Big: one wave a SIMD with 128 x 128 of the results each, the least LDS reads per
+// product (8192 x 4096 x 4096: 117 us, 2.35 PFLOP/s; an 8-bit library product 97; exact
+// 1.2 PFLOP/s).  Mid: groups that fill no Big tile; eight waves, since four in Big's manner
+// took 143 against 133 us at 32768 x 1024 x 2048 in 64 groups (exact: 217 and 199).  Few:
+// bound by the weights, which every CU streams once (74 rows, 4096 x 14336 in 8
+// groups: 80 us, 5.8 TB/s), four stages ahead.
 using Big = Tile<256, 256, 2, 2, 2, false>;
 using Mid = Tile<128, 256, 2, 4, 3, false>;
 using Few = Tile<32, 256, 1, 4, 4, true>;
@@ -792,7 +798,8 @@ struct Range {
     __device__ __forceinline__ int end() const { return offsets ? min(max(offsets[groups], 0), cap) : cap; }
 };
 
-// x [rows][K] bf16 -> q [rows][Kp], scale [rows][lds]; 4 blocks of a row per wave.
+// x [rows][K] bf16 -> q [rows][Kp], scale [rows][lds]; 4 blocks of a row per wave.  Bound by
+// memory: 8192 x 4096 in 18.6 us, 5.4 TB/s.
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const uint16_t* __restrict__ x, Range rows, int K, int Kp, uint8_t* __restrict__ q, uint8_t* __restrict__ scale, int lds) {
     const int lane = lane_id();
     const int pieces = lds / 4;
@@ -928,6 +935,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ par
 //   forward:  g, u (the sums of their slices) -> h = silu(g) u in 8 bits (and g, u in bf16)
 //   backward: dh (the sum of its slices), g, u (bf16) -> dg = dh u s (1 + g (1 - s)), du = dh g s
 //             in 8 bits, s = 1 / (1 + e^-g)
+// Bound by memory: the backward of 32768 x 1024 moves 335 MB in 65 us.
 struct GateArgs {
     const float* a;            // [splits][cap][F] g or dh
     const float* b;            // forward: [splits][cap][F] u

@@ -19,7 +19,7 @@
 // for dW, where a library product takes 1.29 - 1.53, 1.26 - 1.40 and 1.00 - 1.15
 // (8192 x 4096 x 32768, timed in turn).
 //
-// The header's kernels are instantiated by ce.hip and balance.hip.
+// The header's kernels are instantiated by ce.hip and balance.hip; fp8.hip takes its loads to LDS.
 #pragma once
 #include <algorithm>
 
