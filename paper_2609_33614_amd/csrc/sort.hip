@@ -20,8 +20,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kChunk = 256;               // tokens per workgroup of the index kernels
-constexpr int kSumChunks = 64;            // more chunks' counts are added up in a launch of their own
+// Tokens per workgroup of the index kernels: 64 keep the loop over a chunk's tokens short
+// (4097 tokens, 128 experts: 12.2 us for the launches against 13.7, 300 and 256: 10.1 and 14.5), 256
+// the counts of earlier chunks few (16384 tokens, 64 experts: 13.6 against 16.3; 8192: equal).
+constexpr int kChunk = 256, kSmallChunk = 64, kSmallTokens = 8192;
+// Up to so many 64-token words of masks every workgroup counts them all by itself (1000
+// tokens, 64 experts: 9.1 us against 10.5 with a launch of counts; 130 words: 16.2 and 13.5).
+constexpr int kCountPairs = 64;
+constexpr int kSumChunks = 64;            // more chunks of 256 tokens' counts are added up in a launch of their own
 constexpr int kBatch = 8;                 // rows of a token in flight together
 
 // 16 bytes of a row as fp32 numbers and back.
@@ -65,20 +71,21 @@ __device__ __forceinline__ void store_row(uint4* p, const uint4& q) {
 // ---- index -----------------------------------------------------------------
 
 // Selections per expert of each chunk of tokens: cnt[chunk][E].
-__global__ __launch_bounds__(kThreads) void count_kernel(const uint64_t* __restrict__ mask, int T, int E, int W,
-                                                         int32_t* __restrict__ cnt) {
-    __shared__ int part[kWaves][kMaxExperts];
+template <int CHUNK>
+__global__ __launch_bounds__(CHUNK) void count_kernel(const uint64_t* __restrict__ mask, int T, int E, int W,
+                                                      int32_t* __restrict__ cnt) {
+    __shared__ int part[CHUNK / kWave][kMaxExperts];
     const int lane = lane_id(), wave = threadIdx.x / kWave;
-    const int t = blockIdx.x * kChunk + wave * kWave + lane;
+    const int t = blockIdx.x * CHUNK + wave * kWave + lane;
     for (int w = 0; w < W; ++w)
         part[wave][kWave * w + lane] = __popcll(bit_transpose(t < T ? mask[static_cast<size_t>(t) * W + w] : 0ull));
     __syncthreads();
-    const int e = threadIdx.x;
-    if (e >= E) return;
-    int n = 0;
+    for (int e = threadIdx.x; e < E; e += CHUNK) {
+        int n = 0;
 #pragma unroll
-    for (int q = 0; q < kWaves; ++q) n += part[q][e];
-    cnt[static_cast<size_t>(blockIdx.x) * E + e] = n;
+        for (int q = 0; q < CHUNK / kWave; ++q) n += part[q][e];
+        cnt[static_cast<size_t>(blockIdx.x) * E + e] = n;
+    }
 }
 
 // Per expert (a workgroup each): cnt becomes the selections in earlier chunks,
@@ -109,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(int32_t* __restrict__ cn
 struct IndexArgs {
     const uint64_t* mask;      // [T][W]
     int T, E, W, cap;
-    const int32_t* cnt;        // [chunks][E] selections of each chunk, or in earlier chunks where total is set
+    const int32_t* cnt;        // [chunks][E] selections of each chunk, or in earlier chunks where total is set (null: counted here)
     int chunks;
     const int32_t* total;      // [E] or null
     int32_t* offsets;          // [E+1]
@@ -121,8 +128,9 @@ struct IndexArgs {
 // costs 100 instructions per 64 tokens: where every workgroup counted all tokens
 // itself, 16384 tokens of 64 experts took 15 us, and the two launches take 10.
 constexpr int kIndexWaves = 16;
+template <int CHUNK>
 __global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) {
-    constexpr int NW = kIndexWaves, kGroups = kChunk / kWave;
+    constexpr int NW = kIndexWaves, kGroups = CHUNK / kWave;
     // (pairs are counted in unsigned numbers: 2^24 tokens of 256 experts have up to 2^32)
     __shared__ int tot[kMaxExperts], before[kMaxExperts];
     __shared__ uint32_t base[kMaxExperts];
@@ -130,7 +138,7 @@ __global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) 
     __shared__ int own[kGroups][kMaxExperts];
     __shared__ uint64_t cols[kGroups][kMaxExperts];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kWave);
-    const int t0 = blockIdx.x * kChunk, blk = blockIdx.x;
+    const int t0 = blockIdx.x * CHUNK, blk = blockIdx.x;
     // the chunk's own masks: (group, word) pairs, one per wave
     static_assert(kGroups * kMaxExperts / kWave <= NW, "a pair per wave");
     const int og = wave % kGroups, ow = wave / kGroups, ot = t0 + og * kWave + lane;
@@ -142,7 +150,26 @@ __global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) 
         before[e0] = given ? a.cnt[static_cast<size_t>(blk) * a.E + e0] : 0;
     }
     __syncthreads();
-    if (!a.total && e0 < a.E) {
+    if (!a.cnt) {
+        constexpr int kPre = 4;
+        const int pairs = (a.T + kWave - 1) / kWave * a.W;
+        for (int p0 = wave; p0 < pairs; p0 += NW * kPre) {
+            uint64_t m[kPre];
+#pragma unroll
+            for (int i = 0; i < kPre; ++i) {
+                const int p = p0 + NW * i, t = p / a.W * kWave + lane;
+                m[i] = p < pairs && t < a.T ? a.mask[static_cast<size_t>(t) * a.W + p % a.W] : 0ull;
+            }
+#pragma unroll
+            for (int i = 0; i < kPre; ++i) {
+                const int p = p0 + NW * i, e = p % a.W * kWave + lane;
+                if (p >= pairs) break;
+                const int n = __popcll(bit_transpose(m[i]));
+                atomicAdd(&tot[e], n);                     // (whole numbers: any order gives the same sum)
+                if (p / a.W * kWave < t0) atomicAdd(&before[e], n);
+            }
+        }
+    } else if (!a.total && e0 < a.E) {
         constexpr int kStep = NW * kWave / kMaxExperts, kPre = 8;
         int all = 0, pre = 0;
         for (int c0 = part; c0 < a.chunks; c0 += kStep * kPre) {
@@ -155,7 +182,7 @@ __global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) 
                 pre += c0 + kStep * i < blk ? n[i] : 0;
             }
         }
-        atomicAdd(&tot[e0], all);                          // (whole numbers: any order gives the same sum)
+        atomicAdd(&tot[e0], all);
         atomicAdd(&before[e0], pre);
     }
     if (ow < a.W) {
@@ -183,7 +210,7 @@ __global__ __launch_bounds__(kIndexWaves* kWave) void index_kernel(IndexArgs a) 
     __syncthreads();
     // places: the chunk's (group, word) pairs again, in parts of 64 / parts tokens so
     // that every wave has some
-    const int parts = max(1, NW / (kGroups * a.W)), len = kWave / parts;
+    const int share = max(1, NW / (kGroups * a.W)), parts = 1 << (31 - __builtin_clz(share)), len = kWave / parts;
     for (int p = wave; p < kGroups * a.W * parts; p += NW) {
         const int g = p % kGroups, w = p / kGroups % a.W, k0 = p / (kGroups * a.W) * len, e = kWave * w + lane;
         if (e >= a.E) continue;
@@ -505,15 +532,19 @@ RowArgs row_args(const SortCall& c, const void* src, void* dst) {
 
 }  // namespace
 
+static int chunks_of(int T) {
+    const int chunk = T <= kSmallTokens ? kSmallChunk : kChunk;
+    return (T + chunk - 1) / chunk;
+}
 size_t sort_workspace(int32_t T, int E) {
     if (T <= kFusedTokens) return 0;
-    const size_t chunks = (static_cast<size_t>(T) + kChunk - 1) / kChunk;
-    return (chunks + 1) * E * 4;
+    return (static_cast<size_t>(chunks_of(T)) + 1) * E * 4;
 }
 
 hipError_t launch_sort(const SortCall& c, const void* x, void* rows, int32_t* offsets, int32_t* token, int32_t* place,
                        void* ws, hipStream_t s) {
-    const int W = mask_words(c.E), chunks = (c.T + kChunk - 1) / kChunk;
+    const int W = mask_words(c.E), chunks = chunks_of(c.T);
+    const bool small = c.T <= kSmallTokens;
     IndexArgs ia{c.mask, c.T, c.E, W, c.cap, nullptr, chunks, nullptr, offsets, token, place};
     if (c.T <= kFusedTokens) {
         small_sort_kernel<<<std::max(1, c.T), kThreads, 0, s>>>(ia, static_cast<const uint4*>(x), static_cast<uint4*>(rows),
@@ -521,17 +552,22 @@ hipError_t launch_sort(const SortCall& c, const void* x, void* rows, int32_t* of
         return hipGetLastError();
     }
     int32_t* const cnt = static_cast<int32_t*>(ws);
-    ia.cnt = cnt;
-    count_kernel<<<chunks, kThreads, 0, s>>>(c.mask, c.T, c.E, W, cnt);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && chunks > kSumChunks) {
+    hipError_t e = hipSuccess;
+    if ((c.T + kWave - 1) / kWave * W > kCountPairs) {
+        ia.cnt = cnt;
+        if (small) count_kernel<kSmallChunk><<<chunks, kSmallChunk, 0, s>>>(c.mask, c.T, c.E, W, cnt);
+        else count_kernel<kChunk><<<chunks, kChunk, 0, s>>>(c.mask, c.T, c.E, W, cnt);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && !small && chunks > kSumChunks) {
         int32_t* const total = cnt + static_cast<size_t>(chunks) * c.E;
         ia.total = total;
         scan_kernel<<<c.E, kThreads, 0, s>>>(cnt, chunks, c.E, total);
         e = hipGetLastError();
     }
     if (e != hipSuccess) return e;
-    index_kernel<<<chunks, kIndexWaves * kWave, 0, s>>>(ia);
+    if (small) index_kernel<kSmallChunk><<<chunks, kIndexWaves * kWave, 0, s>>>(ia);
+    else index_kernel<kChunk><<<chunks, kIndexWaves * kWave, 0, s>>>(ia);
     e = hipGetLastError();
     if (e != hipSuccess || !rows) return e;
     SortCall p = c;

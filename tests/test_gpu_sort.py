@@ -101,6 +101,8 @@ SIZES = [(1, 1, 64, True, 1, "topk"), (1, 8, 4096, True, 2, "topk"), (1, 128, 20
          (256, 256, 64, True, 8, "topk"), (300, 200, 128, False, 8, "some"), (1000, 60, 1024, False, 4, "topk"), (777, 130, 576, True, 8, "some"),
          (130, 16, 8640, True, 3, "topk"), (70, 33, 2112, False, 5, "topk"), (4097, 128, 64, True, 8, "topk"), (5000, 7, 128, True, 2, "one"),
          (9000, 130, 64, True, 2, "topk"), (20000, 60, 64, True, 2, "some"), (17000, 256, 64, False, 4, "topk"), (16385, 64, 192, True, 3, "topk"),
+         (4096, 64, 64, True, 8, "topk"), (4097, 64, 64, False, 2, "some"), (1024, 256, 64, True, 8, "some"), (1025, 256, 64, True, 2, "topk"),
+         (8192, 130, 64, False, 4, "some"), (8193, 60, 64, True, 8, "topk"), (16384, 8, 64, True, 2, "one"),
          (90, 60, 128, True, 0, "none"), (40000, 8, 64, True, 1, "none")]
 
 
