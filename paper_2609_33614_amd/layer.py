@@ -199,6 +199,8 @@ class EatLayer:
         if cap is None:
             p = self.params
             cap = T * (p.top_k if p.mode == L.EAT_MODE_TOPK else p.top_p_cap if p.mode == L.EAT_MODE_TOPP and p.top_p_cap else E)
+        if not 0 <= cap < 1 << 31:
+            raise ValueError(f"cap: {cap} rows, their numbers have 31 bits")
         if rows is not None and x is None:
             raise ValueError("rows: nothing to write without x")
         _expect("rows", rows, self._act(), (cap, d), dev)

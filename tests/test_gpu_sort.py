@@ -343,6 +343,7 @@ def test_wrong_tensors_are_refused():
                  lambda: lay.combine(rows, b["mask"], b["gate"], place, y=f32),
                  lambda: lay.combine_backward(b["dy"], None, b["mask"], b["gate"], place, dgate=b["gate"]),
                  lambda: lay.combine_backward(b["dy"], rows, b["mask"], b["gate"], place, drows=f32),
+                 lambda: lay.sort(None, b["mask"], cap=2 ** 31), lambda: lay.sort(None, b["mask"], cap=2 ** 32), lambda: lay.sort(None, b["mask"], cap=-1),
                  lambda: lay.sort(b["x"].cpu(), b["mask"])):
         with pytest.raises((ValueError, L.EatError)):
             call()
