@@ -790,7 +790,7 @@ struct ExpertsCall {
         h = c.take(n * K2);
         hs = c.take(n * eat::fp8::scale_bytes(K2));
         // (the first product's slices are used up before the second's are written)
-        const size_t first = back ? up * n * F * 4 : up > 1 ? 2 * up * n * F * 4 : 0;
+        const size_t first = back ? (eat::fp8::back_in_one(r, F, up) ? 0 : up * n * F * 4) : up > 1 ? 2 * up * n * F * 4 : 0;
         part = c.take(std::max<size_t>(first, down > 1 ? down * n * d * 4 : 0));
         total = c.off;
     }
@@ -979,10 +979,8 @@ eat_status_t eat_fp8_experts_backward(eat_handle_t h, const void* dy, const int3
     (void)hipGetLastError();
     hipError_t e = eat::fp8::launch_quantize_rows(static_cast<const uint16_t*>(dy), r, p.d_model, base + c.q, base + c.s, stream);
     if (e == hipSuccess)
-        e = eat::fp8::launch_product(r, base + c.q, base + c.s, ld, matrix_at(b + w.w2t, b + w.s2t, F, p.d_model), false,
-                                     nullptr, c.up, part, stream);
-    if (e == hipSuccess)
-        e = eat::fp8::launch_gate_backward(r, part, c.up, F, static_cast<const uint16_t*>(saved), base + c.h, base + c.hs, l2, stream);
+        e = eat::fp8::launch_gate_backward(r, base + c.q, base + c.s, ld, matrix_at(b + w.w2t, b + w.s2t, F, p.d_model), c.up, part,
+                                           static_cast<const uint16_t*>(saved), base + c.h, base + c.hs, l2, stream);
     if (e == hipSuccess)
         e = eat::fp8::launch_product(r, base + c.h, base + c.hs, l2, matrix_at(b + w.w13t, b + w.s13t, p.d_model, 2 * Fp), true, dx,
                                      c.down, part, stream);

@@ -337,9 +337,10 @@ hipError_t launch_product(const Rows& r, const uint8_t* q, const uint8_t* sq, in
 // h [cap][pad(M)], sh [cap][scale_bytes(M)]: silu(w1 x) (w3 x) in 8 bits; saved [cap][2 M] bf16 or null; part: 2 x the slices
 hipError_t launch_gated(const Rows& r, const uint8_t* q, const uint8_t* sq, int lds, const Matrix& w1, const Matrix& w3,
                             uint8_t* h, uint8_t* sh, uint16_t* saved, int splits, float* part, hipStream_t s);
-// dh's slices [splits][cap][F] and saved -> [dg | du] in 8 bits, [cap][2 pad(F)]
-hipError_t launch_gate_backward(const Rows& r, const float* dh, int splits, int F, const uint16_t* saved, uint8_t* q, uint8_t* scale,
-                                    int lds, hipStream_t s);
+// dh = dy w2 (its slices [splits][cap][F] in part, unless back_in_one) and saved -> [dg | du] in 8 bits, [cap][2 pad(F)]
+bool back_in_one(const Rows& r, int F, int splits);
+hipError_t launch_gate_backward(const Rows& r, const uint8_t* dyq, const uint8_t* sdy, int lddy, const Matrix& w2t, int splits, float* part,
+                                const uint16_t* saved, uint8_t* q, uint8_t* scale, int lds, hipStream_t s);
 }  // namespace fp8
 
 // Forward entry points (api.cpp): host-side argument checks, and the

@@ -69,9 +69,9 @@ using Mid = Tile<128, 256, 2, 4, 3, false>;
 using Few = Tile<32, 256, 1, 4, 4, true>;
 
 // SLICES is fp32 slices of the reduction, EXACT the same on exact sums, as are ROWS32,
-// GATED and SAVED (GATED that also leaves g and u in bf16).
+// GATED, SAVED (GATED that also leaves g and u in bf16) and BACK (dh to dg and du).
 constexpr int kBand = 4;                  // weight tiles side by side in the work list
-enum Out { ROWS16, ROWS32, SLICES, EXACT, GATED, SAVED };
+enum Out { ROWS16, ROWS32, SLICES, EXACT, GATED, SAVED, BACK };
 
 struct Args {
     const uint8_t* wa;         // [groups][M][Kp]
@@ -87,10 +87,10 @@ struct Args {
     int groups, cap, M, Kp;
     int splits;                // SLICES: of the reduction
     int xcds;
-    void* out;                 // ROWS16, ROWS32: [cap][M]; SLICES: [splits][cap][M] fp32; GATED: [cap][Mp] 8 bits
-    uint8_t* sout;             // GATED: [cap][ldo] scales
+    void* out;                 // ROWS16, ROWS32: [cap][M]; SLICES: [splits][cap][M] fp32; GATED: [cap][Mp] 8 bits, BACK: [cap][2 Mp]
+    uint8_t* sout;             // GATED, BACK: [cap][ldo] scales
     int ldo;
-    uint16_t* saved;           // SAVED: [cap][2 M] bf16
+    uint16_t* saved;           // SAVED, BACK: [cap][2 M] bf16
 };
 
 // 16-byte vector v of 128-byte row r in LDS: two rows to a line of the 64 banks,
@@ -125,6 +125,13 @@ struct Loads {
 // do.  Both factors a quarter: the reciprocal gives no denormals.
 __device__ __forceinline__ float swiglu(float a, float b) {
     return 0.25f * a * __builtin_amdgcn_rcpf(fmaf(0.25f, __expf(-a), 0.25f)) * b;
+}
+
+// h = silu(g) u: dg = dh u s (1 + g (1 - s)), du = dh g s with s = 1 / (1 + e^-g).
+__device__ __forceinline__ void gate_backward(float dh, float g, float u, float& dg, float& du) {
+    const float s = 1.f / (1.f + __expf(-g));
+    dg = dh * u * s * (1.f + g * (1.f - s));
+    du = dh * g * s;
 }
 
 // 2^(b - 127) of the lowest byte b (1 to 254).
@@ -754,6 +761,119 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(C::
                 if (r0 < cur.n) ++stored;
             }
             // (what the waves read of `free_stage` is refilled after the next chunk's barrier)
+        } else if constexpr (OUT == BACK) {
+            // dg and du (gate_backward) in place of dh, as gate_kernel works them out from dh in
+            // memory; their blocks of 128 features lie in kPer waves.  g and u come 16 bytes a lane.
+            constexpr int kPer = kBlk / (32 * WF);
+            static_assert(kPer * WF * 32 == kBlk && C::WW % kPer == 0, "blocks of whole waves");
+            const int blocks = (a.M + kBlk - 1) / kBlk, half = wn / kPer, blk = cur.m0 / kBlk + half;
+            float* const most = reinterpret_cast<float*>(free_stage + NW / kBlk * TM * kBlk);      // [2][WW][TM]
+            static_assert(NW / kBlk * TM * kBlk + 2 * C::WW * TM * 4 <= C::kScales, "inside the stage");
+            f32x16 du[WF][TF];
+            auto largest = [&](const f32x16 (&v)[WF][TF], int j, int which) __attribute__((always_inline)) {
+                float m = 0.f;                            // (the maximum passes NaN over)
+#pragma unroll
+                for (int i = 0; i < WF; ++i)
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) m = fmaxf(m, fabsf(v[i][j][q]));
+                if (__any(!is_finite(m))) {               // infinities leave the scale alone
+                    m = 0.f;
+#pragma unroll
+                    for (int i = 0; i < WF; ++i)
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) m = fmaxf(m, finite_abs(v[i][j][q]));
+                }
+                m = fmaxf(m, __shfl_xor(m, 32, kWave));
+                if (lh == 0) most[(which * C::WW + wn) * TM + brow + 32 * j + l32] = m;
+            };
+#pragma unroll
+            for (int j = 0; j < TF; ++j) {
+                int lane = lane_id();
+                asm volatile("" : "+v"(lane));
+                const int l32 = lane & 31, lh = lane >> 5;
+                const int r = brow + 32 * j + l32, f0 = cur.m0 + 32 * WF * wn + 4 * lh;
+                const uint16_t* const sv = a.saved + static_cast<size_t>(cur.r0 + min(r, cur.n - 1)) * 2 * a.M;
+#pragma unroll
+                for (int i = 0; i < WF; ++i) {
+                    // a lane fetches 8 features, the other half of the wave the next 8; then they trade 4
+                    uint32_t gw[8], uw[8];
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        const int f = min(cur.m0 + 32 * (WF * wn + i) + 16 * p + 8 * lh, a.M - 8);
+                        const u32x4 g4 = *reinterpret_cast<const u32x4*>(sv + f), u4 = *reinterpret_cast<const u32x4*>(sv + a.M + f);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const auto gs = __builtin_amdgcn_permlane32_swap(g4[k], g4[2 + k], false, false);
+                            const auto us = __builtin_amdgcn_permlane32_swap(u4[k], u4[2 + k], false, false);
+                            gw[4 * p + k] = gs[0];
+                            gw[4 * p + 2 + k] = gs[1];
+                            uw[4 * p + k] = us[0];
+                            uw[4 * p + 2 + k] = us[1];
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        const uint32_t gp = gw[q / 2], up = uw[q / 2];
+                        const float g = __uint_as_float(q & 1 ? gp & 0xffff0000u : gp << 16), u = __uint_as_float(q & 1 ? up & 0xffff0000u : up << 16);
+                        // (M is a multiple of 8: whole groups of a lane pair lie past it, as zeros)
+                        const bool in = f0 + 32 * i + 8 * (q / 4) < a.M;
+                        float dg, d;
+                        gate_backward(acc[i][j][q], g, u, dg, d);
+                        acc[i][j][q] = in ? dg : 0.f;
+                        du[i][j][q] = in ? d : 0.f;
+                    }
+                    // (one fragment's g and u at a time in registers)
+                    asm volatile("" : "+v"(acc[i][j]), "+v"(du[i][j]));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                largest(acc, j, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                largest(du, j, 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            lds_barrier();
+            const size_t Mp = static_cast<size_t>(blocks) * kBlk;
+            auto put = [&](const f32x16 (&v)[WF][TF], int which) __attribute__((always_inline)) {
+                int lane = lane_id();
+                asm volatile("" : "+v"(lane));            // (addresses worked out here, not kept beside both)
+                const int l32 = lane & 31, lh = lane >> 5;
+#pragma unroll
+                for (int j = 0; j < TF; ++j) {
+                    const int r = brow + 32 * j + l32;
+                    float m = 0.f;
+#pragma unroll
+                    for (int w = 0; w < kPer; ++w) m = fmaxf(m, most[(which * C::WW + half * kPer + w) * TM + r]);
+                    const uint32_t b = scale_byte(m);
+                    const float s = scale_inverse(b);
+                    if (wn % kPer == 0 && lh == 0 && r < cur.n && blk < blocks)
+                        a.sout[static_cast<size_t>(cur.r0 + r) * a.ldo + which * blocks + blk] = static_cast<uint8_t>(b);
+#pragma unroll
+                    for (int i = 0; i < WF; ++i)
+#pragma unroll
+                        for (int qb = 0; qb < 4; ++qb)
+                            *reinterpret_cast<uint32_t*>(free_stage + half * TM * kBlk + at_row(r, 2 * (WF * (wn % kPer) + i) + qb / 2) + 8 * (qb & 1) + 4 * lh) =
+                                pack_e4m3(v[i][j][4 * qb] * s, v[i][j][4 * qb + 1] * s, v[i][j][4 * qb + 2] * s, v[i][j][4 * qb + 3] * s);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                lds_barrier();
+                stored = 0;
+#pragma unroll
+                for (int h = 0; h < NW / kBlk; ++h) {
+                    if (cur.m0 + kBlk * h >= a.M) break;
+#pragma unroll
+                    for (int k = 0; k < TM / 8 / C::kWaves; ++k) {
+                        const int r0 = 8 * (wave + C::kWaves * k), r = r0 + lane / 8, v16 = lane % 8;
+                        if (r < cur.n) {
+                            const u32x4 d = *reinterpret_cast<const u32x4*>(free_stage + h * TM * kBlk + at_row(r, v16));
+                            *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.out) + (cur.r0 + r) * 2 * Mp + which * Mp + cur.m0 + kBlk * h + 16 * v16) = d;
+                        }
+                        if (r0 < cur.n) ++stored;
+                    }
+                }
+            };
+            put(acc, 0);
+            lds_barrier();
+            put(du, 1);
         } else {
 #pragma unroll
             for (int j = 0; j < TF; ++j) {
@@ -933,8 +1053,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ par
 
 // Between the experts' products, 16 lanes per row and 128 features:
 //   forward:  g, u (the sums of their slices) -> h = silu(g) u in 8 bits (and g, u in bf16)
-//   backward: dh (the sum of its slices), g, u (bf16) -> dg = dh u s (1 + g (1 - s)), du = dh g s
-//             in 8 bits, s = 1 / (1 + e^-g)
+//   backward: dh (the sum of its slices), g, u (bf16) -> dg, du (gate_backward) in 8 bits
 // Bound by memory: the backward of 32768 x 1024 moves 335 MB in 65 us.
 struct GateArgs {
     const float* a;            // [splits][cap][F] g or dh
@@ -985,9 +1104,7 @@ __global__ __launch_bounds__(256) void gate_kernel(GateArgs a) {
             for (int j = 0; j < 8; ++j) {
                 const float g = __uint_as_float(j & 1 ? gp[j / 2] & 0xffff0000u : gp[j / 2] << 16);
                 const float u = __uint_as_float(j & 1 ? up[j / 2] & 0xffff0000u : up[j / 2] << 16);
-                const float s = 1.f / (1.f + __expf(-g));
-                o[j] = x[j] * u * s * (1.f + g * (1.f - s));
-                p[j] = x[j] * g * s;
+                gate_backward(x[j], g, u, o[j], p[j]);
             }
         } else {
 #pragma unroll
@@ -1170,10 +1287,26 @@ hipError_t launch_gated(const Rows& r, const uint8_t* q, const uint8_t* sq, int 
     return hipGetLastError();
 }
 
-hipError_t launch_gate_backward(const Rows& r, const float* dh, int splits, int F, const uint16_t* saved, uint8_t* q, uint8_t* scale,
-                                    int lds, hipStream_t s) {
+// Whole sums go to dg and du in the product's epilogue where the registers hold both (Big's
+// are full of dh): dh, 4 F bytes a row, is then neither written nor read (64 experts of 512
+// rows, 2048 x 1024, forward and gradient 923 -> 906 us; 60 of 273, 1024 x 2816: 768 -> 744).
+bool back_in_one(const Rows& r, int F, int splits) { return splits == 1 && tile_rows(r, product_columns(F)) != Big::TM; }
+
+hipError_t launch_gate_backward(const Rows& r, const uint8_t* dyq, const uint8_t* sdy, int lddy, const Matrix& w2t, int splits, float* part,
+                                const uint16_t* saved, uint8_t* q, uint8_t* scale, int lds, hipStream_t s) {
     if (r.cap == 0) return hipSuccess;
-    const GateArgs g{dh, nullptr, splits, F, pad(F), range_of(r), const_cast<uint16_t*>(saved), q, scale, lds};
+    const int F = w2t.M;
+    if (back_in_one(r, F, splits)) {
+        Args a = base_args(r, w2t, dyq, sdy, lddy);
+        a.out = q;
+        a.sout = scale;
+        a.ldo = lds;
+        a.saved = const_cast<uint16_t*>(saved);
+        return tile_rows(r, product_columns(F)) == Mid::TM ? launch_tile<BACK, Mid>(a, r, s) : launch_tile<BACK, Few>(a, r, s);
+    }
+    const hipError_t e = launch_product(r, dyq, sdy, lddy, w2t, false, nullptr, splits, part, s);
+    if (e != hipSuccess) return e;
+    const GateArgs g{part, nullptr, splits, F, pad(F), range_of(r), const_cast<uint16_t*>(saved), q, scale, lds};
     gate_kernel<true><<<some_blocks((static_cast<int64_t>(r.cap) * (g.Fp / kBlk) + 15) / 16), 256, 0, s>>>(g);
     return hipGetLastError();
 }
