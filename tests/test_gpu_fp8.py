@@ -357,6 +357,26 @@ def test_an_overflowing_h_is_not_a_number():
         assert torch.equal(ex.forward(loud, off, token, saved=saved)[~bad], want[~bad]) and saved.isfinite().all()
 
 
+@pytest.mark.parametrize("T,d,F,E", [(20, 256, 192, 2), (300, 256, 384, 4), (3000, 512, 256, 4)])
+def test_an_overflowing_gradient_stays_in_its_row(T, d, F, E):
+    """dh u past fp32 in every third row: NaN there, the others keep their bits."""
+    w, x, off, token = make_experts(T, d, F, E, 1, "even")
+    off, token = off.int().cuda(), torch.arange(T).int().cuda()
+    ex = Fp8Experts(w, gradients=True)
+    saved = torch.empty(T, 2 * F, dtype=torch.bfloat16, device="cuda")
+    ex.forward(x, off, token, saved=saved)
+    saved[:, F:] *= 2.0 ** 30
+    dy = normal(T, d).float().clamp(-3, 3).to(torch.bfloat16)
+    want = ex.backward(dy, saved, off)
+    assert want.isfinite().all()
+    loud = dy.clone()
+    loud[::3] *= 2.0 ** 120
+    got = ex.backward(loud, saved, off)
+    bad = torch.zeros(T, dtype=torch.bool, device="cuda")
+    bad[::3] = True
+    assert got[bad].isnan().all() and torch.equal(got[~bad], want[~bad])
+
+
 def test_streams_and_graphs():
     """Eager, on a named stream behind pending work, and captured and replayed over new inputs."""
     T, d, F, E, k = 60, 256, 320, 8, 2
