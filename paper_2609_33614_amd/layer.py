@@ -68,6 +68,17 @@ def _hand_out(stream, caller, *tensors) -> None:
             t.record_stream(caller)
 
 
+def _take_in(named: bool, on, *tensors) -> None:
+    """Tell torch's allocator that a call uses `tensors` (None passes) on `on`, the
+    current stream, where that is `named` (not their own): dropped, their
+    memory is not given away before `on` is done.  What a graph reads stays its
+    caller's to keep."""
+    if named and not torch.cuda.is_current_stream_capturing():
+        for t in tensors:
+            if t is not None:
+                t.record_stream(on)
+
+
 class EatLayer:
     def __init__(self, params: L.eat_params_t, max_tokens: int, weights: Dict[str, torch.Tensor],
                  device: str = "cuda"):
@@ -150,7 +161,8 @@ class EatLayer:
         to the tensors given.  ``valid`` [T] (bool or uint8): tokens that count.
         Calls of one layer share a workspace: order them on one stream.
         ``stream``: what the call is enqueued on (the current one); the tensors
-        given have to be ready there, and what is returned is ready when it is."""
+        given have to be ready there (outside a capture they may be dropped once the
+        call has returned), and what is returned is ready when it is."""
         T, E, d = prob.shape[0], self.params.E, self.params.d_model
         act = torch.bfloat16 if self.params.act_dtype == L.EAT_BF16 else torch.float32
         W = L.mask_words(E)
@@ -173,6 +185,7 @@ class EatLayer:
             ws = self._bws.get(need, on)
             L.eat_balance_loss(self.handle, x, T, self.w["w_router"], prob, mask, valid, coef, entropy_coef, loss, count,
                                mean, dlogits, dx, dw_router, ws, need, on)
+            _take_in(stream is not None, on, x, self.w["w_router"], prob, mask, valid, dlogits, dx, dw_router)
         _hand_out(stream, caller, loss, count, mean)
         return loss, count, mean
 
@@ -216,6 +229,7 @@ class EatLayer:
             on = torch.cuda.current_stream(dev)
             ws = self._bws.get(need, on) if need else None
             L.eat_sort_tokens(self.handle, x, T, mask, cap, rows, offsets, token, place, ws, need, on)
+            _take_in(stream is not None, on, x, mask, rows if given else None)
         _hand_out(stream, caller, offsets, token, place, *(() if given or rows is None else (rows,)))
         return rows, offsets, token, place
 
@@ -248,6 +262,7 @@ class EatLayer:
                 L.eat_sort_backward(self.handle, rows, cap, T, mask, place, out, on)
             else:
                 L.eat_combine(self.handle, rows, cap, T, mask, gate, place, out, on)
+            _take_in(stream is not None, on, rows, mask, gate, place, out if given else None)
         if not given:
             _hand_out(stream, caller, out)
         return out
@@ -274,8 +289,9 @@ class EatLayer:
         if rows is None and (dgate is not None or dlogits is not None):
             raise ValueError("rows: the gates' gradients need them")
         with _calling_on(stream, dev):
-            L.eat_combine_backward(self.handle, dy, rows, cap, T, mask, gate, place, prob, drows, dgate, dlogits,
-                                   torch.cuda.current_stream(dev))
+            on = torch.cuda.current_stream(dev)
+            L.eat_combine_backward(self.handle, dy, rows, cap, T, mask, gate, place, prob, drows, dgate, dlogits, on)
+            _take_in(stream is not None, on, dy, rows, mask, gate, place, prob, drows, dgate, dlogits)
 
     def close(self) -> None:
         if self.handle:
@@ -322,7 +338,8 @@ class CrossEntropy:
     workspace to stay under where a call can (the vocabulary is then taken in
     smaller pieces).  Calls of one object share its workspace: order them on
     one stream.  ``stream``: what a call is enqueued on (the current one); the
-    tensors given have to be ready there, and what is returned is ready when it is."""
+    tensors given have to be ready there (outside a capture they may be dropped once
+    the call has returned), and what is returned is ready when it is."""
 
     def __init__(self, w_vocab: torch.Tensor, ignore: int = -100, max_workspace: Optional[int] = None):
         if w_vocab.dim() != 2:
@@ -362,6 +379,7 @@ class CrossEntropy:
             ws = self._ws.get(need, on)
             L.eat_ce_loss(h, T, self.d, self.w, self.V, target, self.ignore, int(mean), scale, out, nll, count, dh, dw, ws,
                           need, on)
+            _take_in(stream is not None, on, h, self.w, target, nll, count, dh, dw)
         _hand_out(stream, caller, out)
         return out
 
@@ -374,7 +392,8 @@ class Fp8Matrix:
     ``gradients`` the transposed numbers are kept too, for ``product_backward``.
     Calls of one object share its workspace: order them on one stream.
     ``stream``: what a call is enqueued on (the current one); the tensors given
-    have to be ready there, and what is returned is ready when it is."""
+    have to be ready there (and, outside a capture, may be dropped once the call has
+    returned, as the object may), and what is returned is ready when it is."""
 
     def __init__(self, w: torch.Tensor, gradients: bool = False, stream=None):
         if w.dim() not in (2, 3):
@@ -393,6 +412,8 @@ class Fp8Matrix:
                 s = torch.empty(self.groups, -(-rows // 128), -(-cols // 512) * 4, dtype=torch.uint8, device=w.device)
                 L.eat_fp8_quantize(w, dtype, self.groups, self.M, self.K, len(made) // 2, q, s, on)
                 made += [q, s]
+            _take_in(stream is not None, on, w)
+        self._home = on.cuda_stream
         _hand_out(stream, caller, *made)
         self.q, self.scale = made[:2]
         self.qt, self.scale_t = made[2:] if gradients else (None, None)
@@ -417,6 +438,8 @@ class Fp8Matrix:
             ws = self._ws.get(need, on)
             L.eat_fp8_product(x, src, token, offsets, rows, q, scale, self.groups, M, K, out,
                               L.EAT_BF16 if out.dtype == torch.bfloat16 else L.EAT_F32, ws, need, on)
+            _take_in(on.cuda_stream != self._home, on, q, scale)
+            _take_in(stream is not None, on, x, offsets, token, out if given else None)
         if not given:
             _hand_out(stream, caller, out)
         return out
@@ -456,8 +479,11 @@ class Fp8Experts:
         self.handle = L.eat_create(L.eat_params_default(mode="topk", E=self.E, d_model=self.d, d_ffn=self.F, top_k=1), 1 << 24)
         caller = torch.cuda.current_stream(dev) if stream is not None else None
         with _calling_on(stream, dev):
+            on = torch.cuda.current_stream(dev)
             self.buf = torch.empty(L.eat_fp8_experts_size(self.handle, int(gradients)), dtype=torch.uint8, device=dev)
-            L.eat_fp8_experts_quantize(self.handle, w1, w3, w2, int(gradients), self.buf, torch.cuda.current_stream(dev))
+            L.eat_fp8_experts_quantize(self.handle, w1, w3, w2, int(gradients), self.buf, on)
+            _take_in(stream is not None, on, w1, w3, w2)
+        self._home = on.cuda_stream
         _hand_out(stream, caller, self.buf)
         self._ws = _Workspace(dev)
 
@@ -481,6 +507,8 @@ class Fp8Experts:
             on = torch.cuda.current_stream(dev)
             ws = self._ws.get(need, on)
             L.eat_fp8_experts_forward(self.handle, x, T, token, offsets, rows, self.buf, y, saved, ws, need, on)
+            _take_in(on.cuda_stream != self._home, on, self.buf)
+            _take_in(stream is not None, on, x, offsets, token, saved, y if given else None)
         if not given:
             _hand_out(stream, caller, y)
         return y
@@ -504,6 +532,8 @@ class Fp8Experts:
             on = torch.cuda.current_stream(dev)
             ws = self._ws.get(need, on)
             L.eat_fp8_experts_backward(self.handle, dy, offsets, rows, self.buf, saved, dx, ws, need, on)
+            _take_in(on.cuda_stream != self._home, on, self.buf)
+            _take_in(stream is not None, on, dy, saved, offsets, dx if given else None)
         if not given:
             _hand_out(stream, caller, dx)
         return dx
