@@ -524,7 +524,8 @@ eat_status_t eat_fp8_size(int32_t groups, int32_t M, int32_t K, size_t* q_bytes,
 
 /* w [groups][M][K] (dtype: eat_dtype_t) to q and scale, 256-byte aligned as every
  * array of these calls that holds 8 bits; transposed = 1: the same numbers as a
- * matrix [groups][K][M] (for the gradient of the rows).  Enqueues on `stream` only.
+ * matrix [groups][K][M] (for the gradient of the rows).  The limits are those of the
+ * matrix written.  Enqueues on `stream` only.
  * Nothing may overlap (INVALID_ARG). */
 eat_status_t eat_fp8_quantize(const void* w, int32_t dtype, int32_t groups, int32_t M, int32_t K, int32_t transposed, void* q,
                               void* scale, hipStream_t stream);

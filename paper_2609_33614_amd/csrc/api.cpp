@@ -817,8 +817,8 @@ eat_status_t eat_fp8_size(int32_t groups, int32_t M, int32_t K, size_t* q_out, s
 eat_status_t eat_fp8_quantize(const void* w, int32_t dtype, int32_t groups, int32_t M, int32_t K, int32_t transposed, void* q,
                               void* scale, hipStream_t stream) {
     if ((dtype != EAT_F32 && dtype != EAT_BF16) || (transposed != 0 && transposed != 1)) return EAT_ERR_INVALID_ARG;
-    eat_status_t st = check_fp8(groups, M, K);
-    if (st == EAT_OK) st = check_fp8(groups, K, M);
+    // (the matrix that is written; the limits of the one that is read follow but for its own padding)
+    const eat_status_t st = transposed ? check_fp8(groups, K, M) : check_fp8(groups, M, K);
     if (st != EAT_OK) return st;
     if (!w || !q || !scale || !aligned(w, 16) || !aligned(q, 256) || !aligned(scale, 256)) return EAT_ERR_INVALID_ARG;
     const int32_t rows = transposed ? K : M, cols = transposed ? M : K;
