@@ -562,7 +562,9 @@ eat_status_t eat_fp8_product(const void* x, int32_t src_rows, const int32_t* tok
  *
  * eat_fp8_experts_quantize writes the weights (bf16, eat_moe_forward's row-major
  * layout) to `buf` once: 3 E F d bytes and their scales, with grads = 1 (for
- * eat_fp8_experts_backward) their transposes too. */
+ * eat_fp8_experts_backward) their transposes too.  The limits above hold for
+ * matrices [E][d_ffn][d_model] and [E][d_model][d_ffn], with grads = 1 and for
+ * the backward for [E][d_model][2 d_ffn] too (each d_ffn padded to 128). */
 eat_status_t eat_fp8_experts_size(eat_handle_t h, int32_t grads, size_t* bytes);
 eat_status_t eat_fp8_experts_quantize(eat_handle_t h, const void* w1, const void* w3, const void* w2, int32_t grads, void* buf,
                                       hipStream_t stream);

@@ -796,10 +796,11 @@ struct ExpertsCall {
     }
 };
 
-eat_status_t check_experts(const eat_ctx* h, int32_t T, int32_t rows) {
+// `grads`: of the backward too, whose matrix [dg | du] -> dx has rows of both.
+eat_status_t check_experts(const eat_ctx* h, int32_t T, int32_t rows, bool grads) {
     if (!h || T < 0 || T > h->max_tokens || rows < 0 || (rows > 0 && T == 0)) return EAT_ERR_INVALID_ARG;
     if (h->p.act_dtype != EAT_BF16 || rows > kMaxFp8Rows || T > kMaxFp8Rows) return EAT_ERR_UNSUPPORTED;
-    const eat_status_t st = check_fp8(h->p.E, h->p.d_model, 2 * eat::fp8::pad(h->p.d_ffn));
+    const eat_status_t st = check_fp8(h->p.E, h->p.d_model, grads ? 2 * eat::fp8::pad(h->p.d_ffn) : h->p.d_ffn);
     return st != EAT_OK ? st : check_fp8(h->p.E, h->p.d_ffn, h->p.d_model);
 }
 
@@ -881,7 +882,7 @@ eat_status_t eat_fp8_product(const void* x, int32_t src_rows, const int32_t* tok
 }
 
 eat_status_t eat_fp8_experts_size(eat_handle_t h, int32_t grads, size_t* bytes) {
-    const eat_status_t st = check_experts(h, 0, 0);
+    const eat_status_t st = check_experts(h, 0, 0, grads == 1);
     if (st != EAT_OK) return st;
     if (!bytes || (grads != 0 && grads != 1)) return EAT_ERR_INVALID_ARG;
     *bytes = ExpertsPlan(h->p, grads == 1).total;
@@ -890,7 +891,7 @@ eat_status_t eat_fp8_experts_size(eat_handle_t h, int32_t grads, size_t* bytes) 
 
 eat_status_t eat_fp8_experts_quantize(eat_handle_t h, const void* w1, const void* w3, const void* w2, int32_t grads, void* buf,
                                       hipStream_t stream) {
-    const eat_status_t st = check_experts(h, 0, 0);
+    const eat_status_t st = check_experts(h, 0, 0, grads == 1);
     if (st != EAT_OK) return st;
     if (!w1 || !w3 || !w2 || !buf || (grads != 0 && grads != 1)) return EAT_ERR_INVALID_ARG;
     if (!aligned(w1, 16) || !aligned(w3, 16) || !aligned(w2, 16) || !aligned(buf, 256)) return EAT_ERR_INVALID_ARG;
@@ -911,7 +912,7 @@ eat_status_t eat_fp8_experts_quantize(eat_handle_t h, const void* w1, const void
 }
 
 eat_status_t eat_fp8_experts_workspace_size(eat_handle_t h, int32_t T, int32_t rows, int32_t grads, size_t* bytes) {
-    const eat_status_t st = check_experts(h, grads == 1 && rows > 0 ? 1 : T, rows);
+    const eat_status_t st = check_experts(h, grads == 1 && rows > 0 ? 1 : T, rows, grads == 1);
     if (st != EAT_OK) return st;
     if (!bytes || (grads != 0 && grads != 1)) return EAT_ERR_INVALID_ARG;
     const int32_t dummy = 0;
@@ -922,7 +923,7 @@ eat_status_t eat_fp8_experts_workspace_size(eat_handle_t h, int32_t T, int32_t r
 eat_status_t eat_fp8_experts_forward(eat_handle_t h, const void* x, int32_t T, const int32_t* token, const int32_t* offsets,
                                      int32_t rows, const void* buf, void* y, void* saved, void* ws, size_t ws_bytes,
                                      hipStream_t stream) {
-    const eat_status_t st = check_experts(h, T, rows);
+    const eat_status_t st = check_experts(h, T, rows, false);
     if (st != EAT_OK) return st;
     if (!buf || !offsets || (rows > 0 && (!x || !token || !y))) return EAT_ERR_INVALID_ARG;
     if (!aligned(x, 16) || !aligned(token, 4) || !aligned(offsets, 4) || !aligned(buf, 256) || !aligned(y, 16) || !aligned(saved, 16))
@@ -956,7 +957,7 @@ eat_status_t eat_fp8_experts_forward(eat_handle_t h, const void* x, int32_t T, c
 
 eat_status_t eat_fp8_experts_backward(eat_handle_t h, const void* dy, const int32_t* offsets, int32_t rows, const void* buf,
                                       const void* saved, void* dx, void* ws, size_t ws_bytes, hipStream_t stream) {
-    const eat_status_t st = check_experts(h, rows > 0 ? 1 : 0, rows);
+    const eat_status_t st = check_experts(h, rows > 0 ? 1 : 0, rows, true);
     if (st != EAT_OK) return st;
     if (!buf || !offsets || (rows > 0 && (!dy || !saved || !dx))) return EAT_ERR_INVALID_ARG;
     if (!aligned(dy, 16) || !aligned(offsets, 4) || !aligned(buf, 256) || !aligned(saved, 16) || !aligned(dx, 16)) return EAT_ERR_INVALID_ARG;

@@ -4,8 +4,9 @@ import pytest
 import torch
 
 from paper_2609_33614_amd import _lib as L
-from paper_2609_33614_amd.layer import Fp8Matrix
+from paper_2609_33614_amd.layer import Fp8Experts, Fp8Matrix
 from tests import fp8_reference as R
+from tests import test_gpu_fp8 as Q
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +48,25 @@ def test_the_largest_matrix_transposed():
         want, k = R.quantize(w[:, c: c + 128].T.contiguous(), 128)
         have = torch.exp2(s[0, c // 128, : M // 128].double() - 127).repeat_interleave(128) * q[0, c: c + 128].double()
         assert torch.equal(have, want) and torch.equal(s[0, c // 128, : M // 128].int() - 127, k[0].int())
+
+
+@pytest.mark.parametrize("T", [3, 300])
+def test_experts_too_wide_for_a_gradient(T):
+    """16384 x 65536: 2^30 elements a matrix, whose gradient's [d][2 d_ffn] would have 2^31. Rows of x with
+    one element pick the 8-bit numbers of W1 and W3 as g and u, exactly; y as the other tests of the experts."""
+    d, F = 16384, 65536
+    w = {"w1": big(F, d, 2)[None], "w3": big(F, d, 3)[None], "w2": big(d, F, 4)[None]}
+    for n, k in (("w1", 7), ("w3", 7), ("w2", 8)):
+        w[n].mul_(2.0 ** -k)
+    ex = Fp8Experts(w)
+    with pytest.raises(L.EatError):
+        Fp8Experts(w, gradients=True)
+    x, token, off = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda"), torch.arange(T), torch.tensor([0, T])
+    x[token, (d - 1 - 5003 * token) % d] = 128.0
+    saved = torch.empty(T, 2 * F, dtype=torch.bfloat16, device="cuda")
+    y = ex.forward(x, off.int().cuda(), token.int().cuda(), saved=saved)
+    assert torch.equal(ex.forward(x, off.int().cuda(), token.int().cuda()), y)
+    (ry, by, vy), (rs, _) = Q.experts_reference(x, w, off, token.cuda())
+    assert torch.equal(saved.double(), rs)
+    Q.within(f"wide experts {T}", y, ry, by)
+    assert (y.double() - ry).square().sum() <= vy.sum()
