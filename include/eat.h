@@ -456,7 +456,8 @@ eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const fl
  *             z (p = softmax(z), with expert_scale too) through g = p / (P + eps),
  *             the selections held, as eat_balance_loss gives its own
  *
- * A token that selected no expert gets y 0, dx 0, dg 0 and dz 0.  Sums are in
+ * A token that selected no expert gets y 0, dx 0, dg 0 and dz 0, whatever its rows
+ * of x, dy, p and g hold.  Sums are in
  * fp32, in the experts' order, rounded once.  `cap` is the number of rows that the
  * caller's arrays hold: pairs past it are left out (place -1, offsets and all
  * sums end at cap).  Rows from offsets[E] on are not written.  Places outside

@@ -432,11 +432,13 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
         sync();
         Cursor c = first_rows(a, t);
         float P = 0.f;
+        bool any = false;                                 // the token selected an expert
         for (;;) {
             int rows[kBatch], es[kBatch];
             float gates[kBatch], dot[kBatch];
             const int n = next_rows<true, true>(a, t, c, rows, gates, es);
             if (n == 0) break;
+            any = true;
             if (g.dlogits) {
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b) P += b < n ? g.prob[static_cast<size_t>(t) * a.E + es[b]] : 0.f;
@@ -513,7 +515,8 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(GradArgs g) {
             if (g.dgate) g.dgate[at] = dg;
             if (g.dlogits) {
                 const bool on = (a.mask[static_cast<size_t>(t) * a.W + e / kWave] >> (e % kWave)) & 1ull;
-                const float out = g.prob[at] * G * rest;
+                // (none selected: 0 beside NaN probabilities too, as routing leaves them for rows with NaN)
+                const float out = any ? g.prob[at] * G * rest : 0.f;
                 g.dlogits[at] = on ? fmaf(gs[sub][e], dg - G, -out) : -out;
             }
         }
