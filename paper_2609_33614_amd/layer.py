@@ -242,6 +242,8 @@ class EatLayer:
                 y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """The experts' ``rows`` [cap][d] back to their tokens, weighted by
         ``gate`` (from ``route``; eat_combine): y [T][d]."""
+        if gate is None:
+            raise ValueError("gate: the rows' weights are needed")
         _expect("gate", gate, torch.float32, (mask.shape[0], self.params.E), rows.device)
         return self._from_rows(rows, mask, gate, place, y, "rows", "y", stream)
 
