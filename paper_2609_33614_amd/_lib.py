@@ -158,6 +158,14 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _i32(v) -> int:
+    """A whole number for an int32 argument: ctypes would hand on the low 32 bits of others."""
+    v = int(v)
+    if not -1 << 31 <= v < 1 << 31:
+        raise ValueError(f"{v}: libeat takes 32-bit numbers")
+    return v
+
+
 def _check(status: int, where: str):
     if status != EAT_OK:
         raise EatError(status, where)
@@ -190,7 +198,7 @@ def eat_params_default(**overrides) -> eat_params_t:
 
 def eat_create(params: eat_params_t, max_tokens: int) -> int:
     h = C.c_void_p()
-    _check(load().eat_create(C.byref(params), int(max_tokens), C.byref(h)), "eat_create")
+    _check(load().eat_create(C.byref(params), _i32(max_tokens), C.byref(h)), "eat_create")
     return h.value
 
 
@@ -200,13 +208,13 @@ def eat_destroy(handle: int) -> None:
 
 def eat_workspace_size(handle: int, T: int) -> int:
     b = C.c_size_t()
-    _check(load().eat_workspace_size(handle, int(T), C.byref(b)), "eat_workspace_size")
+    _check(load().eat_workspace_size(handle, _i32(T), C.byref(b)), "eat_workspace_size")
     return b.value
 
 
 def eat_route_workspace_size(handle: int, T: int) -> int:
     b = C.c_size_t()
-    _check(load().eat_route_workspace_size(handle, int(T), C.byref(b)), "eat_route_workspace_size")
+    _check(load().eat_route_workspace_size(handle, _i32(T), C.byref(b)), "eat_route_workspace_size")
     return b.value
 
 
@@ -216,14 +224,14 @@ def eat_reset_accounts(handle: int, acc: eat_accounts_t, stream=None) -> None:
 
 def eat_route(handle: int, x, T: int, w_router, acc: eat_accounts_t, ppl_trend, mask_out, k_out,
               gate_out, prob_out=None, ws=None, ws_bytes: int = 0, stream=None) -> None:
-    _check(load().eat_route(handle, _ptr(x), int(T), _ptr(w_router), acc, _ptr(ppl_trend), _ptr(mask_out),
+    _check(load().eat_route(handle, _ptr(x), _i32(T), _ptr(w_router), acc, _ptr(ppl_trend), _ptr(mask_out),
                             _ptr(k_out), _ptr(gate_out), _ptr(prob_out), _ptr(ws), int(ws_bytes),
                             _stream(stream)), "eat_route")
 
 
 def eat_moe_forward(handle: int, x, T: int, w_router, w1, w3, w2, ws1, ws3, ws2, acc: eat_accounts_t,
                     ppl_trend, y, mask_out, expert_load_out, ws, ws_bytes: int, stream=None) -> None:
-    _check(load().eat_moe_forward(handle, _ptr(x), int(T), _ptr(w_router), _ptr(w1), _ptr(w3), _ptr(w2),
+    _check(load().eat_moe_forward(handle, _ptr(x), _i32(T), _ptr(w_router), _ptr(w1), _ptr(w3), _ptr(w2),
                                   _ptr(ws1), _ptr(ws3), _ptr(ws2), acc, _ptr(ppl_trend), _ptr(y),
                                   _ptr(mask_out), _ptr(expert_load_out), _ptr(ws), int(ws_bytes),
                                   _stream(stream)), "eat_moe_forward")
@@ -236,7 +244,7 @@ def eat_moe_forward_profiled(handle: int, x, T: int, w_router, w1, w3, w2, ws1, 
     stage boundary (EAT_STAGE_*)."""
     events = list(events or [])
     arr = (C.c_void_p * max(1, len(events)))(*[e or None for e in events]) if events else None
-    _check(load().eat_moe_forward_profiled(handle, _ptr(x), int(T), _ptr(w_router), _ptr(w1), _ptr(w3),
+    _check(load().eat_moe_forward_profiled(handle, _ptr(x), _i32(T), _ptr(w_router), _ptr(w1), _ptr(w3),
                                            _ptr(w2), _ptr(ws1), _ptr(ws3), _ptr(ws2), acc, _ptr(ppl_trend),
                                            _ptr(y), _ptr(mask_out), _ptr(expert_load_out), _ptr(ws),
                                            int(ws_bytes), _stream(stream), arr, len(events)),
@@ -245,7 +253,7 @@ def eat_moe_forward_profiled(handle: int, x, T: int, w_router, w1, w3, w2, ws1, 
 
 def eat_moe_forward_noalloc(handle: int, x, T: int, w_router, w1, w3, w2, ws1, ws3, ws2, acc: eat_accounts_t,
                             ppl_trend, y, mask_out, expert_load_out, stream=None) -> None:
-    _check(load().eat_moe_forward_noalloc(handle, _ptr(x), int(T), _ptr(w_router), _ptr(w1), _ptr(w3), _ptr(w2),
+    _check(load().eat_moe_forward_noalloc(handle, _ptr(x), _i32(T), _ptr(w_router), _ptr(w1), _ptr(w3), _ptr(w2),
                                           _ptr(ws1), _ptr(ws3), _ptr(ws2), acc, _ptr(ppl_trend), _ptr(y),
                                           _ptr(mask_out), _ptr(expert_load_out), _stream(stream)),
            "eat_moe_forward_noalloc")
@@ -260,64 +268,64 @@ def stack_layers(entries) -> "C.Array":
 def eat_stack_workspace_size(layers, n_layers: int, T: int) -> int:
     b = C.c_size_t()
     _check(load().eat_stack_workspace_size(C.cast(layers, C.c_void_p) if layers is not None else None,
-                                           int(n_layers), int(T), C.byref(b)), "eat_stack_workspace_size")
+                                           _i32(n_layers), _i32(T), C.byref(b)), "eat_stack_workspace_size")
     return b.value
 
 
 def eat_stack_forward(layers, n_layers: int, x, T: int, ppl_trend, rms_eps: float, h_out, masks_out, probs_out,
                       ws, ws_bytes: int, stream=None) -> None:
-    _check(load().eat_stack_forward(C.cast(layers, C.c_void_p) if layers is not None else None, int(n_layers),
-                                    _ptr(x), int(T), _ptr(ppl_trend), float(rms_eps), _ptr(h_out),
+    _check(load().eat_stack_forward(C.cast(layers, C.c_void_p) if layers is not None else None, _i32(n_layers),
+                                    _ptr(x), _i32(T), _ptr(ppl_trend), float(rms_eps), _ptr(h_out),
                                     _ptr(masks_out), _ptr(probs_out), _ptr(ws), int(ws_bytes), _stream(stream)),
            "eat_stack_forward")
 
 
 def eat_ppl_workspace_size(S: int, d: int, V: int) -> int:
     b = C.c_size_t()
-    _check(load().eat_ppl_workspace_size(int(S), int(d), int(V), C.byref(b)), "eat_ppl_workspace_size")
+    _check(load().eat_ppl_workspace_size(_i32(S), _i32(d), _i32(V), C.byref(b)), "eat_ppl_workspace_size")
     return b.value
 
 
 def eat_ppl_reset(S: int, nll_sum, count, ppl_prev, stream=None) -> None:
-    _check(load().eat_ppl_reset(int(S), _ptr(nll_sum), _ptr(count), _ptr(ppl_prev), _stream(stream)), "eat_ppl_reset")
+    _check(load().eat_ppl_reset(_i32(S), _ptr(nll_sum), _ptr(count), _ptr(ppl_prev), _stream(stream)), "eat_ppl_reset")
 
 
 def eat_ppl_trend(h, S: int, d: int, w_vocab, V: int, target, nll_sum, count, ppl_prev, trend_out, nll_out, ws,
                   ws_bytes: int, stream=None) -> None:
-    _check(load().eat_ppl_trend(_ptr(h), int(S), int(d), _ptr(w_vocab), int(V), _ptr(target), _ptr(nll_sum),
+    _check(load().eat_ppl_trend(_ptr(h), _i32(S), _i32(d), _ptr(w_vocab), _i32(V), _ptr(target), _ptr(nll_sum),
                                 _ptr(count), _ptr(ppl_prev), _ptr(trend_out), _ptr(nll_out), _ptr(ws), int(ws_bytes),
                                 _stream(stream)), "eat_ppl_trend")
 
 
 def eat_pack_weights(src, groups: int, M: int, K: int, dst, stream=None) -> None:
-    _check(load().eat_pack_weights(_ptr(src), int(groups), int(M), int(K), _ptr(dst), _stream(stream)),
+    _check(load().eat_pack_weights(_ptr(src), _i32(groups), _i32(M), _i32(K), _ptr(dst), _stream(stream)),
            "eat_pack_weights")
 
 
 def eat_ce_workspace_size(T: int, d: int, V: int, grads: int = 0) -> "tuple[int, int]":
     """(the largest workspace a call has a use for, the smallest it takes)."""
     b, least = C.c_size_t(), C.c_size_t()
-    _check(load().eat_ce_workspace_size(int(T), int(d), int(V), int(grads), C.byref(b), C.byref(least)),
+    _check(load().eat_ce_workspace_size(_i32(T), _i32(d), _i32(V), _i32(grads), C.byref(b), C.byref(least)),
            "eat_ce_workspace_size")
     return b.value, least.value
 
 
 def eat_ce_loss(h, T: int, d: int, w_vocab, V: int, target, ignore: int, mean: int, scale: float, loss_out, nll_out,
                 count_out, dh, dw, ws, ws_bytes: int, stream=None) -> None:
-    _check(load().eat_ce_loss(_ptr(h), int(T), int(d), _ptr(w_vocab), int(V), _ptr(target), int(ignore), int(mean),
+    _check(load().eat_ce_loss(_ptr(h), _i32(T), _i32(d), _ptr(w_vocab), _i32(V), _ptr(target), _i32(ignore), _i32(mean),
                               float(scale), _ptr(loss_out), _ptr(nll_out), _ptr(count_out), _ptr(dh), _ptr(dw),
                               _ptr(ws), int(ws_bytes), _stream(stream)), "eat_ce_loss")
 
 
 def eat_balance_workspace_size(handle: int, T: int) -> int:
     b = C.c_size_t()
-    _check(load().eat_balance_workspace_size(handle, int(T), C.byref(b)), "eat_balance_workspace_size")
+    _check(load().eat_balance_workspace_size(handle, _i32(T), C.byref(b)), "eat_balance_workspace_size")
     return b.value
 
 
 def eat_balance_loss(handle: int, x, T: int, w_router, prob, mask, valid, coef: float, entropy_coef: float, loss_out,
                      count_out, mean_prob_out, dlogits, dx, dw_router, ws, ws_bytes: int, stream=None) -> None:
-    _check(load().eat_balance_loss(handle, _ptr(x), int(T), _ptr(w_router), _ptr(prob), _ptr(mask), _ptr(valid),
+    _check(load().eat_balance_loss(handle, _ptr(x), _i32(T), _ptr(w_router), _ptr(prob), _ptr(mask), _ptr(valid),
                                    float(coef), float(entropy_coef), _ptr(loss_out), _ptr(count_out),
                                    _ptr(mean_prob_out), _ptr(dlogits), _ptr(dx), _ptr(dw_router), _ptr(ws),
                                    int(ws_bytes), _stream(stream)), "eat_balance_loss")
@@ -325,30 +333,30 @@ def eat_balance_loss(handle: int, x, T: int, w_router, prob, mask, valid, coef: 
 
 def eat_sort_workspace_size(handle: int, T: int) -> int:
     b = C.c_size_t()
-    _check(load().eat_sort_workspace_size(handle, int(T), C.byref(b)), "eat_sort_workspace_size")
+    _check(load().eat_sort_workspace_size(handle, _i32(T), C.byref(b)), "eat_sort_workspace_size")
     return b.value
 
 
 def eat_sort_tokens(handle: int, x, T: int, mask, cap: int, rows_out, offsets_out, token_out, place_out, ws=None,
                     ws_bytes: int = 0, stream=None) -> None:
-    _check(load().eat_sort_tokens(handle, _ptr(x), int(T), _ptr(mask), int(cap), _ptr(rows_out), _ptr(offsets_out),
+    _check(load().eat_sort_tokens(handle, _ptr(x), _i32(T), _ptr(mask), _i32(cap), _ptr(rows_out), _ptr(offsets_out),
                                   _ptr(token_out), _ptr(place_out), _ptr(ws), int(ws_bytes), _stream(stream)),
            "eat_sort_tokens")
 
 
 def eat_sort_backward(handle: int, drows, cap: int, T: int, mask, place, dx, stream=None) -> None:
-    _check(load().eat_sort_backward(handle, _ptr(drows), int(cap), int(T), _ptr(mask), _ptr(place), _ptr(dx),
+    _check(load().eat_sort_backward(handle, _ptr(drows), _i32(cap), _i32(T), _ptr(mask), _ptr(place), _ptr(dx),
                                     _stream(stream)), "eat_sort_backward")
 
 
 def eat_combine(handle: int, rows, cap: int, T: int, mask, gate, place, y, stream=None) -> None:
-    _check(load().eat_combine(handle, _ptr(rows), int(cap), int(T), _ptr(mask), _ptr(gate), _ptr(place), _ptr(y),
+    _check(load().eat_combine(handle, _ptr(rows), _i32(cap), _i32(T), _ptr(mask), _ptr(gate), _ptr(place), _ptr(y),
                               _stream(stream)), "eat_combine")
 
 
 def eat_combine_backward(handle: int, dy, rows, cap: int, T: int, mask, gate, place, prob, drows, dgate, dlogits,
                          stream=None) -> None:
-    _check(load().eat_combine_backward(handle, _ptr(dy), _ptr(rows), int(cap), int(T), _ptr(mask), _ptr(gate), _ptr(place),
+    _check(load().eat_combine_backward(handle, _ptr(dy), _ptr(rows), _i32(cap), _i32(T), _ptr(mask), _ptr(gate), _ptr(place),
                                        _ptr(prob), _ptr(drows), _ptr(dgate), _ptr(dlogits), _stream(stream)),
            "eat_combine_backward")
 
@@ -356,53 +364,53 @@ def eat_combine_backward(handle: int, dy, rows, cap: int, T: int, mask, gate, pl
 def eat_fp8_size(groups: int, M: int, K: int) -> "tuple[int, int]":
     """(bytes of the e4m3 numbers, bytes of the scales) of a matrix [groups][M][K]."""
     q, s = C.c_size_t(), C.c_size_t()
-    _check(load().eat_fp8_size(int(groups), int(M), int(K), C.byref(q), C.byref(s)), "eat_fp8_size")
+    _check(load().eat_fp8_size(_i32(groups), _i32(M), _i32(K), C.byref(q), C.byref(s)), "eat_fp8_size")
     return q.value, s.value
 
 
 def eat_fp8_quantize(w, dtype: int, groups: int, M: int, K: int, transposed: int, q, scale, stream=None) -> None:
-    _check(load().eat_fp8_quantize(_ptr(w), int(dtype), int(groups), int(M), int(K), int(transposed), _ptr(q), _ptr(scale),
+    _check(load().eat_fp8_quantize(_ptr(w), _i32(dtype), _i32(groups), _i32(M), _i32(K), _i32(transposed), _ptr(q), _ptr(scale),
                                    _stream(stream)), "eat_fp8_quantize")
 
 
 def eat_fp8_product_workspace_size(src_rows: int, rows: int, groups: int, M: int, K: int) -> int:
     b = C.c_size_t()
-    _check(load().eat_fp8_product_workspace_size(int(src_rows), int(rows), int(groups), int(M), int(K), C.byref(b)),
+    _check(load().eat_fp8_product_workspace_size(_i32(src_rows), _i32(rows), _i32(groups), _i32(M), _i32(K), C.byref(b)),
            "eat_fp8_product_workspace_size")
     return b.value
 
 
 def eat_fp8_product(x, src_rows: int, token, offsets, rows: int, q, scale, groups: int, M: int, K: int, out, out_dtype: int, ws,
                     ws_bytes: int, stream=None) -> None:
-    _check(load().eat_fp8_product(_ptr(x), int(src_rows), _ptr(token), _ptr(offsets), int(rows), _ptr(q), _ptr(scale), int(groups),
-                                  int(M), int(K), _ptr(out), int(out_dtype), _ptr(ws), int(ws_bytes), _stream(stream)),
+    _check(load().eat_fp8_product(_ptr(x), _i32(src_rows), _ptr(token), _ptr(offsets), _i32(rows), _ptr(q), _ptr(scale), _i32(groups),
+                                  _i32(M), _i32(K), _ptr(out), _i32(out_dtype), _ptr(ws), int(ws_bytes), _stream(stream)),
            "eat_fp8_product")
 
 
 def eat_fp8_experts_size(handle: int, grads: int = 0) -> int:
     b = C.c_size_t()
-    _check(load().eat_fp8_experts_size(handle, int(grads), C.byref(b)), "eat_fp8_experts_size")
+    _check(load().eat_fp8_experts_size(handle, _i32(grads), C.byref(b)), "eat_fp8_experts_size")
     return b.value
 
 
 def eat_fp8_experts_quantize(handle: int, w1, w3, w2, grads: int, buf, stream=None) -> None:
-    _check(load().eat_fp8_experts_quantize(handle, _ptr(w1), _ptr(w3), _ptr(w2), int(grads), _ptr(buf), _stream(stream)),
+    _check(load().eat_fp8_experts_quantize(handle, _ptr(w1), _ptr(w3), _ptr(w2), _i32(grads), _ptr(buf), _stream(stream)),
            "eat_fp8_experts_quantize")
 
 
 def eat_fp8_experts_workspace_size(handle: int, T: int, rows: int, grads: int = 0) -> int:
     b = C.c_size_t()
-    _check(load().eat_fp8_experts_workspace_size(handle, int(T), int(rows), int(grads), C.byref(b)),
+    _check(load().eat_fp8_experts_workspace_size(handle, _i32(T), _i32(rows), _i32(grads), C.byref(b)),
            "eat_fp8_experts_workspace_size")
     return b.value
 
 
 def eat_fp8_experts_forward(handle: int, x, T: int, token, offsets, rows: int, buf, y, saved, ws, ws_bytes: int,
                             stream=None) -> None:
-    _check(load().eat_fp8_experts_forward(handle, _ptr(x), int(T), _ptr(token), _ptr(offsets), int(rows), _ptr(buf), _ptr(y),
+    _check(load().eat_fp8_experts_forward(handle, _ptr(x), _i32(T), _ptr(token), _ptr(offsets), _i32(rows), _ptr(buf), _ptr(y),
                                           _ptr(saved), _ptr(ws), int(ws_bytes), _stream(stream)), "eat_fp8_experts_forward")
 
 
 def eat_fp8_experts_backward(handle: int, dy, offsets, rows: int, buf, saved, dx, ws, ws_bytes: int, stream=None) -> None:
-    _check(load().eat_fp8_experts_backward(handle, _ptr(dy), _ptr(offsets), int(rows), _ptr(buf), _ptr(saved), _ptr(dx), _ptr(ws),
+    _check(load().eat_fp8_experts_backward(handle, _ptr(dy), _ptr(offsets), _i32(rows), _ptr(buf), _ptr(saved), _ptr(dx), _ptr(ws),
                                            int(ws_bytes), _stream(stream)), "eat_fp8_experts_backward")
