@@ -512,7 +512,8 @@ eat_status_t eat_combine_backward(eat_handle_t h, const void* dy, const void* ro
  * instructions, which add 8 products at a time with 13 bits below the largest of them
  * (2^-10 of the eight largest's sum at most, 4e-5 of usual results), results in
  * fp32 and all that is rounded to 8 bits again from exact products; numbers below 2^-126 may
- * count as zeros.  A row that holds NaN or an infinity gives NaN in its own results
+ * count as zeros, magnitudes from 1.9375 2^127 on, which round to 2^128, as
+ * infinities.  A row that holds NaN or an infinity gives NaN in its own results
  * alone, a weight row in its own feature's of its group.
  *
  * Storage of [groups][M][K]: q [groups][M][Kp] bytes, rows padded with zeros to Kp

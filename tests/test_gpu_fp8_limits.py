@@ -70,3 +70,28 @@ def test_experts_too_wide_for_a_gradient(T):
     assert torch.equal(saved.double(), rs)
     Q.within(f"wide experts {T}", y, ry, by)
     assert (y.double() - ry).square().sum() <= vy.sum()
+
+
+@pytest.mark.parametrize("n", [5, 100, 2600])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_largest_magnitudes(n, dtype):
+    """bf16's largest rounds to 2^128: its row's results are those of that number, or not finite; every other
+    row keeps its bits. 1.875 2^127 is held as it is."""
+    K, M = 256, 264
+    top = torch.finfo(torch.bfloat16).max
+    w, x = Q.normal(1, M, K, dtype=torch.float32).clamp(-3, 3) * 2.0 ** -60, Q.normal(n, K)
+    m = Fp8Matrix(w)
+    want = m.product(x, out=torch.empty(n, M, dtype=dtype, device="cuda"))
+    held, big = x.clone(), x.clone()
+    held[1], held[1, 7], big[1, 7], big[n - 1, 200] = 0.0, 1.875 * 2.0 ** 127, top, -top
+    got = m.product(big, out=torch.empty_like(want))
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[1] = keep[n - 1] = False
+    assert torch.equal(got[keep], want[keep])
+    wq = R.quantize(w, 128)[0][0]
+    for r, c, v in ((1, 7, 2.0 ** 128), (n - 1, 200, -2.0 ** 128)):
+        ref = v * wq[:, c]                                # (the block's other numbers lie below 2^-15 of it: zeros)
+        bad = ~got[r].isfinite()
+        assert ((got[r].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -20 * ref.abs().max())[~bad].all()
+    one = m.product(held, out=torch.empty_like(want))
+    assert torch.equal(one[1].double(), 1.875 * 2.0 ** 127 * wq[:, 7]) if dtype == torch.float32 else one[1].isfinite().all()
