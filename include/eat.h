@@ -461,7 +461,7 @@ eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const fl
  * fp32, in the experts' order, rounded once.  `cap` is the number of rows that the
  * caller's arrays hold: pairs past it are left out (place -1, offsets and all
  * sums end at cap).  Rows from offsets[E] on are not written.  Places outside
- * [0, cap) count as -1. */
+ * [0, cap) count as -1.  The workspace's size is not monotonic in T. */
 eat_status_t eat_sort_workspace_size(eat_handle_t h, int32_t T, size_t* bytes);
 
 /* For layer h (its E, d_model, act_dtype; top_k and the mode play no part).
@@ -532,7 +532,8 @@ eat_status_t eat_fp8_size(int32_t groups, int32_t M, int32_t K, size_t* q_bytes,
 eat_status_t eat_fp8_quantize(const void* w, int32_t dtype, int32_t groups, int32_t M, int32_t K, int32_t transposed, void* q,
                               void* scale, hipStream_t stream);
 
-/* Workspace of a product of `rows` rows of K elements out of src_rows. */
+/* Workspace of a product of `rows` rows of K elements out of src_rows.  Not monotonic
+ * (fewer rows can take more slices of the reduction), as eat_workspace_size's. */
 eat_status_t eat_fp8_product_workspace_size(int32_t src_rows, int32_t rows, int32_t groups, int32_t M, int32_t K, size_t* bytes);
 
 /* The product above.
@@ -570,7 +571,9 @@ eat_status_t eat_fp8_product(const void* x, int32_t src_rows, const int32_t* tok
 eat_status_t eat_fp8_experts_size(eat_handle_t h, int32_t grads, size_t* bytes);
 eat_status_t eat_fp8_experts_quantize(eat_handle_t h, const void* w1, const void* w3, const void* w2, int32_t grads, void* buf,
                                       hipStream_t stream);
-/* Workspace of a call of `rows` rows: grads 0 the forward of T tokens, 1 the backward. */
+/* Workspace of a call of `rows` rows: grads 0 the forward of T tokens, 1 the backward
+ * (not monotonic either).  `rows` is the length of the arrays, and tiles, slices and the workspace go
+ * by it, whatever the offsets hold: give the rows there are, or a bound near them. */
 eat_status_t eat_fp8_experts_workspace_size(eat_handle_t h, int32_t T, int32_t rows, int32_t grads, size_t* bytes);
 /*   x [T][d_model] bf16;  token [rows], offsets [E+1] int32 (eat_sort_tokens), as in eat_fp8_product
  *   y [rows][d_model] bf16;  saved [rows][2 d_ffn] bf16 (g, then u) or NULL;  dy, dx [rows][d_model] bf16

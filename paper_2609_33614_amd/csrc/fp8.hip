@@ -11,8 +11,8 @@
 // kept below the largest of them (and cut towards zero; eights are added in fp32):
 // 1.5e-5 of a result of Gaussian numbers, 3.8e-5 where some are 16 times the
 // others, at any K from 128 to 14336 and without a bias, a hundredth of what a bf16
-// result rounds, at 1.5 times the rate of exact products (8192 x 4096 x 4096 with the
-// rows' rounding: 152 and 219 us).  Exact sums go to results in fp32 (ROWS32, EXACT) and to what is rounded to
+// result rounds, at 1.75 times the rate of exact products (8192 x 4096 x 4096 with the
+// rows' rounding, in a long series: 124 us, exact to fp32 217).  Exact sums go to results in fp32 (ROWS32, EXACT) and to what is rounded to
 // 8 bits again (GATED, dh), where a sum off by 2e-5 picks another 4-bit number once
 // in a few thousand: 0.0025 to 0.009 of the result's norm where the rest of the
 // arithmetic has 0.0017.  They take the numbers, which 8 bits of a bf16 hold, as
@@ -59,8 +59,8 @@ struct Tile {
     static_assert(kAhead >= 1 && kAhead <= 3, "waits count up to three chunks");
 };
 // Big: one wave a SIMD with 128 x 128 of the results each, the least LDS reads per
-// product (8192 x 4096 x 4096: 117 us, 2.35 PFLOP/s; an 8-bit library product 97; exact
-// 1.2 PFLOP/s).  Mid: groups that fill no Big tile; eight waves, since four in Big's manner
+// product (8192 x 4096 x 4096 in a long series: 105 us, 2.6 PFLOP/s, an 8-bit library
+// product 89; exact 198, 1.4 PFLOP/s, a bf16 library product 171; after a pause all a quarter longer).  Mid: groups that fill no Big tile; eight waves, since four in Big's manner
 // took 143 against 133 us at 32768 x 1024 x 2048 in 64 groups (exact: 217 and 199).  Few:
 // bound by the weights, which every CU streams once (74 rows, 4096 x 14336 in 8
 // groups: 80 us, 5.8 TB/s), four stages ahead.
@@ -945,7 +945,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const uint16_t* __re
 }
 
 // One 128 x 128 block of w [groups][M][K] per workgroup: 8 bits as they lie (q:
-// rows of ldq bytes, `gq` per group) and, where asked for, transposed (qt).
+// rows of ldq bytes, `gq` per group) and, where asked for, transposed (qt).  Bound by memory: 8
+// x 14336 x 4096 in bf16 258 us (1.4 GB, 5.5 TB/s), transposed 262, in fp32 408 (2.3 GB) and 418;
+// the experts' three matrices, 64 x 1024 x 2048, 255, with their transposes 331.
 struct WeightArgs {
     const void* w;
     int M, K;
@@ -1289,7 +1291,7 @@ hipError_t launch_gated(const Rows& r, const uint8_t* q, const uint8_t* sq, int 
 
 // Whole sums go to dg and du in the product's epilogue where the registers hold both (Big's
 // are full of dh): dh, 4 F bytes a row, is then neither written nor read (64 experts of 512
-// rows, 2048 x 1024, forward and gradient 923 -> 906 us; 60 of 273, 1024 x 2816: 768 -> 744).
+// rows, 2048 x 1024, forward and gradient 841 -> 827 us; 60 of 273, 1024 x 2816: 750 -> 735).
 bool back_in_one(const Rows& r, int F, int splits) { return splits == 1 && tile_rows(r, product_columns(F)) != Big::TM; }
 
 hipError_t launch_gate_backward(const Rows& r, const uint8_t* dyq, const uint8_t* sdy, int lddy, const Matrix& w2t, int splits, float* part,

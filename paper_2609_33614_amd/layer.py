@@ -204,8 +204,9 @@ class EatLayer:
         [cap] int32, place [T][E] int32); rows is None where ``x`` is.  ``cap``:
         the rows to make room for; pairs past it are left out.  Without it, every
         pair that the layer's mode can select has a row (EAT and Top-P: T E of
-        them).  Entries behind the last selected pair are not written.  Calls of one layer
-        share a workspace: order them on one stream.  ``stream`` as in ``balance_loss``."""
+        them, many times those there are: give the sum of ``route``'s k, or a bound
+        near it, where rows go on to ``Fp8Experts``).  Entries behind the last selected pair
+        are not written.  Calls of one layer share a workspace: order them on one stream.  ``stream`` as in ``balance_loss``."""
         T, E, d, dev = mask.shape[0], self.params.E, self.params.d_model, mask.device
         self._expect_mask(mask, T, dev)
         _expect("x", x, self._act(), (T, d), dev)
@@ -466,7 +467,9 @@ class Fp8Experts:
     EatLayer's (w1, w3 [E][F][d], w2 [E][d][F], bf16, row-major), of which the
     object keeps e4m3 numbers with a power of two per 128 x 128 block, with
     ``gradients`` their transposes too.  They are constants: ``backward`` gives
-    the rows' gradient.  Streams and workspace as Fp8Matrix's."""
+    the rows' gradient.  Tiles, memory and the limit of 2^24 rows go by the length of
+    ``token``, not by the rows that ``offsets`` end at.  Streams and workspace as
+    Fp8Matrix's."""
 
     def __init__(self, weights: Dict[str, torch.Tensor], gradients: bool = False, stream=None):
         w1, w3, w2 = weights["w1"], weights["w3"], weights["w2"]
