@@ -459,8 +459,8 @@ eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const fl
  * A token that selected no expert gets y 0, dx 0, dg 0 and dz 0, whatever its rows
  * of x, dy, p and g hold.  Sums are in
  * fp32, in the experts' order, rounded once.  `cap` is the number of rows that the
- * caller's arrays hold: pairs past it are left out (place -1, offsets and all
- * sums end at cap).  Rows from offsets[E] on are not written.  Places outside
+ * caller's arrays hold: pairs past it are left out (place -1, dg 0, offsets and
+ * all sums but P_t, by which the gates are given, end at cap).  Rows from offsets[E] on are not written.  Places outside
  * [0, cap) count as -1.  The workspace's size is not monotonic in T. */
 eat_status_t eat_sort_workspace_size(eat_handle_t h, int32_t T, size_t* bytes);
 
