@@ -34,8 +34,10 @@ class _Workspace:
         self.device, self.buf, self.home, self.captured = device, None, 0, []
 
     def get(self, need: int, stream) -> torch.Tensor:
-        """At least `need` bytes for a call on `stream`, the current one."""
-        if self.buf is None or self.buf.numel() < need:
+        """At least `need` bytes for a call on `stream`, the current one, on its device
+        (a layer's calls run where their tensors are)."""
+        if self.buf is None or self.buf.numel() < need or self.device != stream.device:
+            self.device = stream.device
             self.buf = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
             self.home = stream.cuda_stream
         if torch.cuda.is_current_stream_capturing():
@@ -205,8 +207,9 @@ class EatLayer:
         the rows to make room for; pairs past it are left out.  Without it, every
         pair that the layer's mode can select has a row (EAT and Top-P: T E of
         them, many times those there are: give the sum of ``route``'s k, or a bound
-        near it, where rows go on to ``Fp8Experts``).  Entries behind the last selected pair
-        are not written.  Calls of one layer share a workspace: order them on one stream.  ``stream`` as in ``balance_loss``."""
+        near it, where rows go on to ``Fp8Experts``).  Entries behind the last selected
+        pair are not written.  Calls of one layer share a workspace: order them on one
+        stream.  ``stream`` as in ``balance_loss``."""
         T, E, d, dev = mask.shape[0], self.params.E, self.params.d_model, mask.device
         self._expect_mask(mask, T, dev)
         _expect("x", x, self._act(), (T, d), dev)

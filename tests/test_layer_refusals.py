@@ -38,3 +38,17 @@ def test_numbers_past_32_bits_are_not_cut():
                 call()
     finally:
         L.eat_destroy(h)
+
+
+def test_a_workspace_lies_on_the_calls_device(monkeypatch):
+    """A layer's sort runs where its mask is: memory that a call on another device left is no workspace there."""
+    from types import SimpleNamespace
+    from paper_2609_33614_amd.layer import _Workspace
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    one, two = (SimpleNamespace(cuda_stream=0, device=torch.device(d)) for d in ("cpu", "meta"))
+    ws = _Workspace(one.device)
+    a = ws.get(1000, one)
+    assert a.device == one.device and ws.get(500, one) is a
+    b = ws.get(500, two)
+    assert b.device == two.device and b.numel() >= 500 and ws.get(500, two) is b
+    assert ws.get(500, one).device == one.device

@@ -13,7 +13,7 @@ from paper_2609_33614_amd import layer as M
 
 pytestmark = pytest.mark.skipif(not os.path.exists(L.LIB_PATH), reason="libeat.so not built")
 
-HOME, SIDE = types.SimpleNamespace(cuda_stream=1), types.SimpleNamespace(cuda_stream=2)
+HOME, SIDE = (types.SimpleNamespace(cuda_stream=n, device=torch.device("cpu")) for n in (1, 2))
 
 
 @pytest.fixture
