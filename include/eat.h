@@ -460,8 +460,9 @@ eat_status_t eat_balance_loss(eat_handle_t h, const void* x, int32_t T, const fl
  * of x, dy, p and g hold.  Sums are in
  * fp32, in the experts' order, rounded once.  `cap` is the number of rows that the
  * caller's arrays hold: pairs past it are left out (place -1, dg 0, offsets and
- * all sums but P_t, by which the gates are given, end at cap).  Rows from offsets[E] on are not written.  Places outside
- * [0, cap) count as -1.  The workspace's size is not monotonic in T. */
+ * all sums but P_t, by which the gates are given, end at cap).  Rows from
+ * offsets[E] on are not written.  Places outside [0, cap) count as -1.  The
+ * workspace's size is not monotonic in T. */
 eat_status_t eat_sort_workspace_size(eat_handle_t h, int32_t T, size_t* bytes);
 
 /* For layer h (its E, d_model, act_dtype; top_k and the mode play no part).
